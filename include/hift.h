@@ -511,6 +511,90 @@ hift_status hift_k_cross_entropy(int32_t dtype, int64_t rows, int64_t vocab, int
                                  void *logits_dev, const int32_t *labels_dev, float *rowloss_dev,
                                  float *loss_dev, void *cuda_stream);
 
+/* ---- operators beside the step ---------------------------------------------
+ * What fine-tuning with objectives and updates other than the step's own needs, on caller-owned device buffers.  All
+ * launch on `cuda_stream` (on the device that is current, whose buffers they are given), do not synchronise and do
+ * not allocate; they can be captured into a CUDA graph.  Calls that overlap on the GPU need scratch buffers of their
+ * own.  Inputs and outputs must not overlap except where it is said.  A call that is refused launches nothing. */
+
+/* Log-probabilities of given tokens under rows of logits[rows, ld] (columns >= vocab are padding and not read):
+ *     z = x / temperature,  log p = z - log sum exp z,  logp_dev[r] = log p[tokens_dev[r]],
+ *     entropy_dev[r] = -sum_i p_i log p_i (0 log 0 = 0; may be NULL),
+ *     top_ids_dev / top_logp_dev [rows, n_top]: the n_top most likely tokens in falling order of the logit, equal logits in
+ *     rising order of the id; places without a token whose logit is above -inf hold id -1 and -inf.
+ *     stats_dev fp32 [2*rows] (may be NULL): the row's largest logit x | log sum_i exp(z_i - z_max): what the gradient takes.
+ * The logits are read once and left as they are; sums are fp32, a log p below the range of fp32 is -inf.  A logit of -inf is a
+ * token that cannot occur.  tokens_dev[r] < 0: the
+ * row is ignored, whatever it holds (0, 0, stats 0 | 0, ids -1, -inf); tokens_dev[r] >= vocab: likewise, and *bad_dev
+ * (int32, may be NULL) is set to 1 (and never cleared by the library).  A row with nothing above -inf: logp -inf,
+ * entropy 0, stats -inf | 0, no alternatives.  A row that holds a NaN or +inf: NaN everywhere, ids -1.
+ * dtype 0: fp32 logits, 1: bf16; the rows may start anywhere an element may (any ld >= vocab).  rows = 0 is allowed.
+ * HIFT_ERR_CAPACITY if n_top > HIFT_MAX_TOP. */
+#define HIFT_MAX_TOP 32
+hift_status hift_k_token_logprobs(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void *logits_dev,
+                                  const int32_t *tokens_dev, double temperature, int32_t n_top, float *logp_dev,
+                                  float *entropy_dev, float *stats_dev, int32_t *top_ids_dev, float *top_logp_dev,
+                                  int32_t *bad_dev, void *cuda_stream);
+/* The gradient of sum_r dlogp[r] logp[r] + dentropy[r] entropy[r] into the logits, from what the call above saved:
+ *     dlogits[r, i] = ( dlogp[r] (delta_it - p_i) - dentropy[r] p_i (log p_i + entropy[r]) ) / temperature,
+ * rounded once to the logits' type.  dlogp_dev or dentropy_dev may be NULL (not both; entropy_dev is read with dentropy_dev
+ * only).  dlogits_dev [rows, ld] may be logits_dev itself; padding columns, ignored rows and rows with nothing above -inf
+ * get zeros. */
+hift_status hift_k_token_logprobs_bwd(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void *logits_dev,
+                                      const int32_t *tokens_dev, double temperature, const float *stats_dev,
+                                      const float *entropy_dev, const float *dlogp_dev, const float *dentropy_dev,
+                                      void *dlogits_dev, void *cuda_stream);
+
+/* The junction of a block's output h with the residual stream x, norms after the block and before the next one included:
+ *     x_out = res_scale * x + gate o N1(h),    y = N2(x_out)
+ * N: LayerNorm (kind 0: gain, bias) or RMSNorm (kind 1: gain; biases are not read), both with `eps`.  gain1_dev NULL: no norm
+ * after the block (N1(h) = h); gain2_dev NULL: none before the next (y_dev is not written); gate_dev NULL: no gate.  The
+ * gate is [ceil(rows / rows_per_gate), cols]: row r takes row r / rows_per_gate of it (rows_per_gate >= rows: one learned
+ * vector; the sequence length: one per batch entry; 1: one per token).
+ * x and x_out (which may be x itself) are fp32, the residual stream; h, y, gains, biases and gate have the operand type
+ * (dtype 0 fp32, 1 bf16).  stats_dev: fp32 [4*rows], mean1 | rstd1 | mean2 | rstd2 (means 0 for RMSNorm, zeros for a
+ * norm that is missing).  cols a multiple of 8, at most 16384 (HIFT_ERR_CAPACITY); buffers 16-byte aligned.  rows = 0 is
+ * allowed. */
+hift_status hift_k_join_fwd(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double eps, double res_scale,
+                            const float *x_dev, const void *h_dev, const void *gain1_dev, const void *bias1_dev,
+                            const void *gate_dev, int64_t rows_per_gate, const void *gain2_dev, const void *bias2_dev,
+                            float *x_out_dev, void *y_dev, float *stats_dev, void *cuda_stream);
+/* Its gradient.  dy_dev [rows, cols] (operand type) is the gradient of y (read if gain2_dev is given), dx_out_dev (fp32; may be
+ * NULL if gain2_dev is given) the gradient that reaches x_out past the norm; x_out_dev, h_dev and stats_dev are the forward
+ * pass's.  With d = dx_out + N2'(dy):
+ *     dx = res_scale * d (fp32; may be dx_out_dev itself),  dh = N1'(gate o d) (operand type),
+ *     dgate = sum of d o N1(h) over a gate's rows (fp32, the gate's shape),  dgain1, dbias1, dgain2, dbias2 fp32 [cols].
+ * Each of the last five may be NULL (not wanted); one that belongs to a missing norm, gate or bias is refused.  bias1_dev is
+ * read for dgate only.  Sums over rows run in a fixed order.  scratch_dev: hift_join_bwd_scratch_bytes(rows, cols,
+ * rows_per_gate) bytes (rows_per_gate = rows without a gate), HIFT_ERR_CAPACITY if scratch_bytes is less. */
+size_t      hift_join_bwd_scratch_bytes(int64_t rows, int64_t cols, int64_t rows_per_gate);
+hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double res_scale, const void *dy_dev,
+                            const float *dx_out_dev, const float *x_out_dev, const void *h_dev, const float *stats_dev,
+                            const void *gain1_dev, const void *bias1_dev, const void *gate_dev, int64_t rows_per_gate,
+                            const void *gain2_dev, float *dx_dev, void *dh_dev, float *dgain1_dev, float *dbias1_dev,
+                            float *dgate_dev, float *dgain2_dev, float *dbias2_dev, void *scratch_dev, size_t scratch_bytes,
+                            void *cuda_stream);
+
+/* Orthogonalisation of a matrix by Newton-Schulz products:
+ *     X_0 = G / max(|G|_F, 1e-30),   X <- a X + (b A + c A A) X,  A = X X^T  (right-hand products when rows > cols),
+ * `steps` times, (a, b, c) = (3.4445, -4.7750, 2.0315): every singular value s of X goes to a s + b s^3 + c s^5, which brings all but
+ * the smallest to between 0.68 and 1.14 in five steps.  g_dev [rows, cols] fp32 (dtype 0) or bf16 (1), o_dev bf16 [rows, cols].  A zero matrix
+ * stays zero; NaN or infinity anywhere makes the whole result NaN.  1 <= rows, cols <= HIFT_ORTHOGONALIZE_MAX_DIM
+ * (HIFT_ERR_CAPACITY), 1 <= steps <= 20.  scratch_dev: 256-byte aligned, hift_orthogonalize_scratch_bytes(rows, cols) bytes. */
+#define HIFT_ORTHOGONALIZE_MAX_DIM 65536
+size_t      hift_orthogonalize_scratch_bytes(int64_t rows, int64_t cols);
+hift_status hift_k_orthogonalize(int32_t dtype, int64_t rows, int64_t cols, const void *g_dev, void *o_dev, int32_t steps,
+                                 void *scratch_dev, size_t scratch_bytes, void *cuda_stream);
+/* One update of a weight matrix with it, beside hift_opt_step and hift_adafactor_step (what the Muon optimiser does):
+ *     momentum <- mu momentum + grad;   U = grad + mu momentum (nesterov != 0) or momentum;   X from U as above;
+ *     master <- master (1 - lr weight_decay) - lr 0.2 sqrt(max(rows, cols)) X
+ * (the factor gives the update the size of an AdamW update at the same lr); param_bf16_dev (may be NULL) receives the
+ * bf16 image of the new master.  master, grad and momentum_dev are fp32 [rows, cols].  The products run in 16-bit
+ * floating point with fp32 sums. */
+hift_status hift_muon_step(int64_t rows, int64_t cols, void *param_bf16_dev, float *master_dev, const float *grad_dev,
+                           float *momentum_dev, void *scratch_dev, size_t scratch_bytes, double lr, double momentum,
+                           int32_t nesterov, double weight_decay, int32_t steps, void *cuda_stream);
+
 const char *hift_strerror(hift_status s);
 
 #ifdef __cplusplus

@@ -131,6 +131,15 @@ def _prototypes():
         "hift_k_norm_bwd": (C.c_int, [i32, i32, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
         "hift_k_norm_bwd_static": (C.c_int, [i32, i32, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp]),
         "hift_k_cross_entropy": (C.c_int, [i32, i64, i64, i64, vp, vp, vp, vp, vp]),
+        "hift_k_token_logprobs": (C.c_int, [i32, i64, i64, i64, vp, vp, f64, i32, vp, vp, vp, vp, vp, vp, vp]),
+        "hift_k_token_logprobs_bwd": (C.c_int, [i32, i64, i64, i64, vp, vp, f64, vp, vp, vp, vp, vp, vp]),
+        "hift_k_join_fwd": (C.c_int, [i32, i32, i64, i64, f64, f64, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp]),
+        "hift_join_bwd_scratch_bytes": (sz, [i64, i64, i64]),
+        "hift_k_join_bwd": (C.c_int, [i32, i32, i64, i64, f64, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp,
+                                      vp, sz, vp]),
+        "hift_orthogonalize_scratch_bytes": (sz, [i64, i64]),
+        "hift_k_orthogonalize": (C.c_int, [i32, i64, i64, vp, vp, i32, vp, sz, vp]),
+        "hift_muon_step": (C.c_int, [i64, i64, vp, vp, vp, vp, vp, sz, f64, f64, i32, f64, i32, vp]),
     }
 
 
@@ -574,3 +583,58 @@ def k_norm_bwd_static(dtype, kind, rows, cols, dy, x, stats, gain, add, dx, dgai
 def k_cross_entropy(dtype, rows, vocab, ld, logits, labels, rowloss, loss, stream=None):
     _check(lib().hift_k_cross_entropy(dtype, rows, vocab, ld, _ptr(logits), _ptr(labels), _ptr(rowloss),
                                       _ptr(loss), _st(stream)), "hift_k_cross_entropy")
+
+
+def k_token_logprobs(dtype, rows, vocab, ld, logits, tokens, temperature, n_top, logp, entropy, stats, top_ids=None, top_logp=None,
+                     bad=None, stream=None):
+    _check(lib().hift_k_token_logprobs(dtype, rows, vocab, ld, _ptr(logits), _ptr(tokens), temperature, n_top, _ptr(logp),
+                                       _ptr(entropy), _ptr(stats), _ptr(top_ids), _ptr(top_logp), _ptr(bad), _st(stream)),
+           "hift_k_token_logprobs")
+
+
+def k_token_logprobs_bwd(dtype, rows, vocab, ld, logits, tokens, temperature, stats, entropy, dlogp, dentropy, dlogits, stream=None):
+    _check(lib().hift_k_token_logprobs_bwd(dtype, rows, vocab, ld, _ptr(logits), _ptr(tokens), temperature, _ptr(stats),
+                                           _ptr(entropy), _ptr(dlogp), _ptr(dentropy), _ptr(dlogits), _st(stream)),
+           "hift_k_token_logprobs_bwd")
+
+
+def k_join_fwd(dtype, kind, rows, cols, eps, res_scale, x, h, gain1, bias1, gate, rows_per_gate, gain2, bias2, x_out, y, stats,
+               stream=None):
+    _check(lib().hift_k_join_fwd(dtype, kind, rows, cols, eps, res_scale, _ptr(x), _ptr(h), _ptr(gain1), _ptr(bias1), _ptr(gate),
+                                 rows_per_gate, _ptr(gain2), _ptr(bias2), _ptr(x_out), _ptr(y), _ptr(stats), _st(stream)),
+           "hift_k_join_fwd")
+
+
+def join_bwd_scratch_bytes(rows, cols, rows_per_gate) -> int:
+    return lib().hift_join_bwd_scratch_bytes(rows, cols, rows_per_gate)
+
+
+def _nbytes(t) -> int:
+    return 0 if t is None else t.numel() * t.element_size()
+
+
+def k_join_bwd(dtype, kind, rows, cols, res_scale, dy, dx_out, x_out, h, stats, gain1, bias1, gate, rows_per_gate, gain2, dx, dh,
+               dgain1, dbias1, dgate, dgain2, dbias2, scratch, stream=None):
+    """scratch: a CUDA tensor of join_bwd_scratch_bytes(rows, cols, rows_per_gate) bytes or more."""
+    _check(lib().hift_k_join_bwd(dtype, kind, rows, cols, res_scale, _ptr(dy), _ptr(dx_out), _ptr(x_out), _ptr(h), _ptr(stats),
+                                 _ptr(gain1), _ptr(bias1), _ptr(gate), rows_per_gate, _ptr(gain2), _ptr(dx), _ptr(dh),
+                                 _ptr(dgain1), _ptr(dbias1), _ptr(dgate), _ptr(dgain2), _ptr(dbias2), _ptr(scratch),
+                                 _nbytes(scratch), _st(stream)), "hift_k_join_bwd")
+
+
+def orthogonalize_scratch_bytes(rows, cols) -> int:
+    return lib().hift_orthogonalize_scratch_bytes(rows, cols)
+
+
+def k_orthogonalize(dtype, rows, cols, g, o, steps, scratch, stream=None):
+    """scratch: a CUDA tensor of orthogonalize_scratch_bytes(rows, cols) bytes or more."""
+    _check(lib().hift_k_orthogonalize(dtype, rows, cols, _ptr(g), _ptr(o), steps, _ptr(scratch), _nbytes(scratch), _st(stream)),
+           "hift_k_orthogonalize")
+
+
+def muon_step(rows, cols, param_bf16, master, grad, momentum_buf, scratch, lr, momentum=0.95, nesterov=True, weight_decay=0.0,
+              steps=5, stream=None):
+    """scratch: a CUDA tensor of orthogonalize_scratch_bytes(rows, cols) bytes or more."""
+    _check(lib().hift_muon_step(rows, cols, _ptr(param_bf16), _ptr(master), _ptr(grad), _ptr(momentum_buf), _ptr(scratch),
+                                _nbytes(scratch), lr, momentum, 1 if nesterov else 0, weight_decay, steps, _st(stream)),
+           "hift_muon_step")

@@ -1,0 +1,209 @@
+// Entry points of the operators beside the training step: token log-probabilities, the residual junction and the
+// orthogonalised update (include/hift.h).  Argument checks and launches; the kernels are in the headers.
+#include <math.h>
+
+#include "hift.h"
+#include "kernels_join.cuh"
+#include "kernels_logprobs.cuh"
+#include "kernels_muon.cuh"
+
+using namespace hift;
+
+namespace {
+
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+hift_status done() { return cudaGetLastError() == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA; }
+
+hift_status logprobs_cfg(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, double temperature, float* scale) {
+  if (dtype < 0 || dtype > 1 || rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > INT32_MAX - 65536 || ld < vocab) return HIFT_ERR_CFG;
+  *scale = (float)(1.0 / temperature);
+  if (!(temperature > 0.0) || !isfinite(temperature) || !isnormal(*scale)) return HIFT_ERR_CFG;
+  return HIFT_OK;
+}
+
+// threads of a junction kernel and its chunks of 8 columns per thread
+void join_shape(int64_t cols, int* threads, int* chunks) {
+  const int units = (int)(cols / 8);
+  int th = (units + 31) / 32 * 32;
+  if (th > 512) th = 512;
+  int nc = (units + th - 1) / th;
+  if (nc == 3) nc = 4;
+  *threads = th;
+  *chunks = nc;
+}
+hift_status join_cfg(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double res_scale, const void* gate, int64_t rows_per_gate) {
+  if (dtype < 0 || dtype > 1 || kind < 0 || kind > 1 || rows < 0 || rows > INT32_MAX || cols < 8 || cols % 8) return HIFT_ERR_CFG;
+  if (!isfinite(res_scale) || (gate && rows_per_gate < 1)) return HIFT_ERR_CFG;
+  return cols > kJoinMaxCols ? HIFT_ERR_CAPACITY : HIFT_OK;
+}
+
+#define JOIN_NC(KERNEL, P, K)                                                             \
+  do {                                                                                    \
+    if (nc == 1) KERNEL<P, K, 1><<<grid, th, 0, (cudaStream_t)stream>>>(p);               \
+    else if (nc == 2) KERNEL<P, K, 2><<<grid, th, 0, (cudaStream_t)stream>>>(p);          \
+    else KERNEL<P, K, 4><<<grid, th, 0, (cudaStream_t)stream>>>(p);                       \
+  } while (0)
+#define JOIN_LAUNCH(KERNEL)                                                               \
+  do {                                                                                    \
+    if (dtype == 0) { if (kind == 0) JOIN_NC(KERNEL, float, 0); else JOIN_NC(KERNEL, float, 1); } \
+    else { if (kind == 0) JOIN_NC(KERNEL, bf16, 0); else JOIN_NC(KERNEL, bf16, 1); }      \
+  } while (0)
+
+// how a backward call deals its rows out: the number of blocks, and whether a gate's rows are split over several
+struct JoinPlan { int ctas, split; int64_t gates_per_cta, rows_per_gate, n_gates; };
+JoinPlan join_plan(int64_t rows, int64_t rows_per_gate) {
+  JoinPlan pl;
+  pl.rows_per_gate = rows_per_gate < 1 || rows_per_gate > rows ? (rows > 0 ? rows : 1) : rows_per_gate;
+  pl.n_gates = (rows + pl.rows_per_gate - 1) / pl.rows_per_gate;
+  if (pl.n_gates > kJoinCtas) {
+    pl.split = 0;
+    pl.gates_per_cta = (pl.n_gates + kJoinCtas - 1) / kJoinCtas;
+    pl.ctas = (int)((pl.n_gates + pl.gates_per_cta - 1) / pl.gates_per_cta);
+    return pl;
+  }
+  int64_t split = pl.n_gates > 0 ? kJoinCtas / pl.n_gates : 1;
+  const int64_t most = (pl.rows_per_gate + 3) / 4;         // four rows at least for a block
+  if (split > most) split = most;
+  pl.split = (int)(split < 1 ? 1 : split);
+  pl.gates_per_cta = 1;
+  pl.ctas = (int)(pl.n_gates * pl.split);
+  return pl;
+}
+
+hift_status ns_cfg(int64_t rows, int64_t cols, int32_t steps, const void* scratch, size_t scratch_bytes) {
+  if (rows < 1 || cols < 1 || steps < 1 || steps > 20) return HIFT_ERR_CFG;
+  if (rows > HIFT_ORTHOGONALIZE_MAX_DIM || cols > HIFT_ORTHOGONALIZE_MAX_DIM) return HIFT_ERR_CAPACITY;
+  if (!scratch) return HIFT_ERR_INPUT;
+  if (!aligned(scratch, 256)) return HIFT_ERR_CFG;
+  return scratch_bytes < ns_scratch_bytes(rows, cols) ? HIFT_ERR_CAPACITY : HIFT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+hift_status hift_k_token_logprobs(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void* logits, const int32_t* tokens,
+                                  double temperature, int32_t n_top, float* logp, float* entropy, float* stats, int32_t* top_ids,
+                                  float* top_logp, int32_t* bad, void* stream) {
+  float scale;
+  const hift_status s = logprobs_cfg(dtype, rows, vocab, ld, temperature, &scale);
+  if (s != HIFT_OK) return s;
+  if (n_top < 0) return HIFT_ERR_CFG;
+  if (n_top > HIFT_MAX_TOP) return HIFT_ERR_CAPACITY;
+  if (rows == 0) return HIFT_OK;
+  if (!logits || !tokens || !logp || (n_top > 0 && (!top_ids || !top_logp))) return HIFT_ERR_INPUT;
+  if (!aligned(logits, dtype == 0 ? 4 : 2)) return HIFT_ERR_CFG;
+  const int th = vocab >= 4096 ? 512 : 128;
+  if (dtype == 0)
+    token_logprobs_kernel<float><<<(unsigned)rows, th, 0, (cudaStream_t)stream>>>((const float*)logits, tokens, (int)vocab, ld, rows, scale, n_top, logp, entropy, stats, top_ids, top_logp, bad);
+  else
+    token_logprobs_kernel<bf16><<<(unsigned)rows, th, 0, (cudaStream_t)stream>>>((const bf16*)logits, tokens, (int)vocab, ld, rows, scale, n_top, logp, entropy, stats, top_ids, top_logp, bad);
+  return done();
+}
+
+hift_status hift_k_token_logprobs_bwd(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void* logits, const int32_t* tokens,
+                                      double temperature, const float* stats, const float* entropy, const float* dlogp,
+                                      const float* dentropy, void* dlogits, void* stream) {
+  float scale;
+  const hift_status s = logprobs_cfg(dtype, rows, vocab, ld, temperature, &scale);
+  if (s != HIFT_OK) return s;
+  if (rows == 0) return HIFT_OK;
+  if (!logits || !tokens || !stats || !dlogits || (!dlogp && !dentropy) || (dentropy && !entropy)) return HIFT_ERR_INPUT;
+  if (!aligned(logits, dtype == 0 ? 4 : 2) || !aligned(dlogits, dtype == 0 ? 4 : 2)) return HIFT_ERR_CFG;
+  const int th = vocab >= 4096 ? 512 : 128;
+  if (dtype == 0)
+    token_logprobs_bwd_kernel<float><<<(unsigned)rows, th, 0, (cudaStream_t)stream>>>((const float*)logits, tokens, (int)vocab, ld, rows, scale, stats, entropy, dlogp, dentropy, (float*)dlogits);
+  else
+    token_logprobs_bwd_kernel<bf16><<<(unsigned)rows, th, 0, (cudaStream_t)stream>>>((const bf16*)logits, tokens, (int)vocab, ld, rows, scale, stats, entropy, dlogp, dentropy, (bf16*)dlogits);
+  return done();
+}
+
+hift_status hift_k_join_fwd(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double eps, double res_scale, const float* x,
+                            const void* h, const void* gain1, const void* bias1, const void* gate, int64_t rows_per_gate,
+                            const void* gain2, const void* bias2, float* x_out, void* y, float* stats, void* stream) {
+  const hift_status s = join_cfg(dtype, kind, rows, cols, res_scale, gate, rows_per_gate);
+  if (s != HIFT_OK) return s;
+  if (!(eps >= 0.0) || !isfinite(eps)) return HIFT_ERR_CFG;
+  if (rows == 0) return HIFT_OK;
+  if (!x || !h || !x_out || !stats || (gain2 && !y) || (kind == 0 && ((gain1 && !bias1) || (gain2 && !bias2)))) return HIFT_ERR_INPUT;
+  if (!aligned(x, 16) || !aligned(h, 16) || !aligned(x_out, 16) || !aligned(gain1, 16) || !aligned(bias1, 16) || !aligned(gate, 16) ||
+      !aligned(gain2, 16) || !aligned(bias2, 16) || (gain2 && !aligned(y, 16))) return HIFT_ERR_CFG;
+  JoinFwd p{x, h, gain1, bias1, gate, gain2, bias2, x_out, y, stats, rows, gate ? rows_per_gate : rows, (int)cols, (float)eps, (float)res_scale};
+  int th, nc;
+  join_shape(cols, &th, &nc);
+  const unsigned grid = (unsigned)rows;
+  JOIN_LAUNCH(join_fwd_kernel);
+  return done();
+}
+
+size_t hift_join_bwd_scratch_bytes(int64_t rows, int64_t cols, int64_t rows_per_gate) {
+  if (rows < 1 || cols < 1) return 0;
+  return (size_t)join_plan(rows, rows_per_gate).ctas * cols * kJoinPlanes * sizeof(float);
+}
+
+hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double res_scale, const void* dy,
+                            const float* dx_out, const float* x_out, const void* h, const float* stats, const void* gain1,
+                            const void* bias1, const void* gate, int64_t rows_per_gate, const void* gain2, float* dx, void* dh,
+                            float* dgain1, float* dbias1, float* dgate, float* dgain2, float* dbias2, void* scratch,
+                            size_t scratch_bytes, void* stream) {
+  const hift_status s = join_cfg(dtype, kind, rows, cols, res_scale, gate, rows_per_gate);
+  if (s != HIFT_OK) return s;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (rows == 0) {                                         // no rows: the sums over them are zero
+    for (float* q : {dgain1, dbias1, dgain2, dbias2})
+      if (q && cudaMemsetAsync(q, 0, (size_t)cols * sizeof(float), st) != cudaSuccess) return HIFT_ERR_CUDA;
+    return HIFT_OK;
+  }
+  if (!h || !stats || !dx || !dh || !scratch || (gain2 && (!dy || !x_out)) || (!gain2 && !dx_out)) return HIFT_ERR_INPUT;
+  if ((dgate && !gate) || ((dgain1 || dbias1) && !gain1) || ((dgain2 || dbias2) && !gain2) || (kind == 1 && (dbias1 || dbias2))) return HIFT_ERR_INPUT;
+  if (kind == 0 && gain1 && dgate && !bias1) return HIFT_ERR_INPUT;
+  const void* ptrs[] = {dy, dx_out, x_out, h, gain1, bias1, gate, gain2, dx, dh, dgate, scratch};
+  for (const void* q : ptrs) if (!aligned(q, 16)) return HIFT_ERR_CFG;
+  const JoinPlan pl = join_plan(rows, gate ? rows_per_gate : rows);
+  if (scratch_bytes < (size_t)pl.ctas * cols * kJoinPlanes * sizeof(float)) return HIFT_ERR_CAPACITY;
+  JoinBwd p{dy, dx_out, x_out, h, stats, gain1, bias1, gate, gain2, dx, dh, dgate, (float*)scratch, rows, pl.rows_per_gate, (int)cols,
+            pl.ctas, pl.split, pl.gates_per_cta, (float)res_scale};
+  int th, nc;
+  join_shape(cols, &th, &nc);
+  const unsigned grid = (unsigned)pl.ctas;
+  JOIN_LAUNCH(join_bwd_kernel);
+  if (dgain1 || dbias1 || dgain2 || dbias2 || (dgate && pl.split > 0)) {
+    const JoinSums o{{dgain1, dbias1, dgain2, dbias2, pl.split > 0 ? dgate : nullptr}};
+    const dim3 g((unsigned)((cols + 31) / 32), (unsigned)(kJoinPlanes - 1 + (dgate && pl.split > 0 ? pl.n_gates : 0)));
+    join_sums_kernel<<<g, dim3(32, 8), 0, st>>>((const float*)scratch, o, pl.ctas, (int)cols, pl.split);
+  }
+  return done();
+}
+
+size_t hift_orthogonalize_scratch_bytes(int64_t rows, int64_t cols) {
+  return rows < 1 || cols < 1 || rows > HIFT_ORTHOGONALIZE_MAX_DIM || cols > HIFT_ORTHOGONALIZE_MAX_DIM ? 0 : ns_scratch_bytes(rows, cols);
+}
+
+hift_status hift_k_orthogonalize(int32_t dtype, int64_t rows, int64_t cols, const void* g, void* o, int32_t steps, void* scratch,
+                                 size_t scratch_bytes, void* stream) {
+  if (dtype < 0 || dtype > 1) return HIFT_ERR_CFG;
+  const hift_status s = ns_cfg(rows, cols, steps, scratch, scratch_bytes);
+  if (s != HIFT_OK) return s;
+  if (!g || !o) return HIFT_ERR_INPUT;
+  if (!aligned(g, dtype == 0 ? 4 : 2) || !aligned(o, 2)) return HIFT_ERR_CFG;
+  const NsUpdate to{(bf16*)o, nullptr, nullptr, 0.f, 0.f};
+  const cudaError_t e = dtype == 0 ? launch_orthogonalize((cudaStream_t)stream, rows, cols, (const float*)g, nullptr, 0.f, 0, steps, to, scratch)
+                                   : launch_orthogonalize((cudaStream_t)stream, rows, cols, (const bf16*)g, nullptr, 0.f, 0, steps, to, scratch);
+  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
+}
+
+hift_status hift_muon_step(int64_t rows, int64_t cols, void* param_bf16, float* master, const float* grad, float* momentum_buf,
+                           void* scratch, size_t scratch_bytes, double lr, double momentum, int32_t nesterov, double weight_decay,
+                           int32_t steps, void* stream) {
+  const hift_status s = ns_cfg(rows, cols, steps, scratch, scratch_bytes);
+  if (s != HIFT_OK) return s;
+  if (!isfinite(lr) || !isfinite(weight_decay) || !(momentum >= 0.0 && momentum < 1.0)) return HIFT_ERR_CFG;
+  if (!master || !grad || !momentum_buf) return HIFT_ERR_INPUT;
+  if (!aligned(master, 4) || !aligned(grad, 4) || !aligned(momentum_buf, 4) || !aligned(param_bf16, 2)) return HIFT_ERR_CFG;
+  const double size = lr * 0.2 * sqrt((double)(rows > cols ? rows : cols));
+  const NsUpdate to{nullptr, master, (bf16*)param_bf16, (float)(1.0 - lr * weight_decay), (float)size};
+  const cudaError_t e = launch_orthogonalize((cudaStream_t)stream, rows, cols, grad, momentum_buf, (float)momentum, nesterov != 0, steps, to, scratch);
+  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
+}
+
+}  // extern "C"
