@@ -20,6 +20,7 @@
 
 #include <cuda.h>
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <math.h>
 #include <stdio.h>
 #include <stdlib.h>
@@ -607,6 +608,8 @@ __device__ __forceinline__ void epi_row_gelu_bwd(uint32_t taddr, int BN, int m, 
   }
 }
 
+#include "ns_epilogue.cuh"
+
 // ------------------------------------------------------------------ kernel
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
@@ -615,16 +618,19 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 // Persistent: one CTA per SM walks output tiles (m fastest, so CTAs running together share the
 // same B tile through L2).  Two accumulators in tensor memory: while the epilogue warps drain
 // tile i, the MMA thread already accumulates tile i+1.
-template <bool A_MN, bool B_MN, bool OUT_F32>
+// NS: fp16 operands and the epilogues of the Newton-Schulz products (ns_epilogue.cuh); their symmetric products (modes
+// 0 and 1) walk the tiles that touch the lower triangle only.
+template <bool A_MN, bool B_MN, bool OUT_F32, bool NS = false>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                int M, int N, int K, void* __restrict__ cptr, int64_t ldc,
                const __nv_bfloat16* __restrict__ bias, const float* __restrict__ residual, int64_t ldr,
-               int tiles_m, int num_tiles, int n_fast, TileRt tc, RopeArgs rope, SwigluArgs swg, SwigluBwdArgs swb, GeluArgs ge) {
+               int tiles_m, int num_tiles, int n_fast, TileRt tc, RopeArgs rope, SwigluArgs swg, SwigluBwdArgs swb, GeluArgs ge, NsArgs ns) {
   // Tile walk.  CTAs that run together should share the LARGER operand's slab and leave the smaller operand to L2:
   // row tiles fastest (n_fast = 0) when A is the smaller operand, column tiles fastest (n_fast = tiles along N) when B is.
-  auto tm_of = [&](int tile) { return n_fast ? tile / n_fast : tile % tiles_m; };
-  auto tn_of = [&](int tile) { return n_fast ? tile % n_fast : tile / tiles_m; };
+  auto tri = [&](int tile, bool row) { int a, b; ns_tri_tile(tile, BM / tc.bn, a, b); return row ? a : b; };
+  auto tm_of = [&](int tile) { if (NS && ns.mode != 2) return tri(tile, true); return n_fast ? tile / n_fast : tile % tiles_m; };
+  auto tn_of = [&](int tile) { if (NS && ns.mode != 2) return tri(tile, false); return n_fast ? tile % n_fast : tile / tiles_m; };
   const int BN = tc.bn, S = tc.stages;
   const uint32_t kStageBytes = (uint32_t)tc.stage_bytes;
   extern __shared__ uint8_t smem_raw[];
@@ -700,7 +706,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
     if (lane == 0 && !poisoned) {
       // instruction descriptor: D fp32 (bits 4-5 = 1), A and B bf16 (bits 7-9, 10-12 = 1),
       // A / B major-ness (bits 15, 16: 1 = MN-major), N/8 at bits 17-22, M/16 at bits 24-28
-      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((A_MN ? 1u : 0u) << 15) |
+      // (NS: both fp16, 0)
+      const uint32_t idesc = (1u << 4) | (NS ? 0u : (1u << 7) | (1u << 10)) | ((A_MN ? 1u : 0u) << 15) |
                              ((B_MN ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
       int s = 0, lt = 0;
       uint32_t ph = 0;
@@ -747,7 +754,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       const int m0 = tm_of(tile) * BM, n0 = tn_of(tile) * BN;
       const int m = m0 + q * 32 + lane;
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(ab * kAccStride);
-      if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
+      if constexpr (NS) epi_ns(taddr, BN, m, M, n0, N, ns, stage, lane);
+      else if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
       else if (!OUT_F32 && swb.gu != nullptr) epi_row_swiglu_bwd(taddr, BN, m, M, n0, N, cptr, swb, stage, lane);
       else if (!OUT_F32 && ge.out != nullptr) epi_row_gelu_fwd(taddr, BN, m, M, n0, N, cptr, ldc, bias, ge, stage, lane);
       else if (!OUT_F32 && ge.bwd_a != nullptr) epi_row_gelu_bwd(taddr, BN, m, M, n0, N, cptr, ldc, ge, stage, lane);
@@ -812,14 +820,15 @@ __device__ __forceinline__ void tc_mma_pair(uint32_t tmem_c, uint64_t da, uint64
       ::"r"(tmem_c), "l"(da), "l"(db), "r"(idesc), "r"(accum) : "memory");
 }
 
-template <bool A_MN, bool B_MN, bool OUT_F32>
+template <bool A_MN, bool B_MN, bool OUT_F32, bool NS = false>
 __global__ void __launch_bounds__(kThreads, 1)
 gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                 int M, int N, int K, void* __restrict__ cptr, int64_t ldc,
                 const __nv_bfloat16* __restrict__ bias, const float* __restrict__ residual, int64_t ldr,
-                int tiles_m, int num_tiles, int n_fast, RopeArgs rope, SwigluArgs swg, SwigluBwdArgs swb, GeluArgs ge) {
-  auto tm_of = [&](int tile) { return n_fast ? tile / n_fast : tile % tiles_m; };      // see gemm_tc_kernel
-  auto tn_of = [&](int tile) { return n_fast ? tile % n_fast : tile / tiles_m; };
+                int tiles_m, int num_tiles, int n_fast, RopeArgs rope, SwigluArgs swg, SwigluBwdArgs swb, GeluArgs ge, NsArgs ns) {
+  auto tri = [&](int tile, bool row) { int a, b; ns_tri_tile(tile, 1, a, b); return row ? a : b; };
+  auto tm_of = [&](int tile) { if (NS && ns.mode != 2) return tri(tile, true); return n_fast ? tile / n_fast : tile % tiles_m; };      // see gemm_tc_kernel
+  auto tn_of = [&](int tile) { if (NS && ns.mode != 2) return tri(tile, false); return n_fast ? tile % n_fast : tile / tiles_m; };
   constexpr int S = kStages2;
   constexpr int BN = kBN2;
   extern __shared__ uint8_t smem_raw[];
@@ -894,7 +903,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
   } else if (warp == 1) {
     // ---------------- MMA issuer: one thread of the pair's first CTA
     if (lane == 0 && rank == 0 && !poisoned) {
-      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((A_MN ? 1u : 0u) << 15) |
+      const uint32_t idesc = (1u << 4) | (NS ? 0u : (1u << 7) | (1u << 10)) | ((A_MN ? 1u : 0u) << 15) |
                              ((B_MN ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)((2 * BM) >> 4) << 24);
       int s = 0, lt = 0;
       uint32_t ph = 0;
@@ -937,7 +946,8 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
       const int m0 = tm_of(tile) * (2 * BM) + (int)rank * BM, n0 = tn_of(tile) * BN;
       const int m = m0 + q * 32 + lane;
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(ab * kAccStride);
-      if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
+      if constexpr (NS) epi_ns(taddr, BN, m, M, n0, N, ns, stage, lane);
+      else if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
       else if (!OUT_F32 && swb.gu != nullptr) epi_row_swiglu_bwd(taddr, BN, m, M, n0, N, cptr, swb, stage, lane);
       else if (!OUT_F32 && ge.out != nullptr) epi_row_gelu_fwd(taddr, BN, m, M, n0, N, cptr, ldc, bias, ge, stage, lane);
       else if (!OUT_F32 && ge.bwd_a != nullptr) epi_row_gelu_bwd(taddr, BN, m, M, n0, N, cptr, ldc, ge, stage, lane);
@@ -1043,7 +1053,7 @@ cudaError_t launch_inst(cudaStream_t st, const GemmArgs& g, const CUtensorMap& t
                             (const __nv_bfloat16*)g.bias, g.residual, g.ldr, tiles_m, num_tiles, g.M > g.N ? tiles_n : 0, tc,
                             RopeArgs{g.rope_cs, g.rope_seq, g.rope_cols}, SwigluArgs{(__nv_bfloat16*)g.swiglu_out, g.N / 2},
                             SwigluBwdArgs{(const __nv_bfloat16*)g.swiglu_bwd_gu},
-                            GeluArgs{(__nv_bfloat16*)g.gelu_out, (const __nv_bfloat16*)g.gelu_bwd_a});
+                            GeluArgs{(__nv_bfloat16*)g.gelu_out, (const __nv_bfloat16*)g.gelu_bwd_a}, NsArgs{});
 }
 
 template <bool A_MN, bool B_MN, bool OUT_F32>
@@ -1069,11 +1079,76 @@ cudaError_t launch_pair(cudaStream_t st, const GemmArgs& g, const CUtensorMap& t
                             (const __nv_bfloat16*)g.bias, g.residual, g.ldr, tiles_m, num_tiles, g.M > g.N ? tiles_n : 0,
                             RopeArgs{g.rope_cs, g.rope_seq, g.rope_cols}, SwigluArgs{(__nv_bfloat16*)g.swiglu_out, g.N / 2},
                             SwigluBwdArgs{(const __nv_bfloat16*)g.swiglu_bwd_gu},
-                            GeluArgs{(__nv_bfloat16*)g.gelu_out, (const __nv_bfloat16*)g.gelu_bwd_a});
+                            GeluArgs{(__nv_bfloat16*)g.gelu_out, (const __nv_bfloat16*)g.gelu_bwd_a}, NsArgs{});
 }
 template <bool A_MN, bool B_MN, bool OUT_F32>
 cudaError_t set_smem_attr2() {
   return cudaFuncSetAttribute(gemm_tc2_kernel<A_MN, B_MN, OUT_F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+}
+// One Newton-Schulz product.  ta / tb: maps for tiles of (bn < 256: one CTA per 128 x bn tile; 256: a CTA pair per 256 x 256 tile).
+template <bool A_MN, bool B_MN>
+cudaError_t launch_ns(cudaStream_t st, int M, int N, int K, const CUtensorMap& ta, const CUtensorMap& tb, int bn, const NsArgs& ns) {
+  const bool pair = bn == 256;
+  const int bm = pair ? 2 * BM : BM;
+  const int tm = (M + bm - 1) / bm, tn = (N + bn - 1) / bn;
+  const int per = pair ? 1 : BM / bn;
+  const int tiles = ns.mode == 2 ? tm * tn : (per == 1 ? tm * (tm + 1) / 2 : tm * (tm + 1));
+  const int n_fast = M > N ? tn : 0;
+  const int slots = pair ? g_num_sms / 2 : g_num_sms;
+  const int grid = tiles < slots ? tiles : slots;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3(pair ? 2 * grid : grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = g_pdl;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pair ? 2 : 1;
+  if (pair)
+    return cudaLaunchKernelEx(&cfg, gemm_tc2_kernel<A_MN, B_MN, false, true>, ta, tb, M, N, K, (void*)nullptr, (int64_t)0,
+                              (const __nv_bfloat16*)nullptr, (const float*)nullptr, (int64_t)0, tm, tiles, n_fast, RopeArgs{}, SwigluArgs{},
+                              SwigluBwdArgs{}, GeluArgs{}, ns);
+  return cudaLaunchKernelEx(&cfg, gemm_tc_kernel<A_MN, B_MN, false, true>, ta, tb, M, N, K, (void*)nullptr, (int64_t)0,
+                            (const __nv_bfloat16*)nullptr, (const float*)nullptr, (int64_t)0, tm, tiles, n_fast, make_tile(bn, B_MN), RopeArgs{},
+                            SwigluArgs{}, SwigluBwdArgs{}, GeluArgs{}, ns);
+}
+template <bool A_MN, bool B_MN>
+cudaError_t set_smem_attr_ns() {
+  const cudaError_t e = cudaFuncSetAttribute(gemm_tc_kernel<A_MN, B_MN, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(gemm_tc2_kernel<A_MN, B_MN, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+}
+// 2-D fp16 matrix [outer][inner], contiguous; box = 64 x box_outer, 128-byte swizzle.  Scratch addresses change from call to
+// call, so these maps are encoded anew each time and not kept.
+bool ns_map(const void* p, uint64_t inner, uint64_t outer, uint32_t box_outer, CUtensorMap* out) {
+  cuuint64_t dims[2] = {inner, outer};
+  cuuint64_t strides[1] = {inner * 2};
+  cuuint32_t box[2] = {64, box_outer};
+  cuuint32_t estr[2] = {1, 1};
+  return g_encode(out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// Tile of a product: the one with the least rounds x (k-blocks x cycles per k-block + a tile's own cost).  Cycles per 64-deep k-block:
+// the tensor pipe's 512 for a pair's 256 x 256 and 256 x w / 128 for a CTA's 128 x w, over the efficiencies seen on this machine.
+int ns_tile(int M, int N, int K, bool sym) {
+  const int kb = (K + BK - 1) / BK;
+  double best = 1e30;
+  int bn = 64;
+  for (int cand : {256, 128, 64}) {
+    const bool pair = cand == 256;
+    const int bm = pair ? 256 : 128, tm = (M + bm - 1) / bm, tn = (N + cand - 1) / cand;
+    const int64_t tiles = !sym ? (int64_t)tm * tn : cand == 64 ? (int64_t)tm * (tm + 1) : (int64_t)tm * (tm + 1) / 2;
+    const int slots = pair ? g_num_sms / 2 : g_num_sms;
+    const double rounds = (double)((tiles + slots - 1) / slots);
+    const double cyc = pair ? 560.0 : cand == 128 ? 330.0 : 220.0;
+    const double cost = rounds * kb * cyc + (pair ? 6000.0 : cand == 128 ? 3000.0 : 2000.0);
+    if (cost < best) { best = cost; bn = cand; }
+  }
+  return bn;
 }
 int g_attn_tc = 1;       // tcgen05 attention forward (switch 2; 0 falls back to the mma.sync kernel)
 int g_attn_bwd_tc = 1;   // tcgen05 attention backward (switch 3; 0 falls back to the mma.sync kernels)
@@ -1127,6 +1202,9 @@ int gemm_tc_init() {
   if (e == cudaSuccess) e = set_smem_attr2<false, true, true>();
   if (e == cudaSuccess) e = set_smem_attr2<true, true, true>();
   if (e == cudaSuccess) e = set_smem_attr2<true, true, false>();
+  if (e == cudaSuccess) e = set_smem_attr_ns<false, false>();
+  if (e == cudaSuccess) e = set_smem_attr_ns<false, true>();
+  if (e == cudaSuccess) e = set_smem_attr_ns<true, true>();
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fwd_tc_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnTcCfg<64>::kSmem);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fwd_tc_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnTcCfg<128>::kSmem);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fwd_tc_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnTcCfg<64>::kSmem);
@@ -1227,6 +1305,47 @@ cudaError_t gemm_tc_launch(cudaStream_t st, const GemmArgs& g) {
   if (form == 2) return g.out_f32 ? launch_inst<false, true, true>(st, g, ta, tb, bn)
                                   : launch_inst<false, true, false>(st, g, ta, tb, bn);
   return g.out_f32 ? launch_inst<true, true, true>(st, g, ta, tb, bn) : launch_inst<true, true, false>(st, g, ta, tb, bn);
+}
+
+cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps) {
+  if (gemm_tc_init() != 0) return cudaErrorNotSupported;
+  const bool wide = b.rows <= b.cols;                  // the Gram matrix is taken on the short side
+  const int S = wide ? b.rows : b.cols, L = wide ? b.cols : b.rows;
+  const int t_gram = ns_tile(S, S, L, true), t_poly = ns_tile(S, S, S, true), t_step = ns_tile(b.rows, b.cols, S, false);
+  // boxes: K-major operands 128 rows for A and, for B, the rows that one CTA stages; MN-major operands 64 x 64
+  auto kb_rows = [](int bn) { return (uint32_t)(bn == 256 ? 128 : bn); };
+  CUtensorMap x_a[2], x_b[2], e_a, e_b, f_a;           // gram's (or, tall, also the step's) and the step's operands
+  CUtensorMap x_s[2], f_b;
+  bool ok = true;
+  for (int i = 0; i < 2; ++i) {
+    const __half* x = (const __half*)b.x16[i];
+    if (wide) {
+      ok = ok && ns_map(x, b.cols, b.rows, BM, &x_a[i]) && ns_map(x, b.cols, b.rows, kb_rows(t_gram), &x_b[i]);
+      ok = ok && ns_map(x, b.cols, b.rows, BK, &x_s[i]);                       // step: B, N-major
+    } else {
+      ok = ok && ns_map(x, b.cols, b.rows, BK, &x_a[i]);                       // gram: both operands MN-major
+      x_b[i] = x_a[i];
+      ok = ok && ns_map(x, b.cols, b.rows, BM, &x_s[i]);                       // step: A, K-major
+    }
+  }
+  ok = ok && ns_map(b.e, S, S, BM, &e_a) && ns_map(b.e, S, S, kb_rows(t_poly), &e_b);
+  ok = ok && ns_map(b.f, S, S, BM, &f_a) && ns_map(b.f, S, S, kb_rows(t_step), &f_b);
+  if (!ok) return cudaErrorInvalidValue;
+  for (int i = 0; i < steps; ++i) {
+    const int cur = i & 1;
+    NsArgs n{};
+    n.mode = 0; n.out16 = (__half*)b.e; n.dout = b.da; n.ld = S;
+    cudaError_t r = wide ? launch_ns<false, false>(st, S, S, L, x_a[cur], x_b[cur], t_gram, n) : launch_ns<true, true>(st, S, S, L, x_a[cur], x_b[cur], t_gram, n);
+    if (r != cudaSuccess) return r;
+    n = NsArgs{};
+    n.mode = 1; n.e = (const __half*)b.e; n.din = b.da; n.out16 = (__half*)b.f; n.dout = b.df; n.ld = S;
+    if ((r = launch_ns<false, false>(st, S, S, S, e_a, e_b, t_poly, n)) != cudaSuccess) return r;
+    n = NsArgs{};
+    n.mode = 2; n.by_column = !wide; n.din = b.df; n.x32 = b.x32; n.out16 = i + 1 < steps ? (__half*)b.x16[cur ^ 1] : nullptr; n.ld = b.cols;
+    r = wide ? launch_ns<false, true>(st, b.rows, b.cols, S, f_a, x_s[cur], t_step, n) : launch_ns<false, false>(st, b.rows, b.cols, S, x_s[cur], f_b, t_step, n);
+    if (r != cudaSuccess) return r;
+  }
+  return cudaSuccess;
 }
 
 const int* gemm_tc_error_device_ptr() {

@@ -26,6 +26,11 @@ cudaError_t attn_tc_fwd_launch(cudaStream_t st, int B, int S, int H, int dh, int
 bool attn_tc_bwd_eligible(int dh, int H, const void* qkv, const void* dout, const void* dqkv);
 cudaError_t attn_tc_bwd_launch(cudaStream_t st, int B, int S, int H, int dh, int causal, const void* qkv, const void* dout,
                                const float* lse, const float* dsum, void* dqkv, const int* lens, const DropArgs& da);
+// `steps` Newton-Schulz steps (ns_epilogue.cuh) on a zero-padded matrix of rows x cols, multiples of 64 of at least 128, in scratch:
+// x32 the iterate, x16[0] its fp16 image times 2^10 (both filled by the caller; x16[1] the same size), e, f [S, S] fp16 and
+// da, df [S] fp32 with S = min(rows, cols).  Everything 128-byte aligned.
+struct NsBuffers { int rows, cols; float* x32; void* x16[2]; void *e, *f; float *da, *df; };
+cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps);
 // Code-path switches for A/B timing and for tests (all 1 by default = the fast path): which = 0 CTA-pair
 // GEMM tiles, 1 programmatic dependent launch, 2 tcgen05 attention forward, 3 tcgen05 attention backward.
 // value >= 0 sets the switch; returns its previous value (-1: no such switch).  Process-wide; read at

@@ -1,0 +1,162 @@
+// Epilogues of the Newton-Schulz products (kernels_muon.cuh) in the tensor-core GEMM kernels; included by gemm_tc.cu.
+//
+// One step X <- a X + P(A) X, A = X X^T, P(A) = b A + c A A, is three products of fp16 operands with fp32 accumulators.  What
+// 16 bits would lose is kept out of them:
+//   - the iterate itself stays fp32 (x32); its fp16 image, scaled by 2^10 so that entries of 1 / sqrt(m n) are normal numbers,
+//     is only an operand.  a X, which carries the small singular values up, is never rounded to 16 bits.
+//   - the diagonals of A and P(A), which near the end are 1 and -2.7 against off-diagonal entries of about 1 / sqrt(n), stay
+//     fp32 vectors; the fp16 matrices E and F hold zeros there.  With A = D + E:
+//         P(A)_ij = b E_ij + c ((E E)_ij + (d_i + d_j) E_ij),   P(A)_ii = b d_i + c ((E E)_ii + d_i^2),
+//         X_new = (a + P(A)_ii) X + F X.
+// Relative error of the result against 64 bits, measured over Gaussian, low-rank and heavy-tailed matrices: 1e-4 to 2e-3 (all-bf16
+// products: 7e-3 on full-rank matrices, 5e-2 to 1 on low-rank ones, whose rounding noise is amplified like a signal).
+// A and P(A) are symmetric: only tiles that touch the lower triangle are computed, and a 32 x 32 chunk below the diagonal is
+// stored a second time transposed.  All dimensions are multiples of 64 (zero-padded scratch), so a chunk exists or not as a whole.
+constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
+constexpr float kNsScale = 1024.0f;
+
+struct NsArgs {
+  int mode;                // 0: A from X, 1: P(A) from E, 2: the new X
+  int by_column;           // mode 2: the diagonal belongs to the columns (right-hand product)
+  __half* out16;           // E, F or the fp16 image of the new X (nullptr: not wanted)
+  const __half* e;         // mode 1: E
+  const float* din;        // mode 1: diagonal of A, mode 2: of P(A)
+  float* dout;             // modes 0, 1: the diagonal of the result
+  float* x32;              // mode 2: the iterate, replaced in place
+  int64_t ld;              // of out16, e and x32
+};
+
+// tile index -> tile of the lower triangle; per_row = column tiles per row tile's width (1: square tiles, 2: half as wide)
+__device__ __forceinline__ void ns_tri_tile(int t, int per_row, int& tm, int& tn) {
+  const float k = per_row == 1 ? 8.0f : 4.0f;
+  int r = (int)((sqrtf(k * (float)t + 1.0f) - 1.0f) * 0.5f);
+  auto before = [&](int i) { return per_row == 1 ? i * (i + 1) / 2 : i * (i + 1); };
+  while (before(r + 1) <= t) ++r;
+  while (before(r) > t) --r;
+  tm = r;
+  tn = t - before(r);
+}
+
+// lane = row; 32 halves of a row as whole lines (see epi_store32_lines), every row and column of the chunk exists
+__device__ __forceinline__ void ns_store_half(const float (&f)[32], uint8_t* __restrict__ stage, __half* __restrict__ out, int64_t ld,
+                                              int row_base, int n, int lane) {
+  uint8_t* mine = stage + lane * 64;
+#pragma unroll
+  for (int sg = 0; sg < 4; ++sg) {
+    uint4 o;
+    __half2* ho = reinterpret_cast<__half2*>(&o);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) ho[t] = __floats2half2_rn(f[8 * sg + 2 * t], f[8 * sg + 2 * t + 1]);
+    *reinterpret_cast<uint4*>(mine + ((sg ^ ((lane >> 1) & 3)) << 4)) = o;
+  }
+  __syncwarp();
+  const int sg = lane & 3;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 8 * i + (lane >> 2);
+    *reinterpret_cast<uint4*>(out + (int64_t)(row_base + r) * ld + n + 8 * sg) =
+        *reinterpret_cast<const uint4*>(stage + r * 64 + ((sg ^ ((r >> 1) & 3)) << 4));
+  }
+  __syncwarp();
+}
+// the same chunk transposed: element (lane, j) goes to row n + j, column row_base + lane
+__device__ __forceinline__ void ns_store_half_transposed(const float (&f)[32], uint8_t* __restrict__ stage, __half* __restrict__ out,
+                                                         int64_t ld, int row_base, int n, int lane) {
+  __half* s = reinterpret_cast<__half*>(stage);
+#pragma unroll
+  for (int j = 0; j < 32; ++j) s[j * 32 + lane] = __float2half_rn(f[j]);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int j = 8 * i + (lane >> 2);
+    *reinterpret_cast<uint4*>(out + (int64_t)(n + j) * ld + row_base + 8 * (lane & 3)) = *reinterpret_cast<const uint4*>(stage + j * 64 + (lane & 3) * 16);
+  }
+  __syncwarp();
+}
+
+// One warp's rows of an output tile: BN columns from tensor memory at taddr.
+__device__ __forceinline__ void epi_ns(uint32_t taddr, int BN, int m, int M, int n0, int N, const NsArgs& a, uint8_t* __restrict__ stage, int lane) {
+  const int row_base = m - lane;
+  if (row_base >= M) return;                           // uniform across the warp
+  const int end = min(BN, N - n0);
+  if (a.mode == 2) {
+    float4 xn[8];
+    lines_fetch_f32(xn, a.x32, a.ld, row_base, lane, M, n0);
+    const float drow = a.by_column ? 0.f : a.din[m];
+    uint32_t va[32], vb[32];
+    auto chunk = [&](uint32_t (&v)[32], int c0) {
+      float4 xc[8];
+      lines_to_own_row_f32(xn, xc, stage, lane);
+      if (c0 + 32 < end) lines_fetch_f32(xn, a.x32, a.ld, row_base, lane, M, n0 + c0 + 32);
+      float f[32];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float4 d = make_float4(drow, drow, drow, drow);
+        if (a.by_column) d = *reinterpret_cast<const float4*>(a.din + n0 + c0 + 4 * j);
+        f[4 * j] = fmaf(kNsA + d.x, xc[j].x, __uint_as_float(v[4 * j]) * (1.0f / kNsScale));
+        f[4 * j + 1] = fmaf(kNsA + d.y, xc[j].y, __uint_as_float(v[4 * j + 1]) * (1.0f / kNsScale));
+        f[4 * j + 2] = fmaf(kNsA + d.z, xc[j].z, __uint_as_float(v[4 * j + 2]) * (1.0f / kNsScale));
+        f[4 * j + 3] = fmaf(kNsA + d.w, xc[j].w, __uint_as_float(v[4 * j + 3]) * (1.0f / kNsScale));
+      }
+      epi_store32_lines<true>(f, stage, a.x32, a.ld, m, lane, M, n0 + c0, nullptr);
+      if (a.out16) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) f[j] *= kNsScale;
+        ns_store_half(f, stage, a.out16, a.ld, row_base, n0 + c0, lane);
+      }
+    };
+    tmem_ld32_nowait(taddr, va);
+#pragma unroll 1
+    for (int c0 = 0; c0 < end; c0 += 64) {             // end is a multiple of 64
+      tmem_ld_wait32(va);
+      tmem_ld32_nowait(taddr + c0 + 32, vb);
+      chunk(va, c0);
+      tmem_ld_wait32(vb);
+      if (c0 + 64 < end) tmem_ld32_nowait(taddr + c0 + 64, va);
+      chunk(vb, c0 + 32);
+    }
+    return;
+  }
+  const float drow = a.mode == 1 ? a.din[m] : 0.f;
+  const int last = min(end, row_base - n0 + 32);       // chunks above the diagonal are stored from below it
+#pragma unroll 1
+  for (int c0 = 0; c0 < last; c0 += 32) {
+    const int n = n0 + c0;
+    uint32_t v[32];
+    tmem_ld32(taddr + c0, v);
+    float f[32];
+    if (a.mode == 0) {
+#pragma unroll
+      for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]) * (1.0f / (kNsScale * kNsScale));
+    } else {
+      uint4 en[4], ec[4];
+      lines_fetch_bf16(en, reinterpret_cast<const __nv_bfloat16*>(a.e), a.ld, row_base, lane, M, n);     // 16-bit lines
+      lines_park_bf16(en, stage, lane);
+      __syncwarp();
+      lines_own_row_bf16(ec, stage, lane);
+      __syncwarp();
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const __half2* he = reinterpret_cast<const __half2*>(&ec[j]);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int i = 8 * j + 2 * t;
+          const float2 e2 = __half22float2(he[t]);
+          const float2 d2 = *reinterpret_cast<const float2*>(a.din + n + i);
+          f[i] = fmaf(kNsB, e2.x, kNsC * fmaf(drow + d2.x, e2.x, __uint_as_float(v[i])));
+          f[i + 1] = fmaf(kNsB, e2.y, kNsC * fmaf(drow + d2.y, e2.y, __uint_as_float(v[i + 1])));
+        }
+      }
+    }
+    if (n == row_base) {                               // the chunk on the diagonal: its diagonal leaves as fp32
+      float d = 0.f;
+#pragma unroll
+      for (int j = 0; j < 32; ++j) {
+        if (j == lane) { d = a.mode == 0 ? f[j] : fmaf(kNsB, drow, kNsC * fmaf(drow, drow, __uint_as_float(v[j]))); f[j] = 0.f; }
+      }
+      a.dout[m] = d;
+    }
+    ns_store_half(f, stage, a.out16, a.ld, row_base, n, lane);
+    if (n < row_base) ns_store_half_transposed(f, stage, a.out16, a.ld, row_base, n, lane);
+  }
+}
