@@ -106,6 +106,20 @@ __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+// The issuing warp runs its loop as a whole and only `lead` (one lane) issues: descriptors, addresses and loop state stay
+// uniform, so they live in uniform registers.  With the loop inside `if (lane == 0)` every operand of every MMA is moved there
+// by instructions of its own, and one thread could issue a 64-deep k-block only every 700 cycles, whatever the tile's size.
+__device__ __forceinline__ void tc_commit_lead(uint32_t bar, uint32_t lead) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+               "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(lead) : "memory");
+}
+__device__ __forceinline__ void tc_mma_lead(uint32_t tmem_c, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accum, uint32_t lead) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(tmem_c), "l"(da), "l"(db), "r"(idesc), "r"(accum), "r"(lead) : "memory");
+}
 __device__ __forceinline__ void tc_mma(uint32_t tmem_c, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accum) {
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
@@ -645,7 +659,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
   uint8_t* smem_gen = smem_raw + (base - smem_u32(smem_raw));
   volatile uint32_t* tmem_slot_gen = reinterpret_cast<volatile uint32_t*>(smem_gen + S * kStageBytes + 8 * (2 * S + 4));
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int num_kb = (K + BK - 1) / BK;
 
   if (threadIdx.x == 0) {
@@ -702,8 +716,9 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       }
     }
   } else if (warp == 1) {
-    // ---------------- MMA issuer (one thread)
-    if (lane == 0 && !poisoned) {
+    // ---------------- MMA issuer (one lane of a converged warp)
+    if (!poisoned) {
+      const uint32_t lead = lane == 0;
       // instruction descriptor: D fp32 (bits 4-5 = 1), A and B bf16 (bits 7-9, 10-12 = 1),
       // A / B major-ness (bits 15, 16: 1 = MN-major), N/8 at bits 17-22, M/16 at bits 24-28
       // (NS: both fp16, 0)
@@ -716,11 +731,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
         const int ab = lt & 1;
         const uint32_t aph = (lt >> 1) & 1;
         // the epilogue must have drained this accumulator (passes at once on its first use)
-        if (!mbar_wait(acc_empty(ab), aph ^ 1)) { atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(acc_empty(ab), aph ^ 1))) { if (lead) atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
         tc_fence_after();
         const uint32_t tacc = tmem_base + (uint32_t)(ab * kAccStride);
         for (int kb = 0; kb < num_kb; ++kb) {
-          if (!mbar_wait(full_bar(s), ph)) { atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
+          if (!__all_sync(0xffffffffu, mbar_wait(full_bar(s), ph))) { if (lead) atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
           tc_fence_after();
           const uint32_t sa = base + s * kStageBytes, sb = sa + kABytes;
           const uint64_t da = make_desc(sa, A_MN), db = make_desc(sb, B_MN);
@@ -730,12 +745,12 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             // 16 k-rows of 128 B (MN-major); descriptor addresses are in 16-byte units
             const uint64_t adv_a = A_MN ? (uint64_t)(kk * UMMA_K * 128 >> 4) : (uint64_t)(kk * UMMA_K * 2 >> 4);
             const uint64_t adv_b = B_MN ? (uint64_t)(kk * UMMA_K * 128 >> 4) : (uint64_t)(kk * UMMA_K * 2 >> 4);
-            tc_mma(tacc, da + adv_a, db + adv_b, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+            tc_mma_lead(tacc, da + adv_a, db + adv_b, idesc, (kb > 0 || kk > 0) ? 1u : 0u, lead);
           }
-          tc_commit(empty_bar(s));       // frees the stage once these MMAs have read it
+          tc_commit_lead(empty_bar(s), lead);       // frees the stage once these MMAs have read it
           if (++s == S) { s = 0; ph ^= 1; }
         }
-        tc_commit(acc_full(ab));         // accumulator complete (or abandoned: g_tc_error tells the epilogue)
+        tc_commit_lead(acc_full(ab), lead);         // accumulator complete (or abandoned: g_tc_error tells the epilogue)
       }
     }
   } else {

@@ -6,114 +6,493 @@
 //   H = -sum_i p_i log p_i = L - sum_i exp((x_i - m) / T) (x_i - m) / T / (1 + r)
 //   d x_i = (1 / T) ( g (delta_it - p_i) - h p_i (log p_i + H) )          g = d log p_t, h = d H
 // The maximum's own 1 is kept out of r, so that log1p(r) is exact to fp32 for a row that is nearly sure of one token.
+//
+// Forward: one pass over the row, 16 bytes a load, four loads (a batch) in flight per thread.  A thread keeps a running maximum,
+// moved once per batch, and its sums of e and e (x - m) relative to it; the block (and, for few rows, the up to eight
+// blocks of a cluster that share a row) joins them at the end.  The alternatives cost no second pass: the k-th largest of
+// the threads' own maxima is a lower bound of the k-th largest logit, so only the few threads whose maximum reaches it can
+// hold one, and their warps read those threads' elements again out of L2.  The same re-reading makes r exact when it is
+// small: only the thread that holds the maximum added it to anything.
 #pragma once
 #include "common.cuh"
 
 namespace hift {
 
-
 constexpr float kLowest = -3.402823466e38f;
+constexpr float kLog2E = 1.4426950408889634f, kLogLn2 = 0.6931471805599453f;
+constexpr int kLpMaxTop = 32;
+constexpr int kLpCand = 512;              // alternatives a block can collect before it falls back to whole passes
+constexpr int kLpBatch = 4;
 
-// One block per row, three passes over the row, then one pass per alternative.
+__device__ __forceinline__ float lp_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// two fp32 values in one 64-bit register: one instruction for both
+__device__ __forceinline__ uint64_t f2_pack(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void f2_unpack(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b) { uint64_t r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b) { uint64_t r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) { uint64_t r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+
+// 16 bytes of logits: V elements as V / 2 pairs
+template <typename T> struct LpVec;
+template <> struct LpVec<float> {
+  static constexpr int V = 4;
+  __device__ static uint4 missing() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
+  __device__ static float max(const uint4& v) { return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w))); }
+  __device__ static void pairs(const uint4& v, float (&a)[2], float (&b)[2]) {
+    a[0] = __uint_as_float(v.x); b[0] = __uint_as_float(v.y); a[1] = __uint_as_float(v.z); b[1] = __uint_as_float(v.w);
+  }
+  __device__ static uint4 join(const float (&a)[2], const float (&b)[2]) {
+    return make_uint4(__float_as_uint(a[0]), __float_as_uint(b[0]), __float_as_uint(a[1]), __float_as_uint(b[1]));
+  }
+};
+template <> struct LpVec<bf16> {
+  static constexpr int V = 8;
+  __device__ static uint4 missing() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
+  __device__ static float max(const uint4& v) {
+    const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&v);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+  __device__ static void pairs(const uint4& v, float (&a)[4], float (&b)[4]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { a[i] = __uint_as_float(w[i] << 16); b[i] = __uint_as_float(w[i] & 0xffff0000u); }
+  }
+  __device__ static uint4 join(const float (&a)[4], const float (&b)[4]) {
+    uint4 v;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(a[i], b[i]);
+    return v;
+  }
+};
+
+// A row as 16-byte vectors: `head` elements before the first aligned address, nv vectors, the rest.  The up to 2 (V - 1)
+// single elements outside the vectors are numbered 0 .. ns - 1.
+struct LpRow { int head, nv, ns; };
 template <typename T>
-__global__ void token_logprobs_kernel(const T* __restrict__ logits, const int32_t* __restrict__ tokens, int vocab, int64_t ld,
-                                      int64_t rows, float scale, int n_top, float* __restrict__ logp, float* __restrict__ entropy,
-                                      float* __restrict__ stats, int32_t* __restrict__ top_ids, float* __restrict__ top_logp,
-                                      int32_t* __restrict__ bad) {
-  __shared__ float red[33];
-  __shared__ int first_max;
-  __shared__ unsigned long long best;
-  const int64_t row = blockIdx.x;
-  const T* x = logits + row * ld;
-  const int tok = tokens[row];
-  if (tok < 0 || tok >= vocab) {
-    if (threadIdx.x == 0) {
-      if (tok >= vocab && bad) *bad = 1;
-      logp[row] = 0.f;
-      if (entropy) entropy[row] = 0.f;
-      if (stats) { stats[row] = 0.f; stats[rows + row] = 0.f; }
-      for (int k = 0; k < n_top; ++k) { top_ids[row * n_top + k] = -1; top_logp[row * n_top + k] = -INFINITY; }
-    }
-    return;
-  }
-  float mx = -INFINITY;
-  for (int c = threadIdx.x; c < vocab; c += blockDim.x) mx = fmaxf(mx, to_f(x[c]));
-  mx = block_max(mx, red);
-  const bool none = mx == -INFINITY;                              // nothing above -inf, but for NaN
-  mx = fmaxf(mx, kLowest);
-  if (threadIdx.x == 0) first_max = vocab;
-  __syncthreads();
-  for (int c = threadIdx.x; c < vocab; c += blockDim.x) if (to_f(x[c]) == mx) { atomicMin(&first_max, c); break; }
-  __syncthreads();
-  float r = 0.f, u = 0.f;
-  for (int c = threadIdx.x; c < vocab; c += blockDim.x) {
-    const float t = (to_f(x[c]) - mx) * scale, e = expf(t);     // a NaN, or +inf - +inf, makes r NaN
-    if (c != first_max) r += e;
-    u += e > 0.f ? e * t : 0.f;
-  }
-  r = block_sum(r, red);
-  u = block_sum(u, red);
-  const float nanv = __int_as_float(0x7fc00000);
-  const bool poison = !(r < INFINITY) || mx == INFINITY, empty = none && !poison;
-  const float L = log1pf(r);
-  if (threadIdx.x == 0) {
-    logp[row] = empty ? -INFINITY : poison ? nanv : (to_f(x[tok]) - mx) * scale - L;
-    if (entropy) entropy[row] = empty ? 0.f : poison ? nanv : L - u / (1.0f + r);
-    if (stats) { stats[row] = poison ? nanv : empty ? -INFINITY : mx; stats[rows + row] = empty ? 0.f : poison ? nanv : L; }
-  }
+__device__ __forceinline__ LpRow lp_row(const T* x, int n) {
+  constexpr int V = LpVec<T>::V;
+  LpRow r;
+  const int off = (int)(((uintptr_t)x & 15) / sizeof(T));
+  r.head = min(n, (V - off) % V);
+  r.nv = (n - r.head) / V;
+  r.ns = n - r.nv * V;
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ int lp_single(const LpRow& r, int s) { return s < r.head ? s : r.nv * LpVec<T>::V + s; }
+
+// orders like the value (-0 = +0), -inf lowest; for values that are not NaN
+__device__ __forceinline__ uint32_t lp_order(float v) {
+  const uint32_t o = __float_as_uint(v + 0.0f);
+  return (o & 0x80000000u) ? ~o : (o | 0x80000000u);
+}
+__device__ __forceinline__ float lp_value(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? (o & 0x7fffffffu) : ~o); }
+constexpr uint32_t kLpNone = 0x007fffffu;         // lp_order(-inf)
+
+// largest key of the warp: the values first, then the indexes among the lanes that hold the largest value
+__device__ __forceinline__ unsigned long long lp_warp_max(unsigned long long key) {
+  const uint32_t hi = (uint32_t)(key >> 32);
+  const uint32_t mh = __reduce_max_sync(0xffffffffu, hi);
+  const uint32_t ml = __reduce_max_sync(0xffffffffu, hi == mh ? (uint32_t)key : 0u);
+  return ((unsigned long long)mh << 32) | ml;
+}
+// one warp: the n largest of the `have` distinct keys in falling order into out (0: no more)
+__device__ __forceinline__ void lp_select(unsigned long long* keys, int have, int n, unsigned long long* out, int lane) {
   unsigned long long last = ~0ull;
-  for (int k = 0; k < n_top; ++k) {
+  for (int k = 0; k < n; ++k) {
     unsigned long long mine = 0ull;
-    if (threadIdx.x == 0) best = 0ull;
-    __syncthreads();
-    if (!empty && !poison) {
-      for (int c = threadIdx.x; c < vocab; c += blockDim.x) {
-        const float v = to_f(x[c]);
-        if (v == -INFINITY) continue;
-        uint32_t o = __float_as_uint(v + 0.0f);
-        o = (o & 0x80000000u) ? ~o : (o | 0x80000000u);
-        const unsigned long long key = ((unsigned long long)o << 32) | (uint32_t)~c;
-        if (key < last && key > mine) mine = key;
-      }
-      if (mine) atomicMax(&best, mine);
-    }
-    __syncthreads();
-    last = best;
-    if (threadIdx.x == 0) {
-      const int c = last ? (int)~(uint32_t)last : -1;
-      top_ids[row * n_top + k] = c;
-      top_logp[row * n_top + k] = poison ? nanv : c < 0 ? -INFINITY : (to_f(x[c]) - mx) * scale - L;
-    }
-    __syncthreads();
-    if (last == 0ull) last = 1ull;                               // nothing left: nothing is below this key
+    for (int i = lane; i < have; i += 32) { const unsigned long long q = keys[i]; if (q < last && q > mine) mine = q; }
+    mine = lp_warp_max(mine);
+    if (lane == 0) out[k] = mine;
+    last = mine ? mine : 1ull;
   }
+  __syncwarp();
 }
 
-// One block per row: the gradient from the saved maximum, L and H.
+struct LpShared {
+  float red[4][16];                       // per warp: maximum, sum, weighted sum
+  uint32_t tmax[512];
+  unsigned long long cand[kLpCand];
+  unsigned long long top[kLpMaxTop];
+  unsigned long long best;
+  float m, rest, u, own_rest;             // of this block: maximum, r, sum of e log2 e; the owner's part of r
+  int has, owner, count;
+  uint32_t bound;
+};
+
+struct LpArgs {
+  const int32_t* tokens;
+  int vocab, n_top;
+  int64_t ld, rows;
+  float scale;
+  float *logp, *entropy, *stats, *top_logp;
+  int32_t *top_ids, *bad;
+};
+
 template <typename T>
-__global__ void token_logprobs_bwd_kernel(const T* __restrict__ logits, const int32_t* __restrict__ tokens, int vocab, int64_t ld,
-                                          int64_t rows, float scale, const float* __restrict__ stats, const float* __restrict__ entropy,
-                                          const float* __restrict__ dlogp, const float* __restrict__ dentropy, T* __restrict__ dlogits) {
-  const int64_t row = blockIdx.x;
-  const T* x = logits + row * ld;
-  T* d = dlogits + row * ld;
-  const int tok = tokens[row];
-  const float m = stats[row], L = stats[rows + row];
-  if (tok < 0 || tok >= vocab || m == -INFINITY) {
-    for (int64_t c = threadIdx.x; c < ld; c += blockDim.x) d[c] = from_f<T>(0.f);
+__global__ void __launch_bounds__(512) token_logprobs_kernel(const T* __restrict__ logits, LpArgs a) {
+  constexpr int V = LpVec<T>::V;
+  __shared__ LpShared sh;
+  uint32_t parts, part;                   // blocks of the cluster that share the row
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(parts));
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(part));
+  const int64_t row = blockIdx.x / parts;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, nt = blockDim.x, nw = nt >> 5;
+  const T* x = logits + row * a.ld;
+  const int tok = a.tokens[row];
+  if (tok < 0 || tok >= a.vocab) {        // uniform over the cluster
+    if (part == 0) {
+      if (tid == 0) {
+        if (tok >= 0 && a.bad) *a.bad = 1;
+        a.logp[row] = 0.f;
+        if (a.entropy) a.entropy[row] = 0.f;
+        if (a.stats) { a.stats[row] = 0.f; a.stats[a.rows + row] = 0.f; }
+      }
+      if (tid < a.n_top) { a.top_ids[row * a.n_top + tid] = -1; a.top_logp[row * a.n_top + tid] = -INFINITY; }
+    }
     return;
   }
-  const float g = dlogp ? dlogp[row] : 0.f, h = dentropy ? dentropy[row] : 0.f, H = dentropy ? entropy[row] : 0.f;
-  for (int64_t c = threadIdx.x; c < ld; c += blockDim.x) {
-    float v = 0.f;
-    if (c < vocab) {
-      const float lp = (to_f(x[c]) - m) * scale - L, p = expf(lp);
-      v = c == tok ? -expm1f(lp) * g : -p * g;
-      if (p > 0.f) v -= h * p * (lp + H);
-      v *= scale;
-    }
-    d[c] = from_f<T>(v);
+  const float xt = to_f(x[tok]);
+  const LpRow rw = lp_row(x, a.vocab);
+  const uint4* xv = reinterpret_cast<const uint4*>(x + rw.head);
+  const int per = (rw.nv + (int)parts - 1) / (int)parts;
+  const int v0 = min(rw.nv, per * (int)part), v1 = min(rw.nv, v0 + per);
+  const int ns = part == 0 ? rw.ns : 0;   // the single elements go to the first block's first threads
+  const float s2 = a.scale * kLog2E;
+
+  // ---- one pass: maximum, sum of e, sum of e log2 e (bounded, unlike e (x - m)), all relative to the thread's running maximum
+  float tmax = -INFINITY, m = kLowest;
+  uint64_t s = 0ull, u = 0ull;            // pairs of partial sums
+  auto move_max = [&](float top) {
+    tmax = fmaxf(tmax, top);
+    const float mn = fmaxf(m, top), d = (m - mn) * s2, f = lp_ex2(d), dc = f > 0.f ? d : 0.f;     // d is 0 where the maximum stays
+    const uint64_t ff = f2_pack(f, f);
+    u = f2_mul(f2_fma(s, f2_pack(dc, dc), u), ff);
+    s = f2_mul(s, ff);
+    m = mn;
+  };
+  auto add_pair = [&](float p, float q, uint64_t nm, uint64_t sc) {
+    const uint64_t d = f2_add(f2_pack(p, q), nm), t = f2_mul(d, sc);
+    float t0, t1;
+    f2_unpack(t, t0, t1);
+    const uint64_t e = f2_pack(lp_ex2(t0), lp_ex2(t1));
+    s = f2_add(s, e);
+    u = f2_fma(e, f2_pack(fmaxf(t0, kLowest), fmaxf(t1, kLowest)), u);     // 0 x -inf would be NaN
+  };
+  const uint64_t sc = f2_pack(s2, s2);
+  if (tid < ns) {
+    const float v = to_f(x[lp_single<T>(rw, tid)]);
+    move_max(v);
+    add_pair(v, -INFINITY, f2_pack(-m, -m), sc);
   }
+  for (int c = v0 + tid; c < v1; c += kLpBatch * nt) {
+    uint4 w[kLpBatch];
+#pragma unroll
+    for (int k = 0; k < kLpBatch; ++k) w[k] = c + k * nt < v1 ? __ldg(xv + c + k * nt) : LpVec<T>::missing();
+    float top = LpVec<T>::max(w[0]);
+#pragma unroll
+    for (int k = 1; k < kLpBatch; ++k) top = fmaxf(top, LpVec<T>::max(w[k]));
+    move_max(top);
+    const uint64_t nm = f2_pack(-m, -m);
+#pragma unroll
+    for (int k = 0; k < kLpBatch; ++k) {
+      float p[V / 2], q[V / 2];
+      LpVec<T>::pairs(w[k], p, q);
+#pragma unroll
+      for (int i = 0; i < V / 2; ++i) add_pair(p[i], q[i], nm, sc);
+    }
+  }
+  // ---- the block's maximum, its owner, and the sums relative to it
+  sh.tmax[tid] = lp_order(tmax);
+  const float wm = warp_max(m);
+  if (lane == 0) sh.red[0][warp] = wm;
+  if (tid == 0) { sh.owner = 1 << 30; sh.count = 0; sh.best = 0ull; }
+  __syncthreads();
+  float M = kLowest;
+  for (int i = 0; i < nw; ++i) M = fmaxf(M, sh.red[0][i]);
+  float s0, s1, u0, u1;
+  f2_unpack(s, s0, s1);
+  f2_unpack(u, u0, u1);
+  {
+    const float d = (m - M) * s2, f = lp_ex2(d);
+    float st = s0 + s1, ut = u0 + u1;
+    ut = f > 0.f ? (ut + st * d) * f : 0.f;                            // (a NaN shows in the sum below)
+    st *= f;
+    const bool own = tmax == M;
+    const unsigned who = __ballot_sync(0xffffffffu, own);
+    if (who != 0u && lane == 0) atomicMin(&sh.owner, warp * 32 + __ffs(who) - 1);
+    st = warp_sum(st);
+    ut = warp_sum(ut);
+    if (lane == 0) { sh.red[1][warp] = st; sh.red[2][warp] = ut; }
+  }
+  // ---- a lower bound of the k-th largest: of the threads' maxima the k-th
+  const bool want_top = a.n_top > 0;
+  if (want_top && warp == 0) {
+    uint32_t key[16], bound = kLpNone;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) key[i] = i < nw ? sh.tmax[lane + 32 * i] : 0u;
+    for (int k = 0; k < a.n_top; ++k) {
+      uint32_t best = key[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) best = max(best, key[i]);
+      const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+      if (top <= kLpNone) { bound = kLpNone; break; }
+      bound = top;
+      const unsigned who = __ballot_sync(0xffffffffu, best == top);
+      if (lane == __ffs(who) - 1) {
+        bool gone = false;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) if (!gone && key[i] == top) { key[i] = 0u; gone = true; }
+      }
+    }
+    if (lane == 0) sh.bound = bound;
+  }
+  __syncthreads();
+  float S = 0.f, U = 0.f;
+  for (int i = 0; i < nw; ++i) { S += sh.red[1][i]; U += sh.red[2][i]; }
+  const int owner = sh.owner;
+  const bool has = owner < (1 << 30);                                   // something above -inf
+  float R = has ? S - 1.0f : S;
+  // every element of thread i, read again by its warp: lane j takes the thread's j-th vector, lane 31 a single element
+  auto reread = [&](int i, auto&& see) {
+    for (int c = v0 + i + lane * nt; c < v1; c += 32 * nt) {
+      const uint4 w = __ldg(xv + c);
+      float p[V / 2], q[V / 2];
+      LpVec<T>::pairs(w, p, q);
+#pragma unroll
+      for (int k = 0; k < V / 2; ++k) { see(p[k], rw.head + c * V + 2 * k); see(q[k], rw.head + c * V + 2 * k + 1); }
+    }
+    if (lane == 31 && i < ns) { const int at = lp_single<T>(rw, i); see(to_f(x[at]), at); }
+  };
+  if (has && R < 1.0f) {                                                // r is small: 1 + r has lost bits of it
+    if (warp == owner >> 5) {
+      float mine = 0.f, ties = 0.f;                                     // the owner's elements without one maximum
+      reread(owner, [&](float v, int) { if (v == M) ties += 1.0f; else mine += lp_ex2((v - M) * s2); });
+      mine = warp_sum(mine) + (warp_sum(ties) - 1.0f);
+      if (lane == 0) sh.own_rest = mine;
+    }
+    // the other threads' sums, joined again without the owner's
+    const float d = m - M;
+    float st = tid == owner ? 0.f : (s0 + s1) * lp_ex2(d * s2);
+    st = warp_sum(st);
+    if (lane == 0) sh.red[3][warp] = st;
+    __syncthreads();
+    R = sh.own_rest;
+    for (int i = 0; i < nw; ++i) R += sh.red[3][i];
+  }
+  // ---- alternatives: the threads whose maximum reaches the bound
+  const bool poison = !(S < INFINITY);                                  // a NaN or +inf among the logits
+  if (want_top && !poison && has) {
+    const uint32_t bound = sh.bound;
+    unsigned who = __ballot_sync(0xffffffffu, sh.tmax[tid] >= bound && sh.tmax[tid] > kLpNone);
+    while (who && *(volatile int*)&sh.count <= kLpCand) {
+      const int i = warp * 32 + __ffs(who) - 1;
+      who &= who - 1;
+      reread(i, [&](float v, int at) {
+        const uint32_t o = lp_order(v);
+        if (o >= bound && o > kLpNone) {
+          const int slot = atomicAdd(&sh.count, 1);
+          if (slot < kLpCand) sh.cand[slot] = ((unsigned long long)o << 32) | (uint32_t)~at;
+        }
+      });
+    }
+    __syncthreads();
+    if (sh.count <= kLpCand) {
+      if (warp == 0) lp_select(sh.cand, sh.count, a.n_top, sh.top, lane);
+    } else {                                                            // a great many equal logits: one pass per alternative
+      unsigned long long last = ~0ull;
+      for (int k = 0; k < a.n_top; ++k) {
+        unsigned long long mine = 0ull;
+        auto see = [&](float v, int at) {
+          const unsigned long long q = ((unsigned long long)lp_order(v) << 32) | (uint32_t)~at;
+          if (v > -INFINITY && q < last && q > mine) mine = q;
+        };
+        for (int c = v0 + tid; c < v1; c += nt) {
+          float p[V / 2], q[V / 2];
+          LpVec<T>::pairs(__ldg(xv + c), p, q);
+#pragma unroll
+          for (int i = 0; i < V / 2; ++i) { see(p[i], rw.head + c * V + 2 * i); see(q[i], rw.head + c * V + 2 * i + 1); }
+        }
+        if (tid < ns) { const int at = lp_single<T>(rw, tid); see(to_f(x[at]), at); }
+        mine = lp_warp_max(mine);
+        if (lane == 0 && mine) atomicMax(&sh.best, mine);
+        __syncthreads();
+        last = sh.best;
+        __syncthreads();
+        if (tid == 0) { sh.top[k] = last; sh.best = 0ull; }
+        if (last == 0ull) last = 1ull;
+        __syncthreads();
+      }
+    }
+  } else if (want_top && tid < kLpMaxTop) {
+    sh.top[tid] = 0ull;
+  }
+  // ---- join the blocks of a cluster in the first one
+  if (tid == 0) { sh.m = M; sh.rest = poison ? S : R; sh.u = U; sh.has = has; }
+  if (parts > 1) {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  } else {
+    __syncthreads();
+  }
+  if (part == 0 && warp == 0) {
+    float m_all = sh.m, r_all = sh.rest, u_all = sh.u;
+    int has_all = sh.has;
+    bool bad = poison;
+    unsigned long long* list = sh.top;
+    if (parts > 1) {
+      auto remote = [&](const void* p, uint32_t rank) {
+        uint32_t r;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+        return r;
+      };
+      auto ldf = [&](const void* p, uint32_t rank) { float v; asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote(p, rank))); return v; };
+      for (uint32_t k = 1; k < parts; ++k) {
+        const float mk = ldf(&sh.m, k), rk = ldf(&sh.rest, k), uk = ldf(&sh.u, k);
+        const int hk = __float_as_int(ldf(&sh.has, k));
+        bad = bad || !(rk < INFINITY);
+        if (mk > m_all || (!has_all && hk)) {                          // the other one's maximum leads
+          const float d = (m_all - mk) * s2, f = lp_ex2(d), w = r_all + (has_all ? 1.f : 0.f);
+          u_all = uk + (f > 0.f ? (u_all + w * d) * f : 0.f);
+          r_all = rk + w * f;
+          m_all = mk;
+        } else {
+          const float d = (mk - m_all) * s2, f = lp_ex2(d), w = rk + (hk ? 1.f : 0.f);
+          u_all += f > 0.f ? (uk + w * d) * f : 0.f;
+          r_all += w * f;
+        }
+        has_all |= hk;
+      }
+      if (want_top) {
+        for (int i = lane; i < (int)parts * a.n_top; i += 32) {
+          unsigned long long q;
+          asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(q) : "r"(remote(&sh.top[i % a.n_top], (uint32_t)(i / a.n_top))));
+          sh.cand[i] = q;
+        }
+        __syncwarp();
+        lp_select(sh.cand, (int)parts * a.n_top, a.n_top, sh.top, lane);
+      }
+    }
+    const float nanv = __int_as_float(0x7fc00000);
+    const bool empty = !has_all && !bad;
+    const float L = log1pf(r_all);
+    if (lane == 0) {
+      a.logp[row] = empty ? -INFINITY : bad ? nanv : (xt - m_all) * a.scale - L;
+      if (a.entropy) a.entropy[row] = empty ? 0.f : bad ? nanv : L - u_all * kLogLn2 / (1.0f + r_all);
+      if (a.stats) { a.stats[row] = bad ? nanv : empty ? -INFINITY : m_all; a.stats[a.rows + row] = empty ? 0.f : bad ? nanv : L; }
+    }
+    for (int k = lane; k < a.n_top; k += 32) {
+      const unsigned long long q = bad ? 0ull : list[k];
+      a.top_ids[row * a.n_top + k] = q ? (int32_t)~(uint32_t)q : -1;
+      a.top_logp[row * a.n_top + k] = bad ? nanv : q ? (lp_value((uint32_t)(q >> 32)) - m_all) * a.scale - L : -INFINITY;
+    }
+  }
+  if (parts > 1)                                                        // the peers' shared memory stays until it has been read
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Threads of a block and blocks per row: about four vectors a thread, and several blocks per row (a cluster) while the rows alone
+// leave SMs idle and a block would still have a vector per thread.
+inline void lp_shape(int64_t rows, int64_t vocab, int vec, int* threads, int* parts) {
+  const int64_t nv = vocab / vec;
+  int th = 32;
+  while (th < 512 && nv > 4 * th) th *= 2;
+  int p = 1;
+  while (p < 8 && rows * p * 2 <= 296 && nv >= 2 * p * th) p *= 2;
+  *threads = th;
+  *parts = p;
+}
+template <typename T>
+inline cudaError_t launch_token_logprobs(cudaStream_t st, const T* logits, const LpArgs& a) {
+  int th, parts;
+  lp_shape(a.rows, a.vocab, LpVec<T>::V, &th, &parts);
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof(cfg));
+  cfg.gridDim = dim3((unsigned)(a.rows * parts));
+  cfg.blockDim = dim3(th);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = parts > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, token_logprobs_kernel<T>, logits, a);
+}
+
+// ------------------------------------------------------------------ gradient
+// From the saved maximum, L and H; one pass, each element read and written once.  A task is up to 4 vectors per thread of a row;
+// blocks walk the tasks.  VEC: logits and gradient rows share their alignment, so both move 16 bytes at a time.
+struct LpBwdArgs {
+  const int32_t* tokens;
+  int vocab, chunks;
+  int64_t ld, rows;
+  float scale;
+  const float *stats, *entropy, *dlogp, *dentropy;
+};
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) token_logprobs_bwd_kernel(const T* logits, T* dlogits, LpBwdArgs a) {
+  constexpr int V = LpVec<T>::V;
+  const int tid = threadIdx.x, nt = blockDim.x;
+  for (int64_t task = blockIdx.x; task < a.rows * a.chunks; task += gridDim.x) {
+    const int64_t row = task / a.chunks;
+    const int part = (int)(task % a.chunks);
+    const T* x = logits + row * a.ld;
+    T* d = dlogits + row * a.ld;
+    const int tok = a.tokens[row];
+    const float m = a.stats[row], L = a.stats[a.rows + row];
+    const bool zero = tok < 0 || tok >= a.vocab || m == -INFINITY;
+    const float g = a.dlogp ? a.dlogp[row] * a.scale : 0.f, h = a.dentropy ? a.dentropy[row] * a.scale : 0.f;
+    const float hH = a.dentropy ? h * a.entropy[row] : 0.f, c0 = g + hH;
+    const float s2 = a.scale, l2 = kLog2E;
+    auto grad = [&](float v, int64_t at) {
+      if (zero || at >= a.vocab) return 0.f;
+      const float lp = (v - m) * s2 - L, p = lp_ex2(lp * l2);
+      const float w = fmaxf(lp, -200.f);                     // p is 0 there; p x -inf would be NaN
+      if (at != tok) return -p * fmaf(h, w, c0);
+      return -expm1f(lp) * g - p * fmaf(h, w, hH);         // 1 - p of a token that is nearly sure
+    };
+    if (VEC) {
+      const LpRow rw = lp_row(x, (int)a.ld);
+      const uint4* xv = reinterpret_cast<const uint4*>(x + rw.head);
+      uint4* dv = reinterpret_cast<uint4*>(d + rw.head);
+      const int c0v = part * 4 * nt + tid;
+      uint4 w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) if (!zero && c0v + k * nt < rw.nv) w[k] = xv[c0v + k * nt];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int c = c0v + k * nt;
+        if (c >= rw.nv) break;
+        const int64_t at = rw.head + (int64_t)c * V;
+        float p[V / 2], q[V / 2];
+        LpVec<T>::pairs(w[k], p, q);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) { p[i] = grad(p[i], at + 2 * i); q[i] = grad(q[i], at + 2 * i + 1); }
+        dv[c] = LpVec<T>::join(p, q);
+      }
+      if (part == 0 && tid < rw.ns) { const int at = lp_single<T>(rw, tid); d[at] = from_f<T>(grad(zero ? 0.f : to_f(x[at]), at)); }
+    } else {
+      for (int64_t c = (int64_t)part * 4 * nt * V + tid; c < min(a.ld, ((int64_t)part + 1) * 4 * nt * V); c += nt) d[c] = from_f<T>(grad(zero ? 0.f : to_f(x[c]), c));
+    }
+  }
+}
+template <typename T>
+inline cudaError_t launch_token_logprobs_bwd(cudaStream_t st, const T* logits, T* dlogits, LpBwdArgs a) {
+  constexpr int V = LpVec<T>::V;
+  const int64_t nv = (a.ld + V - 1) / V;
+  int th = 32;
+  while (th < 256 && nv > 4 * th) th *= 2;
+  a.chunks = (int)((nv + 4 * th - 1) / (4 * th));
+  const int64_t tasks = a.rows * a.chunks;
+  const unsigned grid = (unsigned)(tasks < (1 << 30) ? tasks : (1 << 30));
+  if ((((uintptr_t)logits ^ (uintptr_t)dlogits) & 15) == 0) token_logprobs_bwd_kernel<T, true><<<grid, th, 0, st>>>(logits, dlogits, a);
+  else token_logprobs_bwd_kernel<T, false><<<grid, th, 0, st>>>(logits, dlogits, a);
+  return cudaGetLastError();
 }
 
 }  // namespace hift

@@ -9,13 +9,15 @@
 
 using namespace hift;
 
+static_assert(kLpMaxTop == HIFT_MAX_TOP, "");
+
 namespace {
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 hift_status done() { return cudaGetLastError() == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA; }
 
 hift_status logprobs_cfg(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, double temperature, float* scale) {
-  if (dtype < 0 || dtype > 1 || rows < 0 || rows > INT32_MAX || vocab < 1 || vocab > INT32_MAX - 65536 || ld < vocab) return HIFT_ERR_CFG;
+  if (dtype < 0 || dtype > 1 || rows < 0 || rows > INT32_MAX || vocab < 1 || ld < vocab || ld > INT32_MAX - 65536) return HIFT_ERR_CFG;
   *scale = (float)(1.0 / temperature);
   if (!(temperature > 0.0) || !isfinite(temperature) || !isnormal(*scale)) return HIFT_ERR_CFG;
   return HIFT_OK;
@@ -93,12 +95,10 @@ hift_status hift_k_token_logprobs(int32_t dtype, int64_t rows, int64_t vocab, in
   if (rows == 0) return HIFT_OK;
   if (!logits || !tokens || !logp || (n_top > 0 && (!top_ids || !top_logp))) return HIFT_ERR_INPUT;
   if (!aligned(logits, dtype == 0 ? 4 : 2)) return HIFT_ERR_CFG;
-  const int th = vocab >= 4096 ? 512 : 128;
-  if (dtype == 0)
-    token_logprobs_kernel<float><<<(unsigned)rows, th, 0, (cudaStream_t)stream>>>((const float*)logits, tokens, (int)vocab, ld, rows, scale, n_top, logp, entropy, stats, top_ids, top_logp, bad);
-  else
-    token_logprobs_kernel<bf16><<<(unsigned)rows, th, 0, (cudaStream_t)stream>>>((const bf16*)logits, tokens, (int)vocab, ld, rows, scale, n_top, logp, entropy, stats, top_ids, top_logp, bad);
-  return done();
+  const LpArgs a{tokens, (int)vocab, n_top, ld, rows, scale, logp, entropy, stats, top_logp, top_ids, bad};
+  const cudaError_t e = dtype == 0 ? launch_token_logprobs((cudaStream_t)stream, (const float*)logits, a)
+                                   : launch_token_logprobs((cudaStream_t)stream, (const bf16*)logits, a);
+  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
 }
 
 hift_status hift_k_token_logprobs_bwd(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void* logits, const int32_t* tokens,
@@ -110,12 +110,10 @@ hift_status hift_k_token_logprobs_bwd(int32_t dtype, int64_t rows, int64_t vocab
   if (rows == 0) return HIFT_OK;
   if (!logits || !tokens || !stats || !dlogits || (!dlogp && !dentropy) || (dentropy && !entropy)) return HIFT_ERR_INPUT;
   if (!aligned(logits, dtype == 0 ? 4 : 2) || !aligned(dlogits, dtype == 0 ? 4 : 2)) return HIFT_ERR_CFG;
-  const int th = vocab >= 4096 ? 512 : 128;
-  if (dtype == 0)
-    token_logprobs_bwd_kernel<float><<<(unsigned)rows, th, 0, (cudaStream_t)stream>>>((const float*)logits, tokens, (int)vocab, ld, rows, scale, stats, entropy, dlogp, dentropy, (float*)dlogits);
-  else
-    token_logprobs_bwd_kernel<bf16><<<(unsigned)rows, th, 0, (cudaStream_t)stream>>>((const bf16*)logits, tokens, (int)vocab, ld, rows, scale, stats, entropy, dlogp, dentropy, (bf16*)dlogits);
-  return done();
+  const LpBwdArgs a{tokens, (int)vocab, 0, ld, rows, scale, stats, entropy, dlogp, dentropy};
+  const cudaError_t e = dtype == 0 ? launch_token_logprobs_bwd((cudaStream_t)stream, (const float*)logits, (float*)dlogits, a)
+                                   : launch_token_logprobs_bwd((cudaStream_t)stream, (const bf16*)logits, (bf16*)dlogits, a);
+  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
 }
 
 hift_status hift_k_join_fwd(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double eps, double res_scale, const float* x,
