@@ -12,7 +12,6 @@
 namespace hift {
 
 constexpr int kJoinMaxCols = 16384;
-constexpr int kJoinCtas = 592;         // most row chunks of a backward call: 4 per SM
 constexpr int kJoinPlanes = 5;         // column sums of the backward pass: gain and bias of both norms, gate
 
 // sums of two values over the block; `red` is one of two buffers of 64 floats used in turn, so that one barrier does
@@ -44,14 +43,16 @@ __global__ void __launch_bounds__(512) join_fwd_kernel(JoinFwd p) {
   const int64_t row = blockIdx.x;
   const int64_t off = row * p.cols;
   const float inv = 1.0f / (float)p.cols;
-  float v[NC][8];
+  float v[NC][8], xv[NC][8];                           // both streams are under way before the first sum
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
     const int c = (threadIdx.x + k * blockDim.x) * 8;
-    if (c < p.cols) load8((const P*)p.h + off + c, v[k]);
-    else {
+    if (c < p.cols) {
+      load8((const P*)p.h + off + c, v[k]);
+      load8(p.x + off + c, xv[k]);
+    } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[k][i] = 0.f;
+      for (int i = 0; i < 8; ++i) v[k][i] = xv[k][i] = 0.f;
     }
   }
   // mean and reciprocal deviation of the row held in v (two passes over registers)
@@ -85,8 +86,7 @@ __global__ void __launch_bounds__(512) join_fwd_kernel(JoinFwd p) {
   for (int k = 0; k < NC; ++k) {
     const int c = (threadIdx.x + k * blockDim.x) * 8;
     if (c >= p.cols) continue;
-    float xv[8], g[8], b[8];
-    load8(p.x + off + c, xv);
+    float g[8], b[8];
     if (p.gain1) {
       load8((const P*)p.gain1 + c, g);
       if (KIND == 0) load8((const P*)p.bias1 + c, b);
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(512) join_fwd_kernel(JoinFwd p) {
       for (int i = 0; i < 8; ++i) v[k][i] *= g[i];
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[k][i] = fmaf(p.scale, xv[i], v[k][i]);
+    for (int i = 0; i < 8; ++i) v[k][i] = fmaf(p.scale, xv[k][i], v[k][i]);
     store8(p.xo + off + c, v[k]);
   }
   mean = rstd = 0.f;
@@ -125,19 +125,41 @@ struct JoinBwd {
   float* dx; void* dh; float* dgate;
   float* partial;          // [kJoinPlanes][ctas][cols]
   int64_t rows, rows_per_gate;
-  int cols, ctas;
+  int cols, ctas, stages;
   int split;               // > 0: every gate's rows are split over `split` blocks; 0: a block takes whole gates
   int64_t gates_per_cta;   // split == 0
   float scale;
 };
 
+__device__ __forceinline__ void cp_async16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// at most n of this thread's newest groups still under way
+__device__ __forceinline__ void cp_async_wait_upto(int n) {
+  if (n >= 3) cp_async_wait<3>();
+  else if (n == 2) cp_async_wait<2>();
+  else if (n == 1) cp_async_wait<1>();
+  else cp_async_wait<0>();
+}
+// 16-byte units a thread stages per chunk of 8 columns: dy, x', dx', h
+template <typename P> constexpr int join_units = 4 + 2 * ((int)sizeof(P) / 2);
+
 // A block walks its rows; the column sums of its rows stay in registers (each thread owns its columns) and leave as one
 // row of `partial` per plane: gain1, bias1, gain2, bias2, gate (the last only where a gate's rows are split).
-template <typename P, int KIND, int NC>
+// A row is two block-wide sums in sequence, so what bounds a plain loop over rows is latency (one row's loads, two sums, its
+// stores: 502 us at 16384 x 4096 bf16).  Here the next `stages` rows are on their way into shared memory meanwhile: every thread
+// copies the 16-byte units of its own columns and reads them back itself, so the copies need no barrier, and one block per SM
+// keeps 100 to 200 KB of loads in flight.  STAGED = false (rows too wide for shared memory) loads directly.
+template <typename P, int KIND, int NC, bool STAGED>
 __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
+  constexpr int UP = (int)sizeof(P) / 2, UNITS = join_units<P>;     // units of an operand chunk; of a whole chunk
+  extern __shared__ uint4 ring[];
   __shared__ float red[4][64];
   const float inv = 1.0f / (float)p.cols;
   const int64_t rg = p.rows_per_gate;
+  const int tid = threadIdx.x, nt = blockDim.x;
   int64_t r0, r1;
   if (p.split > 0) {
     const int64_t gate = blockIdx.x / p.split, sub = blockIdx.x % p.split;
@@ -148,30 +170,79 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
     r0 = min(p.rows, (int64_t)blockIdx.x * p.gates_per_cta * rg);
     r1 = min(p.rows, r0 + p.gates_per_cta * rg);
   }
+  auto slot = [&](int stage, int k, int unit) { return ring + ((stage * NC + k) * UNITS + unit) * nt + tid; };
+  auto fetch = [&](int64_t row, int stage) {
+    const int64_t off = row * p.cols;
+#pragma unroll
+    for (int k = 0; k < NC; ++k) {
+      const int c = (tid + k * nt) * 8;
+      if (c >= p.cols) continue;
+      if (p.gain2) {
+#pragma unroll
+        for (int q = 0; q < UP; ++q) cp_async16(slot(stage, k, q), (const P*)p.dy + off + c + q * 4);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) cp_async16(slot(stage, k, UP + q), p.xo + off + c + q * 4);
+      }
+      if (p.dxo) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) cp_async16(slot(stage, k, UP + 2 + q), p.dxo + off + c + q * 4);
+      }
+#pragma unroll
+      for (int q = 0; q < UP; ++q) cp_async16(slot(stage, k, UP + 4 + q), (const P*)p.h + off + c + q * 4);
+    }
+  };
+  auto words = [&](const uint4& a, const uint4& b, float (&v)[8]) {
+    v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
+    v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+  };
+  // 8 columns of a stream: unit `u` of the staged row, or from memory
+  auto get32 = [&](const float* base, int64_t off, int c, int stage, int k, int u, float (&v)[8]) {
+    if (STAGED) words(*slot(stage, k, u), *slot(stage, k, u + 1), v);
+    else load8(base + off + c, v);
+  };
+  auto getp = [&](const void* base, int64_t off, int c, int stage, int k, int u, float (&v)[8]) {
+    if (!STAGED) { load8((const P*)base + off + c, v); return; }
+    if (UP == 2) { words(*slot(stage, k, u), *slot(stage, k, u + UP - 1), v); return; }
+    load8((const P*)slot(stage, k, u), v);
+  };
+  if (STAGED)
+    for (int s = 0; s < p.stages; ++s) {
+      if (r0 + s < r1) fetch(r0 + s, s);
+      cp_async_commit();
+    }
   float aq[NC][8], a1[NC][8], b1[NC][8], a2[NC][8], b2[NC][8];
 #pragma unroll
   for (int k = 0; k < NC; ++k)
 #pragma unroll
     for (int i = 0; i < 8; ++i) aq[k][i] = a1[k][i] = b1[k][i] = a2[k][i] = b2[k][i] = 0.f;
+  float st[4], sn[4] = {0.f, 0.f, 0.f, 0.f};                             // statistics, a row ahead
+  if (r0 < r1) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sn[i] = p.stats[i * p.rows + r0];
+  }
+  int64_t gate_row = r0 / rg, gate_end = (gate_row + 1) * rg;
+  int stage = 0;
   for (int64_t row = r0; row < r1; ++row) {
     const int64_t off = row * p.cols;
     float d[NC][8], t[NC][8];
-    const float mean1 = p.stats[row], rstd1 = p.stats[p.rows + row];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { st[i] = sn[i]; if (row + 1 < r1) sn[i] = p.stats[i * p.rows + row + 1]; }
+    if (row == gate_end) { ++gate_row; gate_end += rg; }
+    if (STAGED) cp_async_wait_upto(p.stages - 1);
     // d = dx' + N2'(dy; x')
     if (p.gain2) {
-      const float mean2 = p.stats[2 * p.rows + row], rstd2 = p.stats[3 * p.rows + row];
       float s1 = 0.f, s2 = 0.f;
 #pragma unroll
       for (int k = 0; k < NC; ++k) {
-        const int c = (threadIdx.x + k * blockDim.x) * 8;
+        const int c = (tid + k * nt) * 8;
         if (c >= p.cols) continue;
         float g[8];
-        load8((const P*)p.dy + off + c, d[k]);
-        load8(p.xo + off + c, t[k]);
+        getp(p.dy, off, c, stage, k, 0, d[k]);
+        get32(p.xo, off, c, stage, k, UP, t[k]);
         load8((const P*)p.gain2 + c, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          t[k][i] = (t[k][i] - mean2) * rstd2;
+          t[k][i] = (t[k][i] - st[2]) * st[3];
           a2[k][i] += d[k][i] * t[k][i];
           if (KIND == 0) b2[k][i] += d[k][i];
           d[k][i] *= g[i];
@@ -183,29 +254,29 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
 #pragma unroll
       for (int k = 0; k < NC; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[k][i] = rstd2 * (d[k][i] - (KIND == 0 ? s.x * inv : 0.f) - t[k][i] * (s.y * inv));
+        for (int i = 0; i < 8; ++i) d[k][i] = st[3] * (d[k][i] - (KIND == 0 ? s.x * inv : 0.f) - t[k][i] * (s.y * inv));
     } else {
 #pragma unroll
       for (int k = 0; k < NC; ++k)
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[k][i] = 0.f;
     }
-    const P* gate = p.gate ? (const P*)p.gate + (row / rg) * p.cols : nullptr;
+    const P* gate = p.gate ? (const P*)p.gate + gate_row * p.cols : nullptr;
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-      const int c = (threadIdx.x + k * blockDim.x) * 8;
+      const int c = (tid + k * nt) * 8;
       if (c >= p.cols) continue;
       float w[8], q[8];
       if (p.dxo) {
-        load8(p.dxo + off + c, w);
+        get32(p.dxo, off, c, stage, k, UP + 2, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[k][i] += w[i];
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) w[i] = p.scale * d[k][i];
       store8(p.dx + off + c, w);
-      load8((const P*)p.h + off + c, t[k]);
+      getp(p.h, off, c, stage, k, UP + 4, t[k]);
       if (gate) load8(gate + c, q);
       if (p.gain1) {
         float g[8], b[8];
@@ -213,9 +284,9 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
         if (KIND == 0 && p.bias1) load8((const P*)p.bias1 + c, b);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          t[k][i] = (t[k][i] - mean1) * rstd1;
+          t[k][i] = (t[k][i] - st[0]) * st[1];
           if (gate) {
-            aq[k][i] += d[k][i] * (t[k][i] * g[i] + (KIND == 0 ? b[i] : 0.f));
+            aq[k][i] += d[k][i] * (t[k][i] * g[i] + (KIND == 0 && p.bias1 ? b[i] : 0.f));
             d[k][i] *= q[i];
           }
           a1[k][i] += d[k][i] * t[k][i];
@@ -229,20 +300,25 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
         for (int i = 0; i < 8; ++i) { aq[k][i] += d[k][i] * t[k][i]; d[k][i] *= q[i]; }
       }
     }
+    if (STAGED) {                                                        // this row's slot has been read: the row after the staged ones
+      if (row + p.stages < r1) fetch(row + p.stages, stage);
+      cp_async_commit();
+      if (++stage == p.stages) stage = 0;
+    }
     float2 s = make_float2(0.f, 0.f);
     if (p.gain1) s = block_sum2(KIND == 0 ? s1 : 0.f, s2, red[(row & 1) * 2 + 1]);
-    const bool gate_done = gate && (row + 1 == r1 || (row + 1) % rg == 0);
+    const bool gate_done = p.split == 0 && gate && (row + 1 == r1 || row + 1 == gate_end);
 #pragma unroll
     for (int k = 0; k < NC; ++k) {
-      const int c = (threadIdx.x + k * blockDim.x) * 8;
+      const int c = (tid + k * nt) * 8;
       if (c >= p.cols) continue;
       if (p.gain1) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[k][i] = rstd1 * (d[k][i] - (KIND == 0 ? s.x * inv : 0.f) - t[k][i] * (s.y * inv));
+        for (int i = 0; i < 8; ++i) d[k][i] = st[1] * (d[k][i] - (KIND == 0 ? s.x * inv : 0.f) - t[k][i] * (s.y * inv));
       }
       store8((P*)p.dh + off + c, d[k]);
-      if (gate_done && p.split == 0) {
-        if (p.dgate) store8(p.dgate + (row / rg) * p.cols + c, aq[k]);
+      if (gate_done) {
+        if (p.dgate) store8(p.dgate + gate_row * p.cols + c, aq[k]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) aq[k][i] = 0.f;
       }
@@ -252,36 +328,42 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
   float* out = p.partial + (size_t)blockIdx.x * p.cols;
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
-    const int c = (threadIdx.x + k * blockDim.x) * 8;
+    const int c = (tid + k * nt) * 8;
     if (c >= p.cols) continue;
-    store8(out + c, a1[k]);
-    if (KIND == 0) store8(out + plane + c, b1[k]);
-    store8(out + 2 * plane + c, a2[k]);
-    if (KIND == 0) store8(out + 3 * plane + c, b2[k]);
-    if (p.split > 0) store8(out + 4 * plane + c, aq[k]);
+    if (p.gain1) store8(out + c, a1[k]);
+    if (KIND == 0 && p.gain1) store8(out + plane + c, b1[k]);
+    if (p.gain2) store8(out + 2 * plane + c, a2[k]);
+    if (KIND == 0 && p.gain2) store8(out + 3 * plane + c, b2[k]);
+    if (p.split > 0 && p.gate) store8(out + 4 * plane + c, aq[k]);
   }
+  pdl_launch_next();
 }
 
 struct JoinSums { float* out[kJoinPlanes]; };     // nullptr: not wanted
 // Sums the planes of `partial` over the blocks, in a fixed order: blockIdx.y = plane; the gate's plane holds one sum per
-// gate, over the `split` blocks of that gate.
-__global__ void join_sums_kernel(const float* __restrict__ partial, JoinSums o, int ctas, int cols, int split) {
-  __shared__ double sh[8][33];
+// gate, over the `split` blocks of that gate.  32 columns x 32 runs of blocks per CUDA block.
+__global__ void __launch_bounds__(1024) join_sums_kernel(const float* __restrict__ partial, JoinSums o, int ctas, int cols, int split) {
+  __shared__ double sh[32][33];
   const int plane = min((int)blockIdx.y, kJoinPlanes - 1);
   const int gate = (int)blockIdx.y - (kJoinPlanes - 1);
   float* out = o.out[plane];
   if (out == nullptr) return;
   const int c0 = plane == kJoinPlanes - 1 ? gate * split : 0, cn = plane == kJoinPlanes - 1 ? split : ctas;
   const int col = blockIdx.x * 32 + threadIdx.x;
+  pdl_wait_prior();
   double a = 0.0;
-  if (col < cols)
-    for (int i = threadIdx.y; i < cn; i += 8) a += partial[((size_t)plane * ctas + c0 + i) * cols + col];
+  if (col < cols) {
+    const float* src = partial + ((size_t)plane * ctas + c0) * cols + col;
+#pragma unroll 4
+    for (int i = threadIdx.y; i < cn; i += 32) a += src[(size_t)i * cols];
+  }
   sh[threadIdx.y][threadIdx.x] = a;
   __syncthreads();
-  if (threadIdx.y == 0 && col < cols) {
-    for (int i = 1; i < 8; ++i) a += sh[i][threadIdx.x];
-    out[(plane == kJoinPlanes - 1 ? (size_t)gate * cols : 0) + col] = (float)a;
-  }
+  // warp y joins column y: lane = run
+  double b = sh[threadIdx.x][threadIdx.y];
+  for (int k = 16; k > 0; k >>= 1) b += __shfl_xor_sync(0xffffffffu, b, k);
+  const int mine = blockIdx.x * 32 + threadIdx.y;
+  if (threadIdx.x == 0 && mine < cols) out[(plane == kJoinPlanes - 1 ? (size_t)gate * cols : 0) + mine] = (float)b;
 }
 
 }  // namespace hift

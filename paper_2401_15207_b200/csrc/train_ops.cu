@@ -14,7 +14,6 @@ static_assert(kLpMaxTop == HIFT_MAX_TOP, "");
 namespace {
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-hift_status done() { return cudaGetLastError() == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA; }
 
 hift_status logprobs_cfg(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, double temperature, float* scale) {
   if (dtype < 0 || dtype > 1 || rows < 0 || rows > INT32_MAX || vocab < 1 || ld < vocab || ld > INT32_MAX - 65536) return HIFT_ERR_CFG;
@@ -39,37 +38,60 @@ hift_status join_cfg(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, do
   return cols > kJoinMaxCols ? HIFT_ERR_CAPACITY : HIFT_OK;
 }
 
-#define JOIN_NC(KERNEL, P, K)                                                             \
-  do {                                                                                    \
-    if (nc == 1) KERNEL<P, K, 1><<<grid, th, 0, (cudaStream_t)stream>>>(p);               \
-    else if (nc == 2) KERNEL<P, K, 2><<<grid, th, 0, (cudaStream_t)stream>>>(p);          \
-    else KERNEL<P, K, 4><<<grid, th, 0, (cudaStream_t)stream>>>(p);                       \
-  } while (0)
-#define JOIN_LAUNCH(KERNEL)                                                               \
-  do {                                                                                    \
-    if (dtype == 0) { if (kind == 0) JOIN_NC(KERNEL, float, 0); else JOIN_NC(KERNEL, float, 1); } \
-    else { if (kind == 0) JOIN_NC(KERNEL, bf16, 0); else JOIN_NC(KERNEL, bf16, 1); }      \
-  } while (0)
-
+// Blocks of the backward kernel that an SM holds: its registers (128 a thread at most) and shared memory.
+constexpr size_t kJoinSmem = 208 * 1024;
+int join_ctas_per_sm(int th) { return th >= 512 ? 1 : th >= 256 ? 2 : 4; }
 // how a backward call deals its rows out: the number of blocks, and whether a gate's rows are split over several
 struct JoinPlan { int ctas, split; int64_t gates_per_cta, rows_per_gate, n_gates; };
-JoinPlan join_plan(int64_t rows, int64_t rows_per_gate) {
+JoinPlan join_plan(int64_t rows, int64_t cols, int64_t rows_per_gate) {
+  int th, nc;
+  join_shape(cols, &th, &nc);
+  const int64_t most = 148 * join_ctas_per_sm(th);
   JoinPlan pl;
   pl.rows_per_gate = rows_per_gate < 1 || rows_per_gate > rows ? (rows > 0 ? rows : 1) : rows_per_gate;
   pl.n_gates = (rows + pl.rows_per_gate - 1) / pl.rows_per_gate;
-  if (pl.n_gates > kJoinCtas) {
+  if (pl.n_gates > most) {
     pl.split = 0;
-    pl.gates_per_cta = (pl.n_gates + kJoinCtas - 1) / kJoinCtas;
+    pl.gates_per_cta = (pl.n_gates + most - 1) / most;
     pl.ctas = (int)((pl.n_gates + pl.gates_per_cta - 1) / pl.gates_per_cta);
     return pl;
   }
-  int64_t split = pl.n_gates > 0 ? kJoinCtas / pl.n_gates : 1;
-  const int64_t most = (pl.rows_per_gate + 3) / 4;         // four rows at least for a block
-  if (split > most) split = most;
+  int64_t split = pl.n_gates > 0 ? most / pl.n_gates : 1;
+  const int64_t cap = (pl.rows_per_gate + 3) / 4;          // four rows at least for a block
+  if (split > cap) split = cap;
   pl.split = (int)(split < 1 ? 1 : split);
   pl.gates_per_cta = 1;
   pl.ctas = (int)(pl.n_gates * pl.split);
   return pl;
+}
+
+template <typename P, int KIND>
+cudaError_t launch_join_fwd(cudaStream_t st, int th, int nc, const JoinFwd& p) {
+  const unsigned grid = (unsigned)p.rows;
+  if (nc == 1) join_fwd_kernel<P, KIND, 1><<<grid, th, 0, st>>>(p);
+  else if (nc == 2) join_fwd_kernel<P, KIND, 2><<<grid, th, 0, st>>>(p);
+  else join_fwd_kernel<P, KIND, 4><<<grid, th, 0, st>>>(p);
+  return cudaGetLastError();
+}
+template <typename P, int KIND, int NC, bool STAGED>
+cudaError_t launch_join_bwd_nc(cudaStream_t st, int th, const JoinBwd& p) {
+  const size_t smem = STAGED ? (size_t)p.stages * NC * join_units<P> * th * 16 : 0;
+  if (smem > 40 * 1024) {                                  // idempotent, and cheap beside the launch
+    const cudaError_t e = cudaFuncSetAttribute(join_bwd_kernel<P, KIND, NC, STAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (e != cudaSuccess) return e;
+  }
+  join_bwd_kernel<P, KIND, NC, STAGED><<<(unsigned)p.ctas, th, smem, st>>>(p);
+  return cudaGetLastError();
+}
+// Rows staged ahead: as many as fit, four at most.  None fit: fp32 operands beyond 8192 columns, the direct variant.
+template <typename P, int KIND>
+cudaError_t launch_join_bwd(cudaStream_t st, int th, int nc, JoinBwd p) {
+  const size_t stage = (size_t)nc * join_units<P> * th * 16, budget = kJoinSmem / (size_t)join_ctas_per_sm(th);
+  p.stages = (int)(budget / stage < 4 ? budget / stage : 4);
+  if (p.stages == 0) return launch_join_bwd_nc<P, KIND, 4, false>(st, th, p);
+  if (nc == 1) return launch_join_bwd_nc<P, KIND, 1, true>(st, th, p);
+  if (nc == 2) return launch_join_bwd_nc<P, KIND, 2, true>(st, th, p);
+  return launch_join_bwd_nc<P, KIND, 4, true>(st, th, p);
 }
 
 hift_status ns_cfg(int64_t rows, int64_t cols, int32_t steps, const void* scratch, size_t scratch_bytes) {
@@ -129,14 +151,15 @@ hift_status hift_k_join_fwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
   JoinFwd p{x, h, gain1, bias1, gate, gain2, bias2, x_out, y, stats, rows, gate ? rows_per_gate : rows, (int)cols, (float)eps, (float)res_scale};
   int th, nc;
   join_shape(cols, &th, &nc);
-  const unsigned grid = (unsigned)rows;
-  JOIN_LAUNCH(join_fwd_kernel);
-  return done();
+  cudaStream_t st = (cudaStream_t)stream;
+  const cudaError_t e = dtype == 0 ? (kind == 0 ? launch_join_fwd<float, 0>(st, th, nc, p) : launch_join_fwd<float, 1>(st, th, nc, p))
+                                   : (kind == 0 ? launch_join_fwd<bf16, 0>(st, th, nc, p) : launch_join_fwd<bf16, 1>(st, th, nc, p));
+  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
 }
 
 size_t hift_join_bwd_scratch_bytes(int64_t rows, int64_t cols, int64_t rows_per_gate) {
   if (rows < 1 || cols < 1) return 0;
-  return (size_t)join_plan(rows, rows_per_gate).ctas * cols * kJoinPlanes * sizeof(float);
+  return (size_t)join_plan(rows, cols, rows_per_gate).ctas * cols * kJoinPlanes * sizeof(float);
 }
 
 hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double res_scale, const void* dy,
@@ -157,20 +180,20 @@ hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
   if (kind == 0 && gain1 && dgate && !bias1) return HIFT_ERR_INPUT;
   const void* ptrs[] = {dy, dx_out, x_out, h, gain1, bias1, gate, gain2, dx, dh, dgate, scratch};
   for (const void* q : ptrs) if (!aligned(q, 16)) return HIFT_ERR_CFG;
-  const JoinPlan pl = join_plan(rows, gate ? rows_per_gate : rows);
+  const JoinPlan pl = join_plan(rows, cols, gate ? rows_per_gate : rows);
   if (scratch_bytes < (size_t)pl.ctas * cols * kJoinPlanes * sizeof(float)) return HIFT_ERR_CAPACITY;
   JoinBwd p{dy, dx_out, x_out, h, stats, gain1, bias1, gate, gain2, dx, dh, dgate, (float*)scratch, rows, pl.rows_per_gate, (int)cols,
-            pl.ctas, pl.split, pl.gates_per_cta, (float)res_scale};
+            pl.ctas, 0, pl.split, pl.gates_per_cta, (float)res_scale};
   int th, nc;
   join_shape(cols, &th, &nc);
-  const unsigned grid = (unsigned)pl.ctas;
-  JOIN_LAUNCH(join_bwd_kernel);
-  if (dgain1 || dbias1 || dgain2 || dbias2 || (dgate && pl.split > 0)) {
+  cudaError_t e = dtype == 0 ? (kind == 0 ? launch_join_bwd<float, 0>(st, th, nc, p) : launch_join_bwd<float, 1>(st, th, nc, p))
+                             : (kind == 0 ? launch_join_bwd<bf16, 0>(st, th, nc, p) : launch_join_bwd<bf16, 1>(st, th, nc, p));
+  if (e == cudaSuccess && (dgain1 || dbias1 || dgain2 || dbias2 || (dgate && pl.split > 0))) {
     const JoinSums o{{dgain1, dbias1, dgain2, dbias2, pl.split > 0 ? dgate : nullptr}};
     const dim3 g((unsigned)((cols + 31) / 32), (unsigned)(kJoinPlanes - 1 + (dgate && pl.split > 0 ? pl.n_gates : 0)));
-    join_sums_kernel<<<g, dim3(32, 8), 0, st>>>((const float*)scratch, o, pl.ctas, (int)cols, pl.split);
+    e = launch_pdl(join_sums_kernel, g, dim3(32, 32), 0, st, (const float*)scratch, o, pl.ctas, (int)cols, pl.split);
   }
-  return done();
+  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
 }
 
 size_t hift_orthogonalize_scratch_bytes(int64_t rows, int64_t cols) {
