@@ -14,17 +14,87 @@ namespace hift {
 constexpr int kJoinMaxCols = 16384;
 constexpr int kJoinPlanes = 5;         // column sums of the backward pass: gain and bias of both norms, gate
 
-// sums of two values over the block; `red` is one of two buffers of 64 floats used in turn, so that one barrier does
+// Sums of two values over the block (at most 16 warps).  The warps' two sums go through one run of shuffles: the lower half
+// of the lanes carries a, the upper half b.  `red` is one of several buffers of 32 floats used in turn, so that one barrier does.
 __device__ __forceinline__ float2 block_sum2(float a, float b, float* red) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, nw = blockDim.x >> 5;
+  const bool up = lane & 16;
+  float v = (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (nw > 1) {
+    if ((lane & 15) == 0) red[(up ? 16 : 0) + w] = v;
+    __syncthreads();
+    v = (lane & 15) < nw ? red[lane] : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  }
+  return make_float2(__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16));
+}
+// four values: two runs of the above behind one barrier; `red` holds 64 floats
+__device__ __forceinline__ float4 block_sum4(float a, float b, float c, float d, float* red) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, nw = blockDim.x >> 5;
+  const bool up = lane & 16;
+  float v = (up ? b : a) + __shfl_xor_sync(0xffffffffu, up ? a : b, 16);
+  float u = (up ? d : c) + __shfl_xor_sync(0xffffffffu, up ? c : d, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) { v += __shfl_xor_sync(0xffffffffu, v, o); u += __shfl_xor_sync(0xffffffffu, u, o); }
+  if (nw > 1) {
+    if ((lane & 15) == 0) { red[(up ? 16 : 0) + w] = v; red[32 + (up ? 16 : 0) + w] = u; }
+    __syncthreads();
+    v = (lane & 15) < nw ? red[lane] : 0.f;
+    u = (lane & 15) < nw ? red[32 + lane] : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) { v += __shfl_xor_sync(0xffffffffu, v, o); u += __shfl_xor_sync(0xffffffffu, u, o); }
+  }
+  return make_float4(__shfl_sync(0xffffffffu, v, 0), __shfl_sync(0xffffffffu, v, 16), __shfl_sync(0xffffffffu, u, 0), __shfl_sync(0xffffffffu, u, 16));
+}
+__device__ __forceinline__ float block_sum1(float a, float* red) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, nw = blockDim.x >> 5;
   a = warp_sum(a);
-  b = warp_sum(b);
-  if (nw == 1) return make_float2(a, b);
-  if (lane == 0) { red[w] = a; red[32 + w] = b; }
-  __syncthreads();
-  a = 0.f; b = 0.f;
-  for (int i = 0; i < nw; ++i) { a += red[i]; b += red[32 + i]; }
-  return make_float2(a, b);
+  if (nw > 1) {
+    if (lane == 0) red[w] = a;
+    __syncthreads();
+    a = (lane & 15) < nw ? red[lane & 15] : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
+  }
+  return a;
+}
+
+// A thread's columns: NC chunks of 8, each two groups of 4 that lie 128 columns apart, so that a warp's access to a group is one
+// contiguous run of 512 bytes (fp32) or 256 (bf16).  (8 columns in a row per thread put half of every 32-byte sector into
+// each of two instructions: 289 instead of 216 us for the backward kernel at 16384 x 4096.)  cols is a multiple of 8, so a
+// group exists or not as a whole; where only the first one does, the second is held at zero.
+__device__ __forceinline__ int join_col(int k, int half) {
+  return ((k * (int)(blockDim.x >> 5) + (int)(threadIdx.x >> 5)) << 8) + (half << 7) + ((int)(threadIdx.x & 31) << 2);
+}
+__device__ __forceinline__ void ld4(const float* p, float* v) { const float4 a = *reinterpret_cast<const float4*>(p); v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; }
+__device__ __forceinline__ void ld4(const bf16* p, float* v) {
+  const uint2 a = *reinterpret_cast<const uint2*>(p);
+  v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xffff0000u); v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xffff0000u);
+}
+__device__ __forceinline__ void st4(float* p, const float* v) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); }
+__device__ __forceinline__ void st4(bf16* p, const float* v) {
+  uint2 a;
+  __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&a);
+  h[0] = __floats2bfloat162_rn(v[0], v[1]);
+  h[1] = __floats2bfloat162_rn(v[2], v[3]);
+  *reinterpret_cast<uint2*>(p) = a;
+}
+template <typename T>
+__device__ __forceinline__ void join_ld(const T* row, int k, int cols, float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (join_col(k, h) < cols) ld4(row + join_col(k, h), v + 4 * h);
+    else v[4 * h] = v[4 * h + 1] = v[4 * h + 2] = v[4 * h + 3] = 0.f;
+  }
+}
+template <typename T>
+__device__ __forceinline__ void join_st(T* row, int k, int cols, const float (&v)[8]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    if (join_col(k, h) < cols) st4(row + join_col(k, h), v + 4 * h);
 }
 
 struct JoinFwd {
@@ -39,21 +109,15 @@ struct JoinFwd {
 // One block per row, the row in registers: NC chunks of 8 columns per thread.
 template <typename P, int KIND, int NC>
 __global__ void __launch_bounds__(512) join_fwd_kernel(JoinFwd p) {
-  __shared__ float red[4][64];
+  __shared__ float red[4][32];
   const int64_t row = blockIdx.x;
   const int64_t off = row * p.cols;
   const float inv = 1.0f / (float)p.cols;
   float v[NC][8], xv[NC][8];                           // both streams are under way before the first sum
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
-    const int c = (threadIdx.x + k * blockDim.x) * 8;
-    if (c < p.cols) {
-      load8((const P*)p.h + off + c, v[k]);
-      load8(p.x + off + c, xv[k]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[k][i] = xv[k][i] = 0.f;
-    }
+    join_ld((const P*)p.h + off, k, p.cols, v[k]);
+    join_ld(p.x + off, k, p.cols, xv[k]);
   }
   // mean and reciprocal deviation of the row held in v (two passes over registers)
   auto moments = [&](float* r0, float* r1, float& mean, float& rstd) {
@@ -64,19 +128,18 @@ __global__ void __launch_bounds__(512) join_fwd_kernel(JoinFwd p) {
       for (int k = 0; k < NC; ++k)
 #pragma unroll
         for (int i = 0; i < 8; ++i) s += v[k][i];
-      mean = block_sum2(s, 0.f, r0).x * inv;
+      mean = block_sum1(s, r0) * inv;
     }
     float q = 0.f;
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      if ((int)(threadIdx.x + k * blockDim.x) * 8 >= p.cols) continue;
+    for (int k = 0; k < NC; ++k)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) q += (v[k][i] - mean) * (v[k][i] - mean);
-    }
-    rstd = 1.0f / sqrtf(block_sum2(q, 0.f, r1).x * inv + p.eps);
-  };
-  auto normed = [&](int k, int i, float mean, float rstd, const float (&g)[8], const float (&b)[8]) {
-    return (v[k][i] - mean) * rstd * g[i] + (KIND == 0 ? b[i] : 0.f);
+      for (int h = 0; h < 2; ++h) {
+        if (join_col(k, h) >= p.cols) continue;
+#pragma unroll
+        for (int i = 4 * h; i < 4 * h + 4; ++i) q += (v[k][i] - mean) * (v[k][i] - mean);
+      }
+    rstd = 1.0f / sqrtf(block_sum1(q, r1) * inv + p.eps);
   };
   float mean = 0.f, rstd = 0.f;
   if (p.gain1) moments(red[0], red[1], mean, rstd);
@@ -84,23 +147,21 @@ __global__ void __launch_bounds__(512) join_fwd_kernel(JoinFwd p) {
   const P* gate = p.gate ? (const P*)p.gate + (row / p.rows_per_gate) * p.cols : nullptr;
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
-    const int c = (threadIdx.x + k * blockDim.x) * 8;
-    if (c >= p.cols) continue;
     float g[8], b[8];
     if (p.gain1) {
-      load8((const P*)p.gain1 + c, g);
-      if (KIND == 0) load8((const P*)p.bias1 + c, b);
+      join_ld((const P*)p.gain1, k, p.cols, g);
+      if (KIND == 0) join_ld((const P*)p.bias1, k, p.cols, b);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[k][i] = normed(k, i, mean, rstd, g, b);
+      for (int i = 0; i < 8; ++i) v[k][i] = (v[k][i] - mean) * rstd * g[i] + (KIND == 0 ? b[i] : 0.f);
     }
     if (gate) {
-      load8(gate + c, g);
+      join_ld(gate, k, p.cols, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[k][i] *= g[i];
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[k][i] = fmaf(p.scale, xv[k][i], v[k][i]);
-    store8(p.xo + off + c, v[k]);
+    for (int i = 0; i < 8; ++i) v[k][i] = fmaf(p.scale, xv[k][i], v[k][i]);       // columns that do not exist stay 0
+    join_st(p.xo + off, k, p.cols, v[k]);
   }
   mean = rstd = 0.f;
   if (p.gain2) moments(red[2], red[3], mean, rstd);
@@ -108,14 +169,12 @@ __global__ void __launch_bounds__(512) join_fwd_kernel(JoinFwd p) {
   if (!p.gain2) return;
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
-    const int c = (threadIdx.x + k * blockDim.x) * 8;
-    if (c >= p.cols) continue;
     float g[8], b[8], o[8];
-    load8((const P*)p.gain2 + c, g);
-    if (KIND == 0) load8((const P*)p.bias2 + c, b);
+    join_ld((const P*)p.gain2, k, p.cols, g);
+    if (KIND == 0) join_ld((const P*)p.bias2, k, p.cols, b);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = normed(k, i, mean, rstd, g, b);
-    store8((P*)p.y + off + c, o);
+    for (int i = 0; i < 8; ++i) o[i] = (v[k][i] - mean) * rstd * g[i] + (KIND == 0 ? b[i] : 0.f);
+    join_st((P*)p.y + off, k, p.cols, o);
   }
 }
 
@@ -134,6 +193,11 @@ struct JoinBwd {
 __device__ __forceinline__ void cp_async16(void* dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
 }
+__device__ __forceinline__ void cp_async8(void* dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async4cols(float* dst, const float* src) { cp_async16(dst, src); }
+__device__ __forceinline__ void cp_async4cols(bf16* dst, const bf16* src) { cp_async8(dst, src); }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 // at most n of this thread's newest groups still under way
@@ -143,198 +207,308 @@ __device__ __forceinline__ void cp_async_wait_upto(int n) {
   else if (n == 1) cp_async_wait<1>();
   else cp_async_wait<0>();
 }
-// 16-byte units a thread stages per chunk of 8 columns: dy, x', dx', h
-template <typename P> constexpr int join_units = 4 + 2 * ((int)sizeof(P) / 2);
+// rows a block works on at a time
+template <int NC, bool ONE> constexpr int join_rows = NC == 1 && ONE ? 2 : 1;
+// bytes a thread stages per chunk of 8 columns: x', dx' in fp32, dy, h in the operand type
+template <typename P> constexpr int join_bytes = 2 * 32 + 2 * 8 * (int)sizeof(P);
 
 // A block walks its rows; the column sums of its rows stay in registers (each thread owns its columns) and leave as one
-// row of `partial` per plane: gain1, bias1, gain2, bias2, gate (the last only where a gate's rows are split).
+// row of `partial` per plane: gain1, bias1, gain2, bias2, gate (the last only where a gate's rows are split).  Within one gate
+// q everything after the block follows from two sums per column, S1 = sum d hat1 and S0 = sum d (S0 for LayerNorm only):
+//     dq = gain1 S1 + bias1 S0,  dgain1 = q S1,  dbias1 = q S0
+// (without a norm after the block dq = S1 = sum d h).  ONE: a block's rows share one gate, or there is none; otherwise the
+// sums are turned over to dgate, dgain1 and dbias1 at each gate's end.
 // A row is two block-wide sums in sequence, so what bounds a plain loop over rows is latency (one row's loads, two sums, its
-// stores: 502 us at 16384 x 4096 bf16).  Here the next `stages` rows are on their way into shared memory meanwhile: every thread
-// copies the 16-byte units of its own columns and reads them back itself, so the copies need no barrier, and one block per SM
-// keeps 100 to 200 KB of loads in flight.  STAGED = false (rows too wide for shared memory) loads directly.
-template <typename P, int KIND, int NC, bool STAGED>
+// stores: 502 us at 16384 x 4096 bf16).  Three things against it, with the time that each left:
+//   - the next rows are on their way into shared memory meanwhile: every thread copies its own columns
+//     and reads them back itself, so the copies need no barrier (382 us of 502).  STAGED = false (rows too wide for shared memory): direct loads.
+//   - gains and gate stay in registers where they fit (NC = 1): beside the staging buffers little L1 is left to re-read them
+//     from (286 us).
+//   - two rows at a time (R = 2, for NC = 1 and one gate), so that their sums share barriers and their work interleaves.
+template <typename P, int KIND, int NC, bool STAGED, bool ONE>
 __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
-  constexpr int UP = (int)sizeof(P) / 2, UNITS = join_units<P>;     // units of an operand chunk; of a whole chunk
-  extern __shared__ uint4 ring[];
+  constexpr int BYTES = join_bytes<P>;
+  constexpr bool LN = KIND == 0, HOLD = NC == 1;
+  constexpr int R = join_rows<NC, ONE>;
+  extern __shared__ __align__(16) unsigned char ring[];
   __shared__ float red[4][64];
   const float inv = 1.0f / (float)p.cols;
   const int64_t rg = p.rows_per_gate;
   const int tid = threadIdx.x, nt = blockDim.x;
-  int64_t r0, r1;
+  const bool ragged = p.cols != NC * nt * 8;               // some threads hold columns that do not exist
+  int64_t r0, r1, step = 1;                                // rows r0, r0 + step, ... below r1
   if (p.split > 0) {
     const int64_t gate = blockIdx.x / p.split, sub = blockIdx.x % p.split;
-    const int64_t g0 = gate * rg, gn = min(rg, p.rows - g0), per = (gn + p.split - 1) / p.split;
-    r0 = g0 + min(gn, sub * per);
-    r1 = g0 + min(gn, (sub + 1) * per);
+    r0 = gate * rg + sub;
+    r1 = min(p.rows, (gate + 1) * rg);
+    step = p.split;
   } else {
     r0 = min(p.rows, (int64_t)blockIdx.x * p.gates_per_cta * rg);
     r1 = min(p.rows, r0 + p.gates_per_cta * rg);
   }
-  auto slot = [&](int stage, int k, int unit) { return ring + ((stage * NC + k) * UNITS + unit) * nt + tid; };
-  auto fetch = [&](int64_t row, int stage) {
+  // staged groups of 4 columns: first x' and dx' (stream 0, 1), then dy and h (2, 3), each [half][thread]
+  auto slot32 = [&](int place, int k, int stream, int half) {
+    return reinterpret_cast<float*>(ring + (size_t)(place * NC + k) * BYTES * nt + (size_t)((stream * 2 + half) * nt + tid) * 16);
+  };
+  auto slotp = [&](int place, int k, int stream, int half) {
+    return reinterpret_cast<P*>(ring + (size_t)(place * NC + k) * BYTES * nt + (size_t)64 * nt + (size_t)(((stream - 2) * 2 + half) * nt + tid) * 4 * sizeof(P));
+  };
+  auto fetch_row = [&](int64_t row, int place) {
     const int64_t off = row * p.cols;
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = (tid + k * nt) * 8;
-      if (c >= p.cols) continue;
-      if (p.gain2) {
+    for (int k = 0; k < NC; ++k)
 #pragma unroll
-        for (int q = 0; q < UP; ++q) cp_async16(slot(stage, k, q), (const P*)p.dy + off + c + q * 4);
-#pragma unroll
-        for (int q = 0; q < 2; ++q) cp_async16(slot(stage, k, UP + q), p.xo + off + c + q * 4);
+      for (int h = 0; h < 2; ++h) {
+        const int c = join_col(k, h);
+        if (c >= p.cols) continue;
+        if (p.gain2) {
+          cp_async4cols(slotp(place, k, 2, h), (const P*)p.dy + off + c);
+          cp_async4cols(slot32(place, k, 0, h), p.xo + off + c);
+        }
+        if (p.dxo) cp_async4cols(slot32(place, k, 1, h), p.dxo + off + c);
+        cp_async4cols(slotp(place, k, 3, h), (const P*)p.h + off + c);
       }
-      if (p.dxo) {
+  };
+  auto fetch = [&](int64_t row, int stage) {               // the R rows from `row` on
 #pragma unroll
-        for (int q = 0; q < 2; ++q) cp_async16(slot(stage, k, UP + 2 + q), p.dxo + off + c + q * 4);
-      }
+    for (int j = 0; j < R; ++j)
+      if (row + j * step < r1) fetch_row(row + j * step, stage * R + j);
+  };
+  // 8 columns of a stream: from the staged row, or from memory
+  auto get32 = [&](const float* base, int64_t off, int place, int k, int stream, float (&v)[8]) {
+    if (!STAGED) { join_ld(base + off, k, p.cols, v); return; }
 #pragma unroll
-      for (int q = 0; q < UP; ++q) cp_async16(slot(stage, k, UP + 4 + q), (const P*)p.h + off + c + q * 4);
-    }
+    for (int h = 0; h < 2; ++h) ld4(slot32(place, k, stream, h), v + 4 * h);
   };
-  auto words = [&](const uint4& a, const uint4& b, float (&v)[8]) {
-    v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
-    v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+  auto getp = [&](const void* base, int64_t off, int place, int k, int stream, float (&v)[8]) {
+    if (!STAGED) { join_ld((const P*)base + off, k, p.cols, v); return; }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) ld4(slotp(place, k, stream, h), v + 4 * h);
   };
-  // 8 columns of a stream: unit `u` of the staged row, or from memory
-  auto get32 = [&](const float* base, int64_t off, int c, int stage, int k, int u, float (&v)[8]) {
-    if (STAGED) words(*slot(stage, k, u), *slot(stage, k, u + 1), v);
-    else load8(base + off + c, v);
-  };
-  auto getp = [&](const void* base, int64_t off, int c, int stage, int k, int u, float (&v)[8]) {
-    if (!STAGED) { load8((const P*)base + off + c, v); return; }
-    if (UP == 2) { words(*slot(stage, k, u), *slot(stage, k, u + UP - 1), v); return; }
-    load8((const P*)slot(stage, k, u), v);
-  };
+  // (slots of columns that do not exist are never copied into: they are zeroed once, and stay so)
+  if (STAGED && ragged) {
+    for (int s = 0; s < p.stages * R; ++s)
+#pragma unroll
+      for (int k = 0; k < NC; ++k)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (join_col(k, h) < p.cols) continue;
+          const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+          st4(slot32(s, k, 0, h), zero); st4(slot32(s, k, 1, h), zero); st4(slotp(s, k, 2, h), zero); st4(slotp(s, k, 3, h), zero);
+        }
+  }
   if (STAGED)
     for (int s = 0; s < p.stages; ++s) {
-      if (r0 + s < r1) fetch(r0 + s, s);
+      fetch(r0 + s * R * step, s);
       cp_async_commit();
     }
-  float aq[NC][8], a1[NC][8], b1[NC][8], a2[NC][8], b2[NC][8];
+  constexpr int NB = LN ? NC : 1, NM = ONE ? 1 : NC, NMB = ONE || !LN ? 1 : NC;   // sums that this variant does not take shrink to one
+  float S1[NC][8], S0[NB][8], a2[NC][8], b2[NB][8], a1[NM][8], b1[NMB][8];
 #pragma unroll
-  for (int k = 0; k < NC; ++k)
+  for (int i = 0; i < 8; ++i) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) aq[k][i] = a1[k][i] = b1[k][i] = a2[k][i] = b2[k][i] = 0.f;
-  float st[4], sn[4] = {0.f, 0.f, 0.f, 0.f};                             // statistics, a row ahead
-  if (r0 < r1) {
+    for (int k = 0; k < NC; ++k) S1[k][i] = a2[k][i] = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sn[i] = p.stats[i * p.rows + r0];
+    for (int k = 0; k < NB; ++k) S0[k][i] = b2[k][i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NM; ++k) a1[k][i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NMB; ++k) b1[k][i] = 0.f;
   }
-  int64_t gate_row = r0 / rg, gate_end = (gate_row + 1) * rg;
-  int stage = 0;
-  for (int64_t row = r0; row < r1; ++row) {
-    const int64_t off = row * p.cols;
-    float d[NC][8], t[NC][8];
+  float st[R][4], sn[R][4];                                              // statistics, an iteration ahead
+  auto next_stats = [&](int64_t row) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { st[i] = sn[i]; if (row + 1 < r1) sn[i] = p.stats[i * p.rows + row + 1]; }
-    if (row == gate_end) { ++gate_row; gate_end += rg; }
+    for (int j = 0; j < R; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sn[j][i] = row + j * step < r1 ? p.stats[i * p.rows + row + j * step] : 0.f;
+  };
+  next_stats(r0);
+  int64_t gate_row = r0 / rg, gate_end = (gate_row + 1) * rg;
+  // the sums of one gate, at its end: q S1 and q S0 into v1 and v0, the gate's own gradient into dq
+  auto turn_over = [&](int k, float (&v1)[8], float (&v0)[8], float (&dq)[8]) {
+    float q[8], g[8], b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { q[i] = g[i] = 1.f; b[i] = 0.f; }
+    if (p.gate) join_ld((const P*)p.gate + gate_row * p.cols, k, p.cols, q);
+    if (p.gain1) join_ld((const P*)p.gain1, k, p.cols, g);
+    if (LN && p.gain1 && p.bias1) join_ld((const P*)p.bias1, k, p.cols, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v1[i] = q[i] * S1[k][i];
+      v0[i] = LN ? q[i] * S0[LN ? k : 0][i] : 0.f;
+      dq[i] = g[i] * S1[k][i] + (LN ? b[i] * S0[LN ? k : 0][i] : 0.f);
+    }
+  };
+  // gains and gate as the operand type, in registers
+  P hg2[HOLD ? 8 : 1], hg1[HOLD ? 8 : 1], hq[HOLD && ONE ? 8 : 1];
+  if (HOLD) {
+    auto hold = [&](const void* base, P* v) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[4 * h + i] = join_col(0, h) < p.cols ? ((const P*)base)[join_col(0, h) + i] : from_f<P>(0.f);
+    };
+    if (p.gain2) hold(p.gain2, hg2);
+    if (p.gain1) hold(p.gain1, hg1);
+    if (ONE && p.gate) hold((const P*)p.gate + gate_row * p.cols, hq);
+  }
+  auto param = [&](const void* base, const P* held, bool is_held, int k, float (&v)[8]) {
+    if (!is_held) { join_ld((const P*)base, k, p.cols, v); return; }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = to_f(held[i]);
+  };
+  // the sums of R rows behind one barrier: c1 = scale mean(w), c2 = scale mean(w hat)
+  auto means = [&](const float (&s1)[R], const float (&s2)[R], int which, float (&c1)[R], float (&c2)[R], float* buf) {
+    if constexpr (R == 2) {
+      if (LN) {
+        const float4 s = block_sum4(s1[0], s2[0], s1[1], s2[1], buf);
+        c1[0] = s.x; c2[0] = s.y; c1[1] = s.z; c2[1] = s.w;
+      } else {
+        const float2 s = block_sum2(s2[0], s2[1], buf);
+        c1[0] = c1[1] = 0.f; c2[0] = s.x; c2[1] = s.y;
+      }
+    } else {
+      const float2 s = block_sum2(s1[0], s2[0], buf);
+      c1[0] = s.x; c2[0] = s.y;
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) { c1[j] *= st[j][which] * inv; c2[j] *= st[j][which] * inv; }
+  };
+  int stage = 0, turn = 0;
+  for (int64_t row = r0; row < r1; row += R * step) {
+    float d[R][NC][8], t[R][NC][8], s1[R], s2[R], c1[R], c2[R];
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st[j][i] = sn[j][i];
+      s1[j] = s2[j] = c1[j] = c2[j] = 0.f;
+    }
+    next_stats(row + R * step);
     if (STAGED) cp_async_wait_upto(p.stages - 1);
-    // d = dx' + N2'(dy; x')
-    if (p.gain2) {
-      float s1 = 0.f, s2 = 0.f;
+    if (p.gain2) {                                                       // d = rstd2 w - c1 - c2 hat2 (+ dx')
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        if (R > 1 && row + j * step >= r1) continue;
+#pragma unroll
+        for (int k = 0; k < NC; ++k) {
+          float g[8];
+          getp(p.dy, (row + j * step) * p.cols, stage * R + j, k, 2, d[j][k]);
+          get32(p.xo, (row + j * step) * p.cols, stage * R + j, k, 0, t[j][k]);
+          param(p.gain2, hg2, HOLD, k, g);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            t[j][k][i] = LN ? (t[j][k][i] - st[j][2]) * st[j][3] : t[j][k][i] * st[j][3];
+            a2[k][i] = fmaf(d[j][k][i], t[j][k][i], a2[k][i]);
+            if (LN) b2[LN ? k : 0][i] += d[j][k][i];
+            d[j][k][i] *= g[i];
+            if (LN) s1[j] += d[j][k][i];
+            s2[j] = fmaf(d[j][k][i], t[j][k][i], s2[j]);
+          }
+        }
+      }
+      means(s1, s2, 3, c1, c2, red[turn]);
+    }
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      s1[j] = s2[j] = 0.f;
+      if (R > 1 && row + j * step >= r1) continue;
+      const int64_t off = (row + j * step) * p.cols;
 #pragma unroll
       for (int k = 0; k < NC; ++k) {
-        const int c = (tid + k * nt) * 8;
-        if (c >= p.cols) continue;
-        float g[8];
-        getp(p.dy, off, c, stage, k, 0, d[k]);
-        get32(p.xo, off, c, stage, k, UP, t[k]);
-        load8((const P*)p.gain2 + c, g);
+        float w[8], q[8];
+        if (p.gain2) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          t[k][i] = (t[k][i] - st[2]) * st[3];
-          a2[k][i] += d[k][i] * t[k][i];
-          if (KIND == 0) b2[k][i] += d[k][i];
-          d[k][i] *= g[i];
-          s1 += d[k][i];
-          s2 += d[k][i] * t[k][i];
+          for (int i = 0; i < 8; ++i)
+            d[j][k][i] = fmaf(-c2[j], t[j][k][i], LN ? fmaf(st[j][3], d[j][k][i], -c1[j]) : st[j][3] * d[j][k][i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) d[j][k][i] = 0.f;
         }
-      }
-      const float2 s = block_sum2(KIND == 0 ? s1 : 0.f, s2, red[(row & 1) * 2]);
+        if (p.dxo) {
+          get32(p.dxo, off, stage * R + j, k, 1, w);
 #pragma unroll
-      for (int k = 0; k < NC; ++k)
+          for (int i = 0; i < 8; ++i) d[j][k][i] += w[i];
+        }
+        if (ragged) {                                              // columns that do not exist take no part in the sums below
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[k][i] = st[3] * (d[k][i] - (KIND == 0 ? s.x * inv : 0.f) - t[k][i] * (s.y * inv));
-    } else {
+          for (int i = 0; i < 8; ++i) d[j][k][i] = join_col(k, i >> 2) < p.cols ? d[j][k][i] : 0.f;
+        }
 #pragma unroll
-      for (int k = 0; k < NC; ++k)
+        for (int i = 0; i < 8; ++i) w[i] = p.scale * d[j][k][i];
+        join_st(p.dx + off, k, p.cols, w);
+        getp(p.h, off, stage * R + j, k, 3, t[j][k]);
+        if (p.gate) param((const P*)p.gate + gate_row * p.cols, hq, HOLD && ONE, k, q);
+        if (p.gain1) {
+          float g[8];
+          param(p.gain1, hg1, HOLD, k, g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[k][i] = 0.f;
-    }
-    const P* gate = p.gate ? (const P*)p.gate + gate_row * p.cols : nullptr;
-    float s1 = 0.f, s2 = 0.f;
-#pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = (tid + k * nt) * 8;
-      if (c >= p.cols) continue;
-      float w[8], q[8];
-      if (p.dxo) {
-        get32(p.dxo, off, c, stage, k, UP + 2, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d[k][i] += w[i];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = p.scale * d[k][i];
-      store8(p.dx + off + c, w);
-      getp(p.h, off, c, stage, k, UP + 4, t[k]);
-      if (gate) load8(gate + c, q);
-      if (p.gain1) {
-        float g[8], b[8];
-        load8((const P*)p.gain1 + c, g);
-        if (KIND == 0 && p.bias1) load8((const P*)p.bias1 + c, b);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          t[k][i] = (t[k][i] - st[0]) * st[1];
-          if (gate) {
-            aq[k][i] += d[k][i] * (t[k][i] * g[i] + (KIND == 0 && p.bias1 ? b[i] : 0.f));
-            d[k][i] *= q[i];
+          for (int i = 0; i < 8; ++i) {
+            t[j][k][i] = LN ? (t[j][k][i] - st[j][0]) * st[j][1] : t[j][k][i] * st[j][1];
+            S1[k][i] = fmaf(d[j][k][i], t[j][k][i], S1[k][i]);
+            if (LN) S0[LN ? k : 0][i] += d[j][k][i];
+            d[j][k][i] *= p.gate ? q[i] * g[i] : g[i];
+            if (LN) s1[j] += d[j][k][i];
+            s2[j] = fmaf(d[j][k][i], t[j][k][i], s2[j]);
           }
-          a1[k][i] += d[k][i] * t[k][i];
-          if (KIND == 0) b1[k][i] += d[k][i];
-          d[k][i] *= g[i];
-          s1 += d[k][i];
-          s2 += d[k][i] * t[k][i];
-        }
-      } else if (gate) {
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { aq[k][i] += d[k][i] * t[k][i]; d[k][i] *= q[i]; }
+          for (int i = 0; i < 8; ++i) {
+            S1[k][i] = fmaf(d[j][k][i], t[j][k][i], S1[k][i]);
+            if (p.gate) d[j][k][i] *= q[i];
+          }
+        }
       }
     }
-    if (STAGED) {                                                        // this row's slot has been read: the row after the staged ones
-      if (row + p.stages < r1) fetch(row + p.stages, stage);
+    if (STAGED) {                                                        // these rows' slots have been read: the rows after the staged ones
+      fetch(row + (int64_t)p.stages * R * step, stage);
       cp_async_commit();
       if (++stage == p.stages) stage = 0;
     }
-    float2 s = make_float2(0.f, 0.f);
-    if (p.gain1) s = block_sum2(KIND == 0 ? s1 : 0.f, s2, red[(row & 1) * 2 + 1]);
-    const bool gate_done = p.split == 0 && gate && (row + 1 == r1 || row + 1 == gate_end);
+    if (p.gain1) means(s1, s2, 1, c1, c2, red[turn + 1]);
+    turn ^= 2;
+    const bool gate_done = !ONE && (row + 1 == r1 || row + 1 == gate_end);
 #pragma unroll
-    for (int k = 0; k < NC; ++k) {
-      const int c = (tid + k * nt) * 8;
-      if (c >= p.cols) continue;
-      if (p.gain1) {
+    for (int j = 0; j < R; ++j) {
+      if (R > 1 && row + j * step >= r1) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[k][i] = st[1] * (d[k][i] - (KIND == 0 ? s.x * inv : 0.f) - t[k][i] * (s.y * inv));
-      }
-      store8((P*)p.dh + off + c, d[k]);
-      if (gate_done) {
-        if (p.dgate) store8(p.dgate + gate_row * p.cols + c, aq[k]);
+      for (int k = 0; k < NC; ++k) {
+        if (p.gain1) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) aq[k][i] = 0.f;
+          for (int i = 0; i < 8; ++i)
+            d[j][k][i] = fmaf(-c2[j], t[j][k][i], LN ? fmaf(st[j][1], d[j][k][i], -c1[j]) : st[j][1] * d[j][k][i]);
+        }
+        join_st((P*)p.dh + (row + j * step) * p.cols, k, p.cols, d[j][k]);
+        if (!ONE && gate_done) {
+          float v1[8], v0[8], dq[8];
+          turn_over(k, v1, v0, dq);
+          if (p.dgate) join_st(p.dgate + gate_row * p.cols, k, p.cols, dq);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            a1[ONE ? 0 : k][i] += v1[i];
+            S1[k][i] = 0.f;
+            if (LN) { b1[ONE || !LN ? 0 : k][i] += v0[i]; S0[LN ? k : 0][i] = 0.f; }
+          }
+        }
       }
     }
+    if (!ONE && gate_done) { ++gate_row; gate_end += rg; }
   }
   const size_t plane = (size_t)p.ctas * p.cols;
   float* out = p.partial + (size_t)blockIdx.x * p.cols;
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
-    const int c = (tid + k * nt) * 8;
-    if (c >= p.cols) continue;
-    if (p.gain1) store8(out + c, a1[k]);
-    if (KIND == 0 && p.gain1) store8(out + plane + c, b1[k]);
-    if (p.gain2) store8(out + 2 * plane + c, a2[k]);
-    if (KIND == 0 && p.gain2) store8(out + 3 * plane + c, b2[k]);
-    if (p.split > 0 && p.gate) store8(out + 4 * plane + c, aq[k]);
+    float v1[8], v0[8], dq[8];
+    if (ONE) {
+      turn_over(k, v1, v0, dq);
+      if (p.gate) join_st(out + 4 * plane, k, p.cols, dq);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { v1[i] = a1[ONE ? 0 : k][i]; v0[i] = b1[ONE || !LN ? 0 : k][i]; }
+    }
+    if (p.gain1) join_st(out, k, p.cols, v1);
+    if (LN && p.gain1) join_st(out + plane, k, p.cols, v0);
+    if (p.gain2) join_st(out + 2 * plane, k, p.cols, a2[k]);
+    if (LN && p.gain2) join_st(out + 3 * plane, k, p.cols, b2[LN ? k : 0]);
   }
   pdl_launch_next();
 }

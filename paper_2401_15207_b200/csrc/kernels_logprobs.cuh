@@ -23,6 +23,7 @@ constexpr float kLog2E = 1.4426950408889634f, kLogLn2 = 0.6931471805599453f;
 constexpr int kLpMaxTop = 32;
 constexpr int kLpCand = 512;              // alternatives a block can collect before it falls back to whole passes
 constexpr int kLpBatch = 4;
+constexpr int kLpThreads = 256;           // at most, of a block
 
 __device__ __forceinline__ float lp_ex2(float x) {
   float y;
@@ -116,8 +117,8 @@ __device__ __forceinline__ void lp_select(unsigned long long* keys, int have, in
 }
 
 struct LpShared {
-  float red[4][16];                       // per warp: maximum, sum, weighted sum
-  uint32_t tmax[512];
+  float red[4][kLpThreads / 32];                       // per warp: maximum, sum, weighted sum
+  uint32_t tmax[kLpThreads];
   unsigned long long cand[kLpCand];
   unsigned long long top[kLpMaxTop];
   unsigned long long best;
@@ -136,7 +137,7 @@ struct LpArgs {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(512) token_logprobs_kernel(const T* __restrict__ logits, LpArgs a) {
+__global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const T* __restrict__ logits, LpArgs a) {
   constexpr int V = LpVec<T>::V;
   __shared__ LpShared sh;
   uint32_t parts, part;                   // blocks of the cluster that share the row
@@ -234,13 +235,13 @@ __global__ void __launch_bounds__(512) token_logprobs_kernel(const T* __restrict
   // ---- a lower bound of the k-th largest: of the threads' maxima the k-th
   const bool want_top = a.n_top > 0;
   if (want_top && warp == 0) {
-    uint32_t key[16], bound = kLpNone;
+    uint32_t key[kLpThreads / 32], bound = kLpNone;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) key[i] = i < nw ? sh.tmax[lane + 32 * i] : 0u;
+    for (int i = 0; i < kLpThreads / 32; ++i) key[i] = i < nw ? sh.tmax[lane + 32 * i] : 0u;
     for (int k = 0; k < a.n_top; ++k) {
       uint32_t best = key[0];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) best = max(best, key[i]);
+      for (int i = 1; i < kLpThreads / 32; ++i) best = max(best, key[i]);
       const uint32_t top = __reduce_max_sync(0xffffffffu, best);
       if (top <= kLpNone) { bound = kLpNone; break; }
       bound = top;
@@ -248,7 +249,7 @@ __global__ void __launch_bounds__(512) token_logprobs_kernel(const T* __restrict
       if (lane == __ffs(who) - 1) {
         bool gone = false;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) if (!gone && key[i] == top) { key[i] = 0u; gone = true; }
+        for (int i = 0; i < kLpThreads / 32; ++i) if (!gone && key[i] == top) { key[i] = 0u; gone = true; }
       }
     }
     if (lane == 0) sh.bound = bound;
@@ -396,14 +397,17 @@ __global__ void __launch_bounds__(512) token_logprobs_kernel(const T* __restrict
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// Threads of a block and blocks per row: about four vectors a thread, and several blocks per row (a cluster) while the rows alone
-// leave SMs idle and a block would still have a vector per thread.
+// Threads of a block and blocks per row.  Small blocks: the end of a row (sums, alternatives) is a chain of short steps that other
+// rows' blocks on the same SM hide (4096 x 50257 bf16: 158 us with 512 threads, 93 with 256, 89 with 128); but enough
+// threads in all, or loads in flight run short (512 x 128000: 75 us with 128, 51 with 256).  While the rows alone still leave
+// SMs idle, up to eight blocks (a cluster) share a row, as long as each has two vectors a thread.
 inline void lp_shape(int64_t rows, int64_t vocab, int vec, int* threads, int* parts) {
-  const int64_t nv = vocab / vec;
+  const int64_t nv = vocab / vec, fill = 148 * 1024;
   int th = 32;
-  while (th < 512 && nv > 4 * th) th *= 2;
+  while (th < 128 && nv > 4 * th) th *= 2;
+  if (th == 128 && rows * th < fill && nv > 8 * th) th = kLpThreads;
   int p = 1;
-  while (p < 8 && rows * p * 2 <= 296 && nv >= 2 * p * th) p *= 2;
+  while (p < 8 && rows * th * p < fill && nv >= 2 * p * th) p *= 2;
   *threads = th;
   *parts = p;
 }

@@ -22,14 +22,12 @@ hift_status logprobs_cfg(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld,
   return HIFT_OK;
 }
 
-// threads of a junction kernel and its chunks of 8 columns per thread
+// threads of a junction kernel (a warp per 256 columns, 16 warps at most) and its chunks of 8 columns per thread
 void join_shape(int64_t cols, int* threads, int* chunks) {
-  const int units = (int)(cols / 8);
-  int th = (units + 31) / 32 * 32;
-  if (th > 512) th = 512;
-  int nc = (units + th - 1) / th;
+  const int units = (int)((cols + 255) / 256), warps = units < 16 ? units : 16;
+  int nc = (units + warps - 1) / warps;
   if (nc == 3) nc = 4;
-  *threads = th;
+  *threads = 32 * warps;
   *chunks = nc;
 }
 hift_status join_cfg(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double res_scale, const void* gate, int64_t rows_per_gate) {
@@ -40,7 +38,7 @@ hift_status join_cfg(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, do
 
 // Blocks of the backward kernel that an SM holds: its registers (128 a thread at most) and shared memory.
 constexpr size_t kJoinSmem = 208 * 1024;
-int join_ctas_per_sm(int th) { return th >= 512 ? 1 : th >= 256 ? 2 : 4; }
+int join_ctas_per_sm(int th) { return th <= 64 ? 8 : 512 / th; }
 // how a backward call deals its rows out: the number of blocks, and whether a gate's rows are split over several
 struct JoinPlan { int ctas, split; int64_t gates_per_cta, rows_per_gate, n_gates; };
 JoinPlan join_plan(int64_t rows, int64_t cols, int64_t rows_per_gate) {
@@ -73,25 +71,29 @@ cudaError_t launch_join_fwd(cudaStream_t st, int th, int nc, const JoinFwd& p) {
   else join_fwd_kernel<P, KIND, 4><<<grid, th, 0, st>>>(p);
   return cudaGetLastError();
 }
-template <typename P, int KIND, int NC, bool STAGED>
+template <typename P, int KIND, int NC, bool STAGED, bool ONE>
 cudaError_t launch_join_bwd_nc(cudaStream_t st, int th, const JoinBwd& p) {
-  const size_t smem = STAGED ? (size_t)p.stages * NC * join_units<P> * th * 16 : 0;
+  const size_t smem = STAGED ? (size_t)p.stages * join_rows<NC, ONE> * NC * join_bytes<P> * th : 0;
   if (smem > 40 * 1024) {                                  // idempotent, and cheap beside the launch
-    const cudaError_t e = cudaFuncSetAttribute(join_bwd_kernel<P, KIND, NC, STAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    const cudaError_t e = cudaFuncSetAttribute(join_bwd_kernel<P, KIND, NC, STAGED, ONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
   }
-  join_bwd_kernel<P, KIND, NC, STAGED><<<(unsigned)p.ctas, th, smem, st>>>(p);
+  join_bwd_kernel<P, KIND, NC, STAGED, ONE><<<(unsigned)p.ctas, th, smem, st>>>(p);
   return cudaGetLastError();
 }
-// Rows staged ahead: as many as fit, four at most.  None fit: fp32 operands beyond 8192 columns, the direct variant.
+// Iterations (of one or two rows) staged ahead: two, or what fits.  None fits: fp32 operands beyond 8192 columns, the direct variant.
+template <typename P, int KIND, bool ONE>
+cudaError_t launch_join_bwd_one(cudaStream_t st, int th, int nc, JoinBwd p) {
+  const size_t stage = (size_t)nc * join_bytes<P> * th * (nc == 1 ? join_rows<1, ONE> : 1), budget = kJoinSmem / (size_t)join_ctas_per_sm(th);
+  p.stages = (int)(budget / stage < 2 ? budget / stage : 2);
+  if (p.stages == 0) return launch_join_bwd_nc<P, KIND, 4, false, ONE>(st, th, p);
+  if (nc == 1) return launch_join_bwd_nc<P, KIND, 1, true, ONE>(st, th, p);
+  if (nc == 2) return launch_join_bwd_nc<P, KIND, 2, true, ONE>(st, th, p);
+  return launch_join_bwd_nc<P, KIND, 4, true, ONE>(st, th, p);
+}
 template <typename P, int KIND>
-cudaError_t launch_join_bwd(cudaStream_t st, int th, int nc, JoinBwd p) {
-  const size_t stage = (size_t)nc * join_units<P> * th * 16, budget = kJoinSmem / (size_t)join_ctas_per_sm(th);
-  p.stages = (int)(budget / stage < 4 ? budget / stage : 4);
-  if (p.stages == 0) return launch_join_bwd_nc<P, KIND, 4, false>(st, th, p);
-  if (nc == 1) return launch_join_bwd_nc<P, KIND, 1, true>(st, th, p);
-  if (nc == 2) return launch_join_bwd_nc<P, KIND, 2, true>(st, th, p);
-  return launch_join_bwd_nc<P, KIND, 4, true>(st, th, p);
+cudaError_t launch_join_bwd(cudaStream_t st, int th, int nc, const JoinBwd& p) {
+  return p.split > 0 ? launch_join_bwd_one<P, KIND, true>(st, th, nc, p) : launch_join_bwd_one<P, KIND, false>(st, th, nc, p);
 }
 
 hift_status ns_cfg(int64_t rows, int64_t cols, int32_t steps, const void* scratch, size_t scratch_bytes) {
