@@ -171,8 +171,9 @@ def _check(status: int, where: str):
 
 
 def _stream_ptr() -> int:
+    # torch.cuda.current_stream().cuda_stream without the Stream object it builds (0.5 instead of 3.4 us a call)
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _ptr(t) -> Optional[int]:
