@@ -680,7 +680,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
   // An earlier launch timed out: do nothing but release the tensor memory.  The flag is global memory, so
   // it is read after the wait above; every role takes its own reading, and if two of them ever disagreed
   // the bounded waits below would end the launch the same way.
-  const bool poisoned = *(volatile int*)&g_tc_error != 0;
+  const bool poisoned = !NS && *(volatile int*)&g_tc_error != 0;
 
   if (warp == 0) {
     // ---------------- TMA producer (one thread)
@@ -761,16 +761,22 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
     for (int tile = blockIdx.x; tile < num_tiles && !poisoned; tile += gridDim.x, ++lt) {
       const int ab = lt & 1;
       const uint32_t aph = (lt >> 1) & 1;
-      const bool ready = mbar_wait(acc_full(ab), aph);
-      if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 3);
-      tc_fence_after();
+      auto wait_acc = [&]() {
+        const bool done = mbar_wait(acc_full(ab), aph);
+        if (!done && lane == 0) atomicCAS(&g_tc_error, 0, 3);
+        tc_fence_after();
+        return done;
+      };
+      bool ready = true;
+      if (!NS) ready = wait_acc();
       // one decision for the whole warp: the tensor-memory loads below are warp-collective
-      if (!__all_sync(0xffffffffu, ready && *(volatile int*)&g_tc_error == 0)) break;
+      if (!NS && !__all_sync(0xffffffffu, ready && *(volatile int*)&g_tc_error == 0)) break;
       const int m0 = tm_of(tile) * BM, n0 = tn_of(tile) * BN;
       const int m = m0 + q * 32 + lane;
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(ab * kAccStride);
-      if constexpr (NS) epi_ns(taddr, BN, m, M, n0, N, ns, stage, lane);
-      else if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
+      if constexpr (NS) {                              // (its final kernel reads the flag; see ns_products_launch)
+        if (!epi_ns(taddr, BN, m, M, n0, N, ns, stage, lane, [&] { return (bool)__all_sync(0xffffffffu, wait_acc()); })) break;
+      } else if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
       else if (!OUT_F32 && swb.gu != nullptr) epi_row_swiglu_bwd(taddr, BN, m, M, n0, N, cptr, swb, stage, lane);
       else if (!OUT_F32 && ge.out != nullptr) epi_row_gelu_fwd(taddr, BN, m, M, n0, N, cptr, ldc, bias, ge, stage, lane);
       else if (!OUT_F32 && ge.bwd_a != nullptr) epi_row_gelu_bwd(taddr, BN, m, M, n0, N, cptr, ldc, ge, stage, lane);
@@ -879,7 +885,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
   const uint32_t tmem_base = *tmem_slot_gen;
   pdl_trigger();
   pdl_wait();                                          // set-up above overlaps the predecessor's tail
-  const bool poisoned = *(volatile int*)&g_tc_error != 0;   // read after the pair sync; see the exit below
+  const bool poisoned = !NS && *(volatile int*)&g_tc_error != 0;   // read after the pair sync; see the exit below
 
   if (warp == 0) {
     // ---------------- TMA producer (one thread per CTA): own rows of A, own columns of B;
@@ -954,15 +960,21 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
     for (int tile = pair; tile < num_tiles && !poisoned; tile += num_pairs, ++lt) {
       const int ab = lt & 1;
       const uint32_t aph = (lt >> 1) & 1;
-      const bool ready = mbar_wait(acc_full(ab), aph);
-      if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 3);
-      tc_fence_after();
-      if (!__all_sync(0xffffffffu, ready && *(volatile int*)&g_tc_error == 0)) break;
+      auto wait_acc = [&]() {
+        const bool done = mbar_wait(acc_full(ab), aph);
+        if (!done && lane == 0) atomicCAS(&g_tc_error, 0, 3);
+        tc_fence_after();
+        return done;
+      };
+      bool ready = true;
+      if (!NS) ready = wait_acc();
+      if (!NS && !__all_sync(0xffffffffu, ready && *(volatile int*)&g_tc_error == 0)) break;
       const int m0 = tm_of(tile) * (2 * BM) + (int)rank * BM, n0 = tn_of(tile) * BN;
       const int m = m0 + q * 32 + lane;
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(ab * kAccStride);
-      if constexpr (NS) epi_ns(taddr, BN, m, M, n0, N, ns, stage, lane);
-      else if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
+      if constexpr (NS) {                              // (its final kernel reads the flag; see ns_products_launch)
+        if (!epi_ns(taddr, BN, m, M, n0, N, ns, stage, lane, [&] { return (bool)__all_sync(0xffffffffu, wait_acc()); })) break;
+      } else if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
       else if (!OUT_F32 && swb.gu != nullptr) epi_row_swiglu_bwd(taddr, BN, m, M, n0, N, cptr, swb, stage, lane);
       else if (!OUT_F32 && ge.out != nullptr) epi_row_gelu_fwd(taddr, BN, m, M, n0, N, cptr, ldc, bias, ge, stage, lane);
       else if (!OUT_F32 && ge.bwd_a != nullptr) epi_row_gelu_bwd(taddr, BN, m, M, n0, N, cptr, ldc, ge, stage, lane);
@@ -1147,8 +1159,9 @@ bool ns_map(const void* p, uint64_t inner, uint64_t outer, uint32_t box_outer, C
   return g_encode(out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// Tile of a product: the one with the least rounds x (k-blocks x cycles per k-block + a tile's own cost).  Cycles per 64-deep k-block:
-// the tensor pipe's 512 for a pair's 256 x 256 and 256 x w / 128 for a CTA's 128 x w, over the efficiencies seen on this machine.
+// Tile of a product: the one with the least rounds x k-blocks x cycles per k-block + a tile's own cost.  Cycles per 64-deep k-block
+// follow the operand bytes that an SM can take from L2 (about 57 a cycle, measured): 32 KB per CTA for a pair's 256 x 256 and
+// for a CTA's 128 x 128, 24 KB for 128 x 64; the tensor pipe would need 512, 256 and 128.
 int ns_tile(int M, int N, int K, bool sym) {
   const int kb = (K + BK - 1) / BK;
   double best = 1e30;
@@ -1159,8 +1172,8 @@ int ns_tile(int M, int N, int K, bool sym) {
     const int64_t tiles = !sym ? (int64_t)tm * tn : cand == 64 ? (int64_t)tm * (tm + 1) : (int64_t)tm * (tm + 1) / 2;
     const int slots = pair ? g_num_sms / 2 : g_num_sms;
     const double rounds = (double)((tiles + slots - 1) / slots);
-    const double cyc = pair ? 560.0 : cand == 128 ? 330.0 : 220.0;
-    const double cost = rounds * kb * cyc + (pair ? 6000.0 : cand == 128 ? 3000.0 : 2000.0);
+    const double cyc = pair ? 630.0 : cand == 128 ? 575.0 : 430.0;
+    const double cost = rounds * kb * cyc + (pair ? 8000.0 : cand == 128 ? 4000.0 : 2000.0);
     if (cost < best) { best = cost; bn = cand; }
   }
   return bn;

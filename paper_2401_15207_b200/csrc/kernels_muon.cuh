@@ -15,77 +15,141 @@ namespace hift {
 constexpr float kNsOperandScale = 1024.0f;    // of the iterate's fp16 image (kNsScale in ns_epilogue.cuh)
 constexpr int kNsParts = 592;
 
-// momentum update (mom != nullptr) and the sum of squares of what will be orthogonalised, one double per block
-template <typename T>
-__global__ void ns_sumsq_kernel(const T* __restrict__ g, float* __restrict__ mom, size_t n, float mu, int nesterov,
-                                double* __restrict__ part) {
-  __shared__ double sh[32];
-  double s = 0.0;
-  for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < n; i += (size_t)gridDim.x * blockDim.x) {
-    float u = to_f(g[i]);
-    if (mom) {
-      const float m = fmaf(mu, mom[i], u);
-      mom[i] = m;
-      u = nesterov ? fmaf(mu, m, u) : m;
+// Blocks are 256 threads as 256 / tx rows of tx threads, 4 columns a thread: a matrix row is walked without an index division.
+// VEC: rows of the caller's matrices start on 16-byte boundaries (8-byte for bf16), so the 4 columns move at once.
+template <bool VEC, typename T>
+__device__ __forceinline__ void ns_ld4(const T* p, int left, float (&v)[4]) {       // left: columns that exist from here on
+  if (VEC) {
+    if (sizeof(T) == 4) {
+      const float4 a = *reinterpret_cast<const float4*>(p);
+      v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2*>(p);
+      v[0] = __uint_as_float(a.x << 16); v[1] = __uint_as_float(a.x & 0xffff0000u); v[2] = __uint_as_float(a.y << 16); v[3] = __uint_as_float(a.y & 0xffff0000u);
     }
-    s += (double)u * u;
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = k < left ? to_f(p[k]) : 0.f;
+}
+template <bool VEC>
+__device__ __forceinline__ void ns_st4(float* p, int left, const float (&v)[4]) {
+  if (VEC) { *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]); return; }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) if (k < left) p[k] = v[k];
+}
+template <bool VEC>
+__device__ __forceinline__ void ns_st4(bf16* p, int left, const float (&v)[4]) {
+  if (VEC) {
+    uint2 a;
+    __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&a);
+    h[0] = __floats2bfloat162_rn(v[0], v[1]);
+    h[1] = __floats2bfloat162_rn(v[2], v[3]);
+    *reinterpret_cast<uint2*>(p) = a;
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) if (k < left) p[k] = __float2bfloat16_rn(v[k]);
+}
+
+// momentum update (mom != nullptr) and the sum of squares of what will be orthogonalised, one double per block
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) ns_sumsq_kernel(const T* __restrict__ g, float* __restrict__ mom, int rows, int cols, float mu, int nesterov,
+                                                       double* __restrict__ part) {
+  __shared__ double sh[8];
+  const int tid = threadIdx.y * blockDim.x + threadIdx.x;
+  double s = 0.0;
+  for (int r = blockIdx.x * blockDim.y + threadIdx.y; r < rows; r += gridDim.x * blockDim.y) {
+    const size_t off = (size_t)r * cols;
+#pragma unroll 2
+    for (int c = threadIdx.x * 4; c < cols; c += blockDim.x * 4) {
+      float u[4];
+      ns_ld4<VEC>(g + off + c, cols - c, u);
+      if (mom) {
+        float m[4];
+        ns_ld4<VEC>(mom + off + c, cols - c, m);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { m[k] = fmaf(mu, m[k], u[k]); u[k] = nesterov ? fmaf(mu, m[k], u[k]) : m[k]; }
+        ns_st4<VEC>(mom + off + c, cols - c, m);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s = fma((double)u[k], (double)u[k], s);
+    }
   }
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
+  if ((tid & 31) == 0) sh[tid >> 5] = s;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < (int)blockDim.x / 32; ++i) s += sh[i];
+  if (tid == 0) {
+    for (int i = 1; i < 8; ++i) s += sh[i];
     part[blockIdx.x] = s;
   }
 }
-// X_0 = U / |U| into the zero-padded scratch, fp32 and as the first products' fp16 operand.  One thread per 4 columns of a row.
-template <typename T>
-__global__ void ns_start_kernel(const T* __restrict__ g, const float* __restrict__ mom, int rows, int cols, float mu, int nesterov,
-                                const double* __restrict__ part, int nparts, int prows, int pcols, float* __restrict__ x32, __half* __restrict__ x16) {
-  __shared__ double sh[32];
+// X_0 = U / |U| into the zero-padded scratch, fp32 and as the first products' fp16 operand.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) ns_start_kernel(const T* __restrict__ g, const float* __restrict__ mom, int rows, int cols, float mu, int nesterov,
+                                                       const double* __restrict__ part, int nparts, int prows, int pcols, float* __restrict__ x32,
+                                                       __half* __restrict__ x16) {
+  __shared__ double sh[8];
   __shared__ float s_inv;
+  const int tid = threadIdx.y * blockDim.x + threadIdx.x;
   double s = 0.0;
-  for (int i = threadIdx.x; i < nparts; i += blockDim.x) s += part[i];
+  pdl_wait_prior();
+  for (int i = tid; i < nparts; i += 256) s += part[i];
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
+  if ((tid & 31) == 0) sh[tid >> 5] = s;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int i = 1; i < (int)blockDim.x / 32; ++i) s += sh[i];
+  if (tid == 0) {
+    for (int i = 1; i < 8; ++i) s += sh[i];
     const double n = sqrt(s);
     s_inv = (float)(1.0 / (n < 1e-30 ? 1e-30 : n));     // a NaN stays one
   }
   __syncthreads();
   const float inv = s_inv;
-  const int q = pcols / 4;
-  for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < (size_t)prows * q; i += (size_t)gridDim.x * blockDim.x) {
-    const int r = (int)(i / q), c = (int)(i % q) * 4;
-    float v[4];
+  for (int r = blockIdx.x * blockDim.y + threadIdx.y; r < prows; r += gridDim.x * blockDim.y) {
+    const size_t off = (size_t)r * cols;
+#pragma unroll 2
+    for (int c = threadIdx.x * 4; c < pcols; c += blockDim.x * 4) {
+      float v[4] = {0.f, 0.f, 0.f, 0.f};
+      if (r < rows && c < cols) {
+        ns_ld4<VEC>(g + off + c, cols - c, v);
+        if (mom) {
+          float m[4];
+          ns_ld4<VEC>(mom + off + c, cols - c, m);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      v[k] = 0.f;
-      if (r < rows && c + k < cols) {
-        const size_t at = (size_t)r * cols + c + k;
-        float u = to_f(g[at]);
-        if (mom) u = nesterov ? fmaf(mu, mom[at], u) : mom[at];
-        v[k] = u * inv;
+          for (int k = 0; k < 4; ++k) v[k] = nesterov ? fmaf(mu, m[k], v[k]) : m[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] *= inv;
       }
+      *reinterpret_cast<float4*>(x32 + (size_t)r * pcols + c) = make_float4(v[0], v[1], v[2], v[3]);
+      __half2 h[2] = {__floats2half2_rn(v[0] * kNsOperandScale, v[1] * kNsOperandScale), __floats2half2_rn(v[2] * kNsOperandScale, v[3] * kNsOperandScale)};
+      *reinterpret_cast<uint2*>(x16 + (size_t)r * pcols + c) = *reinterpret_cast<uint2*>(h);
     }
-    *reinterpret_cast<float4*>(x32 + (size_t)r * pcols + c) = make_float4(v[0], v[1], v[2], v[3]);
-    __half2 h[2] = {__floats2half2_rn(v[0] * kNsOperandScale, v[1] * kNsOperandScale), __floats2half2_rn(v[2] * kNsOperandScale, v[3] * kNsOperandScale)};
-    *reinterpret_cast<uint2*>(x16 + (size_t)r * pcols + c) = *reinterpret_cast<uint2*>(h);
   }
+  pdl_launch_next();
 }
 // The result out of the padded scratch: o in bf16, or the update of the master.  Writes nothing after a product gave up on a wait.
-__global__ void ns_finish_kernel(const float* __restrict__ x, int rows, int cols, int pcols, bf16* __restrict__ o, float* __restrict__ master,
-                                 bf16* __restrict__ param, float decay, float size, const int* __restrict__ tc_error) {
+template <bool VEC>
+__global__ void __launch_bounds__(256) ns_finish_kernel(const float* __restrict__ x, int rows, int cols, int pcols, bf16* __restrict__ o,
+                                                        float* __restrict__ master, bf16* __restrict__ param, float decay, float size,
+                                                        const int* __restrict__ tc_error) {
+  pdl_wait_prior();
   if (tc_error != nullptr && *tc_error != 0) return;
-  for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < (size_t)rows * cols; i += (size_t)gridDim.x * blockDim.x) {
-    const float v = x[(i / cols) * pcols + i % cols];
-    if (o) o[i] = __float2bfloat16_rn(v);
-    if (master) {
-      const float t = master[i] * decay - size * v;
-      master[i] = t;
-      if (param) param[i] = __float2bfloat16_rn(t);
+  for (int r = blockIdx.x * blockDim.y + threadIdx.y; r < rows; r += gridDim.x * blockDim.y) {
+    const size_t off = (size_t)r * cols;
+#pragma unroll 2
+    for (int c = threadIdx.x * 4; c < cols; c += blockDim.x * 4) {
+      float v[4];
+      ns_ld4<true>(x + (size_t)r * pcols + c, 4, v);
+      if (o) ns_st4<VEC>(o + off + c, cols - c, v);
+      if (master) {
+        float t[4];
+        ns_ld4<VEC>(master + off + c, cols - c, t);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[k] = t[k] * decay - size * v[k];
+        ns_st4<VEC>(master + off + c, cols - c, t);
+        if (param) ns_st4<VEC>(param + off + c, cols - c, t);
+      }
     }
   }
 }
@@ -101,7 +165,6 @@ struct NsUpdate { bf16* o; float* master; bf16* param; float decay, size; };   /
 template <typename T>
 inline cudaError_t launch_orthogonalize(cudaStream_t st, int64_t rows, int64_t cols, const T* g, float* mom, float mu, int nesterov,
                                         int steps, const NsUpdate& to, void* scratch) {
-  const size_t n = (size_t)rows * cols;
   const int pr = ns_pad(rows), pc = ns_pad(cols), s = pr < pc ? pr : pc;
   char* w = (char*)scratch;
   auto take = [&](size_t bytes) { char* p = w; w += (bytes + 255) / 256 * 256; return p; };
@@ -115,15 +178,26 @@ inline cudaError_t launch_orthogonalize(cudaStream_t st, int64_t rows, int64_t c
   b.f = take((size_t)s * s * 2);
   b.da = (float*)take((size_t)s * 4);
   b.df = (float*)take((size_t)s * 4);
-  const int grid = (int)((n + 255) / 256 < kNsParts ? (n + 255) / 256 : kNsParts);
-  const size_t np = (size_t)pr * pc / 4;
-  const int pgrid = (int)((np + 255) / 256 < 2 * kNsParts ? (np + 255) / 256 : 2 * kNsParts);
-  ns_sumsq_kernel<T><<<grid, 256, 0, st>>>(g, mom, n, mu, nesterov, part);
-  ns_start_kernel<T><<<pgrid, 256, 0, st>>>(g, mom, (int)rows, (int)cols, mu, nesterov, part, grid, pr, pc, b.x32, (__half*)b.x16[0]);
-  const cudaError_t e = ns_products_launch(st, b, steps);
+  // threads across a row, rows per block, blocks
+  int tx = 32;
+  while (tx < 256 && tx * 4 < pc) tx *= 2;
+  const dim3 block(tx, 256 / tx);
+  auto blocks = [&](int r) { const int b = (r + (int)block.y - 1) / (int)block.y; return dim3((unsigned)(b < kNsParts ? b : kNsParts)); };
+  const dim3 grid = blocks((int)rows), pgrid = blocks(pr);
+  auto at = [](const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; };
+  const bool vec = cols % 4 == 0 && at(g, 4 * sizeof(T)) && at(mom, 16) && at(to.o, 8) && at(to.master, 16) && at(to.param, 8);
+  const int R = (int)rows, C = (int)cols;
+  if (vec) ns_sumsq_kernel<T, true><<<grid, block, 0, st>>>(g, mom, R, C, mu, nesterov, part);
+  else ns_sumsq_kernel<T, false><<<grid, block, 0, st>>>(g, mom, R, C, mu, nesterov, part);
+  cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return e;
-  ns_finish_kernel<<<grid, 256, 0, st>>>(b.x32, (int)rows, (int)cols, pc, to.o, to.master, to.param, to.decay, to.size, gemm_tc_error_device_ptr());
-  return cudaGetLastError();
+  e = vec ? launch_pdl(ns_start_kernel<T, true>, pgrid, block, 0, st, g, (const float*)mom, R, C, mu, nesterov, (const double*)part, (int)grid.x, pr, pc, b.x32, (__half*)b.x16[0])
+          : launch_pdl(ns_start_kernel<T, false>, pgrid, block, 0, st, g, (const float*)mom, R, C, mu, nesterov, (const double*)part, (int)grid.x, pr, pc, b.x32, (__half*)b.x16[0]);
+  if (e != cudaSuccess) return e;
+  e = ns_products_launch(st, b, steps);
+  if (e != cudaSuccess) return e;
+  return vec ? launch_pdl(ns_finish_kernel<true>, grid, block, 0, st, (const float*)b.x32, R, C, pc, to.o, to.master, to.param, to.decay, to.size, gemm_tc_error_device_ptr())
+             : launch_pdl(ns_finish_kernel<false>, grid, block, 0, st, (const float*)b.x32, R, C, pc, to.o, to.master, to.param, to.decay, to.size, gemm_tc_error_device_ptr());
 }
 
 }  // namespace hift

@@ -74,15 +74,19 @@ __device__ __forceinline__ void ns_store_half_transposed(const float (&f)[32], u
   __syncwarp();
 }
 
-// One warp's rows of an output tile: BN columns from tensor memory at taddr.
-__device__ __forceinline__ void epi_ns(uint32_t taddr, int BN, int m, int M, int n0, int N, const NsArgs& a, uint8_t* __restrict__ stage, int lane) {
+// One warp's rows of an output tile: BN columns from tensor memory at taddr.  `ready()` waits for the accumulator (false: the wait
+// gave up); what the first chunk reads from memory is fetched before it.
+template <typename Ready>
+__device__ __forceinline__ bool epi_ns(uint32_t taddr, int BN, int m, int M, int n0, int N, const NsArgs& a, uint8_t* __restrict__ stage, int lane,
+                                       Ready&& ready) {
   const int row_base = m - lane;
-  if (row_base >= M) return;                           // uniform across the warp
+  if (row_base >= M) return ready();                   // uniform across the warp
   const int end = min(BN, N - n0);
   if (a.mode == 2) {
     float4 xn[8];
     lines_fetch_f32(xn, a.x32, a.ld, row_base, lane, M, n0);
     const float drow = a.by_column ? 0.f : a.din[m];
+    if (!ready()) return false;
     uint32_t va[32], vb[32];
     auto chunk = [&](uint32_t (&v)[32], int c0) {
       float4 xc[8];
@@ -115,36 +119,43 @@ __device__ __forceinline__ void epi_ns(uint32_t taddr, int BN, int m, int M, int
       if (c0 + 64 < end) tmem_ld32_nowait(taddr + c0 + 64, va);
       chunk(vb, c0 + 32);
     }
-    return;
+    return true;
   }
   const float drow = a.mode == 1 ? a.din[m] : 0.f;
   const int last = min(end, row_base - n0 + 32);       // chunks above the diagonal are stored from below it
+  uint4 en[4];
+  const __nv_bfloat16* e16 = reinterpret_cast<const __nv_bfloat16*>(a.e);             // 16-bit lines, whatever they hold
+  if (a.mode == 1 && last > 0) lines_fetch_bf16(en, e16, a.ld, row_base, lane, M, n0);
+  if (!ready()) return false;
 #pragma unroll 1
   for (int c0 = 0; c0 < last; c0 += 32) {
     const int n = n0 + c0;
     uint32_t v[32];
-    tmem_ld32(taddr + c0, v);
+    tmem_ld32_nowait(taddr + c0, v);
     float f[32];
     if (a.mode == 0) {
+      tmem_ld_wait32(v);
 #pragma unroll
       for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]) * (1.0f / (kNsScale * kNsScale));
     } else {
-      uint4 en[4], ec[4];
-      lines_fetch_bf16(en, reinterpret_cast<const __nv_bfloat16*>(a.e), a.ld, row_base, lane, M, n);     // 16-bit lines
+      uint4 ec[4];
       lines_park_bf16(en, stage, lane);
       __syncwarp();
       lines_own_row_bf16(ec, stage, lane);
       __syncwarp();
+      if (c0 + 32 < last) lines_fetch_bf16(en, e16, a.ld, row_base, lane, M, n + 32);
+      tmem_ld_wait32(v);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const __half2* he = reinterpret_cast<const __half2*>(&ec[j]);
+        const float4 d4[2] = {*reinterpret_cast<const float4*>(a.din + n + 8 * j), *reinterpret_cast<const float4*>(a.din + n + 8 * j + 4)};
+        const float* dc = reinterpret_cast<const float*>(d4);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           const int i = 8 * j + 2 * t;
           const float2 e2 = __half22float2(he[t]);
-          const float2 d2 = *reinterpret_cast<const float2*>(a.din + n + i);
-          f[i] = fmaf(kNsB, e2.x, kNsC * fmaf(drow + d2.x, e2.x, __uint_as_float(v[i])));
-          f[i + 1] = fmaf(kNsB, e2.y, kNsC * fmaf(drow + d2.y, e2.y, __uint_as_float(v[i + 1])));
+          f[i] = fmaf(kNsB, e2.x, kNsC * fmaf(drow + dc[2 * t], e2.x, __uint_as_float(v[i])));
+          f[i + 1] = fmaf(kNsB, e2.y, kNsC * fmaf(drow + dc[2 * t + 1], e2.y, __uint_as_float(v[i + 1])));
         }
       }
     }
@@ -159,4 +170,5 @@ __device__ __forceinline__ void epi_ns(uint32_t taddr, int BN, int m, int M, int
     ns_store_half(f, stage, a.out16, a.ld, row_base, n, lane);
     if (n < row_base) ns_store_half_transposed(f, stage, a.out16, a.ld, row_base, n, lane);
   }
+  return true;
 }
