@@ -48,6 +48,9 @@ constexpr int kABytes = BM * BK * 2;
 constexpr int kSmemBudget = 196608;                 // operand ring
 constexpr int kStoreStage = 4096;                   // per epilogue warp: one 32 x 32 fp32 chunk on its way to global memory
 constexpr int kSmemBytes = kSmemBudget + 1024 /*alignment slack*/ + 256 /*barriers*/ + 4 * kStoreStage;
+// Newton-Schulz products: eight epilogue warps, because their epilogues wait for memory (the iterate, E) rather than for the store path
+constexpr int kThreadsNs = 320;
+constexpr int kSmemBytesNs = kSmemBytes + 4 * kStoreStage;
 constexpr int kMaxStages = 8;
 constexpr int kAccStride = 256;                     // tensor-memory columns between the two accumulators
 struct TileRt { int bn, b_bytes, stage_bytes, stages; };
@@ -622,6 +625,14 @@ __device__ __forceinline__ void epi_row_gelu_bwd(uint32_t taddr, int BN, int m, 
   }
 }
 
+__device__ __forceinline__ uint32_t cluster_ctarank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 #include "ns_epilogue.cuh"
 
 // ------------------------------------------------------------------ kernel
@@ -635,7 +646,7 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 // NS: fp16 operands and the epilogues of the Newton-Schulz products (ns_epilogue.cuh); their symmetric products (modes
 // 0 and 1) walk the tiles that touch the lower triangle only.
 template <bool A_MN, bool B_MN, bool OUT_F32, bool NS = false>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(NS ? kThreadsNs : kThreads, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                int M, int N, int K, void* __restrict__ cptr, int64_t ldc,
                const __nv_bfloat16* __restrict__ bias, const float* __restrict__ residual, int64_t ldr,
@@ -661,10 +672,13 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int num_kb = (K + BK - 1) / BK;
+  // NS: `split` CTAs of a cluster share a tile, each takes its part of the k-blocks (one tile per cluster then)
+  const int Z = NS ? ns.split : 1, zr = Z > 1 ? (int)cluster_ctarank() : 0;
+  const int kb0 = num_kb * zr / Z, kb1 = num_kb * (zr + 1) / Z, tile0 = blockIdx.x / Z, tile_step = gridDim.x / Z;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 4); }
+    for (int a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), NS ? 8 : 4); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -688,9 +702,9 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       int s = 0;
       uint32_t ph = 0;                   // ring position and its phase, advanced without divisions
       bool ok = true;
-      for (int tile = blockIdx.x; tile < num_tiles && ok; tile += gridDim.x) {
+      for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
         const int m0 = tm_of(tile) * BM, n0 = tn_of(tile) * BN;
-        for (int kb = 0; kb < num_kb; ++kb) {
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_wait(empty_bar(s), ph ^ 1)) { atomicCAS(&g_tc_error, 0, 1); ok = false; break; }
           const uint32_t sa = base + s * kStageBytes, sb = sa + kABytes;
           mbar_expect_tx(full_bar(s), kStageBytes);
@@ -727,14 +741,14 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       int s = 0, lt = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int tile = blockIdx.x; tile < num_tiles && ok; tile += gridDim.x, ++lt) {
+      for (int tile = tile0; tile < num_tiles && ok; tile += tile_step, ++lt) {
         const int ab = lt & 1;
         const uint32_t aph = (lt >> 1) & 1;
         // the epilogue must have drained this accumulator (passes at once on its first use)
         if (!__all_sync(0xffffffffu, mbar_wait(acc_empty(ab), aph ^ 1))) { if (lead) atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
         tc_fence_after();
         const uint32_t tacc = tmem_base + (uint32_t)(ab * kAccStride);
-        for (int kb = 0; kb < num_kb; ++kb) {
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (!__all_sync(0xffffffffu, mbar_wait(full_bar(s), ph))) { if (lead) atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
           tc_fence_after();
           const uint32_t sa = base + s * kStageBytes, sb = sa + kABytes;
@@ -745,7 +759,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             // 16 k-rows of 128 B (MN-major); descriptor addresses are in 16-byte units
             const uint64_t adv_a = A_MN ? (uint64_t)(kk * UMMA_K * 128 >> 4) : (uint64_t)(kk * UMMA_K * 2 >> 4);
             const uint64_t adv_b = B_MN ? (uint64_t)(kk * UMMA_K * 128 >> 4) : (uint64_t)(kk * UMMA_K * 2 >> 4);
-            tc_mma_lead(tacc, da + adv_a, db + adv_b, idesc, (kb > 0 || kk > 0) ? 1u : 0u, lead);
+            tc_mma_lead(tacc, da + adv_a, db + adv_b, idesc, (kb > kb0 || kk > 0) ? 1u : 0u, lead);
           }
           tc_commit_lead(empty_bar(s), lead);       // frees the stage once these MMAs have read it
           if (++s == S) { s = 0; ph ^= 1; }
@@ -754,11 +768,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       }
     }
   } else {
-    // ---------------- epilogue: warps 2..5 own tensor-memory lanes 32*(warp%4) .. +31
+    // ---------------- epilogue: warps 2..5 (NS: and 6..9) own tensor-memory lanes 32*(warp%4) .. +31
     const int q = warp & 3;
     uint8_t* stage = smem_gen + S * kStageBytes + 256 + (warp - 2) * kStoreStage;   // behind the barriers
     int lt = 0;
-    for (int tile = blockIdx.x; tile < num_tiles && !poisoned; tile += gridDim.x, ++lt) {
+    for (int tile = tile0; tile < num_tiles && !poisoned; tile += tile_step, ++lt) {
       const int ab = lt & 1;
       const uint32_t aph = (lt >> 1) & 1;
       auto wait_acc = [&]() {
@@ -775,7 +789,23 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       const int m = m0 + q * 32 + lane;
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(ab * kAccStride);
       if constexpr (NS) {                              // (its final kernel reads the flag; see ns_products_launch)
-        if (!epi_ns(taddr, BN, m, M, n0, N, ns, stage, lane, [&] { return (bool)__all_sync(0xffffffffu, wait_acc()); })) break;
+        const NsShare share{Z, zr};
+        const int half = (warp - 2) >> 2, chunks = BN >> 5, w = share.ways();
+        auto get = [&] {
+          const bool done = __all_sync(0xffffffffu, wait_acc());
+          if (Z > 1) {                                 // also after a wait that gave up: every member comes here
+            cluster_sync_all();                        // all members' products are done, their operand rings free
+            tc_fence_after();
+            ns_send_units(taddr, chunks, half, q, share, base, 1, 0, lane);
+            __syncwarp();
+            cluster_sync_all();
+          }
+          return done;
+        };
+        // two warps share a row: of a whole tile each takes half the columns, of a member's share every other chunk
+        const int first = Z > 1 ? share.first(q) + half * w : half * (chunks >> 1), step = Z > 1 ? 2 * w : 1;
+        if (!epi_ns(taddr, first, Z > 1 ? BN : (half + 1) * (BN >> 1), step, m, M, n0, N, ns, stage, lane, get,
+                    [&](uint32_t (&v)[32], int c) { if (Z > 1) ns_add_units(v, c, chunks, q, share, smem_gen, lane); })) break;
       } else if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
       else if (!OUT_F32 && swb.gu != nullptr) epi_row_swiglu_bwd(taddr, BN, m, M, n0, N, cptr, swb, stage, lane);
       else if (!OUT_F32 && ge.out != nullptr) epi_row_gelu_fwd(taddr, BN, m, M, n0, N, cptr, ldc, bias, ge, stage, lane);
@@ -786,6 +816,11 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       __syncwarp();
       if (lane == 0) mbar_arrive(acc_empty(ab));
     }
+  }
+  if (NS && Z > 1 && warp < 2) {                       // the other warps' two meetings (in `get` above)
+    __syncwarp();
+    cluster_sync_all();
+    cluster_sync_all();
   }
   tc_fence_before();
   __syncthreads();
@@ -807,18 +842,10 @@ constexpr int kB2Bytes = (kBN2 / 2) * BK * 2;          // this CTA's half of B
 constexpr int kStage2Bytes = kABytes + kB2Bytes;       // 32 KB
 constexpr int kStages2 = kSmemBudget / kStage2Bytes;   // 6
 
-__device__ __forceinline__ uint32_t cluster_ctarank() {
-  uint32_t r;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
 __device__ __forceinline__ uint32_t map_to_cta(uint32_t saddr, uint32_t rank) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(saddr), "r"(rank));
   return r;
-}
-__device__ __forceinline__ void cluster_sync_all() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
@@ -829,9 +856,9 @@ __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap
       "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
       ::"r"(dst), "l"((uint64_t)map), "r"(bar_cluster_addr), "r"(x), "r"(y) : "memory");
 }
-__device__ __forceinline__ void tc_commit_pair(uint32_t bar) {      // arrives on `bar` in both CTAs of the pair
+__device__ __forceinline__ void tc_commit_pair(uint32_t bar, uint32_t lead_rank) {      // arrives on `bar` in both CTAs of the pair
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-               ::"r"(bar), "h"((uint16_t)3) : "memory");
+               ::"r"(bar), "h"((uint16_t)(3u << lead_rank)) : "memory");
 }
 __device__ __forceinline__ void tc_mma_pair(uint32_t tmem_c, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accum) {
   asm volatile(
@@ -842,7 +869,7 @@ __device__ __forceinline__ void tc_mma_pair(uint32_t tmem_c, uint64_t da, uint64
 }
 
 template <bool A_MN, bool B_MN, bool OUT_F32, bool NS = false>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(NS ? kThreadsNs : kThreads, 1)
 gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                 int M, int N, int K, void* __restrict__ cptr, int64_t ldc,
                 const __nv_bfloat16* __restrict__ bias, const float* __restrict__ residual, int64_t ldr,
@@ -855,7 +882,9 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
   extern __shared__ uint8_t smem_raw[];
   // both CTAs of a pair read the same flag value only by luck, so decide nothing on it before the
   // pair has synchronised once; an early exit of one CTA alone would strand its peer
-  const uint32_t rank = cluster_ctarank();
+  // NS: `split` pairs of a cluster share a tile, each takes its part of the k-blocks (one tile per cluster then)
+  const uint32_t crank = cluster_ctarank(), rank = crank & 1, lead_rank = crank & ~1u;
+  const int Z = NS ? ns.split : 1, zr = (int)(crank >> 1);
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t bar_base = base + S * kStage2Bytes;
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
@@ -868,11 +897,12 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int num_kb = (K + BK - 1) / BK;
-  const int pair = blockIdx.x >> 1, num_pairs = gridDim.x >> 1;
+  const int kb0 = num_kb * zr / Z, kb1 = num_kb * (zr + 1) / Z;
+  const int pair = (int)(blockIdx.x >> 1) / Z, num_pairs = (int)(gridDim.x >> 1) / Z;     // of a split: the cluster
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-    for (int a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), 8); }
+    for (int a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), NS ? 16 : 8); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -899,10 +929,10 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
         // this CTA's 128 columns of B; gate | up: the first CTA stages the gate rows, the second the up rows
         const int n0 = (!B_MN && swg.out != nullptr) ? tn_of(tile) * 128 + (int)rank * swg.half
                                                      : tn_of(tile) * BN + (int)rank * (BN / 2);
-        for (int kb = 0; kb < num_kb; ++kb) {
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_wait(empty_bar(s), ph ^ 1)) { atomicCAS(&g_tc_error, 0, 1); ok = false; break; }
           const uint32_t sa = base + s * kStage2Bytes, sb = sa + kABytes;
-          const uint32_t fb = map_to_cta(full_bar(s), 0);
+          const uint32_t fb = map_to_cta(full_bar(s), lead_rank);
           if (rank == 0) mbar_expect_tx(full_bar(s), 2 * kStage2Bytes);
           const int k0 = kb * BK;
           if (A_MN) {
@@ -935,7 +965,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
         if (!mbar_wait(acc_empty(ab), aph ^ 1)) { atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
         tc_fence_after();
         const uint32_t tacc = tmem_base + (uint32_t)(ab * kAccStride);
-        for (int kb = 0; kb < num_kb; ++kb) {
+        for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_wait(full_bar(s), ph)) { atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
           tc_fence_after();
           const uint32_t sa = base + s * kStage2Bytes, sb = sa + kABytes;
@@ -944,12 +974,12 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
           for (int kk = 0; kk < BK / UMMA_K; ++kk) {
             const uint64_t adv_a = A_MN ? (uint64_t)(kk * UMMA_K * 128 >> 4) : (uint64_t)(kk * UMMA_K * 2 >> 4);
             const uint64_t adv_b = B_MN ? (uint64_t)(kk * UMMA_K * 128 >> 4) : (uint64_t)(kk * UMMA_K * 2 >> 4);
-            tc_mma_pair(tacc, da + adv_a, db + adv_b, idesc, (kb > 0 || kk > 0) ? 1u : 0u);
+            tc_mma_pair(tacc, da + adv_a, db + adv_b, idesc, (kb > kb0 || kk > 0) ? 1u : 0u);
           }
-          tc_commit_pair(empty_bar(s));      // frees the stage in both CTAs
+          tc_commit_pair(empty_bar(s), lead_rank);      // frees the stage in both CTAs
           if (++s == S) { s = 0; ph ^= 1; }
         }
-        tc_commit_pair(acc_full(ab));        // both CTAs' epilogues may drain their half
+        tc_commit_pair(acc_full(ab), lead_rank);        // both CTAs' epilogues may drain their half
       }
     }
   } else {
@@ -973,7 +1003,23 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
       const int m = m0 + q * 32 + lane;
       const uint32_t taddr = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(ab * kAccStride);
       if constexpr (NS) {                              // (its final kernel reads the flag; see ns_products_launch)
-        if (!epi_ns(taddr, BN, m, M, n0, N, ns, stage, lane, [&] { return (bool)__all_sync(0xffffffffu, wait_acc()); })) break;
+        const NsShare share{Z, zr};
+        const int half = (warp - 2) >> 2, chunks = BN >> 5, w = share.ways();
+        auto get = [&] {
+          const bool done = __all_sync(0xffffffffu, wait_acc());
+          if (Z > 1) {                                 // also after a wait that gave up: every member comes here
+            cluster_sync_all();                        // all members' products are done, their operand rings free
+            tc_fence_after();
+            ns_send_units(taddr, chunks, half, q, share, base, 2, (int)rank, lane);
+            __syncwarp();
+            cluster_sync_all();
+          }
+          return done;
+        };
+        // two warps share a row: of a whole tile each takes half the columns, of a member's share every other chunk
+        const int first = Z > 1 ? share.first(q) + half * w : half * (chunks >> 1), step = Z > 1 ? 2 * w : 1;
+        if (!epi_ns(taddr, first, Z > 1 ? BN : (half + 1) * (BN >> 1), step, m, M, n0, N, ns, stage, lane, get,
+                    [&](uint32_t (&v)[32], int c) { if (Z > 1) ns_add_units(v, c, chunks, q, share, smem_gen, lane); })) break;
       } else if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
       else if (!OUT_F32 && swb.gu != nullptr) epi_row_swiglu_bwd(taddr, BN, m, M, n0, N, cptr, swb, stage, lane);
       else if (!OUT_F32 && ge.out != nullptr) epi_row_gelu_fwd(taddr, BN, m, M, n0, N, cptr, ldc, bias, ge, stage, lane);
@@ -982,8 +1028,13 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
       // hand this CTA's half of the accumulator back: the MMA thread counts 8 warps (4 per CTA)
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty(ab), 0));
+      if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty(ab), lead_rank));
     }
+  }
+  if (NS && Z > 1 && warp < 2) {                       // the other warps' two meetings (in `get` above)
+    __syncwarp();
+    cluster_sync_all();
+    cluster_sync_all();
   }
   // nobody leaves while the peer may still signal this CTA's barriers or read its shared memory
   tc_fence_before();
@@ -1112,30 +1163,34 @@ template <bool A_MN, bool B_MN, bool OUT_F32>
 cudaError_t set_smem_attr2() {
   return cudaFuncSetAttribute(gemm_tc2_kernel<A_MN, B_MN, OUT_F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
 }
-// One Newton-Schulz product.  ta / tb: maps for tiles of (bn < 256: one CTA per 128 x bn tile; 256: a CTA pair per 256 x 256 tile).
+// How a product is tiled: bn < 256: one CTA per 128 x bn tile; 256: a CTA pair per 256 x 256 tile; split: CTAs or pairs per tile.
+struct NsTile { int bn, split; };
+// One Newton-Schulz product.
 template <bool A_MN, bool B_MN>
-cudaError_t launch_ns(cudaStream_t st, int M, int N, int K, const CUtensorMap& ta, const CUtensorMap& tb, int bn, const NsArgs& ns) {
+cudaError_t launch_ns(cudaStream_t st, int M, int N, int K, const CUtensorMap& ta, const CUtensorMap& tb, const NsTile& tile, NsArgs ns) {
+  const int bn = tile.bn;
   const bool pair = bn == 256;
+  ns.split = tile.split;
   const int bm = pair ? 2 * BM : BM;
   const int tm = (M + bm - 1) / bm, tn = (N + bn - 1) / bn;
   const int per = pair ? 1 : BM / bn;
   const int tiles = ns.mode == 2 ? tm * tn : (per == 1 ? tm * (tm + 1) / 2 : tm * (tm + 1));
   const int n_fast = M > N ? tn : 0;
   const int slots = pair ? g_num_sms / 2 : g_num_sms;
-  const int grid = tiles < slots ? tiles : slots;
+  const int grid = tile.split > 1 ? tiles * tile.split : tiles < slots ? tiles : slots;     // a split has one tile per cluster
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3(pair ? 2 * grid : grid);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = kSmemBytes;
+  cfg.blockDim = dim3(kThreadsNs);
+  cfg.dynamicSmemBytes = kSmemBytesNs;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = g_pdl;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = 2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  attr[1].val.clusterDim.x = (pair ? 2 : 1) * tile.split; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = pair ? 2 : 1;
+  cfg.numAttrs = pair || tile.split > 1 ? 2 : 1;
   if (pair)
     return cudaLaunchKernelEx(&cfg, gemm_tc2_kernel<A_MN, B_MN, false, true>, ta, tb, M, N, K, (void*)nullptr, (int64_t)0,
                               (const __nv_bfloat16*)nullptr, (const float*)nullptr, (int64_t)0, tm, tiles, n_fast, RopeArgs{}, SwigluArgs{},
@@ -1146,8 +1201,8 @@ cudaError_t launch_ns(cudaStream_t st, int M, int N, int K, const CUtensorMap& t
 }
 template <bool A_MN, bool B_MN>
 cudaError_t set_smem_attr_ns() {
-  const cudaError_t e = cudaFuncSetAttribute(gemm_tc_kernel<A_MN, B_MN, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(gemm_tc2_kernel<A_MN, B_MN, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+  const cudaError_t e = cudaFuncSetAttribute(gemm_tc_kernel<A_MN, B_MN, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesNs);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(gemm_tc2_kernel<A_MN, B_MN, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesNs);
 }
 // 2-D fp16 matrix [outer][inner], contiguous; box = 64 x box_outer, 128-byte swizzle.  Scratch addresses change from call to
 // call, so these maps are encoded anew each time and not kept.
@@ -1159,24 +1214,31 @@ bool ns_map(const void* p, uint64_t inner, uint64_t outer, uint32_t box_outer, C
   return g_encode(out, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
-// Tile of a product: the one with the least rounds x k-blocks x cycles per k-block + a tile's own cost.  Cycles per 64-deep k-block
-// follow the operand bytes that an SM can take from L2 (about 57 a cycle, measured): 32 KB per CTA for a pair's 256 x 256 and
-// for a CTA's 128 x 128, 24 KB for 128 x 64; the tensor pipe would need 512, 256 and 128.
-int ns_tile(int M, int N, int K, bool sym) {
+// Tile of a product by a model of its time in cycles, fitted to timings of every choice at 768 x 768, 2048 x 2048, 5120 x 1280 and
+// 300 x 8000:  rounds of k-blocks, each round but the first at least as long as the epilogue that runs beside it, and the last epilogue.
+//   k-block of 64: the operand bytes an SM can take from L2 set it (about 57 a cycle): 32 KB per CTA for a pair's 256 x 256 and for
+//   128 x 128, 24 KB for 128 x 64 (the tensor pipe would need 512, 256 and 128); more where both operands are MN-major (`mn`).
+//   epilogue: the new iterate (three streams of it) costs more than a symmetric product.
+// A symmetric product whose tiles leave SMs idle is split along k over a cluster, as long as all of it runs at once (15 clusters of
+// 8 do): 300 x 8000 269 -> 167 us, 5120 x 1280 383 -> 330 us, but 768 x 768 123 -> 137 us, where the exchange costs more than it saves.
+NsTile ns_tile(int M, int N, int K, bool sym, bool mn) {
   const int kb = (K + BK - 1) / BK;
   double best = 1e30;
-  int bn = 64;
-  for (int cand : {256, 128, 64}) {
-    const bool pair = cand == 256;
-    const int bm = pair ? 256 : 128, tm = (M + bm - 1) / bm, tn = (N + cand - 1) / cand;
-    const int64_t tiles = !sym ? (int64_t)tm * tn : cand == 64 ? (int64_t)tm * (tm + 1) : (int64_t)tm * (tm + 1) / 2;
-    const int slots = pair ? g_num_sms / 2 : g_num_sms;
-    const double rounds = (double)((tiles + slots - 1) / slots);
-    const double cyc = pair ? 630.0 : cand == 128 ? 575.0 : 430.0;
-    const double cost = rounds * kb * cyc + (pair ? 8000.0 : cand == 128 ? 4000.0 : 2000.0);
-    if (cost < best) { best = cost; bn = cand; }
+  NsTile t{64, 1};
+  for (int cand : {64, 128, 256}) {
+    const int i = cand == 64 ? 0 : cand == 128 ? 1 : 2, bm = i == 2 ? 256 : 128;
+    const int tm = (M + bm - 1) / bm, tn = (N + cand - 1) / cand;
+    const int64_t tiles = !sym ? (int64_t)tm * tn : i == 0 ? (int64_t)tm * (tm + 1) : (int64_t)tm * (tm + 1) / 2;
+    const int slots = i == 2 ? g_num_sms / 2 : g_num_sms;
+    const double k_cyc[2][3] = {{430, 575, 630}, {620, 712, 594}}, e_cyc[2][3] = {{3500, 6500, 17000}, {2000, 2500, 9000}};
+    for (int z = 1; z <= (i == 2 ? 4 : 8); z *= 2) {
+      if (z > 1 && (!sym || i == 0 || tiles * z * (i == 2 ? 2 : 1) > 120 || z > kb)) break;
+      const double rounds = (double)((tiles + slots - 1) / slots), main = (kb + z - 1) / z * k_cyc[mn][i], epi = e_cyc[sym][i];
+      const double cost = main + (rounds - 1) * (main > epi ? main : epi) + epi + (z > 1 ? (i == 2 ? 10000.0 : 5000.0) : 0.0);
+      if (cost < best) { best = cost; t = NsTile{cand, z}; }
+    }
   }
-  return bn;
+  return t;
 }
 int g_attn_tc = 1;       // tcgen05 attention forward (switch 2; 0 falls back to the mma.sync kernel)
 int g_attn_bwd_tc = 1;   // tcgen05 attention backward (switch 3; 0 falls back to the mma.sync kernels)
@@ -1339,9 +1401,9 @@ cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps) {
   if (gemm_tc_init() != 0) return cudaErrorNotSupported;
   const bool wide = b.rows <= b.cols;                  // the Gram matrix is taken on the short side
   const int S = wide ? b.rows : b.cols, L = wide ? b.cols : b.rows;
-  const int t_gram = ns_tile(S, S, L, true), t_poly = ns_tile(S, S, S, true), t_step = ns_tile(b.rows, b.cols, S, false);
+  const NsTile t_gram = ns_tile(S, S, L, true, !wide), t_poly = ns_tile(S, S, S, true, false), t_step = ns_tile(b.rows, b.cols, S, false, false);
   // boxes: K-major operands 128 rows for A and, for B, the rows that one CTA stages; MN-major operands 64 x 64
-  auto kb_rows = [](int bn) { return (uint32_t)(bn == 256 ? 128 : bn); };
+  auto kb_rows = [](const NsTile& t) { return (uint32_t)(t.bn == 256 ? 128 : t.bn); };
   CUtensorMap x_a[2], x_b[2], e_a, e_b, f_a;           // gram's (or, tall, also the step's) and the step's operands
   CUtensorMap x_s[2], f_b;
   bool ok = true;

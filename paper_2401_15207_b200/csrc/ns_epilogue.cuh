@@ -24,7 +24,53 @@ struct NsArgs {
   float* dout;             // modes 0, 1: the diagonal of the result
   float* x32;              // mode 2: the iterate, replaced in place
   int64_t ld;              // of out16, e and x32
+  int split;               // modes 0, 1: CTAs (or CTA pairs) of a cluster that share a tile, each with its part of k; 1 otherwise
 };
+// Which 32-column chunks of a tile's lane quarter q are finished by member z of a split (`split` members, 2, 4 or 8 of them; 8 for
+// tiles of 128 columns only, where a member takes one chunk of two quarters): chunk `first`, every `step`-th after it.
+struct NsShare {
+  int split, z;
+  __device__ __forceinline__ int ways() const { return split < 4 ? split : 4; }
+  __device__ __forceinline__ int owner(int chunk, int q) const { return split == 8 ? chunk * 2 + (q >> 1) : chunk % split; }
+  __device__ __forceinline__ int first(int q) const { return split == 8 ? ((q >> 1) == (z & 1) ? z >> 1 : 1 << 20) : z; }
+  // place of a unit (chunk, q) among those that its owner receives from one peer
+  __device__ __forceinline__ int unit(int chunk, int q) const { return split == 8 ? (q & 1) : (chunk / split) * 4 + q; }
+  __device__ __forceinline__ int units(int chunks) const { return split == 8 ? 2 : chunks / split * 4; }
+};
+// A split tile: each member's accumulator holds its part of k.  Every warp sends the 32 x 32 units that it does not finish to their
+// owners' shared memory (the operand ring, which nobody reads any more), as [peer][unit][8 column groups][32 lanes] of 16 bytes.
+// `stride`, `base`: cluster rank of member i = i * stride + base.
+__device__ __forceinline__ void ns_send_units(uint32_t taddr, int chunks, int half, int q, const NsShare& s, uint32_t ring, int stride, int base, int lane) {
+  const int units = s.units(chunks);
+#pragma unroll 1
+  for (int c = half; c < chunks; c += 2) {
+    const int o = s.owner(c, q);
+    if (o == s.z) continue;                            // uniform across the warp
+    uint32_t v[32], dst;
+    tmem_ld32(taddr + 32 * c, v);
+    const int slot = s.z < o ? s.z : s.z - 1;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"(ring + (uint32_t)((slot * units + s.unit(c, q)) * 4096 + lane * 16)), "r"(o * stride + base));
+#pragma unroll
+    for (int g = 0; g < 8; ++g)
+      asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + g * 512), "r"(v[4 * g]), "r"(v[4 * g + 1]), "r"(v[4 * g + 2]), "r"(v[4 * g + 3]) : "memory");
+  }
+}
+// adds what the peers sent for this unit, in the order of their places
+__device__ __forceinline__ void ns_add_units(uint32_t (&v)[32], int chunk, int chunks, int q, const NsShare& s, const uint8_t* ring, int lane) {
+  const int units = s.units(chunks);
+#pragma unroll 1
+  for (int slot = 0; slot < s.split - 1; ++slot) {
+    const uint8_t* src = ring + (size_t)(slot * units + s.unit(chunk, q)) * 4096 + lane * 16;
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+      const float4 x = *reinterpret_cast<const float4*>(src + g * 512);
+      v[4 * g] = __float_as_uint(__uint_as_float(v[4 * g]) + x.x);
+      v[4 * g + 1] = __float_as_uint(__uint_as_float(v[4 * g + 1]) + x.y);
+      v[4 * g + 2] = __float_as_uint(__uint_as_float(v[4 * g + 2]) + x.z);
+      v[4 * g + 3] = __float_as_uint(__uint_as_float(v[4 * g + 3]) + x.w);
+    }
+  }
+}
 
 // tile index -> tile of the lower triangle; per_row = column tiles per row tile's width (1: square tiles, 2: half as wide)
 __device__ __forceinline__ void ns_tri_tile(int t, int per_row, int& tm, int& tn) {
@@ -74,24 +120,29 @@ __device__ __forceinline__ void ns_store_half_transposed(const float (&f)[32], u
   __syncwarp();
 }
 
-// One warp's rows of an output tile: BN columns from tensor memory at taddr.  `ready()` waits for the accumulator (false: the wait
-// gave up); what the first chunk reads from memory is fetched before it.
-template <typename Ready>
-__device__ __forceinline__ bool epi_ns(uint32_t taddr, int BN, int m, int M, int n0, int N, const NsArgs& a, uint8_t* __restrict__ stage, int lane,
-                                       Ready&& ready) {
-  const int row_base = m - lane;
-  if (row_base >= M) return ready();                   // uniform across the warp
-  const int end = min(BN, N - n0);
+// One warp's rows of an output tile: the 32-column chunks first, first + step, ... below `end` of the tile, from tensor memory at
+// taddr.  `ready()` waits for the accumulator (false: the wait gave up); what the first chunk reads from memory is fetched
+// before it.  `more(v, chunk)` adds what a split tile's other members hold.
+template <typename Ready, typename More>
+__device__ __forceinline__ bool epi_ns(uint32_t taddr, int first, int end, int step, int m, int M, int n0, int N, const NsArgs& a,
+                                       uint8_t* __restrict__ stage, int lane, Ready&& ready, More&& more) {
+  const int row_base = m - lane, lo = 32 * first;
+  step *= 32;
+  end = min(end, N - n0);
+  if (row_base >= M || lo >= end) return ready();      // uniform across the warp
   if (a.mode == 2) {
     float4 xn[8];
-    lines_fetch_f32(xn, a.x32, a.ld, row_base, lane, M, n0);
+    lines_fetch_f32(xn, a.x32, a.ld, row_base, lane, M, n0 + lo);
     const float drow = a.by_column ? 0.f : a.din[m];
     if (!ready()) return false;
-    uint32_t va[32], vb[32];
-    auto chunk = [&](uint32_t (&v)[32], int c0) {
+#pragma unroll 1
+    for (int c0 = lo; c0 < end; c0 += step) {
+      uint32_t v[32];
+      tmem_ld32_nowait(taddr + c0, v);
       float4 xc[8];
       lines_to_own_row_f32(xn, xc, stage, lane);
-      if (c0 + 32 < end) lines_fetch_f32(xn, a.x32, a.ld, row_base, lane, M, n0 + c0 + 32);
+      if (c0 + step < end) lines_fetch_f32(xn, a.x32, a.ld, row_base, lane, M, n0 + c0 + step);
+      tmem_ld_wait32(v);
       float f[32];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -108,16 +159,6 @@ __device__ __forceinline__ bool epi_ns(uint32_t taddr, int BN, int m, int M, int
         for (int j = 0; j < 32; ++j) f[j] *= kNsScale;
         ns_store_half(f, stage, a.out16, a.ld, row_base, n0 + c0, lane);
       }
-    };
-    tmem_ld32_nowait(taddr, va);
-#pragma unroll 1
-    for (int c0 = 0; c0 < end; c0 += 64) {             // end is a multiple of 64
-      tmem_ld_wait32(va);
-      tmem_ld32_nowait(taddr + c0 + 32, vb);
-      chunk(va, c0);
-      tmem_ld_wait32(vb);
-      if (c0 + 64 < end) tmem_ld32_nowait(taddr + c0 + 64, va);
-      chunk(vb, c0 + 32);
     }
     return true;
   }
@@ -125,16 +166,17 @@ __device__ __forceinline__ bool epi_ns(uint32_t taddr, int BN, int m, int M, int
   const int last = min(end, row_base - n0 + 32);       // chunks above the diagonal are stored from below it
   uint4 en[4];
   const __nv_bfloat16* e16 = reinterpret_cast<const __nv_bfloat16*>(a.e);             // 16-bit lines, whatever they hold
-  if (a.mode == 1 && last > 0) lines_fetch_bf16(en, e16, a.ld, row_base, lane, M, n0);
+  if (a.mode == 1 && last > lo) lines_fetch_bf16(en, e16, a.ld, row_base, lane, M, n0 + lo);
   if (!ready()) return false;
 #pragma unroll 1
-  for (int c0 = 0; c0 < last; c0 += 32) {
+  for (int c0 = lo; c0 < last; c0 += step) {
     const int n = n0 + c0;
     uint32_t v[32];
     tmem_ld32_nowait(taddr + c0, v);
     float f[32];
     if (a.mode == 0) {
       tmem_ld_wait32(v);
+      more(v, c0 >> 5);
 #pragma unroll
       for (int j = 0; j < 32; ++j) f[j] = __uint_as_float(v[j]) * (1.0f / (kNsScale * kNsScale));
     } else {
@@ -143,8 +185,9 @@ __device__ __forceinline__ bool epi_ns(uint32_t taddr, int BN, int m, int M, int
       __syncwarp();
       lines_own_row_bf16(ec, stage, lane);
       __syncwarp();
-      if (c0 + 32 < last) lines_fetch_bf16(en, e16, a.ld, row_base, lane, M, n + 32);
+      if (c0 + step < last) lines_fetch_bf16(en, e16, a.ld, row_base, lane, M, n + step);
       tmem_ld_wait32(v);
+      more(v, c0 >> 5);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const __half2* he = reinterpret_cast<const __half2*>(&ec[j]);

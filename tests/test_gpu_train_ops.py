@@ -546,7 +546,8 @@ def _orth(g, code, steps=5):
 
 @pytest.mark.parametrize("code", [0, 1])
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 9), (9, 1), (2, 3), (16, 16), (63, 65), (64, 64), (127, 129), (128, 128), (129, 300), (300, 129),
-                                       (513, 255), (768, 768), (257, 1000), (1100, 600), (40, 3001), (3001, 40)])
+                                       (513, 255), (768, 768), (257, 1000), (1100, 600), (40, 3001), (3001, 40), (1300, 2600), (2600, 1300),
+                                       (700, 4000), (4000, 330), (50, 11008), (2100, 1400), (9000, 200)])
 def test_orthogonalize_matches_the_definition(code, rows, cols):
     g = _dev(_matrix("gauss", rows, cols, rows * 7 + cols), _dt(code))
     assert rel_l2(_orth(g, code), R.orthogonalize(g.double().cpu().numpy())) < NS_TOL
