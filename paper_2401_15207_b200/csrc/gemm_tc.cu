@@ -643,9 +643,9 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
 // Persistent: one CTA per SM walks output tiles (m fastest, so CTAs running together share the
 // same B tile through L2).  Two accumulators in tensor memory: while the epilogue warps drain
 // tile i, the MMA thread already accumulates tile i+1.
-// NS: fp16 operands and the epilogues of the Newton-Schulz products (ns_epilogue.cuh); their symmetric products (modes
-// 0 and 1) walk the tiles that touch the lower triangle only.
-template <bool A_MN, bool B_MN, bool OUT_F32, bool NS = false>
+// NS: fp16 operands and the epilogues of the Newton-Schulz products (ns_epilogue.cuh): 1 the symmetric ones (modes 0 and 1), which
+// walk the tiles that touch the lower triangle only, 2 the new iterate.
+template <bool A_MN, bool B_MN, bool OUT_F32, int NS = 0>
 __global__ void __launch_bounds__(NS ? kThreadsNs : kThreads, 1)
 gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                int M, int N, int K, void* __restrict__ cptr, int64_t ldc,
@@ -654,8 +654,8 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
   // Tile walk.  CTAs that run together should share the LARGER operand's slab and leave the smaller operand to L2:
   // row tiles fastest (n_fast = 0) when A is the smaller operand, column tiles fastest (n_fast = tiles along N) when B is.
   auto tri = [&](int tile, bool row) { int a, b; ns_tri_tile(tile, BM / tc.bn, a, b); return row ? a : b; };
-  auto tm_of = [&](int tile) { if (NS && ns.mode != 2) return tri(tile, true); return n_fast ? tile / n_fast : tile % tiles_m; };
-  auto tn_of = [&](int tile) { if (NS && ns.mode != 2) return tri(tile, false); return n_fast ? tile % n_fast : tile / tiles_m; };
+  auto tm_of = [&](int tile) { if (NS == 1) return tri(tile, true); return n_fast ? tile / n_fast : tile % tiles_m; };
+  auto tn_of = [&](int tile) { if (NS == 1) return tri(tile, false); return n_fast ? tile % n_fast : tile / tiles_m; };
   const int BN = tc.bn, S = tc.stages;
   const uint32_t kStageBytes = (uint32_t)tc.stage_bytes;
   extern __shared__ uint8_t smem_raw[];
@@ -673,7 +673,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int num_kb = (K + BK - 1) / BK;
   // NS: `split` CTAs of a cluster share a tile, each takes its part of the k-blocks (one tile per cluster then)
-  const int Z = NS ? ns.split : 1, zr = Z > 1 ? (int)cluster_ctarank() : 0;
+  const int Z = NS == 1 ? ns.split : 1, zr = Z > 1 ? (int)cluster_ctarank() : 0;
   const int kb0 = num_kb * zr / Z, kb1 = num_kb * (zr + 1) / Z, tile0 = blockIdx.x / Z, tile_step = gridDim.x / Z;
 
   if (threadIdx.x == 0) {
@@ -804,7 +804,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
         };
         // two warps share a row: of a whole tile each takes half the columns, of a member's share every other chunk
         const int first = Z > 1 ? share.first(q) + half * w : half * (chunks >> 1), step = Z > 1 ? 2 * w : 1;
-        if (!epi_ns(taddr, first, Z > 1 ? BN : (half + 1) * (BN >> 1), step, m, M, n0, N, ns, stage, lane, get,
+        if (!epi_ns<NS == 2>(taddr, first, Z > 1 ? BN : (half + 1) * (BN >> 1), step, m, M, n0, N, ns, stage, lane, get,
                     [&](uint32_t (&v)[32], int c) { if (Z > 1) ns_add_units(v, c, chunks, q, share, smem_gen, lane); })) break;
       } else if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
       else if (!OUT_F32 && swb.gu != nullptr) epi_row_swiglu_bwd(taddr, BN, m, M, n0, N, cptr, swb, stage, lane);
@@ -817,7 +817,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       if (lane == 0) mbar_arrive(acc_empty(ab));
     }
   }
-  if (NS && Z > 1 && warp < 2) {                       // the other warps' two meetings (in `get` above)
+  if (NS == 1 && Z > 1 && warp < 2) {                       // the other warps' two meetings (in `get` above)
     __syncwarp();
     cluster_sync_all();
     cluster_sync_all();
@@ -868,15 +868,15 @@ __device__ __forceinline__ void tc_mma_pair(uint32_t tmem_c, uint64_t da, uint64
       ::"r"(tmem_c), "l"(da), "l"(db), "r"(idesc), "r"(accum) : "memory");
 }
 
-template <bool A_MN, bool B_MN, bool OUT_F32, bool NS = false>
+template <bool A_MN, bool B_MN, bool OUT_F32, int NS = 0>
 __global__ void __launch_bounds__(NS ? kThreadsNs : kThreads, 1)
 gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_b,
                 int M, int N, int K, void* __restrict__ cptr, int64_t ldc,
                 const __nv_bfloat16* __restrict__ bias, const float* __restrict__ residual, int64_t ldr,
                 int tiles_m, int num_tiles, int n_fast, RopeArgs rope, SwigluArgs swg, SwigluBwdArgs swb, GeluArgs ge, NsArgs ns) {
   auto tri = [&](int tile, bool row) { int a, b; ns_tri_tile(tile, 1, a, b); return row ? a : b; };
-  auto tm_of = [&](int tile) { if (NS && ns.mode != 2) return tri(tile, true); return n_fast ? tile / n_fast : tile % tiles_m; };      // see gemm_tc_kernel
-  auto tn_of = [&](int tile) { if (NS && ns.mode != 2) return tri(tile, false); return n_fast ? tile % n_fast : tile / tiles_m; };
+  auto tm_of = [&](int tile) { if (NS == 1) return tri(tile, true); return n_fast ? tile / n_fast : tile % tiles_m; };      // see gemm_tc_kernel
+  auto tn_of = [&](int tile) { if (NS == 1) return tri(tile, false); return n_fast ? tile % n_fast : tile / tiles_m; };
   constexpr int S = kStages2;
   constexpr int BN = kBN2;
   extern __shared__ uint8_t smem_raw[];
@@ -884,7 +884,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
   // pair has synchronised once; an early exit of one CTA alone would strand its peer
   // NS: `split` pairs of a cluster share a tile, each takes its part of the k-blocks (one tile per cluster then)
   const uint32_t crank = cluster_ctarank(), rank = crank & 1, lead_rank = crank & ~1u;
-  const int Z = NS ? ns.split : 1, zr = (int)(crank >> 1);
+  const int Z = NS == 1 ? ns.split : 1, zr = (int)(crank >> 1);
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t bar_base = base + S * kStage2Bytes;
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
@@ -1018,7 +1018,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
         };
         // two warps share a row: of a whole tile each takes half the columns, of a member's share every other chunk
         const int first = Z > 1 ? share.first(q) + half * w : half * (chunks >> 1), step = Z > 1 ? 2 * w : 1;
-        if (!epi_ns(taddr, first, Z > 1 ? BN : (half + 1) * (BN >> 1), step, m, M, n0, N, ns, stage, lane, get,
+        if (!epi_ns<NS == 2>(taddr, first, Z > 1 ? BN : (half + 1) * (BN >> 1), step, m, M, n0, N, ns, stage, lane, get,
                     [&](uint32_t (&v)[32], int c) { if (Z > 1) ns_add_units(v, c, chunks, q, share, smem_gen, lane); })) break;
       } else if (!OUT_F32 && swg.out != nullptr) epi_row_swiglu(taddr, m, M, tn_of(tile) * 128, cptr, ldc, bias, swg, stage, lane);
       else if (!OUT_F32 && swb.gu != nullptr) epi_row_swiglu_bwd(taddr, BN, m, M, n0, N, cptr, swb, stage, lane);
@@ -1031,7 +1031,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
       if (lane == 0) mbar_arrive_remote(map_to_cta(acc_empty(ab), lead_rank));
     }
   }
-  if (NS && Z > 1 && warp < 2) {                       // the other warps' two meetings (in `get` above)
+  if (NS == 1 && Z > 1 && warp < 2) {                       // the other warps' two meetings (in `get` above)
     __syncwarp();
     cluster_sync_all();
     cluster_sync_all();
@@ -1166,7 +1166,7 @@ cudaError_t set_smem_attr2() {
 // How a product is tiled: bn < 256: one CTA per 128 x bn tile; 256: a CTA pair per 256 x 256 tile; split: CTAs or pairs per tile.
 struct NsTile { int bn, split; };
 // One Newton-Schulz product.
-template <bool A_MN, bool B_MN>
+template <bool A_MN, bool B_MN, int NS>
 cudaError_t launch_ns(cudaStream_t st, int M, int N, int K, const CUtensorMap& ta, const CUtensorMap& tb, const NsTile& tile, NsArgs ns) {
   const int bn = tile.bn;
   const bool pair = bn == 256;
@@ -1174,7 +1174,7 @@ cudaError_t launch_ns(cudaStream_t st, int M, int N, int K, const CUtensorMap& t
   const int bm = pair ? 2 * BM : BM;
   const int tm = (M + bm - 1) / bm, tn = (N + bn - 1) / bn;
   const int per = pair ? 1 : BM / bn;
-  const int tiles = ns.mode == 2 ? tm * tn : (per == 1 ? tm * (tm + 1) / 2 : tm * (tm + 1));
+  const int tiles = NS == 2 ? tm * tn : (per == 1 ? tm * (tm + 1) / 2 : tm * (tm + 1));
   const int n_fast = M > N ? tn : 0;
   const int slots = pair ? g_num_sms / 2 : g_num_sms;
   const int grid = tile.split > 1 ? tiles * tile.split : tiles < slots ? tiles : slots;     // a split has one tile per cluster
@@ -1192,17 +1192,17 @@ cudaError_t launch_ns(cudaStream_t st, int M, int N, int K, const CUtensorMap& t
   cfg.attrs = attr;
   cfg.numAttrs = pair || tile.split > 1 ? 2 : 1;
   if (pair)
-    return cudaLaunchKernelEx(&cfg, gemm_tc2_kernel<A_MN, B_MN, false, true>, ta, tb, M, N, K, (void*)nullptr, (int64_t)0,
+    return cudaLaunchKernelEx(&cfg, gemm_tc2_kernel<A_MN, B_MN, false, NS>, ta, tb, M, N, K, (void*)nullptr, (int64_t)0,
                               (const __nv_bfloat16*)nullptr, (const float*)nullptr, (int64_t)0, tm, tiles, n_fast, RopeArgs{}, SwigluArgs{},
                               SwigluBwdArgs{}, GeluArgs{}, ns);
-  return cudaLaunchKernelEx(&cfg, gemm_tc_kernel<A_MN, B_MN, false, true>, ta, tb, M, N, K, (void*)nullptr, (int64_t)0,
+  return cudaLaunchKernelEx(&cfg, gemm_tc_kernel<A_MN, B_MN, false, NS>, ta, tb, M, N, K, (void*)nullptr, (int64_t)0,
                             (const __nv_bfloat16*)nullptr, (const float*)nullptr, (int64_t)0, tm, tiles, n_fast, make_tile(bn, B_MN), RopeArgs{},
                             SwigluArgs{}, SwigluBwdArgs{}, GeluArgs{}, ns);
 }
-template <bool A_MN, bool B_MN>
+template <bool A_MN, bool B_MN, int NS>
 cudaError_t set_smem_attr_ns() {
-  const cudaError_t e = cudaFuncSetAttribute(gemm_tc_kernel<A_MN, B_MN, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesNs);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(gemm_tc2_kernel<A_MN, B_MN, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesNs);
+  const cudaError_t e = cudaFuncSetAttribute(gemm_tc_kernel<A_MN, B_MN, false, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesNs);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(gemm_tc2_kernel<A_MN, B_MN, false, NS>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytesNs);
 }
 // 2-D fp16 matrix [outer][inner], contiguous; box = 64 x box_outer, 128-byte swizzle.  Scratch addresses change from call to
 // call, so these maps are encoded anew each time and not kept.
@@ -1292,9 +1292,10 @@ int gemm_tc_init() {
   if (e == cudaSuccess) e = set_smem_attr2<false, true, true>();
   if (e == cudaSuccess) e = set_smem_attr2<true, true, true>();
   if (e == cudaSuccess) e = set_smem_attr2<true, true, false>();
-  if (e == cudaSuccess) e = set_smem_attr_ns<false, false>();
-  if (e == cudaSuccess) e = set_smem_attr_ns<false, true>();
-  if (e == cudaSuccess) e = set_smem_attr_ns<true, true>();
+  if (e == cudaSuccess) e = set_smem_attr_ns<false, false, 1>();
+  if (e == cudaSuccess) e = set_smem_attr_ns<true, true, 1>();
+  if (e == cudaSuccess) e = set_smem_attr_ns<false, false, 2>();
+  if (e == cudaSuccess) e = set_smem_attr_ns<false, true, 2>();
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fwd_tc_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnTcCfg<64>::kSmem);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fwd_tc_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnTcCfg<128>::kSmem);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fwd_tc_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnTcCfg<64>::kSmem);
@@ -1425,14 +1426,14 @@ cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps) {
     const int cur = i & 1;
     NsArgs n{};
     n.mode = 0; n.out16 = (__half*)b.e; n.dout = b.da; n.ld = S;
-    cudaError_t r = wide ? launch_ns<false, false>(st, S, S, L, x_a[cur], x_b[cur], t_gram, n) : launch_ns<true, true>(st, S, S, L, x_a[cur], x_b[cur], t_gram, n);
+    cudaError_t r = wide ? launch_ns<false, false, 1>(st, S, S, L, x_a[cur], x_b[cur], t_gram, n) : launch_ns<true, true, 1>(st, S, S, L, x_a[cur], x_b[cur], t_gram, n);
     if (r != cudaSuccess) return r;
     n = NsArgs{};
     n.mode = 1; n.e = (const __half*)b.e; n.din = b.da; n.out16 = (__half*)b.f; n.dout = b.df; n.ld = S;
-    if ((r = launch_ns<false, false>(st, S, S, S, e_a, e_b, t_poly, n)) != cudaSuccess) return r;
+    if ((r = launch_ns<false, false, 1>(st, S, S, S, e_a, e_b, t_poly, n)) != cudaSuccess) return r;
     n = NsArgs{};
     n.mode = 2; n.by_column = !wide; n.din = b.df; n.x32 = b.x32; n.out16 = i + 1 < steps ? (__half*)b.x16[cur ^ 1] : nullptr; n.ld = b.cols;
-    r = wide ? launch_ns<false, true>(st, b.rows, b.cols, S, f_a, x_s[cur], t_step, n) : launch_ns<false, false>(st, b.rows, b.cols, S, x_s[cur], f_b, t_step, n);
+    r = wide ? launch_ns<false, true, 2>(st, b.rows, b.cols, S, f_a, x_s[cur], t_step, n) : launch_ns<false, false, 2>(st, b.rows, b.cols, S, x_s[cur], f_b, t_step, n);
     if (r != cudaSuccess) return r;
   }
   return cudaSuccess;

@@ -123,14 +123,15 @@ __device__ __forceinline__ void ns_store_half_transposed(const float (&f)[32], u
 // One warp's rows of an output tile: the 32-column chunks first, first + step, ... below `end` of the tile, from tensor memory at
 // taddr.  `ready()` waits for the accumulator (false: the wait gave up); what the first chunk reads from memory is fetched
 // before it.  `more(v, chunk)` adds what a split tile's other members hold.
-template <typename Ready, typename More>
+// STEP: mode 2, otherwise modes 0 and 1.
+template <bool STEP, typename Ready, typename More>
 __device__ __forceinline__ bool epi_ns(uint32_t taddr, int first, int end, int step, int m, int M, int n0, int N, const NsArgs& a,
                                        uint8_t* __restrict__ stage, int lane, Ready&& ready, More&& more) {
   const int row_base = m - lane, lo = 32 * first;
   step *= 32;
   end = min(end, N - n0);
   if (row_base >= M || lo >= end) return ready();      // uniform across the warp
-  if (a.mode == 2) {
+  if constexpr (STEP) {
     float4 xn[8];
     lines_fetch_f32(xn, a.x32, a.ld, row_base, lane, M, n0 + lo);
     const float drow = a.by_column ? 0.f : a.din[m];
@@ -161,7 +162,7 @@ __device__ __forceinline__ bool epi_ns(uint32_t taddr, int first, int end, int s
       }
     }
     return true;
-  }
+  } else {
   const float drow = a.mode == 1 ? a.din[m] : 0.f;
   const int last = min(end, row_base - n0 + 32);       // chunks above the diagonal are stored from below it
   uint4 en[4];
@@ -214,4 +215,5 @@ __device__ __forceinline__ bool epi_ns(uint32_t taddr, int first, int end, int s
     if (n < row_base) ns_store_half_transposed(f, stage, a.out16, a.ld, row_base, n, lane);
   }
   return true;
+  }
 }
