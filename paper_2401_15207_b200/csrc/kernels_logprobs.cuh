@@ -11,7 +11,7 @@
 // moved once per batch, and its sums of e and e (x - m) relative to it; the block (and, for few rows, the up to eight
 // blocks of a cluster that share a row) joins them at the end.  The alternatives cost no second pass: the k-th largest of
 // the threads' own maxima is a lower bound of the k-th largest logit, so only the few threads whose maximum reaches it can
-// hold one, and their warps read those threads' elements again out of L2.  The same re-reading makes r exact when it is
+// hold one, and their warps read those threads' elements again out of L2, all at once.  The same re-reading makes r exact when it is
 // small: only the thread that holds the maximum added it to anything.
 #pragma once
 #include "common.cuh"
@@ -103,8 +103,27 @@ __device__ __forceinline__ unsigned long long lp_warp_max(unsigned long long key
   const uint32_t ml = __reduce_max_sync(0xffffffffu, hi == mh ? (uint32_t)key : 0u);
   return ((unsigned long long)mh << 32) | ml;
 }
-// one warp: the n largest of the `have` distinct keys in falling order into out (0: no more)
-__device__ __forceinline__ void lp_select(unsigned long long* keys, int have, int n, unsigned long long* out, int lane) {
+// one warp: the n largest of the `have` keys (distinct, or 0 for none) in falling order into out (0: no more).  Few keys: a key's
+// place is the number of larger ones, counted by every lane for its own; many: n rounds of the largest that is left.
+__device__ __forceinline__ void lp_select(const unsigned long long* keys, int have, int n, unsigned long long* out, int lane) {
+  if (have <= 96) {
+    if (lane < kLpMaxTop) out[lane] = 0ull;
+    unsigned long long q[3];
+    int above[3] = {0, 0, 0};
+#pragma unroll
+    for (int j = 0; j < 3; ++j) q[j] = lane + 32 * j < have ? keys[lane + 32 * j] : 0ull;
+    __syncwarp();
+#pragma unroll 4
+    for (int i = 0; i < have; ++i) {
+      const unsigned long long k = keys[i];
+#pragma unroll
+      for (int j = 0; j < 3; ++j) above[j] += k > q[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 3; ++j) if (q[j] != 0ull && above[j] < n) out[above[j]] = q[j];
+    __syncwarp();
+    return;
+  }
   unsigned long long last = ~0ull;
   for (int k = 0; k < n; ++k) {
     unsigned long long mine = 0ull;
@@ -119,6 +138,7 @@ __device__ __forceinline__ void lp_select(unsigned long long* keys, int have, in
 struct LpShared {
   float red[4][kLpThreads / 32];                       // per warp: maximum, sum, weighted sum
   uint32_t tmax[kLpThreads];
+  uint8_t few[kLpThreads];                // per warp: its lanes that can hold an alternative
   unsigned long long cand[kLpCand];
   unsigned long long top[kLpMaxTop];
   unsigned long long best;
@@ -291,17 +311,31 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const T* __r
   const bool poison = !(S < INFINITY);                                  // a NaN or +inf among the logits
   if (want_top && !poison && has) {
     const uint32_t bound = sh.bound;
-    unsigned who = __ballot_sync(0xffffffffu, sh.tmax[tid] >= bound && sh.tmax[tid] > kLpNone);
-    while (who && *(volatile int*)&sh.count <= kLpCand) {
-      const int i = warp * 32 + __ffs(who) - 1;
-      who &= who - 1;
-      reread(i, [&](float v, int at) {
-        const uint32_t o = lp_order(v);
-        if (o >= bound && o > kLpNone) {
-          const int slot = atomicAdd(&sh.count, 1);
-          if (slot < kLpCand) sh.cand[slot] = ((unsigned long long)o << 32) | (uint32_t)~at;
-        }
-      });
+    const bool can = sh.tmax[tid] >= bound && sh.tmax[tid] > kLpNone;
+    const unsigned who = __ballot_sync(0xffffffffu, can);
+    uint8_t* few = sh.few + warp * 32;
+    if (can) few[__popc(who & ((1u << lane) - 1u))] = (uint8_t)lane;
+    __syncwarp();
+    // all their elements at once: a lane takes one vector of one of them at a time
+    const int each = (v1 - v0 + nt - 1) / nt + (ns > 0 ? 1 : 0), items = __popc(who) * each;
+    auto see = [&](float v, int at) {
+      const uint32_t o = lp_order(v);
+      if (o >= bound && o > kLpNone) {
+        const int slot = atomicAdd(&sh.count, 1);
+        if (slot < kLpCand) sh.cand[slot] = ((unsigned long long)o << 32) | (uint32_t)~at;
+      }
+    };
+    for (int k = lane; k < items && *(volatile int*)&sh.count <= kLpCand; k += 32) {
+      const int i = warp * 32 + few[k / each], j = k % each;
+      const int c = v0 + i + j * nt;
+      if (ns > 0 && j == each - 1) {                                    // the thread's single element
+        if (i < ns) { const int at = lp_single<T>(rw, i); see(to_f(x[at]), at); }
+      } else if (c < v1) {
+        float p[V / 2], q[V / 2];
+        LpVec<T>::pairs(__ldg(xv + c), p, q);
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) { see(p[e], rw.head + c * V + 2 * e); see(q[e], rw.head + c * V + 2 * e + 1); }
+      }
     }
     __syncthreads();
     if (sh.count <= kLpCand) {
@@ -353,9 +387,11 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const T* __r
         return r;
       };
       auto ldf = [&](const void* p, uint32_t rank) { float v; asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote(p, rank))); return v; };
+      float pm = 0.f, pr = 0.f, pu = 0.f, ph = 0.f;                     // lane k: what block k found
+      if (lane < (int)parts) { pm = ldf(&sh.m, lane); pr = ldf(&sh.rest, lane); pu = ldf(&sh.u, lane); ph = ldf(&sh.has, lane); }
       for (uint32_t k = 1; k < parts; ++k) {
-        const float mk = ldf(&sh.m, k), rk = ldf(&sh.rest, k), uk = ldf(&sh.u, k);
-        const int hk = __float_as_int(ldf(&sh.has, k));
+        const float mk = __shfl_sync(0xffffffffu, pm, k), rk = __shfl_sync(0xffffffffu, pr, k), uk = __shfl_sync(0xffffffffu, pu, k);
+        const int hk = __float_as_int(__shfl_sync(0xffffffffu, ph, k));
         bad = bad || !(rk < INFINITY);
         if (mk > m_all || (!has_all && hk)) {                          // the other one's maximum leads
           const float d = (m_all - mk) * s2, f = lp_ex2(d), w = r_all + (has_all ? 1.f : 0.f);
@@ -439,7 +475,7 @@ struct LpBwdArgs {
   const float *stats, *entropy, *dlogp, *dentropy;
 };
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) token_logprobs_bwd_kernel(const T* logits, T* dlogits, LpBwdArgs a) {
+__global__ void __launch_bounds__(128) token_logprobs_bwd_kernel(const T* logits, T* dlogits, LpBwdArgs a) {
   constexpr int V = LpVec<T>::V;
   const int tid = threadIdx.x, nt = blockDim.x;
   for (int64_t task = blockIdx.x; task < a.rows * a.chunks; task += gridDim.x) {
@@ -447,36 +483,46 @@ __global__ void __launch_bounds__(256) token_logprobs_bwd_kernel(const T* logits
     const int part = (int)(task % a.chunks);
     const T* x = logits + row * a.ld;
     T* d = dlogits + row * a.ld;
+    LpRow rw;
+    uint4 w[4];
+    const int first = part * 4 * nt + tid;
+    if (VEC) {                                               // under way before the row's scalars are known
+      rw = lp_row(x, (int)a.ld);
+      const uint4* xv = reinterpret_cast<const uint4*>(x + rw.head);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) if (first + k * nt < rw.nv) w[k] = xv[first + k * nt];
+    }
     const int tok = a.tokens[row];
     const float m = a.stats[row], L = a.stats[a.rows + row];
     const bool zero = tok < 0 || tok >= a.vocab || m == -INFINITY;
     const float g = a.dlogp ? a.dlogp[row] * a.scale : 0.f, h = a.dentropy ? a.dentropy[row] * a.scale : 0.f;
-    const float hH = a.dentropy ? h * a.entropy[row] : 0.f, c0 = g + hH;
-    const float s2 = a.scale, l2 = kLog2E;
+    const float hH = a.dentropy ? h * a.entropy[row] : 0.f, c0 = g + hH, s = a.scale;
+    auto plain = [&](float v) {                              // any column but the token's
+      const float lp = fmaf(v - m, s, -L);
+      return -lp_ex2(lp * kLog2E) * fmaf(h, fmaxf(lp, -200.f), c0);        // p is 0 below -200; p x -inf would be NaN
+    };
     auto grad = [&](float v, int64_t at) {
       if (zero || at >= a.vocab) return 0.f;
-      const float lp = (v - m) * s2 - L, p = lp_ex2(lp * l2);
-      const float w = fmaxf(lp, -200.f);                     // p is 0 there; p x -inf would be NaN
-      if (at != tok) return -p * fmaf(h, w, c0);
-      return -expm1f(lp) * g - p * fmaf(h, w, hH);         // 1 - p of a token that is nearly sure
+      if (at != tok) return plain(v);
+      const float lp = fmaf(v - m, s, -L);
+      return -expm1f(lp) * g - lp_ex2(lp * kLog2E) * fmaf(h, fmaxf(lp, -200.f), hH);     // 1 - p of a token that is nearly sure
     };
     if (VEC) {
-      const LpRow rw = lp_row(x, (int)a.ld);
-      const uint4* xv = reinterpret_cast<const uint4*>(x + rw.head);
       uint4* dv = reinterpret_cast<uint4*>(d + rw.head);
-      const int c0v = part * 4 * nt + tid;
-      uint4 w[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) if (!zero && c0v + k * nt < rw.nv) w[k] = xv[c0v + k * nt];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const int c = c0v + k * nt;
+        const int c = first + k * nt;
         if (c >= rw.nv) break;
         const int64_t at = rw.head + (int64_t)c * V;
         float p[V / 2], q[V / 2];
         LpVec<T>::pairs(w[k], p, q);
+        if (!zero && at + V <= a.vocab && (unsigned)(tok - at) >= (unsigned)V) {
 #pragma unroll
-        for (int i = 0; i < V / 2; ++i) { p[i] = grad(p[i], at + 2 * i); q[i] = grad(q[i], at + 2 * i + 1); }
+          for (int i = 0; i < V / 2; ++i) { p[i] = plain(p[i]); q[i] = plain(q[i]); }
+        } else {
+#pragma unroll
+          for (int i = 0; i < V / 2; ++i) { p[i] = grad(p[i], at + 2 * i); q[i] = grad(q[i], at + 2 * i + 1); }
+        }
         dv[c] = LpVec<T>::join(p, q);
       }
       if (part == 0 && tid < rw.ns) { const int at = lp_single<T>(rw, tid); d[at] = from_f<T>(grad(zero ? 0.f : to_f(x[at]), at)); }
@@ -490,7 +536,7 @@ inline cudaError_t launch_token_logprobs_bwd(cudaStream_t st, const T* logits, T
   constexpr int V = LpVec<T>::V;
   const int64_t nv = (a.ld + V - 1) / V;
   int th = 32;
-  while (th < 256 && nv > 4 * th) th *= 2;
+  while (th < 128 && nv > 4 * th) th *= 2;
   a.chunks = (int)((nv + 4 * th - 1) / (4 * th));
   const int64_t tasks = a.rows * a.chunks;
   const unsigned grid = (unsigned)(tasks < (1 << 30) ? tasks : (1 << 30));
