@@ -31,6 +31,11 @@ cudaError_t attn_tc_bwd_launch(cudaStream_t st, int B, int S, int H, int dh, int
 // da, df [S] fp32 with S = min(rows, cols).  Everything 128-byte aligned.
 struct NsBuffers { int rows, cols; float* x32; void* x16[2]; void *e, *f; float *da, *df; };
 cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps);
+// The whole operation in one launch (ns_small.cuh) for a short side of at most 128 and a long one of at most 4096: momentum (if not
+// nullptr), normalisation, steps, and the result as o, or as the update of master (and param).
+bool ns_small_eligible(int64_t rows, int64_t cols);
+cudaError_t ns_small_launch(cudaStream_t st, bool g_bf16, int64_t rows, int64_t cols, const void* g, float* mom, float mu, int nesterov, int steps,
+                            void* o, float* master, void* param, float decay, float size);
 // Code-path switches for A/B timing and for tests (all 1 by default = the fast path): which = 0 CTA-pair
 // GEMM tiles, 1 programmatic dependent launch, 2 tcgen05 attention forward, 3 tcgen05 attention backward.
 // value >= 0 sets the switch; returns its previous value (-1: no such switch).  Process-wide; read at

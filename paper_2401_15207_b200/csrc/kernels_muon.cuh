@@ -165,6 +165,8 @@ struct NsUpdate { bf16* o; float* master; bf16* param; float decay, size; };   /
 template <typename T>
 inline cudaError_t launch_orthogonalize(cudaStream_t st, int64_t rows, int64_t cols, const T* g, float* mom, float mu, int nesterov,
                                         int steps, const NsUpdate& to, void* scratch) {
+  if (ns_small_eligible(rows, cols))
+    return ns_small_launch(st, sizeof(T) == 2, rows, cols, g, mom, mu, nesterov, steps, to.o, to.master, to.param, to.decay, to.size);
   const int pr = ns_pad(rows), pc = ns_pad(cols), s = pr < pc ? pr : pc;
   char* w = (char*)scratch;
   auto take = [&](size_t bytes) { char* p = w; w += (bytes + 255) / 256 * 256; return p; };
