@@ -8,7 +8,7 @@
 //   A = X X^T: every CTA's part by tcgen05.mma over its own columns; the 32 x 32 units of the lower triangle are summed by one CTA
 //   each (fixed order) and handed to all as fp16 E and fp32 diagonal, through distributed shared memory;
 //   P(A): every CTA for itself, one 128 x 128 x 128 product;  X <- (a + diag) X + F X: its own columns.
-constexpr int kSmThreads = 256;
+constexpr int kSmThreads = 512;                        // 16 warps: lane quarter q = warp mod 4, of every 128 columns the 32-column chunk warp / 4
 constexpr int kSmTile = 128 * 128;                     // bytes of a [128][64] fp16 tile
 struct NsSmallArgs {
   const void* g; float* mom;                           // the matrix (fp32 or bf16), and the momentum to update or nullptr
@@ -16,7 +16,7 @@ struct NsSmallArgs {
   int rows, cols, steps, nesterov;
   float mu, decay, size;
 };
-template <int NH> constexpr int ns_small_smem = 1024 + (2 * NH + 4) * kSmTile + 60 * 1024 + 8 * 2048 + 3 * 512 + 16 * 8 + 64;
+template <int NH> constexpr int ns_small_smem = 1024 + (2 * NH + 4) * kSmTile + 64 * 1024 + 3 * 512 + 16 * 8 + 64;
 
 // shared-memory descriptor, 128-byte swizzle, 8-row groups 1024 bytes apart; `lead`: bytes to the next 64-wide box of an MN-major tile
 __device__ __forceinline__ uint64_t ns_desc(uint32_t saddr, uint32_t lead) {
@@ -58,12 +58,13 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
   extern __shared__ uint8_t smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* sm = smem_raw + (base - smem_u32(smem_raw));
-  const uint32_t xt = base, et = xt + 2 * NH * kSmTile, ft = et + 2 * kSmTile, recv = ft + 2 * kSmTile, stg = recv + 60 * 1024;
-  const uint32_t da_s = stg + 8 * 2048, df_s = da_s + 512, red_s = df_s + 512, nrm_s = red_s + 512, bar = nrm_s + 128, slot_s = bar + 8;
+  const uint32_t xt = base, et = xt + 2 * NH * kSmTile, ft = et + 2 * kSmTile, recv = ft + 2 * kSmTile;
+  const uint32_t stg = ft;                              // 2 KB per warp to turn a unit over: F is written later
+  const uint32_t da_s = recv + 64 * 1024, df_s = da_s + 512, red_s = df_s + 512, nrm_s = red_s + 512, bar = nrm_s + 128, slot_s = bar + 8;
   auto gen = [&](uint32_t s) { return sm + (s - base); };
   float *dA = (float*)gen(da_s), *dF = (float*)gen(df_s);
   double *red = (double*)gen(red_s), *nrm = (double*)gen(nrm_s);
-  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, q = warp & 3, half = warp >> 2;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, q = warp & 3, sub = warp >> 2;
   uint32_t C, me;
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
   me = cluster_ctarank();
@@ -85,11 +86,11 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
   // the step's accumulator of column block h; the second block's takes the place of the polynomial's, which is done by then
   auto acc2 = [&](int h) { return h == 0 ? acc1 + 128 : acc1; };
 
-  // ---- the matrix: this thread's row m of the turned matrix and, of every 128 columns, 64 in two chunks of 32
+  // ---- the matrix: this thread's row m of the turned matrix and, of every 128 columns, one chunk of 32
   const bool wide = a.rows <= a.cols;
   const int S0 = wide ? a.rows : a.cols, L0 = wide ? a.cols : a.rows;
   const int m = q * 32 + lane;
-  auto col = [&](int k) { return (k >> 1) * 128 + half * 64 + (k & 1) * 32; };                     // of this CTA's columns
+  auto col = [&](int k) { return k * 128 + sub * 32; };                                           // of this CTA's columns
   // A chunk is 32 x 32: lines of 32 consecutive elements in memory, ni of them with nl elements that exist.  If the rows are as
   // in memory a line is a row and goes to its lane through shared memory (the receive buffer, free at both ends); else it is a column.
   struct Chunk { size_t at; int ni, nl; };
@@ -97,19 +98,19 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
     const int j = (int)me * (128 * NH) + col(k), rows_left = max(0, min(32, S0 - q * 32)), cols_left = max(0, min(32, L0 - j));
     return wide ? Chunk{(size_t)(q * 32) * a.cols + j, rows_left, cols_left} : Chunk{(size_t)j * a.cols + q * 32, cols_left, rows_left};
   };
-  float* turn = reinterpret_cast<float*>(gen(recv)) + warp * (32 * 33);
+  float* turn = reinterpret_cast<float*>(gen(recv)) + warp * 1024;
   auto turned = [&](float (&f)[32]) {                  // f[i] of lane l <-> f[l] of lane i
     if (!wide) return;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) turn[i * 33 + lane] = f[i];
+    for (int i = 0; i < 32; ++i) turn[i * 32 + (lane ^ i)] = f[i];
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < 32; ++i) f[i] = turn[lane * 33 + i];
+    for (int i = 0; i < 32; ++i) f[i] = turn[lane * 32 + (lane ^ i)];
     __syncwarp();
   };
   double s = 0.0;
 #pragma unroll 1
-  for (int k = 0; k < 2 * NH; ++k) {
+  for (int k = 0; k < NH; ++k) {
     const Chunk ch = chunk(k);
     const bool in = lane < ch.nl;
     const T* gp = reinterpret_cast<const T*>(a.g) + ch.at + lane;
@@ -144,7 +145,7 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
   cluster_sync_all();                                  // and every CTA of the cluster has started
   if (tid < (int)C) {                                  // this CTA's sum to all
     double t = 0.0;
-    for (int w = 0; w < 8; ++w) t += red[w];
+    for (int w = 0; w < kSmThreads / 32; ++w) t += red[w];
     asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(ns_peer(nrm_s + 8 * me, tid)), "d"(t) : "memory");
   }
   cluster_sync_all();
@@ -158,14 +159,14 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
   // chunk k of the iterate: kept in tensor memory, and its fp16 image in the operand tiles
   auto put_x = [&](int k, float (&f)[32]) {
     tmem_st32(xtm + lanes + col(k), f);
-    uint8_t* tile = gen(xt) + (2 * (k >> 1) + half) * kSmTile;
+    uint8_t* tile = gen(xt) + (2 * k + (sub >> 1)) * kSmTile;
 #pragma unroll
     for (int i = 0; i < 32; ++i) f[i] *= kNsScale;
 #pragma unroll
-    for (int sg = 0; sg < 4; ++sg) *reinterpret_cast<uint4*>(tile + ns_seg(m, (k & 1) * 4 + sg)) = ns_half8(f + 8 * sg);
+    for (int sg = 0; sg < 4; ++sg) *reinterpret_cast<uint4*>(tile + ns_seg(m, (sub & 1) * 4 + sg)) = ns_half8(f + 8 * sg);
   };
 #pragma unroll 1
-  for (int k = 0; k < 2 * NH; ++k) {
+  for (int k = 0; k < NH; ++k) {
     uint32_t v[32];
     float f[32];
     tmem_ld32(xtm + lanes + col(k), v);
@@ -202,11 +203,9 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
         for (int kk = 0; kk < 4; ++kk) tc_mma(acc1, d + kk * 2, d + kk * 2, kIdesc, (t | kk) != 0);
       }
     });
-    // ---- sum of the parts: unit (q, c), c <= q, number l = q (q + 1) / 2 + c, belongs to CTA l mod C, to the warp (q, c mod 2) of it
-#pragma unroll 1
-    for (int c = half; c <= q; c += 2) {
-      const int l = q * (q + 1) / 2 + c, o = l % (int)C;
-      if (o == (int)me) continue;                      // uniform across the warp
+    // ---- sum of the parts: unit (q, c), c <= q, number l = q (q + 1) / 2 + c, belongs to CTA l mod C, to the warp (q, c) of it
+    const int c = sub, l = q * (q + 1) / 2 + c, o = l % (int)C;
+    if (c <= q && o != (int)me) {                      // uniform across the warp
       uint32_t v[32];
       tmem_ld32(acc1 + lanes + 32 * c, v);
       const int from = (int)me < o ? (int)me : (int)me - 1;
@@ -216,10 +215,7 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
     }
     __syncwarp();
     cluster_sync_all();
-#pragma unroll 1
-    for (int c = half; c <= q; c += 2) {
-      const int l = q * (q + 1) / 2 + c;
-      if (l % (int)C != (int)me) continue;
+    if (c <= q && o == (int)me) {
       uint32_t v[32];
       tmem_ld32(acc1 + lanes + 32 * c, v);
       float f[32];
@@ -280,8 +276,7 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
     });
     // ---- F = b E + c (E E + (d_i + d_j) E), the diagonal apart
     const float dm = dA[m];
-#pragma unroll 1
-    for (int c = 2 * half; c < 2 * half + 2; ++c) {
+    {
       uint32_t v[32];
       tmem_ld32(acc1 + lanes + 32 * c, v);
       const uint8_t* er = gen(et) + (c >> 1) * kSmTile;
@@ -319,10 +314,10 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
     });
     const float scale = kNsA + dF[m];
 #pragma unroll 1
-    for (int k = 0; k < 2 * NH; ++k) {
+    for (int k = 0; k < NH; ++k) {
       uint32_t v[32], xo[32];
       float f[32];
-      tmem_ld32_nowait(acc2(k >> 1) + lanes + 64 * half + 32 * (k & 1), v);
+      tmem_ld32_nowait(acc2(k) + lanes + 32 * sub, v);
       tmem_ld32(xtm + lanes + col(k), xo);
       tmem_ld_wait32(v);
 #pragma unroll
@@ -334,7 +329,7 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
   // ---- the result, unless a product gave up on a wait
   const bool write = *(volatile int*)&g_tc_error == 0;
 #pragma unroll 1
-  for (int k = 0; k < 2 * NH; ++k) {
+  for (int k = 0; k < NH; ++k) {
     uint32_t v[32];
     float f[32];
     tmem_ld32(xtm + lanes + col(k), v);
