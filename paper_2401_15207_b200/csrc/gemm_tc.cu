@@ -1473,7 +1473,7 @@ cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps) {
     n.mode = 1; n.e = (const __half*)b.e; n.din = b.da; n.out16 = (__half*)b.f; n.dout = b.df; n.ld = S;
     if ((r = launch_ns<false, false, 1>(st, S, S, S, e_a, e_b, t_poly, n)) != cudaSuccess) return r;
     n = NsArgs{};
-    n.mode = 2; n.by_column = !wide; n.din = b.df; n.x32 = b.x32; n.out16 = i + 1 < steps ? (__half*)b.x16[cur ^ 1] : nullptr; n.ld = b.cols;
+    n.mode = 2; n.late = i + 2 >= steps; n.by_column = !wide; n.din = b.df; n.x32 = b.x32; n.out16 = i + 1 < steps ? (__half*)b.x16[cur ^ 1] : nullptr; n.ld = b.cols;
     r = wide ? launch_ns<false, true, 2>(st, b.rows, b.cols, S, f_a, x_s[cur], t_step, n) : launch_ns<false, false, 2>(st, b.rows, b.cols, S, x_s[cur], f_b, t_step, n);
     if (r != cudaSuccess) return r;
   }

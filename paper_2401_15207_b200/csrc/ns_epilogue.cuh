@@ -7,17 +7,29 @@
 //   - the diagonals of A and P(A), which near the end are 1 and -2.7 against off-diagonal entries of about 1 / sqrt(n), stay
 //     fp32 vectors; the fp16 matrices E and F hold zeros there.  With A = D + E:
 //         P(A)_ij = b E_ij + c ((E E)_ij + (d_i + d_j) E_ij),   P(A)_ii = b d_i + c ((E E)_ii + d_i^2),
-//         X_new = (a + P(A)_ii) X + F X.
-// Relative error of the result against 64 bits, measured over Gaussian, low-rank and heavy-tailed matrices: 1e-4 to 2e-3 (all-bf16
-// products: 7e-3 on full-rank matrices, 5e-2 to 1 on low-rank ones, whose rounding noise is amplified like a signal).
+//         X_new = a X + P(A)_ii Y + F X16 / 2^10.
+//     Y is the iterate as the products see it (rounded) in all but the last two steps, so that P(A) as a whole acts on one and the same
+//     matrix: if P(A) has a low rank so has the rounding noise that it passes on, which the later steps would amplify like a signal
+//     (with the fp32 iterate there, a rank-1 16 x 300 matrix comes out 2e-2 off).  In the last two steps nothing amplifies any more,
+//     and Y is the fp32 iterate, which spares the large diagonals that rounding.
+// Relative error of the result before its own rounding, from a CPU model of these roundings over Gaussian, low-rank (1 to 8), decaying,
+// sparse, one-row and outlier matrices of 4 x 40 to 512 x 512: at most 2.4e-3, typically 3e-4 to 1e-3 (all-bf16 products: 7e-3 on
+// full-rank matrices, 5e-2 to 1 on low-rank ones).
 // A and P(A) are symmetric: only tiles that touch the lower triangle are computed, and a 32 x 32 chunk below the diagonal is
 // stored a second time transposed.  All dimensions are multiples of 64 (zero-padded scratch), so a chunk exists or not as a whole.
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kNsScale = 1024.0f;
 
+// one element of the new iterate: x the old one, d the diagonal of P(A), acc = (F X16)
+__device__ __forceinline__ float ns_new_x(float x, float d, float acc, int late) {
+  const float y = late ? x * kNsScale : __half2float(__float2half_rn(x * kNsScale));
+  return fmaf(kNsA, x, fmaf(d, y, acc) * (1.0f / kNsScale));
+}
+
 struct NsArgs {
   int mode;                // 0: A from X, 1: P(A) from E, 2: the new X
   int by_column;           // mode 2: the diagonal belongs to the columns (right-hand product)
+  int late;                // mode 2: one of the last two steps: the diagonal acts on the fp32 iterate
   __half* out16;           // E, F or the fp16 image of the new X (nullptr: not wanted)
   const __half* e;         // mode 1: E
   const float* din;        // mode 1: diagonal of A, mode 2: of P(A)
@@ -149,10 +161,10 @@ __device__ __forceinline__ bool epi_ns(uint32_t taddr, int first, int end, int s
       for (int j = 0; j < 8; ++j) {
         float4 d = make_float4(drow, drow, drow, drow);
         if (a.by_column) d = *reinterpret_cast<const float4*>(a.din + n0 + c0 + 4 * j);
-        f[4 * j] = fmaf(kNsA + d.x, xc[j].x, __uint_as_float(v[4 * j]) * (1.0f / kNsScale));
-        f[4 * j + 1] = fmaf(kNsA + d.y, xc[j].y, __uint_as_float(v[4 * j + 1]) * (1.0f / kNsScale));
-        f[4 * j + 2] = fmaf(kNsA + d.z, xc[j].z, __uint_as_float(v[4 * j + 2]) * (1.0f / kNsScale));
-        f[4 * j + 3] = fmaf(kNsA + d.w, xc[j].w, __uint_as_float(v[4 * j + 3]) * (1.0f / kNsScale));
+        const float xs[4] = {xc[j].x, xc[j].y, xc[j].z, xc[j].w}, ds[4] = {d.x, d.y, d.z, d.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          f[4 * j + i] = ns_new_x(xs[i], ds[i], __uint_as_float(v[4 * j + i]), a.late);
       }
       epi_store32_lines<true>(f, stage, a.x32, a.ld, m, lane, M, n0 + c0, nullptr);
       if (a.out16) {

@@ -7,7 +7,7 @@
 // Per step (arithmetic as in ns_epilogue.cuh):
 //   A = X X^T: every CTA's part by tcgen05.mma over its own columns; the 32 x 32 units of the lower triangle are summed by one CTA
 //   each (fixed order) and handed to all as fp16 E and fp32 diagonal, through distributed shared memory;
-//   P(A): every CTA for itself, one 128 x 128 x 128 product;  X <- (a + diag) X + F X: its own columns.
+//   P(A): every CTA for itself, one 128 x 128 x 128 product;  the new X: its own columns.
 constexpr int kSmThreads = 512;                        // 16 warps: lane quarter q = warp mod 4, of every 128 columns the 32-column chunk warp / 4
 constexpr int kSmTile = 128 * 128;                     // bytes of a [128][64] fp16 tile
 struct NsSmallArgs {
@@ -312,7 +312,8 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
         for (int kk = 0; kk < 4; ++kk) tc_mma(acc2(t >> 1), da + kk * 2, db + kk * (16 * 128 >> 4), kIdescN, ((t & 1) | kk) != 0);
       }
     });
-    const float scale = kNsA + dF[m];
+    const float df = dF[m];
+    const int late = step + 2 >= a.steps;
 #pragma unroll 1
     for (int k = 0; k < NH; ++k) {
       uint32_t v[32], xo[32];
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
       tmem_ld32(xtm + lanes + col(k), xo);
       tmem_ld_wait32(v);
 #pragma unroll
-      for (int i = 0; i < 32; ++i) f[i] = fmaf(scale, __uint_as_float(xo[i]), __uint_as_float(v[i]) * (1.0f / kNsScale));
+      for (int i = 0; i < 32; ++i) f[i] = ns_new_x(__uint_as_float(xo[i]), df, __uint_as_float(v[i]), late);
       put_x(k, f);
     }
     fence_proxy_async_all();

@@ -13,12 +13,18 @@ static_assert(kLpMaxTop == HIFT_MAX_TOP, "");
 
 namespace {
 
+// a launch's result; an error does not stay behind for the next call's check
+hift_status status_of(cudaError_t e) {
+  if (e == cudaSuccess) return HIFT_OK;
+  cudaGetLastError();
+  return HIFT_ERR_CUDA;
+}
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 hift_status logprobs_cfg(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, double temperature, float* scale) {
   if (dtype < 0 || dtype > 1 || rows < 0 || rows > INT32_MAX || vocab < 1 || ld < vocab || ld > INT32_MAX - 65536) return HIFT_ERR_CFG;
   *scale = (float)(1.0 / temperature);
-  if (!(temperature > 0.0) || !isfinite(temperature) || !isnormal(*scale)) return HIFT_ERR_CFG;
+  if (!(temperature > 0.0) || !isfinite(temperature) || !isnormal(*scale) || !isfinite(*scale * kLog2E)) return HIFT_ERR_CFG;
   return HIFT_OK;
 }
 
@@ -122,7 +128,7 @@ hift_status hift_k_token_logprobs(int32_t dtype, int64_t rows, int64_t vocab, in
   const LpArgs a{tokens, (int)vocab, n_top, ld, rows, scale, logp, entropy, stats, top_logp, top_ids, bad};
   const cudaError_t e = dtype == 0 ? launch_token_logprobs((cudaStream_t)stream, (const float*)logits, a)
                                    : launch_token_logprobs((cudaStream_t)stream, (const bf16*)logits, a);
-  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
+  return status_of(e);
 }
 
 hift_status hift_k_token_logprobs_bwd(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void* logits, const int32_t* tokens,
@@ -137,7 +143,7 @@ hift_status hift_k_token_logprobs_bwd(int32_t dtype, int64_t rows, int64_t vocab
   const LpBwdArgs a{tokens, (int)vocab, 0, ld, rows, scale, stats, entropy, dlogp, dentropy};
   const cudaError_t e = dtype == 0 ? launch_token_logprobs_bwd((cudaStream_t)stream, (const float*)logits, (float*)dlogits, a)
                                    : launch_token_logprobs_bwd((cudaStream_t)stream, (const bf16*)logits, (bf16*)dlogits, a);
-  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
+  return status_of(e);
 }
 
 hift_status hift_k_join_fwd(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double eps, double res_scale, const float* x,
@@ -157,7 +163,7 @@ hift_status hift_k_join_fwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
   cudaStream_t st = (cudaStream_t)stream;
   const cudaError_t e = dtype == 0 ? (kind == 0 ? launch_join_fwd<float, 0>(st, th, nc, p) : launch_join_fwd<float, 1>(st, th, nc, p))
                                    : (kind == 0 ? launch_join_fwd<bf16, 0>(st, th, nc, p) : launch_join_fwd<bf16, 1>(st, th, nc, p));
-  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
+  return status_of(e);
 }
 
 size_t hift_join_bwd_scratch_bytes(int64_t rows, int64_t cols, int64_t rows_per_gate) {
@@ -196,7 +202,7 @@ hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
     const dim3 g((unsigned)((cols + 31) / 32), (unsigned)(kJoinPlanes - 1 + (dgate && pl.split > 0 ? pl.n_gates : 0)));
     e = launch_pdl(join_sums_kernel, g, dim3(32, 32), 0, st, (const float*)scratch, o, pl.ctas, (int)cols, pl.split);
   }
-  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
+  return status_of(e);
 }
 
 size_t hift_orthogonalize_scratch_bytes(int64_t rows, int64_t cols) {
@@ -213,7 +219,7 @@ hift_status hift_k_orthogonalize(int32_t dtype, int64_t rows, int64_t cols, cons
   const NsUpdate to{(bf16*)o, nullptr, nullptr, 0.f, 0.f};
   const cudaError_t e = dtype == 0 ? launch_orthogonalize((cudaStream_t)stream, rows, cols, (const float*)g, nullptr, 0.f, 0, steps, to, scratch)
                                    : launch_orthogonalize((cudaStream_t)stream, rows, cols, (const bf16*)g, nullptr, 0.f, 0, steps, to, scratch);
-  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
+  return status_of(e);
 }
 
 hift_status hift_muon_step(int64_t rows, int64_t cols, void* param_bf16, float* master, const float* grad, float* momentum_buf,
@@ -227,7 +233,7 @@ hift_status hift_muon_step(int64_t rows, int64_t cols, void* param_bf16, float* 
   const double size = lr * 0.2 * sqrt((double)(rows > cols ? rows : cols));
   const NsUpdate to{nullptr, master, (bf16*)param_bf16, (float)(1.0 - lr * weight_decay), (float)size};
   const cudaError_t e = launch_orthogonalize((cudaStream_t)stream, rows, cols, grad, momentum_buf, (float)momentum, nesterov != 0, steps, to, scratch);
-  return e == cudaSuccess ? HIFT_OK : HIFT_ERR_CUDA;
+  return status_of(e);
 }
 
 }  // extern "C"

@@ -26,7 +26,7 @@ def _logp(L, **kw):
 @pytest.mark.parametrize("kw,want", [
     (dict(dtype=2), CFG), (dict(rows=-1), CFG), (dict(rows=1 << 31), CFG), (dict(vocab=0), CFG), (dict(ld=99), CFG),
     (dict(vocab=1 << 31, ld=1 << 31), CFG), (dict(temp=0.0), CFG), (dict(temp=-1.0), CFG), (dict(temp=float("nan")), CFG),
-    (dict(temp=float("inf")), CFG), (dict(temp=1e-40), CFG), (dict(temp=1e40), CFG), (dict(top=-1), CFG), (dict(top=33), CAPACITY),
+    (dict(temp=float("inf")), CFG), (dict(temp=1e-40), CFG), (dict(temp=3.2e-39), CFG), (dict(temp=1e40), CFG), (dict(top=-1), CFG), (dict(top=33), CAPACITY),
     (dict(logits=None), INPUT), (dict(tokens=None), INPUT), (dict(logp=None), INPUT), (dict(ids=None), INPUT), (dict(vals=None), INPUT),
     (dict(logits=P + 1), CFG), (dict(dtype=0, logits=P + 2), CFG), (dict(rows=0, logits=None, tokens=None, logp=None), 0)])
 def test_token_logprobs_refuses(L, kw, want):
