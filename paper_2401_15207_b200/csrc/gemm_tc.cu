@@ -1047,6 +1047,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
 #include "attention_tc.cuh"
 #include "attention_bwd_tc.cuh"
 #include "ns_small.cuh"
+#include "ns_tiny.cuh"
 
 // ------------------------------------------------------------------ host side
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -1241,25 +1242,24 @@ NsTile ns_tile(int M, int N, int K, bool sym, bool mn) {
   }
   return t;
 }
-template <typename T, int NH>
-cudaError_t set_smem_attr_small() {
-  const cudaError_t e = cudaFuncSetAttribute(ns_small_kernel<T, NH>, cudaFuncAttributeMaxDynamicSharedMemorySize, ns_small_smem<NH>);
-  return e != cudaSuccess ? e : cudaFuncSetAttribute(ns_small_kernel<T, NH>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+// One cluster of `ctas` (up to 16, which is beyond the portable size) for the whole matrix.
+cudaError_t set_attr_ns_cluster(void (*kernel)(NsSmallArgs), int smem) {
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
-template <typename T, int NH>
-cudaError_t launch_ns_small(cudaStream_t st, int ctas, const NsSmallArgs& a) {
+cudaError_t launch_ns_cluster(cudaStream_t st, void (*kernel)(NsSmallArgs), int smem, int threads, int ctas, const NsSmallArgs& a) {
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
   cfg.gridDim = dim3(ctas);
-  cfg.blockDim = dim3(kSmThreads);
-  cfg.dynamicSmemBytes = ns_small_smem<NH>;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = ctas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, ns_small_kernel<T, NH>, a);
+  return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 int g_attn_tc = 1;       // tcgen05 attention forward (switch 2; 0 falls back to the mma.sync kernel)
 int g_attn_bwd_tc = 1;   // tcgen05 attention backward (switch 3; 0 falls back to the mma.sync kernels)
@@ -1313,10 +1313,14 @@ int gemm_tc_init() {
   if (e == cudaSuccess) e = set_smem_attr2<false, true, true>();
   if (e == cudaSuccess) e = set_smem_attr2<true, true, true>();
   if (e == cudaSuccess) e = set_smem_attr2<true, true, false>();
-  if (e == cudaSuccess) e = set_smem_attr_small<float, 1>();
-  if (e == cudaSuccess) e = set_smem_attr_small<float, 2>();
-  if (e == cudaSuccess) e = set_smem_attr_small<__nv_bfloat16, 1>();
-  if (e == cudaSuccess) e = set_smem_attr_small<__nv_bfloat16, 2>();
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<float, 1>, ns_small_smem<1>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<float, 2>, ns_small_smem<2>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<__nv_bfloat16, 1>, ns_small_smem<1>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<__nv_bfloat16, 2>, ns_small_smem<2>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<float, 1>, ns_tiny_smem<1>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<float, 2>, ns_tiny_smem<2>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<__nv_bfloat16, 1>, ns_tiny_smem<1>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<__nv_bfloat16, 2>, ns_tiny_smem<2>);
   if (e == cudaSuccess) e = set_smem_attr_ns<false, false, 1>();
   if (e == cudaSuccess) e = set_smem_attr_ns<true, true, 1>();
   if (e == cudaSuccess) e = set_smem_attr_ns<false, false, 2>();
@@ -1425,18 +1429,23 @@ cudaError_t gemm_tc_launch(cudaStream_t st, const GemmArgs& g) {
 
 bool ns_small_eligible(int64_t rows, int64_t cols) {
   const int64_t s = rows < cols ? rows : cols, l = rows < cols ? cols : rows;
-  return s <= 128 && l <= 16 * 256;
+  return s <= kTinyRows ? l <= 16 * kTinyThreads * 2 : s <= 128 && l <= 16 * 256;
 }
 cudaError_t ns_small_launch(cudaStream_t st, bool g_bf16, int64_t rows, int64_t cols, const void* g, float* mom, float mu, int nesterov, int steps,
                             void* o, float* master, void* param, float decay, float size) {
   if (gemm_tc_init() != 0) return cudaErrorNotSupported;
-  const int L = (int)(rows < cols ? cols : rows);
+  const int S = (int)(rows < cols ? rows : cols), L = (int)(rows < cols ? cols : rows);
   const NsSmallArgs a{g, mom, (__nv_bfloat16*)o, master, (__nv_bfloat16*)param, (int)rows, (int)cols, steps, nesterov, mu, decay, size};
-  const int nh = L <= 16 * 128 ? 1 : 2;
+  const bool tiny = S <= kTinyRows;
+  const int unit = tiny ? kTinyThreads : 128, per = L <= 16 * unit ? 1 : 2;      // columns of a CTA: unit * per
   int ctas = 1;
-  while (ctas * 128 * nh < L) ctas *= 2;
-  if (g_bf16) return nh == 1 ? launch_ns_small<__nv_bfloat16, 1>(st, ctas, a) : launch_ns_small<__nv_bfloat16, 2>(st, ctas, a);
-  return nh == 1 ? launch_ns_small<float, 1>(st, ctas, a) : launch_ns_small<float, 2>(st, ctas, a);
+  while (ctas * unit * per < L) ctas *= 2;
+  if (tiny) {
+    auto k = g_bf16 ? (per == 1 ? ns_tiny_kernel<__nv_bfloat16, 1> : ns_tiny_kernel<__nv_bfloat16, 2>) : (per == 1 ? ns_tiny_kernel<float, 1> : ns_tiny_kernel<float, 2>);
+    return launch_ns_cluster(st, k, per == 1 ? ns_tiny_smem<1> : ns_tiny_smem<2>, kTinyThreads, ctas, a);
+  }
+  auto k = g_bf16 ? (per == 1 ? ns_small_kernel<__nv_bfloat16, 1> : ns_small_kernel<__nv_bfloat16, 2>) : (per == 1 ? ns_small_kernel<float, 1> : ns_small_kernel<float, 2>);
+  return launch_ns_cluster(st, k, per == 1 ? ns_small_smem<1> : ns_small_smem<2>, kSmThreads, ctas, a);
 }
 
 cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps) {

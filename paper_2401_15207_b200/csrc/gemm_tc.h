@@ -31,8 +31,8 @@ cudaError_t attn_tc_bwd_launch(cudaStream_t st, int B, int S, int H, int dh, int
 // da, df [S] fp32 with S = min(rows, cols).  Everything 128-byte aligned.
 struct NsBuffers { int rows, cols; float* x32; void* x16[2]; void *e, *f; float *da, *df; };
 cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps);
-// The whole operation in one launch (ns_small.cuh) for a short side of at most 128 and a long one of at most 4096: momentum (if not
-// nullptr), normalisation, steps, and the result as o, or as the update of master (and param).
+// The whole operation in one launch for a short side of at most 16 and a long one of at most 16384 (ns_tiny.cuh) or of at most 128 and
+// 4096 (ns_small.cuh): momentum (if not nullptr), normalisation, steps, and the result as o, or as the update of master (and param).
 bool ns_small_eligible(int64_t rows, int64_t cols);
 cudaError_t ns_small_launch(cudaStream_t st, bool g_bf16, int64_t rows, int64_t cols, const void* g, float* mom, float mu, int nesterov, int steps,
                             void* o, float* master, void* param, float decay, float size);

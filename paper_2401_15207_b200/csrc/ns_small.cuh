@@ -1,4 +1,5 @@
-// The whole orthogonalisation of a matrix with a short side of at most 128 in one launch; included by gemm_tc.cu.
+// The whole orthogonalisation of a matrix with a short side of 17 to 128 and a long one of at most 4096 in one launch; included by
+// gemm_tc.cu.
 //
 // Through separate products such a matrix is 18 launches of a few microseconds each, whatever its size (64 x 300: 80 us, most of it
 // launch latency, and 65 us of host time).  Here the matrix, turned so that the short side are the rows, stays on chip: a cluster of up to 16
