@@ -514,8 +514,9 @@ hift_status hift_k_cross_entropy(int32_t dtype, int64_t rows, int64_t vocab, int
 /* ---- operators beside the step ---------------------------------------------
  * What fine-tuning with objectives and updates other than the step's own needs, on caller-owned device buffers.  All
  * launch on `cuda_stream` (on the device that is current, whose buffers they are given), do not synchronise and do
- * not allocate; they can be captured into a CUDA graph.  Calls that overlap on the GPU need scratch buffers of their
- * own.  Inputs and outputs must not overlap except where it is said.  A call that is refused launches nothing. */
+ * not allocate.  They can be captured into a CUDA graph; the first call of an operator on a device sets its kernels up
+ * and is made before any capture.  Calls that overlap on the GPU need scratch buffers of their own.  Inputs and outputs
+ * must not overlap except where it is said.  A call that is refused launches nothing. */
 
 /* Log-probabilities of given tokens under rows of logits[rows, ld] (columns >= vocab are padding and not read):
  *     z = x / temperature,  log p = z - log sum exp z,  logp_dev[r] = log p[tokens_dev[r]],
@@ -524,8 +525,7 @@ hift_status hift_k_cross_entropy(int32_t dtype, int64_t rows, int64_t vocab, int
  *     rising order of the id; places without a token whose logit is above -inf hold id -1 and -inf.
  *     stats_dev fp32 [2*rows] (may be NULL): the row's largest logit x | log sum_i exp(z_i - z_max): what the gradient takes.
  * The logits are read once and left as they are; sums are fp32, a log p below the range of fp32 is -inf.  A logit of -inf is a
- * token that cannot occur.  tokens_dev[r] < 0: the
- * row is ignored, whatever it holds (0, 0, stats 0 | 0, ids -1, -inf); tokens_dev[r] >= vocab: likewise, and *bad_dev
+ * token that cannot occur.  tokens_dev[r] < 0: the row is ignored, whatever it holds (0, 0, stats 0 | 0, ids -1, -inf); tokens_dev[r] >= vocab: likewise, and *bad_dev
  * (int32, may be NULL) is set to 1 (and never cleared by the library).  A row with nothing above -inf: logp -inf,
  * entropy 0, stats -inf | 0, no alternatives.  A row that holds a NaN or +inf: NaN everywhere, ids -1.
  * dtype 0: fp32 logits, 1: bf16; the rows may start anywhere an element may (any ld >= vocab).  rows = 0 is allowed.
@@ -578,9 +578,12 @@ hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
 /* Orthogonalisation of a matrix by Newton-Schulz products:
  *     X_0 = G / max(|G|_F, 1e-30),   X <- a X + (b A + c A A) X,  A = X X^T  (right-hand products when rows > cols),
  * `steps` times, (a, b, c) = (3.4445, -4.7750, 2.0315): every singular value s of X goes to a s + b s^3 + c s^5, which brings all but
- * the smallest to between 0.68 and 1.14 in five steps.  g_dev [rows, cols] fp32 (dtype 0) or bf16 (1), o_dev bf16 [rows, cols].  A zero matrix
+ * the smallest to between 0.68 and 1.14 in five steps.  g_dev [rows, cols] fp32 (dtype 0) or bf16 (1), o_dev bf16 [rows, cols].
+ * The products run in 16-bit floating point with fp32 sums, around an iterate kept in fp32 (all in fp32 for a short side of at most 16):
+ * before its rounding to bf16 the result is within 2^-8 of the definition, relative to its Frobenius norm.  A zero matrix
  * stays zero; NaN or infinity anywhere makes the whole result NaN.  1 <= rows, cols <= HIFT_ORTHOGONALIZE_MAX_DIM
- * (HIFT_ERR_CAPACITY), 1 <= steps <= 20.  scratch_dev: 256-byte aligned, hift_orthogonalize_scratch_bytes(rows, cols) bytes. */
+ * (HIFT_ERR_CAPACITY), 1 <= steps <= 20.  scratch_dev: 256-byte aligned, hift_orthogonalize_scratch_bytes(rows, cols) bytes.
+ * A call after a time-out (hift_tc_error_flag) writes no result. */
 #define HIFT_ORTHOGONALIZE_MAX_DIM 65536
 size_t      hift_orthogonalize_scratch_bytes(int64_t rows, int64_t cols);
 hift_status hift_k_orthogonalize(int32_t dtype, int64_t rows, int64_t cols, const void *g_dev, void *o_dev, int32_t steps,
@@ -589,8 +592,9 @@ hift_status hift_k_orthogonalize(int32_t dtype, int64_t rows, int64_t cols, cons
  *     momentum <- mu momentum + grad;   U = grad + mu momentum (nesterov != 0) or momentum;   X from U as above;
  *     master <- master (1 - lr weight_decay) - lr 0.2 sqrt(max(rows, cols)) X
  * (the factor gives the update the size of an AdamW update at the same lr); param_bf16_dev (may be NULL) receives the
- * bf16 image of the new master.  master, grad and momentum_dev are fp32 [rows, cols].  The products run in 16-bit
- * floating point with fp32 sums. */
+ * bf16 image of the new master.  master, grad and momentum_dev are fp32 [rows, cols].  The update is as exact as
+ * hift_k_orthogonalize's result before rounding.  After a time-out master and param keep their values, while momentum has
+ * been updated. */
 hift_status hift_muon_step(int64_t rows, int64_t cols, void *param_bf16_dev, float *master_dev, const float *grad_dev,
                            float *momentum_dev, void *scratch_dev, size_t scratch_bytes, double lr, double momentum,
                            int32_t nesterov, double weight_decay, int32_t steps, void *cuda_stream);
