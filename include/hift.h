@@ -525,9 +525,10 @@ hift_status hift_k_cross_entropy(int32_t dtype, int64_t rows, int64_t vocab, int
  *     rising order of the id; places without a token whose logit is above -inf hold id -1 and -inf.
  *     stats_dev fp32 [2*rows] (may be NULL): the row's largest logit x | log sum_i exp(z_i - z_max): what the gradient takes.
  * The logits are read once and left as they are; sums are fp32, a log p below the range of fp32 is -inf.  A logit of -inf is a
- * token that cannot occur.  tokens_dev[r] < 0: the row is ignored, whatever it holds (0, 0, stats 0 | 0, ids -1, -inf); tokens_dev[r] >= vocab: likewise, and *bad_dev
- * (int32, may be NULL) is set to 1 (and never cleared by the library).  A row with nothing above -inf: logp -inf,
- * entropy 0, stats -inf | 0, no alternatives.  A row that holds a NaN or +inf: NaN everywhere, ids -1.
+ * token that cannot occur.  tokens_dev[r] < 0: the row is ignored, whatever it holds (0, 0, stats 0 | 0, ids -1, -inf);
+ * tokens_dev[r] >= vocab: likewise, and *bad_dev (int32, may be NULL) is set to 1 (and never cleared by the library).  A row
+ * with nothing above -inf: logp -inf, entropy 0, stats -inf | 0, no alternatives.  A row that holds a NaN or +inf: NaN
+ * everywhere, ids -1.
  * dtype 0: fp32 logits, 1: bf16; the rows may start anywhere an element may (any ld >= vocab).  rows = 0 is allowed.
  * HIFT_ERR_CAPACITY if n_top > HIFT_MAX_TOP. */
 #define HIFT_MAX_TOP 32
@@ -577,8 +578,9 @@ hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
 
 /* Orthogonalisation of a matrix by Newton-Schulz products:
  *     X_0 = G / max(|G|_F, 1e-30),   X <- a X + (b A + c A A) X,  A = X X^T  (right-hand products when rows > cols),
- * `steps` times, (a, b, c) = (3.4445, -4.7750, 2.0315): every singular value s of X goes to a s + b s^3 + c s^5, which brings all but
- * the smallest to between 0.68 and 1.14 in five steps.  g_dev [rows, cols] fp32 (dtype 0) or bf16 (1), o_dev bf16 [rows, cols].
+ * `steps` times, (a, b, c) = (3.4445, -4.7750, 2.0315): every singular value s of X goes to a s + b s^3 + c s^5, which brings
+ * all of 0.01 and more to between 0.68 and 1.14 in five steps.  g_dev [rows, cols] fp32 (dtype 0) or bf16 (1), o_dev bf16
+ * [rows, cols].
  * The products run in 16-bit floating point with fp32 sums, around an iterate kept in fp32 (all in fp32 for a short side of at most 16):
  * before its rounding to bf16 the result is within 2^-8 of the definition, relative to its Frobenius norm.  A zero matrix
  * stays zero; NaN or infinity anywhere makes the whole result NaN.  1 <= rows, cols <= HIFT_ORTHOGONALIZE_MAX_DIM

