@@ -113,6 +113,8 @@ __global__ void __launch_bounds__(512) join_fwd_kernel(JoinFwd p) {
   const int64_t row = blockIdx.x;
   const int64_t off = row * p.cols;
   const float inv = 1.0f / (float)p.cols;
+  pdl_launch_next();
+  pdl_wait_prior();
   float v[NC][8], xv[NC][8];                           // both streams are under way before the first sum
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
@@ -297,6 +299,8 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
           st4(slot32(s, k, 0, h), zero); st4(slot32(s, k, 1, h), zero); st4(slotp(s, k, 2, h), zero); st4(slotp(s, k, 3, h), zero);
         }
   }
+  pdl_launch_next();
+  pdl_wait_prior();
   if (STAGED)
     for (int s = 0; s < p.stages; ++s) {
       fetch(r0 + s * R * step, s);
@@ -510,14 +514,14 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
     if (p.gain2) join_st(out + 2 * plane, k, p.cols, a2[k]);
     if (LN && p.gain2) join_st(out + 3 * plane, k, p.cols, b2[LN ? k : 0]);
   }
-  pdl_launch_next();
 }
 
 struct JoinSums { float* out[kJoinPlanes]; };     // nullptr: not wanted
 // Sums the planes of `partial` over the blocks, in a fixed order: blockIdx.y = plane; the gate's plane holds one sum per
 // gate, over the `split` blocks of that gate.  32 columns x 32 runs of blocks per CUDA block.
-__global__ void __launch_bounds__(1024) join_sums_kernel(const float* __restrict__ partial, JoinSums o, int ctas, int cols, int split) {
+__global__ void __launch_bounds__(1024) join_sums_kernel(const float* partial, JoinSums o, int ctas, int cols, int split) {
   __shared__ double sh[32][33];
+  pdl_launch_next();
   const int plane = min((int)blockIdx.y, kJoinPlanes - 1);
   const int gate = (int)blockIdx.y - (kJoinPlanes - 1);
   float* out = o.out[plane];

@@ -54,11 +54,12 @@ __device__ __forceinline__ void ns_st4(bf16* p, int left, const float (&v)[4]) {
 
 // momentum update (mom != nullptr) and the sum of squares of what will be orthogonalised, one double per block
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) ns_sumsq_kernel(const T* __restrict__ g, float* __restrict__ mom, int rows, int cols, float mu, int nesterov,
-                                                       double* __restrict__ part) {
+__global__ void __launch_bounds__(256) ns_sumsq_kernel(const T* g, float* mom, int rows, int cols, float mu, int nesterov,
+                                                       double* part) {
   __shared__ double sh[8];
   const int tid = threadIdx.y * blockDim.x + threadIdx.x;
   double s = 0.0;
+  pdl_wait_prior();
   for (int r = blockIdx.x * blockDim.y + threadIdx.y; r < rows; r += gridDim.x * blockDim.y) {
     const size_t off = (size_t)r * cols;
 #pragma unroll 2
@@ -86,9 +87,9 @@ __global__ void __launch_bounds__(256) ns_sumsq_kernel(const T* __restrict__ g, 
 }
 // X_0 = U / |U| into the zero-padded scratch, fp32 and as the first products' fp16 operand.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) ns_start_kernel(const T* __restrict__ g, const float* __restrict__ mom, int rows, int cols, float mu, int nesterov,
-                                                       const double* __restrict__ part, int nparts, int prows, int pcols, float* __restrict__ x32,
-                                                       __half* __restrict__ x16) {
+__global__ void __launch_bounds__(256) ns_start_kernel(const T* g, const float* mom, int rows, int cols, float mu, int nesterov,
+                                                       const double* part, int nparts, int prows, int pcols, float* x32,
+                                                       __half* x16) {
   __shared__ double sh[8];
   __shared__ float s_inv;
   const int tid = threadIdx.y * blockDim.x + threadIdx.x;
@@ -130,9 +131,9 @@ __global__ void __launch_bounds__(256) ns_start_kernel(const T* __restrict__ g, 
 }
 // The result out of the padded scratch: o in bf16, or the update of the master.  Writes nothing after a product gave up on a wait.
 template <bool VEC>
-__global__ void __launch_bounds__(256) ns_finish_kernel(const float* __restrict__ x, int rows, int cols, int pcols, bf16* __restrict__ o,
-                                                        float* __restrict__ master, bf16* __restrict__ param, float decay, float size,
-                                                        const int* __restrict__ tc_error) {
+__global__ void __launch_bounds__(256) ns_finish_kernel(const float* x, int rows, int cols, int pcols, bf16* o,
+                                                        float* master, bf16* param, float decay, float size,
+                                                        const int* tc_error) {
   pdl_wait_prior();
   if (tc_error != nullptr && *tc_error != 0) return;
   for (int r = blockIdx.x * blockDim.y + threadIdx.y; r < rows; r += gridDim.x * blockDim.y) {
@@ -189,9 +190,7 @@ inline cudaError_t launch_orthogonalize(cudaStream_t st, int64_t rows, int64_t c
   auto at = [](const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; };
   const bool vec = cols % 4 == 0 && at(g, 4 * sizeof(T)) && at(mom, 16) && at(to.o, 8) && at(to.master, 16) && at(to.param, 8);
   const int R = (int)rows, C = (int)cols;
-  if (vec) ns_sumsq_kernel<T, true><<<grid, block, 0, st>>>(g, mom, R, C, mu, nesterov, part);
-  else ns_sumsq_kernel<T, false><<<grid, block, 0, st>>>(g, mom, R, C, mu, nesterov, part);
-  cudaError_t e = cudaGetLastError();
+  cudaError_t e = launch_pdl(vec ? ns_sumsq_kernel<T, true> : ns_sumsq_kernel<T, false>, grid, block, 0, st, g, mom, R, C, mu, nesterov, part);
   if (e != cudaSuccess) return e;
   e = vec ? launch_pdl(ns_start_kernel<T, true>, pgrid, block, 0, st, g, (const float*)mom, R, C, mu, nesterov, (const double*)part, (int)grid.x, pr, pc, b.x32, (__half*)b.x16[0])
           : launch_pdl(ns_start_kernel<T, false>, pgrid, block, 0, st, g, (const float*)mom, R, C, mu, nesterov, (const double*)part, (int)grid.x, pr, pc, b.x32, (__half*)b.x16[0]);

@@ -83,6 +83,8 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *(volatile uint32_t*)gen(slot_s);
+  pdl_trigger();
+  pdl_wait();                                          // nothing global before this
   const uint32_t lanes = (uint32_t)(q * 32) << 16, xtm = tmem, acc1 = tmem + 128 * NH;
   // the step's accumulator of column block h; the second block's takes the place of the polynomial's, which is done by then
   auto acc2 = [&](int h) { return h == 0 ? acc1 + 128 : acc1; };

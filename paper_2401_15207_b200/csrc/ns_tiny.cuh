@@ -23,6 +23,8 @@ __global__ void __launch_bounds__(kTinyThreads, 1) ns_tiny_kernel(NsSmallArgs a)
   uint32_t C;
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
   const uint32_t me = cluster_ctarank();
+  pdl_trigger();
+  pdl_wait();
   const bool wide = a.rows <= a.cols;
   const int S0 = wide ? a.rows : a.cols, L0 = wide ? a.cols : a.rows;
   auto column = [&](int p) { return ((int)me * CP + p) * kTinyThreads + tid; };

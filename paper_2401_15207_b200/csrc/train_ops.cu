@@ -71,11 +71,8 @@ JoinPlan join_plan(int64_t rows, int64_t cols, int64_t rows_per_gate) {
 
 template <typename P, int KIND>
 cudaError_t launch_join_fwd(cudaStream_t st, int th, int nc, const JoinFwd& p) {
-  const unsigned grid = (unsigned)p.rows;
-  if (nc == 1) join_fwd_kernel<P, KIND, 1><<<grid, th, 0, st>>>(p);
-  else if (nc == 2) join_fwd_kernel<P, KIND, 2><<<grid, th, 0, st>>>(p);
-  else join_fwd_kernel<P, KIND, 4><<<grid, th, 0, st>>>(p);
-  return cudaGetLastError();
+  auto kernel = nc == 1 ? join_fwd_kernel<P, KIND, 1> : nc == 2 ? join_fwd_kernel<P, KIND, 2> : join_fwd_kernel<P, KIND, 4>;
+  return launch_pdl(kernel, dim3((unsigned)p.rows), dim3(th), 0, st, p);
 }
 template <typename P, int KIND, int NC, bool STAGED, bool ONE>
 cudaError_t launch_join_bwd_nc(cudaStream_t st, int th, const JoinBwd& p) {
@@ -84,8 +81,7 @@ cudaError_t launch_join_bwd_nc(cudaStream_t st, int th, const JoinBwd& p) {
     const cudaError_t e = cudaFuncSetAttribute(join_bwd_kernel<P, KIND, NC, STAGED, ONE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
   }
-  join_bwd_kernel<P, KIND, NC, STAGED, ONE><<<(unsigned)p.ctas, th, smem, st>>>(p);
-  return cudaGetLastError();
+  return launch_pdl(join_bwd_kernel<P, KIND, NC, STAGED, ONE>, dim3((unsigned)p.ctas), dim3(th), smem, st, p);
 }
 // Iterations (of one or two rows) staged ahead: two, or what fits.  None fits: fp32 operands beyond 8192 columns, the direct variant.
 template <typename P, int KIND, bool ONE>

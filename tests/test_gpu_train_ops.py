@@ -723,6 +723,68 @@ def test_operators_captured_in_a_graph_give_the_bits_of_the_calls():
         assert all(torch.equal(eager[n], b[n]) for n in names)
 
 
+@pytest.mark.parametrize("rows,cols,vocab", [(8, 64, 129), (300, 1024, 4099)])
+def test_calls_behind_one_another_wait_for_what_they_read(rows, cols, vocab):
+    """A kernel may be resident before its predecessor has ended.  Each call here reads what the one before it wrote, over buffers
+    and scratch that the next round writes again; the bits are those of a run that waits for the device after every call."""
+    from paper_2401_15207_b200 import (join_bwd_scratch_bytes, k_join_bwd, k_join_fwd, k_orthogonalize, k_token_logprobs, k_token_logprobs_bwd, muon_step,
+                                       orthogonalize_scratch_bytes)
+    torch = _torch()
+    f, h = torch.float32, torch.bfloat16
+    v = _join_inputs(rows, cols, 1, 0, rows, True, True, seed=rows)
+    logits0, _ = _logits(rows, vocab, vocab, 1, 0, seed=3)
+    tok = _dev((np.arange(rows) * 11 % vocab).astype(np.int32))
+    shapes = [(12, 700), (90, 260), (rows, cols)]      # the last of 300 x 1024 goes through tiled products, the others are single launches
+    mats = [_dev(_matrix("gauss", r, c, 4)) for r, c in shapes]
+    need = max(orthogonalize_scratch_bytes(r, c) for r, c in shapes)
+
+    def buffers():
+        e = lambda *s, d=f: torch.zeros(*s, dtype=d, device="cuda")  # noqa: E731
+        return dict(xo=e(rows, cols), x2=v["x"][0].clone(), y=e(rows, cols, d=h), st=e(4 * rows), dx=v["dxo"][0].clone(), dx2=e(rows, cols), dh=e(rows, cols, d=h),
+                    dg1=e(cols), db1=e(cols), dq=e(1, cols), dg2=e(cols), db2=e(cols), w1=e(join_bwd_scratch_bytes(rows, cols, rows), d=torch.uint8),
+                    t=logits0.clone(), lp=e(rows), en=e(rows), ls=e(2 * rows), ids=e(rows, 3, d=torch.int32), tv=e(rows, 3), w2=e(need, d=torch.uint8),
+                    **{f"{n}{i}": e(r, c, d=h if n == "o" else f) for i, (r, c) in enumerate(shapes) for n in ("o", "master", "mom")})
+
+    def run(b, done):
+        for k in range(4):
+            xin, xout = (b["x2"], b["xo"]) if k % 2 == 0 else (b["xo"], b["x2"])
+            k_join_fwd(1, 0, rows, cols, 1e-5, 1.0, xin, v["h"][0], v["gain1"][0], v["bias1"][0], v["gate"][0], rows, v["gain2"][0], v["bias2"][0],
+                       xout, b["y"], b["st"])
+            done()
+            din, dout = (b["dx"], b["dx2"]) if k % 2 == 0 else (b["dx2"], b["dx"])
+            k_join_bwd(1, 0, rows, cols, 1.0, b["y"], din, xout, v["h"][0], b["st"], v["gain1"][0], v["bias1"][0], v["gate"][0], rows,
+                       v["gain2"][0], dout, b["dh"], b["dg1"], b["db1"], b["dq"], b["dg2"], b["db2"], b["w1"])
+            done()
+            k_token_logprobs(1, rows, vocab, vocab, b["t"], tok, 1.0, 3, b["lp"], b["en"], b["ls"], b["ids"], b["tv"])
+            done()
+            k_token_logprobs_bwd(1, rows, vocab, vocab, b["t"], tok, 1.0, b["ls"], b["en"], b["lp"], b["en"], b["t"])      # in place: the next round's logits
+            done()
+            for i, (r, c) in enumerate(shapes):
+                muon_step(r, c, None, b[f"master{i}"], mats[i] if i < 2 else b["dx2"], b[f"mom{i}"], b["w2"], 1e-2)
+                done()
+                k_orthogonalize(0, r, c, b[f"master{i}"], b[f"o{i}"], 5, b["w2"])
+                done()
+    want, got = buffers(), buffers()
+    torch.cuda.synchronize()
+    run(want, torch.cuda.synchronize)
+    run(got, lambda: None)
+    names = [n for n in got if not n.startswith("w")]
+    torch.cuda.synchronize()
+    assert [n for n in names if not torch.equal(want[n], got[n])] == []
+    assert all(bool(torch.isfinite(want[n].float()).all()) for n in names if n not in ("ids", "tv"))
+    again = buffers()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(again, lambda: None)
+    fresh = buffers()
+    for _ in range(3):                               # the copies are other people's kernels between two replays
+        for n in again:
+            again[n].copy_(fresh[n])
+        graph.replay()
+    torch.cuda.synchronize()
+    assert [n for n in names if not torch.equal(want[n], again[n])] == []
+
+
 @pytest.mark.parametrize("code", [0, 1])
 def test_a_fine_tuning_step_out_of_the_operators(code):
     """Junction -> head product -> log-probabilities with entropy -> their gradient -> head products' gradients -> junction backward
