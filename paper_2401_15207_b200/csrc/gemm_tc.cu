@@ -26,6 +26,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <atomic>
 #include <mutex>
 #include <unordered_map>
 
@@ -1315,18 +1316,6 @@ int gemm_tc_init() {
   if (e == cudaSuccess) e = set_smem_attr2<false, true, true>();
   if (e == cudaSuccess) e = set_smem_attr2<true, true, true>();
   if (e == cudaSuccess) e = set_smem_attr2<true, true, false>();
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<float, 1>, ns_small_smem<1>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<float, 2>, ns_small_smem<2>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<__nv_bfloat16, 1>, ns_small_smem<1>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<__nv_bfloat16, 2>, ns_small_smem<2>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<float, 1>, ns_tiny_smem<1>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<float, 2>, ns_tiny_smem<2>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<__nv_bfloat16, 1>, ns_tiny_smem<1>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<__nv_bfloat16, 2>, ns_tiny_smem<2>);
-  if (e == cudaSuccess) e = set_smem_attr_ns<false, false, 1>();
-  if (e == cudaSuccess) e = set_smem_attr_ns<true, true, 1>();
-  if (e == cudaSuccess) e = set_smem_attr_ns<false, false, 2>();
-  if (e == cudaSuccess) e = set_smem_attr_ns<false, true, 2>();
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fwd_tc_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnTcCfg<64>::kSmem);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fwd_tc_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnTcCfg<128>::kSmem);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fwd_tc_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, AttnTcCfg<64>::kSmem);
@@ -1429,13 +1418,42 @@ cudaError_t gemm_tc_launch(cudaStream_t st, const GemmArgs& g) {
   return g.out_f32 ? launch_inst<true, true, true>(st, g, ta, tb, bn) : launch_inst<true, true, false>(st, g, ta, tb, bn);
 }
 
+// The Newton-Schulz kernels' attributes and the address of the time-out flag belong to a device: set up per device, for these
+// operators take whichever device is current.  Returns the flag's address, nullptr where the kernels cannot run.
+constexpr int kNsMaxDevices = 64;
+const int* ns_device_flag() {
+  static std::atomic<const int*> flag[kNsMaxDevices];      // zero-initialised
+  int dev = 0, major = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev >= kNsMaxDevices) return nullptr;
+  if (const int* p = flag[dev].load(std::memory_order_acquire)) return p;
+  if (gemm_tc_init() != 0) return nullptr;
+  void* p = nullptr;
+  cudaError_t e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
+  if (e == cudaSuccess && major != 10) return nullptr;
+  if (e == cudaSuccess) e = cudaGetSymbolAddress(&p, g_tc_error);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<float, 1>, ns_small_smem<1>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<float, 2>, ns_small_smem<2>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<__nv_bfloat16, 1>, ns_small_smem<1>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<__nv_bfloat16, 2>, ns_small_smem<2>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<float, 1>, ns_tiny_smem<1>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<float, 2>, ns_tiny_smem<2>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<__nv_bfloat16, 1>, ns_tiny_smem<1>);
+  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<__nv_bfloat16, 2>, ns_tiny_smem<2>);
+  if (e == cudaSuccess) e = set_smem_attr_ns<false, false, 1>();
+  if (e == cudaSuccess) e = set_smem_attr_ns<true, true, 1>();
+  if (e == cudaSuccess) e = set_smem_attr_ns<false, false, 2>();
+  if (e == cudaSuccess) e = set_smem_attr_ns<false, true, 2>();
+  if (e != cudaSuccess) { cudaGetLastError(); return nullptr; }
+  flag[dev].store((const int*)p, std::memory_order_release);
+  return (const int*)p;
+}
+
 bool ns_small_eligible(int64_t rows, int64_t cols) {
   const int64_t s = rows < cols ? rows : cols, l = rows < cols ? cols : rows;
   return s <= kTinyRows ? l <= 16 * kTinyThreads * 2 : s <= 128 && l <= 16 * 256;
 }
 cudaError_t ns_small_launch(cudaStream_t st, bool g_bf16, int64_t rows, int64_t cols, const void* g, float* mom, float mu, int nesterov, int steps,
                             void* o, float* master, void* param, float decay, float size) {
-  if (gemm_tc_init() != 0) return cudaErrorNotSupported;
   const int S = (int)(rows < cols ? rows : cols), L = (int)(rows < cols ? cols : rows);
   const NsSmallArgs a{g, mom, (__nv_bfloat16*)o, master, (__nv_bfloat16*)param, (int)rows, (int)cols, steps, nesterov, mu, decay, size};
   const bool tiny = S <= kTinyRows;
@@ -1451,7 +1469,6 @@ cudaError_t ns_small_launch(cudaStream_t st, bool g_bf16, int64_t rows, int64_t 
 }
 
 cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps) {
-  if (gemm_tc_init() != 0) return cudaErrorNotSupported;
   const bool wide = b.rows <= b.cols;                  // the Gram matrix is taken on the short side
   const int S = wide ? b.rows : b.cols, L = wide ? b.cols : b.rows;
   const NsTile t_gram = ns_tile(S, S, L, true, !wide), t_poly = ns_tile(S, S, S, true, false), t_step = ns_tile(b.rows, b.cols, S, false, false);

@@ -49,5 +49,7 @@ int gemm_tc_poll_error();
 int gemm_tc_set_error(int v);
 // Device address of that flag (an int), or nullptr if it cannot be resolved.
 const int* gemm_tc_error_device_ptr();
+// The same of the device that is current, whose Newton-Schulz kernels it sets up at the first call; nullptr: not available there.
+const int* ns_device_flag();
 
 }  // namespace hift

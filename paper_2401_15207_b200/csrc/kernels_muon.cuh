@@ -166,6 +166,8 @@ struct NsUpdate { bf16* o; float* master; bf16* param; float decay, size; };   /
 template <typename T>
 inline cudaError_t launch_orthogonalize(cudaStream_t st, int64_t rows, int64_t cols, const T* g, float* mom, float mu, int nesterov,
                                         int steps, const NsUpdate& to, void* scratch) {
+  const int* flag = ns_device_flag();                  // sets this device up
+  if (!flag) return cudaErrorNotSupported;
   if (ns_small_eligible(rows, cols))
     return ns_small_launch(st, sizeof(T) == 2, rows, cols, g, mom, mu, nesterov, steps, to.o, to.master, to.param, to.decay, to.size);
   const int pr = ns_pad(rows), pc = ns_pad(cols), s = pr < pc ? pr : pc;
@@ -197,8 +199,8 @@ inline cudaError_t launch_orthogonalize(cudaStream_t st, int64_t rows, int64_t c
   if (e != cudaSuccess) return e;
   e = ns_products_launch(st, b, steps);
   if (e != cudaSuccess) return e;
-  return vec ? launch_pdl(ns_finish_kernel<true>, grid, block, 0, st, (const float*)b.x32, R, C, pc, to.o, to.master, to.param, to.decay, to.size, gemm_tc_error_device_ptr())
-             : launch_pdl(ns_finish_kernel<false>, grid, block, 0, st, (const float*)b.x32, R, C, pc, to.o, to.master, to.param, to.decay, to.size, gemm_tc_error_device_ptr());
+  return vec ? launch_pdl(ns_finish_kernel<true>, grid, block, 0, st, (const float*)b.x32, R, C, pc, to.o, to.master, to.param, to.decay, to.size, flag)
+             : launch_pdl(ns_finish_kernel<false>, grid, block, 0, st, (const float*)b.x32, R, C, pc, to.o, to.master, to.param, to.decay, to.size, flag);
 }
 
 }  // namespace hift
