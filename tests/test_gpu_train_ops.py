@@ -667,6 +667,88 @@ def test_orthogonalize_writes_nothing_after_a_time_out(rows, cols):
     assert rel_l2(o.double().cpu().numpy(), R.orthogonalize(g.double().cpu().numpy())) < NS_TOL
 
 
+# ------------------------------------------------------------------ offsets beyond 32 bits
+def _same_bits(a, b):
+    torch = _torch()
+    i = {2: torch.int16, 4: torch.int32}[a.element_size()]
+    return torch.equal(a.contiguous().view(i), b.contiguous().view(i))
+
+
+def test_logprobs_of_rows_beyond_32_bit_offsets():
+    """Rows 2^30 + 8 elements apart: the last starts beyond 2^31.  Same bits as the rows side by side; padding gets zeros."""
+    from paper_2401_15207_b200 import k_token_logprobs, k_token_logprobs_bwd
+    torch = _torch()
+    rows, vocab, ld = 3, 1003, 2 ** 30 + 8
+    near, _ = _logits(rows, vocab, 1008, 1, 0, seed=6)
+    far = torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda").view(rows, ld)
+    far[:, :vocab] = near[:, :vocab]
+    far[:, vocab:vocab + 40] = NAN
+    far[:, -40:] = NAN
+    tok, w = _dev(np.array([1002, 0, 500], np.int32)), _dev(np.array([1.0, -2.0, 0.5], np.float32))
+    outs = []
+    for t, d in ((near, 1008), (far, ld)):
+        o = [torch.zeros(n, device="cuda") for n in (rows, rows, 2 * rows)] + [torch.zeros(rows, 5, dtype=torch.int32, device="cuda"), torch.zeros(rows, 5, device="cuda")]
+        k_token_logprobs(1, rows, vocab, d, t, tok, 1.0, 5, *o)
+        k_token_logprobs_bwd(1, rows, vocab, d, t, tok, 1.0, o[2], o[1], w, w, t)
+        outs.append(o)
+    assert all(_same_bits(a, b) for a, b in zip(*outs))
+    assert _same_bits(near[:, :vocab], far[:, :vocab])
+    assert all(not bool(far[r, vocab:].any()) for r in range(rows))
+
+
+def test_join_of_a_tensor_beyond_32_bit_offsets():
+    """2.1e9 elements: the rows around and behind the 2^31st give the bits of the same rows alone."""
+    from paper_2401_15207_b200 import join_bwd_scratch_bytes, k_join_bwd, k_join_fwd
+    torch = _torch()
+    cols, rows, n = 16384, 2 ** 17 + 40, 64
+    v = _join_inputs(n, cols, 1, 0, n, True, True, seed=12)
+    f, h = torch.float32, torch.bfloat16
+
+    def run(x, hh, dy, dxo, r):
+        y, st, dh = torch.zeros(r, cols, dtype=h, device="cuda"), torch.zeros(4 * r, device="cuda"), torch.zeros(r, cols, dtype=h, device="cuda")
+        g = [torch.zeros(cols, device="cuda") for _ in range(4)]
+        dq = torch.zeros(1, cols, device="cuda")
+        k_join_fwd(1, 0, r, cols, 1e-5, 1.0, x, hh, v["gain1"][0], v["bias1"][0], v["gate"][0], r, v["gain2"][0], v["bias2"][0], x, y, st)
+        w = torch.empty(join_bwd_scratch_bytes(r, cols, r), dtype=torch.uint8, device="cuda")
+        k_join_bwd(1, 0, r, cols, 1.0, dy, dxo, x, hh, st, v["gain1"][0], v["bias1"][0], v["gate"][0], r, v["gain2"][0], dxo, dh, g[0], g[1], dq, g[2], g[3], w)
+        return dict(x=x, y=y, dx=dxo, dh=dh), g + [dq]
+    few, sums = run(v["x"][0].clone(), v["h"][0], v["dy"][0], v["dxo"][0].clone(), n)
+    big = [torch.zeros(rows, cols, dtype=d, device="cuda") for d in (f, h, h, f)]
+    for t, name in zip(big, ("x", "h", "dy", "dxo")):
+        t[-n:] = v[name][0]                          # the rows before them are zeros, with gradients of zero: they add nothing to the sums
+    many, msums = run(*big, rows)
+    for name in few:
+        assert _same_bits(many[name][-n:], few[name]), name
+    assert not bool(many["dx"][:-n].any()) and not bool(many["dh"][:-n].any())
+    for a, b in zip(msums, sums):                    # fp32 sums of at most 64 terms, in two orders
+        assert float((a - b).norm()) <= 64 * 2 * R.U32 * float(b.abs().sum())
+    del big, many
+    torch.cuda.empty_cache()
+
+
+def test_orthogonalize_of_a_matrix_beyond_32_bit_offsets():
+    """65536 x 33000 with values in few rows and columns, the last ones among them: their submatrix is orthogonalised, the rest stays zero."""
+    from paper_2401_15207_b200 import k_orthogonalize, orthogonalize_scratch_bytes
+    torch = _torch()
+    rows, cols = 65536, 33000
+    r = [0, 1, 17, 40000, 65000, 65534, 65535]
+    c = torch.cat([torch.arange(0, 33000, 331, device="cuda"), torch.tensor([32998, 32999], device="cuda")])
+    sub = _dev(_matrix("gauss", len(r), len(c), 7))
+    g = torch.zeros(rows, cols, device="cuda")
+    for i, k in enumerate(r):
+        g[k][c] = sub[i]
+    w = torch.empty(orthogonalize_scratch_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    o = torch.empty(rows, cols, dtype=torch.bfloat16, device="cuda")
+    k_orthogonalize(0, rows, cols, g, o, 5, w)
+    got = torch.stack([o[k][c] for k in r])
+    assert rel_l2(got.double().cpu().numpy(), R.orthogonalize(sub.double().cpu().numpy())) < NS_TOL
+    for k in r:
+        o[k][c] = 0
+    assert int(torch.count_nonzero(o)) == 0
+    del g, w, o
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------------------ streams, graphs, and the whole run
 def test_operators_captured_in_a_graph_give_the_bits_of_the_calls():
     from paper_2401_15207_b200 import (join_bwd_scratch_bytes, k_join_bwd, k_join_fwd, k_token_logprobs, k_token_logprobs_bwd,
