@@ -11,7 +11,8 @@
 // moved once per batch, and its sums of e and e (x - m) relative to it; the block (and, for few rows, the up to eight
 // blocks of a cluster that share a row) joins them at the end.  The alternatives cost no second pass: the k-th largest of
 // the threads' own maxima is a lower bound of the k-th largest logit, so only the few threads whose maximum reaches it can
-// hold one, and their warps read those threads' elements again out of L2, all at once.  The same re-reading makes r exact when it is
+// hold one, and their warps read again out of L2 the batch of four vectors that held such a thread's maximum, or all its elements
+// if another batch reaches the bound too.  The same re-reading makes r exact when it is
 // small: only the thread that holds the maximum added it to anything.
 #pragma once
 #include "common.cuh"
@@ -192,8 +193,12 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const T* log
 
   // ---- one pass: maximum, sum of e, sum of e log2 e (bounded, unlike e (x - m)), all relative to the thread's running maximum
   float tmax = -INFINITY, m = kLowest;
+  float tmax2 = -INFINITY;                // largest logit outside the batch that holds the thread's maximum (the first such batch)
+  int at_max = -1;                        // that batch's first vector; -1: the single element
   uint64_t s = 0ull, u = 0ull;            // pairs of partial sums
-  auto move_max = [&](float top) {
+  auto move_max = [&](float top, int batch) {
+    tmax2 = fmaxf(tmax2, fminf(tmax, top));
+    if (top > tmax) at_max = batch;
     tmax = fmaxf(tmax, top);
     const float mn = fmaxf(m, top), d = (m - mn) * s2, f = lp_ex2(d), dc = f > 0.f ? d : 0.f;     // d is 0 where the maximum stays
     const uint64_t ff = f2_pack(f, f);
@@ -212,7 +217,7 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const T* log
   const uint64_t sc = f2_pack(s2, s2);
   if (tid < ns) {
     const float v = to_f(x[lp_single<T>(rw, tid)]);
-    move_max(v);
+    move_max(v, -1);
     add_pair(v, -INFINITY, f2_pack(-m, -m), sc);
   }
   for (int c = v0 + tid; c < v1; c += kLpBatch * nt) {
@@ -222,7 +227,7 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const T* log
     float top = LpVec<T>::max(w[0]);
 #pragma unroll
     for (int k = 1; k < kLpBatch; ++k) top = fmaxf(top, LpVec<T>::max(w[k]));
-    move_max(top);
+    move_max(top, c);
     const uint64_t nm = f2_pack(-m, -m);
 #pragma unroll
     for (int k = 0; k < kLpBatch; ++k) {
@@ -313,32 +318,46 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const T* log
   // ---- alternatives: the threads whose maximum reaches the bound
   const bool poison = !(S < INFINITY);                                  // a NaN or +inf among the logits
   if (want_top && !poison && has) {
-    const uint32_t bound = sh.bound;
-    const bool can = sh.tmax[tid] >= bound && sh.tmax[tid] > kLpNone;
-    const unsigned who = __ballot_sync(0xffffffffu, can);
+    const uint32_t least = max(sh.bound, kLpNone + 1u);
+    const bool can = sh.tmax[tid] >= least, wide = can && lp_order(tmax2) >= least;
     uint8_t* few = sh.few + warp * 32;
-    if (can) few[__popc(who & ((1u << lane) - 1u))] = (uint8_t)lane;
-    __syncwarp();
-    // all their elements at once: a lane takes one vector of one of them at a time
-    const int each = (v1 - v0 + nt - 1) / nt + (ns > 0 ? 1 : 0), items = __popc(who) * each;
+    auto list = [&](bool in) {                                          // the warp's lanes that answer yes, and how many
+      const unsigned who = __ballot_sync(0xffffffffu, in);
+      __syncwarp();
+      if (in) few[__popc(who & ((1u << lane) - 1u))] = (uint8_t)lane;
+      __syncwarp();
+      return __popc(who);
+    };
     auto see = [&](float v, int at) {
       const uint32_t o = lp_order(v);
-      if (o >= bound && o > kLpNone) {
+      if (o >= least) {
         const int slot = atomicAdd(&sh.count, 1);
         if (slot < kLpCand) sh.cand[slot] = ((unsigned long long)o << 32) | (uint32_t)~at;
       }
     };
-    for (int k = lane; k < items && *(volatile int*)&sh.count <= kLpCand; k += 32) {
-      const int i = warp * 32 + few[k / each], j = k % each;
-      const int c = v0 + i + j * nt;
-      if (ns > 0 && j == each - 1) {                                    // the thread's single element
-        if (i < ns) { const int at = lp_single<T>(rw, i); see(to_f(x[at]), at); }
-      } else if (c < v1) {
-        float p[V / 2], q[V / 2];
-        LpVec<T>::pairs(xv[c], p, q);
+    auto see_vector = [&](int c) {
+      float p[V / 2], q[V / 2];
+      LpVec<T>::pairs(xv[c], p, q);
 #pragma unroll
-        for (int e = 0; e < V / 2; ++e) { see(p[e], rw.head + c * V + 2 * e); see(q[e], rw.head + c * V + 2 * e + 1); }
-      }
+      for (int e = 0; e < V / 2; ++e) { see(p[e], rw.head + c * V + 2 * e); see(q[e], rw.head + c * V + 2 * e + 1); }
+    };
+    auto see_single = [&](int i) {
+      if (i < ns) { const int at = lp_single<T>(rw, i); see(to_f(x[at]), at); }
+    };
+    // most of them reach it in one batch only: a lane takes one vector of a thread's batch
+    const int one = list(can && !wide) * kLpBatch;
+    for (int k0 = 0; k0 < one; k0 += 32) {
+      const int k = min(k0 + lane, one - 1), i = few[k / kLpBatch], b = __shfl_sync(0xffffffffu, at_max, i), c = b + (k % kLpBatch) * nt;
+      if (k0 + lane >= one) continue;
+      if (b < 0) { if (k % kLpBatch == 0) see_single(warp * 32 + i); }
+      else if (c < v1) see_vector(c);
+    }
+    // of the others all elements: a lane takes one vector of one of them at a time
+    const int each = (v1 - v0 + nt - 1) / nt + (ns > 0 ? 1 : 0), items = list(wide) * each;
+    for (int k = lane; k < items && *(volatile int*)&sh.count <= kLpCand; k += 32) {
+      const int i = warp * 32 + few[k / each], j = k % each, c = v0 + i + j * nt;
+      if (ns > 0 && j == each - 1) see_single(i);                       // the thread's single element
+      else if (c < v1) see_vector(c);
     }
     __syncthreads();
     if (sh.count <= kLpCand) {

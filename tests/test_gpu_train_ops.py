@@ -166,6 +166,28 @@ def test_logprobs_masks_ties_and_bad_rows(code, vocab):
     assert int(flag) == 0
 
 
+@pytest.mark.parametrize("code", [0, 1])
+@pytest.mark.parametrize("stride", [1, 2, 31, 128, 256, 512, 1024, 2048, 4096])
+def test_logprobs_alternatives_that_one_thread_holds(code, stride):
+    """The largest logits a fixed distance apart: side by side, or in different loads of one and the same thread."""
+    from paper_2401_15207_b200 import k_token_logprobs
+    torch = _torch()
+    rows, vocab, n = 600, 90000, 20                  # enough rows for one block each
+    t, _ = _logits(rows, vocab, vocab, code, 0, seed=stride)
+    t.clamp_(max=3.0)
+    first = np.arange(rows) * 5 % 7001
+    ids = first[:, None] + stride * np.arange(n)[None]
+    order = np.argsort(np.random.default_rng(stride).random((rows, n)), axis=1)
+    t.scatter_(1, _dev(ids.astype(np.int64)), _dev((8.0 + 0.5 * order).astype(np.float32)).to(t.dtype))
+    e = lambda *s, d=torch.float32: torch.empty(*s, dtype=d, device="cuda")  # noqa: E731
+    lp, en, st, got, val = e(rows), e(rows), e(2 * rows), e(rows, n + 3, d=torch.int32), e(rows, n + 3)
+    k_token_logprobs(code, rows, vocab, vocab, t, _dev(ids[:, 0].astype(np.int32)), 1.0, n + 3, lp, en, st, got, val)
+    want = np.take_along_axis(ids, np.argsort(-order, axis=1), axis=1)
+    assert np.array_equal(got.cpu().numpy()[:, :n], want)
+    rest = torch.topk(t.float().scatter(1, _dev(ids.astype(np.int64)), -INF), 3, dim=1).values
+    assert torch.equal(torch.gather(t.float(), 1, got[:, n:].long()), rest)
+
+
 def test_logprobs_read_no_padding_and_keep_the_logits():
     torch = _torch()
     t, _ = _logits(6, 1000, 1032, 1, 0, seed=5)
