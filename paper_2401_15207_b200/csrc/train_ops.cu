@@ -196,7 +196,9 @@ hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
   if (e == cudaSuccess && (dgain1 || dbias1 || dgain2 || dbias2 || (dgate && pl.split > 0))) {
     const JoinSums o{{dgain1, dbias1, dgain2, dbias2, pl.split > 0 ? dgate : nullptr}};
     const dim3 g((unsigned)((cols + 31) / 32), (unsigned)(kJoinPlanes - 1 + (dgate && pl.split > 0 ? pl.n_gates : 0)));
-    e = launch_pdl(join_sums_kernel, g, dim3(32, 32), 0, st, (const float*)scratch, o, pl.ctas, (int)cols, pl.split);
+    int th = 256;
+    while (th < 1024 && pl.ctas > th / 8 * 4) th *= 2;
+    e = launch_pdl(join_sums_kernel, g, dim3(th), 0, st, (const float*)scratch, o, pl.ctas, (int)cols, pl.split);
   }
   return status_of(e);
 }
