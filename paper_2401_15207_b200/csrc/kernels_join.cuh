@@ -214,6 +214,26 @@ template <int NC, bool ONE> constexpr int join_rows = NC == 1 && ONE ? 2 : 1;
 // bytes a thread stages per chunk of 8 columns: x', dx' in fp32, dy, h in the operand type
 template <typename P> constexpr int join_bytes = 2 * 32 + 2 * 8 * (int)sizeof(P);
 
+// Two columns.  Packed: one instruction for both, in the LayerNorm variants, which are short of issue slots (main kernel at 16384 x 2048:
+// 155 -> 122 us, at 16384 x 4096 310 -> 293); the RMSNorm ones, nearer to the memory's rate, run faster on single registers (204 against 218 us).
+template <bool PACKED> struct JoinPair;
+template <> struct JoinPair<true> {
+  using T = uint64_t;
+  __device__ static T make(float a, float b) { return f2_pack(a, b); }
+  __device__ static void split(T v, float& a, float& b) { f2_unpack(v, a, b); }
+  __device__ static T add(T a, T b) { return f2_add(a, b); }
+  __device__ static T mul(T a, T b) { return f2_mul(a, b); }
+  __device__ static T fma(T a, T b, T c) { return f2_fma(a, b, c); }
+};
+template <> struct JoinPair<false> {
+  using T = float2;
+  __device__ static T make(float a, float b) { return make_float2(a, b); }
+  __device__ static void split(T v, float& a, float& b) { a = v.x; b = v.y; }
+  __device__ static T add(T a, T b) { return make_float2(a.x + b.x, a.y + b.y); }
+  __device__ static T mul(T a, T b) { return make_float2(a.x * b.x, a.y * b.y); }
+  __device__ static T fma(T a, T b, T c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
+};
+
 // A block walks its rows; the column sums of its rows stay in registers (each thread owns its columns) and leave as one
 // row of `partial` per plane: gain1, bias1, gain2, bias2, gate (the last only where a gate's rows are split).  Within one gate
 // q everything after the block follows from two sums per column, S1 = sum d hat1 and S0 = sum d (S0 for LayerNorm only):
@@ -229,6 +249,8 @@ template <typename P> constexpr int join_bytes = 2 * 32 + 2 * 8 * (int)sizeof(P)
 //   - two rows at a time (R = 2, for NC = 1 and one gate), so that their sums share barriers and their work interleaves.
 template <typename P, int KIND, int NC, bool STAGED, bool ONE>
 __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
+  using Q = JoinPair<KIND == 0>;
+  using V = typename Q::T;
   constexpr int BYTES = join_bytes<P>;
   constexpr bool LN = KIND == 0, HOLD = NC == 1;
   constexpr int R = join_rows<NC, ONE>;
@@ -307,17 +329,17 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
       cp_async_commit();
     }
   constexpr int NB = LN ? NC : 1, NM = ONE ? 1 : NC, NMB = ONE || !LN ? 1 : NC;   // sums that this variant does not take shrink to one
-  float S1[NC][8], S0[NB][8], a2[NC][8], b2[NB][8], a1[NM][8], b1[NMB][8];
+  V S1[NC][4], S0[NB][4], a2[NC][4], b2[NB][4], a1[NM][4], b1[NMB][4];     // pairs of columns
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < 4; ++i) {
 #pragma unroll
-    for (int k = 0; k < NC; ++k) S1[k][i] = a2[k][i] = 0.f;
+    for (int k = 0; k < NC; ++k) S1[k][i] = a2[k][i] = Q::make(0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < NB; ++k) S0[k][i] = b2[k][i] = 0.f;
+    for (int k = 0; k < NB; ++k) S0[k][i] = b2[k][i] = Q::make(0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < NM; ++k) a1[k][i] = 0.f;
+    for (int k = 0; k < NM; ++k) a1[k][i] = Q::make(0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < NMB; ++k) b1[k][i] = 0.f;
+    for (int k = 0; k < NMB; ++k) b1[k][i] = Q::make(0.f, 0.f);
   }
   float st[R][4], sn[R][4];                                              // statistics, an iteration ahead
   auto next_stats = [&](int64_t row) {
@@ -328,22 +350,36 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
   };
   next_stats(r0);
   int64_t gate_row = r0 / rg, gate_end = (gate_row + 1) * rg;
+  auto pairs = [](const float (&v)[8], V (&o)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = Q::make(v[2 * i], v[2 * i + 1]);
+  };
+  auto singles = [](const V (&v)[4], float (&o)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) Q::split(v[i], o[2 * i], o[2 * i + 1]);
+  };
+  auto load = [&](const void* base, int k, float other, V (&o)[4]) {        // a parameter's columns, or `other`
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = other;
+    if (base) join_ld((const P*)base, k, p.cols, v);
+    pairs(v, o);
+  };
   // the sums of one gate, at its end: q S1 and q S0 into v1 and v0, the gate's own gradient into dq
-  auto turn_over = [&](int k, float (&v1)[8], float (&v0)[8], float (&dq)[8]) {
-    float q[8], g[8], b[8];
+  auto turn_over = [&](int k, V (&v1)[4], V (&v0)[4], V (&dq)[4]) {
+    V q[4], g[4], b[4];
+    load(p.gate ? (const P*)p.gate + gate_row * p.cols : nullptr, k, 1.f, q);
+    load(p.gain1, k, 1.f, g);
+    if (LN) load(p.gain1 ? p.bias1 : nullptr, k, 0.f, b);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { q[i] = g[i] = 1.f; b[i] = 0.f; }
-    if (p.gate) join_ld((const P*)p.gate + gate_row * p.cols, k, p.cols, q);
-    if (p.gain1) join_ld((const P*)p.gain1, k, p.cols, g);
-    if (LN && p.gain1 && p.bias1) join_ld((const P*)p.bias1, k, p.cols, b);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v1[i] = q[i] * S1[k][i];
-      v0[i] = LN ? q[i] * S0[LN ? k : 0][i] : 0.f;
-      dq[i] = g[i] * S1[k][i] + (LN ? b[i] * S0[LN ? k : 0][i] : 0.f);
+    for (int i = 0; i < 4; ++i) {
+      v1[i] = Q::mul(q[i], S1[k][i]);
+      v0[i] = LN ? Q::mul(q[i], S0[LN ? k : 0][i]) : Q::make(0.f, 0.f);
+      dq[i] = LN ? Q::fma(g[i], S1[k][i], Q::mul(b[i], S0[LN ? k : 0][i])) : Q::mul(g[i], S1[k][i]);
     }
   };
-  // gains and gate as the operand type, in registers
+  // gains (with one gate: its product with the first) in registers; join_ld leaves zeros in columns that do not exist
+  // gains and gate as the operand type, in registers (kept as fp32, gate times gain1 at once: 210 instead of 204 us at 16384 x 4096, RMSNorm)
   P hg2[HOLD ? 8 : 1], hg1[HOLD ? 8 : 1], hq[HOLD && ONE ? 8 : 1];
   if (HOLD) {
     auto hold = [&](const void* base, P* v) {
@@ -356,10 +392,20 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
     if (p.gain1) hold(p.gain1, hg1);
     if (ONE && p.gate) hold((const P*)p.gate + gate_row * p.cols, hq);
   }
-  auto param = [&](const void* base, const P* held, bool is_held, int k, float (&v)[8]) {
-    if (!is_held) { join_ld((const P*)base, k, p.cols, v); return; }
+  auto param = [&](const void* base, const P* held, bool is_held, int k, V (&v)[4]) {
+    if (!is_held) { load(base, k, 1.f, v); return; }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = to_f(held[i]);
+    for (int i = 0; i < 4; ++i) v[i] = Q::make(to_f(held[2 * i]), to_f(held[2 * i + 1]));
+  };
+  auto gain2_of = [&](int k, V (&g)[4]) { param(p.gain2, hg2, HOLD, k, g); };
+  auto gated_gain1_of = [&](int k, V (&g)[4]) {              // gate times gain1, of what there is
+    if (p.gain1) param(p.gain1, hg1, HOLD, k, g);
+    if (p.gate) {
+      V q[4];
+      param((const P*)p.gate + gate_row * p.cols, hq, HOLD && ONE, k, q);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = p.gain1 ? Q::mul(q[i], g[i]) : q[i];
+    }
   };
   // the sums of R rows behind one barrier: c1 = scale mean(w), c2 = scale mean(w hat)
   auto means = [&](const float (&s1)[R], const float (&s2)[R], int which, float (&c1)[R], float (&c2)[R], float* buf) {
@@ -380,12 +426,34 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
   };
   int stage = 0, turn = 0;
   for (int64_t row = r0; row < r1; row += R * step) {
-    float d[R][NC][8], t[R][NC][8], s1[R], s2[R], c1[R], c2[R];
+    V d[R][NC][4], t[R][NC][4], p1[R], p2[R];
+    float s1[R], s2[R], c1[R], c2[R];
+    auto sums = [&] {
+#pragma unroll
+      for (int j = 0; j < R; ++j) {
+        float a, b;
+        Q::split(p1[j], a, b);
+        s1[j] = a + b;
+        Q::split(p2[j], a, b);
+        s2[j] = a + b;
+      }
+    };
+    // t <- (t - mean) rstd
+    auto normalise = [&](V v, int j, int which) {
+      if (LN) v = Q::add(v, Q::make(-st[j][which], -st[j][which]));
+      return Q::mul(v, Q::make(st[j][which + 1], st[j][which + 1]));
+    };
+    // rstd w - c1 - c2 hat
+    auto norm_grad = [&](V w, V hat, int j, int which) {
+      const V r = Q::make(st[j][which + 1], st[j][which + 1]);
+      return Q::fma(Q::make(-c2[j], -c2[j]), hat, LN ? Q::fma(r, w, Q::make(-c1[j], -c1[j])) : Q::mul(r, w));
+    };
 #pragma unroll
     for (int j = 0; j < R; ++j) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) st[j][i] = sn[j][i];
-      s1[j] = s2[j] = c1[j] = c2[j] = 0.f;
+      p1[j] = p2[j] = Q::make(0.f, 0.f);
+      c1[j] = c2[j] = 0.f;
     }
     next_stats(row + R * step);
     if (STAGED) cp_async_wait_upto(p.stages - 1);
@@ -395,74 +463,82 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
         if (R > 1 && row + j * step >= r1) continue;
 #pragma unroll
         for (int k = 0; k < NC; ++k) {
-          float g[8];
-          getp(p.dy, (row + j * step) * p.cols, stage * R + j, k, 2, d[j][k]);
-          get32(p.xo, (row + j * step) * p.cols, stage * R + j, k, 0, t[j][k]);
-          param(p.gain2, hg2, HOLD, k, g);
+          float v[8];
+          V g[4];
+          getp(p.dy, (row + j * step) * p.cols, stage * R + j, k, 2, v);
+          pairs(v, d[j][k]);
+          get32(p.xo, (row + j * step) * p.cols, stage * R + j, k, 0, v);
+          pairs(v, t[j][k]);
+          gain2_of(k, g);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            t[j][k][i] = LN ? (t[j][k][i] - st[j][2]) * st[j][3] : t[j][k][i] * st[j][3];
-            a2[k][i] = fmaf(d[j][k][i], t[j][k][i], a2[k][i]);
-            if (LN) b2[LN ? k : 0][i] += d[j][k][i];
-            d[j][k][i] *= g[i];
-            if (LN) s1[j] += d[j][k][i];
-            s2[j] = fmaf(d[j][k][i], t[j][k][i], s2[j]);
+          for (int i = 0; i < 4; ++i) {
+            t[j][k][i] = normalise(t[j][k][i], j, 2);
+            a2[k][i] = Q::fma(d[j][k][i], t[j][k][i], a2[k][i]);
+            if (LN) b2[LN ? k : 0][i] = Q::add(b2[LN ? k : 0][i], d[j][k][i]);
+            d[j][k][i] = Q::mul(d[j][k][i], g[i]);
+            if (LN) p1[j] = Q::add(p1[j], d[j][k][i]);
+            p2[j] = Q::fma(d[j][k][i], t[j][k][i], p2[j]);
           }
         }
       }
+      sums();
       means(s1, s2, 3, c1, c2, red[turn]);
     }
+    const V scale = Q::make(p.scale, p.scale);
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-      s1[j] = s2[j] = 0.f;
+      p1[j] = p2[j] = Q::make(0.f, 0.f);
       if (R > 1 && row + j * step >= r1) continue;
       const int64_t off = (row + j * step) * p.cols;
 #pragma unroll
       for (int k = 0; k < NC; ++k) {
-        float w[8], q[8];
+        float v[8];
+        V w[4];
         if (p.gain2) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            d[j][k][i] = fmaf(-c2[j], t[j][k][i], LN ? fmaf(st[j][3], d[j][k][i], -c1[j]) : st[j][3] * d[j][k][i]);
+          for (int i = 0; i < 4; ++i) d[j][k][i] = norm_grad(d[j][k][i], t[j][k][i], j, 2);
         } else {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d[j][k][i] = 0.f;
+          for (int i = 0; i < 4; ++i) d[j][k][i] = Q::make(0.f, 0.f);
         }
         if (p.dxo) {
-          get32(p.dxo, off, stage * R + j, k, 1, w);
+          get32(p.dxo, off, stage * R + j, k, 1, v);
+          pairs(v, w);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d[j][k][i] += w[i];
+          for (int i = 0; i < 4; ++i) d[j][k][i] = Q::add(d[j][k][i], w[i]);
         }
         if (ragged) {                                              // columns that do not exist take no part in the sums below
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d[j][k][i] = join_col(k, i >> 2) < p.cols ? d[j][k][i] : 0.f;
+          for (int i = 0; i < 4; ++i) d[j][k][i] = join_col(k, i >> 1) < p.cols ? d[j][k][i] : Q::make(0.f, 0.f);
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = p.scale * d[j][k][i];
-        join_st(p.dx + off, k, p.cols, w);
-        getp(p.h, off, stage * R + j, k, 3, t[j][k]);
-        if (p.gate) param((const P*)p.gate + gate_row * p.cols, hq, HOLD && ONE, k, q);
+        for (int i = 0; i < 4; ++i) w[i] = Q::mul(scale, d[j][k][i]);
+        singles(w, v);
+        join_st(p.dx + off, k, p.cols, v);
+        getp(p.h, off, stage * R + j, k, 3, v);
+        pairs(v, t[j][k]);
         if (p.gain1) {
-          float g[8];
-          param(p.gain1, hg1, HOLD, k, g);
+          gated_gain1_of(k, w);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            t[j][k][i] = LN ? (t[j][k][i] - st[j][0]) * st[j][1] : t[j][k][i] * st[j][1];
-            S1[k][i] = fmaf(d[j][k][i], t[j][k][i], S1[k][i]);
-            if (LN) S0[LN ? k : 0][i] += d[j][k][i];
-            d[j][k][i] *= p.gate ? q[i] * g[i] : g[i];
-            if (LN) s1[j] += d[j][k][i];
-            s2[j] = fmaf(d[j][k][i], t[j][k][i], s2[j]);
+          for (int i = 0; i < 4; ++i) {
+            t[j][k][i] = normalise(t[j][k][i], j, 0);
+            S1[k][i] = Q::fma(d[j][k][i], t[j][k][i], S1[k][i]);
+            if (LN) S0[LN ? k : 0][i] = Q::add(S0[LN ? k : 0][i], d[j][k][i]);
+            d[j][k][i] = Q::mul(d[j][k][i], w[i]);
+            if (LN) p1[j] = Q::add(p1[j], d[j][k][i]);
+            p2[j] = Q::fma(d[j][k][i], t[j][k][i], p2[j]);
           }
         } else {
+          if (p.gate) gated_gain1_of(k, w);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            S1[k][i] = fmaf(d[j][k][i], t[j][k][i], S1[k][i]);
-            if (p.gate) d[j][k][i] *= q[i];
+          for (int i = 0; i < 4; ++i) {
+            S1[k][i] = Q::fma(d[j][k][i], t[j][k][i], S1[k][i]);
+            if (p.gate) d[j][k][i] = Q::mul(d[j][k][i], w[i]);
           }
         }
       }
     }
+    sums();
     if (STAGED) {                                                        // these rows' slots have been read: the rows after the staged ones
       fetch(row + (int64_t)p.stages * R * step, stage);
       cp_async_commit();
@@ -478,19 +554,21 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
       for (int k = 0; k < NC; ++k) {
         if (p.gain1) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            d[j][k][i] = fmaf(-c2[j], t[j][k][i], LN ? fmaf(st[j][1], d[j][k][i], -c1[j]) : st[j][1] * d[j][k][i]);
+          for (int i = 0; i < 4; ++i) d[j][k][i] = norm_grad(d[j][k][i], t[j][k][i], j, 0);
         }
-        join_st((P*)p.dh + (row + j * step) * p.cols, k, p.cols, d[j][k]);
+        float v[8];
+        singles(d[j][k], v);
+        join_st((P*)p.dh + (row + j * step) * p.cols, k, p.cols, v);
         if (!ONE && gate_done) {
-          float v1[8], v0[8], dq[8];
+          V v1[4], v0[4], dq[4];
           turn_over(k, v1, v0, dq);
-          if (p.dgate) join_st(p.dgate + gate_row * p.cols, k, p.cols, dq);
+          singles(dq, v);
+          if (p.dgate) join_st(p.dgate + gate_row * p.cols, k, p.cols, v);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            a1[ONE ? 0 : k][i] += v1[i];
-            S1[k][i] = 0.f;
-            if (LN) { b1[ONE || !LN ? 0 : k][i] += v0[i]; S0[LN ? k : 0][i] = 0.f; }
+          for (int i = 0; i < 4; ++i) {
+            a1[ONE ? 0 : k][i] = Q::add(a1[ONE ? 0 : k][i], v1[i]);
+            S1[k][i] = Q::make(0.f, 0.f);
+            if (LN) { b1[ONE || !LN ? 0 : k][i] = Q::add(b1[ONE || !LN ? 0 : k][i], v0[i]); S0[LN ? k : 0][i] = Q::make(0.f, 0.f); }
           }
         }
       }
@@ -501,18 +579,20 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
   float* out = p.partial + (size_t)blockIdx.x * p.cols;
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
-    float v1[8], v0[8], dq[8];
+    V v1[4], v0[4], dq[4];
+    float v[8];
+    auto put = [&](int plane_no, const V (&s)[4]) { singles(s, v); join_st(out + plane_no * plane, k, p.cols, v); };
     if (ONE) {
       turn_over(k, v1, v0, dq);
-      if (p.gate) join_st(out + 4 * plane, k, p.cols, dq);
+      if (p.gate) put(4, dq);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) { v1[i] = a1[ONE ? 0 : k][i]; v0[i] = b1[ONE || !LN ? 0 : k][i]; }
+      for (int i = 0; i < 4; ++i) { v1[i] = a1[ONE ? 0 : k][i]; v0[i] = b1[ONE || !LN ? 0 : k][i]; }
     }
-    if (p.gain1) join_st(out, k, p.cols, v1);
-    if (LN && p.gain1) join_st(out + plane, k, p.cols, v0);
-    if (p.gain2) join_st(out + 2 * plane, k, p.cols, a2[k]);
-    if (LN && p.gain2) join_st(out + 3 * plane, k, p.cols, b2[LN ? k : 0]);
+    if (p.gain1) put(0, v1);
+    if (LN && p.gain1) put(1, v0);
+    if (p.gain2) put(2, a2[k]);
+    if (LN && p.gain2) put(3, b2[LN ? k : 0]);
   }
 }
 
