@@ -188,6 +188,27 @@ def test_logprobs_alternatives_that_one_thread_holds(code, stride):
     assert torch.equal(torch.gather(t.float(), 1, got[:, n:].long()), rest)
 
 
+@pytest.mark.parametrize("code", [0, 1])
+@pytest.mark.parametrize("vocab,ld", [(2001, 2001), (8100, 8104), (16001, 16001)])
+def test_logprobs_of_many_short_rows(code, vocab, ld):
+    """Rows enough to fill the GPU with small blocks.  A thread's run of a sum is up to V / 64 terms there: V / 128 roundings more."""
+    rows, top = 8192, 6
+    t, _ = _logits(rows, vocab, ld, code, 1, seed=vocab)
+    tok = np.random.default_rng(vocab).integers(0, vocab, rows)
+    logp, ent, st, ids, vals = _run_logp(t, tok, vocab, 0.9, top, code)
+    some = np.r_[0:16, 4000:4016, rows - 16:rows]
+    x = t[some][:, :vocab].double().cpu().numpy()
+    rl, re, rs, ri, rv = R.token_logprobs(x, tok[some], 0.9, top)
+    sl = _logp_slack(x, 0.9, rs) + R.U32 * vocab / 128
+    assert np.array_equal(ids[some], ri) and np.array_equal(st[0, some], rs[0].astype(np.float32))
+    for g, ref, s in ((logp[some], rl, sl), (st[1, some], rs[1], sl), (ent[some], re, sl * (1 + np.abs(re)) + 8 * R.U32 * np.abs(re)),
+                      (vals[some], rv, np.broadcast_to(sl[:, None], rv.shape))):
+        assert_elem(g, ref, 6 * R.U32, s, "short rows")
+    all_top = _torch().topk(t[:, :vocab].float(), top, dim=1).values.double().cpu().numpy()
+    lse = _torch().logsumexp(t[:, :vocab].double() / 0.9, dim=1).cpu().numpy()
+    assert np.abs(vals - (all_top / 0.9 - lse[:, None])).max() < 1e-4       # every row: alternatives of the right logits
+
+
 def test_logprobs_read_no_padding_and_keep_the_logits():
     torch = _torch()
     t, _ = _logits(6, 1000, 1032, 1, 0, seed=5)
