@@ -8,7 +8,7 @@
 // 107 -> 17 and of 4096 x 16 86 -> 52 us.
 constexpr int kTinyRows = 16, kTinyThreads = 512;
 template <int CP> constexpr int kTinyPitch = kTinyThreads * CP + 4;      // floats between rows of the copy: float4 reads of 16 rows, two per bank
-template <int CP> constexpr int ns_tiny_smem = (kTinyRows * kTinyPitch<CP> + 2048 + 2 * 16 * 256 + 2 * 256) * 4 + 2 * 16 * 8;
+template <int CP> constexpr int ns_tiny_smem = (kTinyRows * kTinyPitch<CP> + 2048 + 2 * 16 * 256 + 2 * 256) * 4 + 2 * 16 * 8 + 17 * 4;
 
 template <typename T, int CP>
 __global__ void __launch_bounds__(kTinyThreads, 1) ns_tiny_kernel(NsSmallArgs a) {
@@ -19,6 +19,7 @@ __global__ void __launch_bounds__(kTinyThreads, 1) ns_tiny_kernel(NsSmallArgs a)
   float* A = gather + 2 * 16 * 256;
   float* P = A + 256;
   double* dred = reinterpret_cast<double*>(P + 256);   // [16] of this CTA, [16] of the cluster's CTAs
+  int* held = reinterpret_cast<int*>(dred + 32);       // results held back after a time-out: [16] as the cluster's CTAs read the flag, then this CTA's reading
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   uint32_t C;
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
@@ -30,6 +31,9 @@ __global__ void __launch_bounds__(kTinyThreads, 1) ns_tiny_kernel(NsSmallArgs a)
   auto column = [&](int p) { return ((int)me * CP + p) * kTinyThreads + tid; };
   auto at = [&](int m, int j) { return wide ? (size_t)m * a.cols + j : (size_t)j * a.cols + m; };
 
+  // No product of this kernel can time out, but the matrix may come out of one that did.  Other streams may raise the flag meanwhile, so
+  // each CTA takes one reading and sends it round with its sum: all decide alike.
+  const int raised = tid == 0 ? *(volatile int*)&g_tc_error : 0;
   float x[CP][kTinyRows];
   double s = 0.0;
 #pragma unroll
@@ -60,11 +64,13 @@ __global__ void __launch_bounds__(kTinyThreads, 1) ns_tiny_kernel(NsSmallArgs a)
   }
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if (lane == 0) dred[warp] = s;
+  if (tid == 0) held[16] = raised != 0;
   cluster_sync_all();                                  // and every CTA of the cluster has started
   if (tid < (int)C) {
     double t = 0.0;
     for (int w = 0; w < kTinyThreads / 32; ++w) t += dred[w];
     asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(ns_peer(smem_u32(dred + 16 + me), tid)), "d"(t) : "memory");
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(ns_peer(smem_u32(held + me), tid)), "r"(held[16]) : "memory");
   }
   cluster_sync_all();
   {
@@ -161,6 +167,9 @@ __global__ void __launch_bounds__(kTinyThreads, 1) ns_tiny_kernel(NsSmallArgs a)
 #pragma unroll
       for (int m = 0; m < kTinyRows; ++m) x[p][m] = y[p][m];
   }
+  int hold = 0;
+  for (int w = 0; w < (int)C; ++w) hold |= held[w];
+  if (hold) return;                                    // (no peer reads this CTA's shared memory any more)
 #pragma unroll
   for (int p = 0; p < CP; ++p) {
     const int j = column(p);
