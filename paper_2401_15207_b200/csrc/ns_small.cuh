@@ -180,6 +180,7 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
   fence_proxy_async_all();
 
   uint32_t phase = 0;
+  bool ok = true;
   auto run = [&](auto&& issue) {                       // all threads: operands are ready; one issues, all wait for the products
     tc_fence_before();
     __syncthreads();
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
       if (lane == 0) { issue(); tc_commit(bar); }
       __syncwarp();
     }
-    if (!mbar_wait(bar, phase)) atomicCAS(&g_tc_error, 0, 3);       // the result is then not written
+    if (!mbar_wait(bar, phase)) { ok = false; atomicCAS(&g_tc_error, 0, 3); }       // the result is then not written
     phase ^= 1;
     tc_fence_after();
   };
@@ -330,8 +331,18 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
     }
     fence_proxy_async_all();
   }
-  // ---- the result, unless a product gave up on a wait
-  const bool write = *(volatile int*)&g_tc_error == 0;
+  // ---- the result, unless a product gave up on a wait: here, in another CTA of the cluster, or before this launch.  Every CTA sends its
+  // reading of the flag round, so that all decide alike and no matrix is half updated.
+  const int gave_up = __syncthreads_or(!ok);
+  if (warp == 0) {
+    const int raised = __shfl_sync(0xffffffffu, lane == 0 ? *(volatile int*)&g_tc_error : 0, 0) | gave_up;
+    if (lane < (int)C) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(ns_peer(nrm_s + 4 * me, lane)), "r"(raised) : "memory");   // (the norm has been read)
+    __syncwarp();
+  }
+  cluster_sync_all();
+  int hold = 0;
+  for (int w = 0; w < (int)C; ++w) hold |= reinterpret_cast<const int*>(nrm)[w];
+  const bool write = hold == 0;
 #pragma unroll 1
   for (int k = 0; k < NH; ++k) {
     uint32_t v[32];
