@@ -351,10 +351,12 @@ int32_t hift_tc_error_flag(int32_t set_value);
 
 /* Code-path switches for tests and A/B timing; every one defaults to 1, the fast path.  which = 0: CTA-pair
  * tiles in the tensor-core GEMM (0 = one CTA per tile); 1: programmatic dependent launch (0 = plain stream
- * order); 2: tcgen05 attention forward, 3: tcgen05 attention backward (0 = the warp-level mma.sync kernels).
+ * order); 2: tcgen05 attention forward, 3: tcgen05 attention backward (0 = the warp-level mma.sync kernels); 6: the
+ * orthogonalised update of small matrices in one launch (0 = the products of the large ones, which also run where a
+ * device cannot hold the cluster of up to 16 blocks that the one launch takes).
  * value >= 0 sets the switch, value < 0 only reads it; returns the previous value, or -1 for an unknown
  * switch.  Process-wide, consulted at every launch, not thread-safe.  Results do not depend on switches 0
- * and 1 (same bits); 2 and 3 select kernels with a different summation order.
+ * and 1 (same bits); 2, 3 and 6 select kernels with a different summation order (6: and other roundings).
  * Two more, for fault-path tests that need no faulting GPU: which = 4: the value-th pinned host allocation
  * from now on (0 = the next one) fails as if the host were out of pinned memory, once (value -1 = off),
  * so that hift_create's HIFT_ERR_OOM_PINNED path and its clean-up run; which = 5: contexts created while it

@@ -501,7 +501,7 @@ def tc_error_flag(set_value: int = -1) -> int:
     return lib().hift_tc_error_flag(set_value)
 
 
-SWITCH_GEMM_PAIR, SWITCH_PDL, SWITCH_ATTN_FWD_TC, SWITCH_ATTN_BWD_TC, SWITCH_FAIL_PINNED, SWITCH_CHECKED_ARENA = 0, 1, 2, 3, 4, 5
+SWITCH_GEMM_PAIR, SWITCH_PDL, SWITCH_ATTN_FWD_TC, SWITCH_ATTN_BWD_TC, SWITCH_FAIL_PINNED, SWITCH_CHECKED_ARENA, SWITCH_NS_ONE_LAUNCH = 0, 1, 2, 3, 4, 5, 6
 
 
 def code_path_switch(which: int, value: int = -1) -> int:

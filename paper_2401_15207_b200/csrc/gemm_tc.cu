@@ -1264,6 +1264,26 @@ cudaError_t launch_ns_cluster(cudaStream_t st, void (*kernel)(NsSmallArgs), int 
   cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
+int g_ns_one_launch = 1; // one-launch kernels of the orthogonalised update (switch 6; 0: the tiled products)
+// Largest cluster of `kernel`, up to 16 CTAs, of which this device can hold one; 0 if there is none.
+int ns_largest_cluster(void (*kernel)(NsSmallArgs), int smem, int threads) {
+  for (int c = 16; c > 0; c /= 2) {
+    cudaLaunchConfig_t cfg;
+    memset(&cfg, 0, sizeof(cfg));
+    cfg.gridDim = dim3(c);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = c; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0) return c;
+    cudaGetLastError();
+  }
+  return 0;
+}
 int g_attn_tc = 1;       // tcgen05 attention forward (switch 2; 0 falls back to the mma.sync kernel)
 int g_attn_bwd_tc = 1;   // tcgen05 attention backward (switch 3; 0 falls back to the mma.sync kernels)
 template <int DH, int MODE>
@@ -1279,8 +1299,8 @@ int g_pair_mode = 1;     // CTA-pair kernel for 256-wide tiles (switch 0; 0 fall
 }  // namespace
 
 int gemm_tc_switch(int which, int value) {
-  int* sw[4] = {&g_pair_mode, &g_pdl, &g_attn_tc, &g_attn_bwd_tc};
-  if (which < 0 || which > 3) return -1;
+  int* sw[7] = {&g_pair_mode, &g_pdl, &g_attn_tc, &g_attn_bwd_tc, nullptr, nullptr, &g_ns_one_launch};
+  if (which < 0 || which > 6 || !sw[which]) return -1;
   const int old = *sw[which];
   if (value >= 0) *sw[which] = value;
   return old;
@@ -1421,51 +1441,67 @@ cudaError_t gemm_tc_launch(cudaStream_t st, const GemmArgs& g) {
 // The Newton-Schulz kernels' attributes and the address of the time-out flag belong to a device: set up per device, for these
 // operators take whichever device is current.  Returns the flag's address, nullptr where the kernels cannot run.
 constexpr int kNsMaxDevices = 64;
+std::atomic<const int*> g_ns_flag[kNsMaxDevices];          // zero-initialised
+int g_ns_cluster[kNsMaxDevices][2];                        // largest cluster of the one-launch kernels: [0] ns_small, [1] ns_tiny; written before the flag
 const int* ns_device_flag() {
-  static std::atomic<const int*> flag[kNsMaxDevices];      // zero-initialised
   int dev = 0, major = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev >= kNsMaxDevices) return nullptr;
-  if (const int* p = flag[dev].load(std::memory_order_acquire)) return p;
+  if (const int* p = g_ns_flag[dev].load(std::memory_order_acquire)) return p;
   if (gemm_tc_init() != 0) return nullptr;
+  std::lock_guard<std::mutex> lk(g_mu);
+  if (const int* p = g_ns_flag[dev].load(std::memory_order_acquire)) return p;
   void* p = nullptr;
   cudaError_t e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev);
   if (e == cudaSuccess && major != 10) return nullptr;
   if (e == cudaSuccess) e = cudaGetSymbolAddress(&p, g_tc_error);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<float, 1>, ns_small_smem<1>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<float, 2>, ns_small_smem<2>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<__nv_bfloat16, 1>, ns_small_smem<1>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_small_kernel<__nv_bfloat16, 2>, ns_small_smem<2>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<float, 1>, ns_tiny_smem<1>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<float, 2>, ns_tiny_smem<2>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<__nv_bfloat16, 1>, ns_tiny_smem<1>);
-  if (e == cudaSuccess) e = set_attr_ns_cluster(ns_tiny_kernel<__nv_bfloat16, 2>, ns_tiny_smem<2>);
+  struct { void (*kernel)(NsSmallArgs); int smem, threads; } one[] = {
+      {ns_small_kernel<float, 1>, ns_small_smem<1>, kSmThreads}, {ns_small_kernel<__nv_bfloat16, 1>, ns_small_smem<1>, kSmThreads},
+      {ns_small_kernel<float, 2>, ns_small_smem<2>, kSmThreads}, {ns_small_kernel<__nv_bfloat16, 2>, ns_small_smem<2>, kSmThreads},
+      {ns_tiny_kernel<float, 1>, ns_tiny_smem<1>, kTinyThreads}, {ns_tiny_kernel<__nv_bfloat16, 1>, ns_tiny_smem<1>, kTinyThreads},
+      {ns_tiny_kernel<float, 2>, ns_tiny_smem<2>, kTinyThreads}, {ns_tiny_kernel<__nv_bfloat16, 2>, ns_tiny_smem<2>, kTinyThreads}};
+  g_ns_cluster[dev][0] = g_ns_cluster[dev][1] = 16;
+  for (int i = 0; i < 8 && e == cudaSuccess; ++i) {
+    e = set_attr_ns_cluster(one[i].kernel, one[i].smem);
+    const int c = e == cudaSuccess ? ns_largest_cluster(one[i].kernel, one[i].smem, one[i].threads) : 0;
+    if (c < g_ns_cluster[dev][i / 4]) g_ns_cluster[dev][i / 4] = c;
+  }
   if (e == cudaSuccess) e = set_smem_attr_ns<false, false, 1>();
   if (e == cudaSuccess) e = set_smem_attr_ns<true, true, 1>();
   if (e == cudaSuccess) e = set_smem_attr_ns<false, false, 2>();
   if (e == cudaSuccess) e = set_smem_attr_ns<false, true, 2>();
   if (e != cudaSuccess) { cudaGetLastError(); return nullptr; }
-  flag[dev].store((const int*)p, std::memory_order_release);
+  g_ns_flag[dev].store((const int*)p, std::memory_order_release);
   return (const int*)p;
 }
 
-bool ns_small_eligible(int64_t rows, int64_t cols) {
+// One-launch kernel of a matrix: columns of a CTA (in units of kTinyThreads or 128) and CTAs; ctas = 0: too large for one cluster.
+struct NsSmallShape { bool tiny; int per, ctas; };
+static NsSmallShape ns_small_shape(int64_t rows, int64_t cols) {
   const int64_t s = rows < cols ? rows : cols, l = rows < cols ? cols : rows;
-  return s <= kTinyRows ? l <= 16 * kTinyThreads * 2 : s <= 128 && l <= 16 * 256;
+  NsSmallShape sh{s <= kTinyRows, 1, 0};
+  const int unit = sh.tiny ? kTinyThreads : 128;
+  if (s > 128 || l > 16 * 2 * unit) return sh;
+  if (l > 16 * unit) sh.per = 2;
+  for (sh.ctas = 1; (int64_t)sh.ctas * unit * sh.per < l;) sh.ctas *= 2;
+  return sh;
+}
+bool ns_small_eligible(int64_t rows, int64_t cols) {
+  int dev = 0;
+  if (!g_ns_one_launch || cudaGetDevice(&dev) != cudaSuccess || dev >= kNsMaxDevices) return false;
+  const NsSmallShape sh = ns_small_shape(rows, cols);
+  return sh.ctas > 0 && sh.ctas <= g_ns_cluster[dev][sh.tiny];
 }
 cudaError_t ns_small_launch(cudaStream_t st, bool g_bf16, int64_t rows, int64_t cols, const void* g, float* mom, float mu, int nesterov, int steps,
                             void* o, float* master, void* param, float decay, float size) {
-  const int S = (int)(rows < cols ? rows : cols), L = (int)(rows < cols ? cols : rows);
   const NsSmallArgs a{g, mom, (__nv_bfloat16*)o, master, (__nv_bfloat16*)param, (int)rows, (int)cols, steps, nesterov, mu, decay, size};
-  const bool tiny = S <= kTinyRows;
-  const int unit = tiny ? kTinyThreads : 128, per = L <= 16 * unit ? 1 : 2;      // columns of a CTA: unit * per
-  int ctas = 1;
-  while (ctas * unit * per < L) ctas *= 2;
-  if (tiny) {
+  const NsSmallShape sh = ns_small_shape(rows, cols);
+  const int per = sh.per;
+  if (sh.tiny) {
     auto k = g_bf16 ? (per == 1 ? ns_tiny_kernel<__nv_bfloat16, 1> : ns_tiny_kernel<__nv_bfloat16, 2>) : (per == 1 ? ns_tiny_kernel<float, 1> : ns_tiny_kernel<float, 2>);
-    return launch_ns_cluster(st, k, per == 1 ? ns_tiny_smem<1> : ns_tiny_smem<2>, kTinyThreads, ctas, a);
+    return launch_ns_cluster(st, k, per == 1 ? ns_tiny_smem<1> : ns_tiny_smem<2>, kTinyThreads, sh.ctas, a);
   }
   auto k = g_bf16 ? (per == 1 ? ns_small_kernel<__nv_bfloat16, 1> : ns_small_kernel<__nv_bfloat16, 2>) : (per == 1 ? ns_small_kernel<float, 1> : ns_small_kernel<float, 2>);
-  return launch_ns_cluster(st, k, per == 1 ? ns_small_smem<1> : ns_small_smem<2>, kSmThreads, ctas, a);
+  return launch_ns_cluster(st, k, per == 1 ? ns_small_smem<1> : ns_small_smem<2>, kSmThreads, sh.ctas, a);
 }
 
 cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps) {

@@ -33,11 +33,12 @@ struct NsBuffers { int rows, cols; float* x32; void* x16[2]; void *e, *f; float 
 cudaError_t ns_products_launch(cudaStream_t st, const NsBuffers& b, int steps);
 // The whole operation in one launch for a short side of at most 16 and a long one of at most 16384 (ns_tiny.cuh) or of at most 128 and
 // 4096 (ns_small.cuh): momentum (if not nullptr), normalisation, steps, and the result as o, or as the update of master (and param).
+// Eligible: the current device, which ns_device_flag has set up, holds the cluster that this takes (up to 16 CTAs); else the tiled products do it.
 bool ns_small_eligible(int64_t rows, int64_t cols);
 cudaError_t ns_small_launch(cudaStream_t st, bool g_bf16, int64_t rows, int64_t cols, const void* g, float* mom, float mu, int nesterov, int steps,
                             void* o, float* master, void* param, float decay, float size);
 // Code-path switches for A/B timing and for tests (all 1 by default = the fast path): which = 0 CTA-pair
-// GEMM tiles, 1 programmatic dependent launch, 2 tcgen05 attention forward, 3 tcgen05 attention backward.
+// GEMM tiles, 1 programmatic dependent launch, 2 tcgen05 attention forward, 3 tcgen05 attention backward, 6 one-launch orthogonalisation.
 // value >= 0 sets the switch; returns its previous value (-1: no such switch).  Process-wide; read at
 // each launch.
 int gemm_tc_switch(int which, int value);
