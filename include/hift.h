@@ -569,7 +569,8 @@ hift_status hift_k_join_fwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
  *     dgate = sum of d o N1(h) over a gate's rows (fp32, the gate's shape),  dgain1, dbias1, dgain2, dbias2 fp32 [cols].
  * Each of the last five may be NULL (not wanted); one that belongs to a missing norm, gate or bias is refused.  bias1_dev is
  * read for dgate only.  Sums over rows run in a fixed order.  scratch_dev: hift_join_bwd_scratch_bytes(rows, cols,
- * rows_per_gate) bytes (rows_per_gate = rows without a gate), HIFT_ERR_CAPACITY if scratch_bytes is less. */
+ * rows_per_gate) bytes (rows_per_gate = rows without a gate; 0 for rows and columns that the call does not take),
+ * HIFT_ERR_CAPACITY if scratch_bytes is less. */
 size_t      hift_join_bwd_scratch_bytes(int64_t rows, int64_t cols, int64_t rows_per_gate);
 hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double res_scale, const void *dy_dev,
                             const float *dx_out_dev, const float *x_out_dev, const void *h_dev, const float *stats_dev,

@@ -161,3 +161,10 @@ def test_reference_orthogonalisation_maps_singular_values():
         for _ in range(5):
             s = R.NS[0] * s + R.NS[1] * s ** 3 + R.NS[2] * s ** 5
         assert np.abs(R.orthogonalize(g) - (u * s) @ vt).max() < 1e-9
+
+
+@pytest.mark.parametrize("rows,cols", [(1000, 16392), (1000, 2 ** 40), (1000, 2 ** 63 - 8), (2 ** 31, 64), (2 ** 62, 16384)])
+def test_join_scratch_of_sizes_that_are_refused(L, rows, cols):
+    """No size for rows and columns that the call does not take (their products wrapped around)."""
+    assert L.hift_join_bwd_scratch_bytes(rows, cols, rows) == 0
+    assert L.hift_join_bwd_scratch_bytes(1000, 16384, 1000) > 0
