@@ -171,9 +171,11 @@ def _check(status: int, where: str):
 
 
 def _stream_ptr() -> int:
-    # torch.cuda.current_stream().cuda_stream without the Stream object it builds (0.5 instead of 3.4 us a call)
+    # torch.cuda.current_stream().cuda_stream without the Stream object it builds (0.5 instead of 3.4 us a call), where this
+    # torch has that call, which is not a public one
     import torch
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
 
 
 def _ptr(t) -> Optional[int]:

@@ -168,3 +168,16 @@ def test_join_scratch_of_sizes_that_are_refused(L, rows, cols):
     """No size for rows and columns that the call does not take (their products wrapped around)."""
     assert L.hift_join_bwd_scratch_bytes(rows, cols, rows) == 0
     assert L.hift_join_bwd_scratch_bytes(1000, 16384, 1000) > 0
+
+
+def test_current_stream_without_torchs_private_call(monkeypatch):
+    """The stream of a call is torch's current one, also with a torch that lacks the private call which tells it sooner."""
+    import types
+
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: types.SimpleNamespace(cuda_stream=77))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 100 + device, raising=False)
+    assert B._stream_ptr() == 103
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    assert B._stream_ptr() == 77
