@@ -12,9 +12,13 @@
 //     matrix: if P(A) has a low rank so has the rounding noise that it passes on, which the later steps would amplify like a signal
 //     (with the fp32 iterate there, a rank-1 16 x 300 matrix comes out 2e-2 off).  In the last two steps nothing amplifies any more,
 //     and Y is the fp32 iterate, which spares the large diagonals that rounding.
-// Relative error of the result before its own rounding, from a CPU model of these roundings over Gaussian, low-rank (1 to 8), decaying,
-// sparse, one-row and outlier matrices of 4 x 40 to 512 x 512: at most 2.4e-3, typically 3e-4 to 1e-3 (all-bf16 products: 7e-3 on
-// full-rank matrices, 5e-2 to 1 on low-rank ones).
+// Relative error of the result of five steps before its own rounding, from a CPU model of these roundings and as measured.  Where the
+// roundings average out (Gaussian, low-rank, decaying, sparse, one-row and outlier matrices of 4 x 40 to 4096 x 11008): at most 2.4e-3,
+// typically 3e-4 to 1e-3 (all-bf16 products: 7e-3 on full-rank matrices, 5e-2 to 1 on low-rank ones).  Where they line up, because there
+// are few distinct values: constant 64 x 67 6e-3, blocks of 4 x 4 ones at 32 x 32 9e-3, the model's worst single singular value 3.6e-2 (it
+// starts at 0.63, so that four steps amplify).  High and low halves of X and F (three products each) would give 2e-3, of E too 2e-5, at
+// up to three times the tensor work.  Further steps: up to 1.6 times each on what is there, 3.44 on the null space's noise, which is the product
+// of two roundings (2^-24): rank 3 at 4096 x 4096 1.7e-3 after five steps, 4.6e-2 after eight (fp32 products: 2.4e-4, 6.3e-3); no digit after 15.
 // A and P(A) are symmetric: only tiles that touch the lower triangle are computed, and a 32 x 32 chunk below the diagonal is
 // stored a second time transposed.  All dimensions are multiples of 64 (zero-padded scratch), so a chunk exists or not as a whole.
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;

@@ -99,7 +99,7 @@ cudaError_t launch_join_bwd(cudaStream_t st, int th, int nc, const JoinBwd& p) {
 }
 
 hift_status ns_cfg(int64_t rows, int64_t cols, int32_t steps, const void* scratch, size_t scratch_bytes) {
-  if (rows < 1 || cols < 1 || steps < 1 || steps > 20) return HIFT_ERR_CFG;
+  if (rows < 1 || cols < 1 || steps < 1 || steps > HIFT_ORTHOGONALIZE_MAX_STEPS) return HIFT_ERR_CFG;
   if (rows > HIFT_ORTHOGONALIZE_MAX_DIM || cols > HIFT_ORTHOGONALIZE_MAX_DIM) return HIFT_ERR_CAPACITY;
   if (!scratch) return HIFT_ERR_INPUT;
   if (!aligned(scratch, 256)) return HIFT_ERR_CFG;

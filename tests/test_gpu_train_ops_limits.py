@@ -1,6 +1,7 @@
 """The orthogonalised update at its limits: every one of its three paths (one fp32 launch for a short side of at most 16, one launch
 for one of at most 128, tiled products), both orientations, with inputs whose roundings line up, zeros, bad values, extreme scales
 and a raised time-out flag."""
+import numpy as np
 import pytest
 
 import train_ops_ref as R
@@ -8,6 +9,32 @@ from gpu_util import rel_l2
 from test_gpu_train_ops import NS_TOL, _dev, _matrix, _ns_tol, _orth, _torch
 
 pytestmark = pytest.mark.gpu
+# one fp32 launch, one CTA and several; one launch on tensor cores, one CTA, several, two column blocks a CTA; tiled
+PATHS = [(1, 1), (2, 3), (16, 300), (9000, 16), (64, 64), (120, 500), (40, 3001), (3001, 40), (130, 200), (200, 130)]
+
+
+def _unrounded(g, steps=5):
+    """The result before its rounding to bf16: the update of a matrix of zeros without momentum is -lr 0.2 sqrt(max(rows, cols)) X."""
+    from paper_2401_15207_b200 import muon_step, orthogonalize_scratch_bytes
+    torch = _torch()
+    rows, cols = g.shape
+    master, mom = torch.zeros(rows, cols, device="cuda"), torch.zeros(rows, cols, device="cuda")
+    w = torch.empty(orthogonalize_scratch_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    muon_step(rows, cols, None, master, g, mom, w, 1.0, momentum=0.0, nesterov=False, steps=steps)
+    torch.cuda.synchronize()
+    return -master.double().cpu().numpy() / (0.2 * np.sqrt(max(rows, cols)))
+
+
+def _few_values(kind, rows, cols):
+    if kind == "constant":
+        return np.ones((rows, cols), np.float32)
+    if kind == "diagonal":
+        return np.eye(rows, cols, dtype=np.float32)
+    n, g = int(kind[6:]), np.zeros((rows, cols), np.float32)
+    for i in range(0, rows, n):
+        j = i * cols // rows
+        g[i:i + n, j:j + n] = 1
+    return g
 
 
 @pytest.mark.parametrize("rows,cols", [(1, 1), (2, 3), (16, 300), (300, 2), (9000, 16), (64, 64), (40, 3001), (3001, 40), (130, 200)])
@@ -54,3 +81,27 @@ def test_small_matrices_on_the_tiled_products(code, rows, cols):
     assert rel_l2(one, ref) < _ns_tol(rows * cols)
     if min(rows, cols) <= 16 and rows * cols >= 100:     # fp32 there, 16-bit operands here: the switch reached another kernel
         assert not (tiled == one).all()
+
+
+@pytest.mark.parametrize("kind", ["constant", "diagonal", "blocks4", "blocks16"])
+@pytest.mark.parametrize("rows,cols", [(16, 300), (20, 100), (32, 32), (48, 48), (64, 67), (128, 128), (64, 200), (300, 40), (200, 512), (512, 200), (300, 700)])
+def test_orthogonalize_where_roundings_line_up(kind, rows, cols):
+    """Few distinct values: every entry is rounded the same way, so nothing averages out.  The bounds are those of the header: a scalar
+    model of the products' roundings (X to fp16 in both products, E, F; 1.2e7 blocks of ones of random sizes and scales) is at most 3.6e-2
+    off after five steps and 1.4e-1 after eight.  With everything in fp32 the same line-up has 2^-24 in the place of 2^-11, 2^-4 becomes
+    2^-17, and sums of up to 300 equal terms, whose partial sums are all rounded alike, put at most 8 times that on it."""
+    g = _few_values(kind, rows, cols)
+    for steps, tol in ((1, 2.0 ** -4), (3, 2.0 ** -4), (5, 2.0 ** -4), (8, 2.0 ** -2)):
+        if min(rows, cols) <= 16:
+            tol *= 2.0 ** -10
+        assert rel_l2(_unrounded(_dev(g), steps), R.orthogonalize(g.astype(np.float64), steps)) < tol, steps
+
+
+@pytest.mark.parametrize("kind", ["gauss", "rank1", "rank3"])
+@pytest.mark.parametrize("rows,cols", PATHS + [(300, 700)])
+def test_orthogonalize_steps_on_every_path(kind, rows, cols):
+    """Where roundings average out 2^-8 up to five steps.  Three more multiply the null space's noise by 3.44 each, 41 in all, the rest
+    by up to 1.6: 2^-4."""
+    g = _matrix(kind, rows, cols, 5)
+    for steps in (1, 2, 3, 5, 8):
+        assert rel_l2(_unrounded(_dev(g), steps), R.orthogonalize(g.astype(np.float64), steps)) < (NS_TOL if steps <= 5 else 2.0 ** -4), steps

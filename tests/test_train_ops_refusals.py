@@ -181,3 +181,11 @@ def test_current_stream_without_torchs_private_call(monkeypatch):
     assert B._stream_ptr() == 103
     monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
     assert B._stream_ptr() == 77
+
+
+@pytest.mark.parametrize("steps,want", [(1, INPUT), (8, INPUT), (9, CFG), (20, CFG)])
+def test_orthogonalisation_takes_eight_steps_at_most(L, steps, want):
+    """Noise in directions that a matrix lacks grows by 3.44 a step, in fp32 too: more steps would keep no digit of a low-rank matrix.
+    (INPUT: the scratch buffer is missing, which is looked at after the steps.)"""
+    assert L.hift_k_orthogonalize(0, 4, 64, P, P, steps, None, 1 << 30, None) == want
+    assert L.hift_muon_step(4, 64, P, P, P, P, None, 1 << 30, 1e-3, 0.95, 1, 0.0, steps, None) == want
