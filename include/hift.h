@@ -584,13 +584,13 @@ hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
  * `steps` times, (a, b, c) = (3.4445, -4.7750, 2.0315): every singular value s of X goes to a s + b s^3 + c s^5, which brings
  * all of 0.01 and more to between 0.68 and 1.14 in five steps.  g_dev [rows, cols] fp32 (dtype 0) or bf16 (1), o_dev bf16
  * [rows, cols].
- * The products run in 16-bit floating point with fp32 sums, around an iterate kept in fp32 (all in fp32 for a short side of at most 16):
- * before its rounding to bf16 and relative to its Frobenius norm, the result of up to five steps is within 2^-8 of the definition
- * where the products' roundings average out, as over random entries and gradients of any rank, up to a short side of 4096 (found: 2e-4
- * to 2.4e-3), and within 2^-4 where they line up, in matrices of few distinct values (all entries equal, equal blocks, diagonal ones;
- * found: up to 9e-3, 3.6e-2 on a single singular value).  Every further step multiplies what is there by up to 1.6, and noise in
- * directions that the matrix lacks, which fp32 sums have too, by 3.44: 2^-4 and 2^-2 after eight, beyond which no digit of a low-rank
- * matrix could be kept.  A zero matrix stays zero; NaN or infinity anywhere makes the whole result NaN.
+ * The products run in 16-bit floating point with fp32 sums, around an iterate kept in fp32 (all in fp32 for a short side of at most 16
+ * beside a long one of at most 16384).  Before its rounding to bf16 and relative to its Frobenius norm, the result of up to five steps is
+ * within 2^-8 of the definition where the products' roundings average out, as over random entries and gradients of any rank, up to a
+ * short side of 4096 (found: 2e-4 to 2.4e-3), and within 2^-4 where they line up, in matrices of few distinct values (all entries
+ * equal, equal blocks, diagonal ones; found: up to 9e-3, 3.6e-2 on a single singular value).  Every further step multiplies what is
+ * there by up to 1.6, and noise in directions that the matrix lacks, which fp32 sums have too, by 3.44: 2^-4 and 2^-2 after eight.
+ * More would keep no digit of a low-rank matrix.  A zero matrix stays zero; NaN or infinity anywhere makes the whole result NaN.
  * 1 <= rows, cols <= HIFT_ORTHOGONALIZE_MAX_DIM (HIFT_ERR_CAPACITY), 1 <= steps <= HIFT_ORTHOGONALIZE_MAX_STEPS.  scratch_dev: 256-byte
  * aligned, hift_orthogonalize_scratch_bytes(rows, cols) bytes.  A call after a time-out (hift_tc_error_flag) writes no result. */
 #define HIFT_ORTHOGONALIZE_MAX_DIM 65536

@@ -105,3 +105,13 @@ def test_orthogonalize_steps_on_every_path(kind, rows, cols):
     g = _matrix(kind, rows, cols, 5)
     for steps in (1, 2, 3, 5, 8):
         assert rel_l2(_unrounded(_dev(g), steps), R.orthogonalize(g.astype(np.float64), steps)) < (NS_TOL if steps <= 5 else 2.0 ** -4), steps
+
+
+@pytest.mark.parametrize("kind", ["gauss", "rank1"])
+@pytest.mark.parametrize("rows,cols", [(3, 16384), (16384, 16), (1, 16384), (3, 16385), (16385, 16), (16, 20000), (1, 50257), (65536, 2)])
+def test_orthogonalize_both_sides_of_the_fp32_limit(kind, rows, cols):
+    """A short side of at most 16: all in fp32 up to a long side of 16384, where five steps leave noise of 2^-24 in each of up to 16
+    directions, grown by 3.44^5: 1.2e-4 < 2^-12.  Longer ones take the 16-bit products: 2^-8."""
+    g = _matrix(kind, rows, cols, 5)
+    tol = 2.0 ** -12 if max(rows, cols) <= 16384 else NS_TOL
+    assert rel_l2(_unrounded(_dev(g)), R.orthogonalize(g.astype(np.float64))) < tol
