@@ -6,7 +6,7 @@ import pytest
 
 import train_ops_ref as R
 from gpu_util import rel_l2
-from test_gpu_train_ops import NS_TOL, _dev, _matrix, _ns_tol, _orth, _torch
+from test_gpu_train_ops import INF, NAN, NS_TOL, _dev, _matrix, _ns_tol, _orth, _torch
 
 pytestmark = pytest.mark.gpu
 # one fp32 launch, one CTA and several; one launch on tensor cores, one CTA, several, two column blocks a CTA; tiled
@@ -115,3 +115,30 @@ def test_orthogonalize_both_sides_of_the_fp32_limit(kind, rows, cols):
     g = _matrix(kind, rows, cols, 5)
     tol = 2.0 ** -12 if max(rows, cols) <= 16384 else NS_TOL
     assert rel_l2(_unrounded(_dev(g)), R.orthogonalize(g.astype(np.float64))) < tol
+
+
+@pytest.mark.parametrize("tiled", [False, True])
+@pytest.mark.parametrize("rows,cols", PATHS)
+def test_scales_zeros_and_bad_values_on_every_path(rows, cols, tiled):
+    """Squares beyond fp32 both ways, zeros, and a NaN or an infinity in a corner, on the path that a matrix takes and on the tiled one."""
+    from paper_2401_15207_b200 import code_path_switch
+    from paper_2401_15207_b200.binding import SWITCH_NS_ONE_LAUNCH
+    torch = _torch()
+    base = _matrix("gauss", rows, cols, 8)
+    ref = R.orthogonalize(base.astype(np.float64))
+    tol = _ns_tol(rows * cols) if not tiled or rows * cols >= 100 else 2.0 ** -4 + 2.0 ** -8    # a few elements on 16-bit products
+    old = code_path_switch(SWITCH_NS_ONE_LAUNCH, 0 if tiled else 1)
+    try:
+        for s in (1e-25, 1e-6, 1e6, 1e30, 1e37):
+            assert rel_l2(_orth(_dev((base.astype(np.float64) * s).astype(np.float32)), 0), ref) < tol, s
+        assert not _orth(torch.zeros(rows, cols, device="cuda"), 0).any()
+        assert not _orth(torch.zeros(rows, cols, device="cuda", dtype=torch.bfloat16), 1).any()
+        for bad in (NAN, INF, -INF):
+            g = _dev(base)
+            g[rows - 1, cols - 1] = bad
+            assert np.isnan(_orth(g, 0)).all()
+            g = _dev(base).bfloat16()
+            g[0, cols // 2] = bad
+            assert np.isnan(_orth(g, 1)).all()
+    finally:
+        code_path_switch(SWITCH_NS_ONE_LAUNCH, old)
