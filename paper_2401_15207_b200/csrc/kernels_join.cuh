@@ -215,7 +215,10 @@ template <int NC, bool ONE> constexpr int join_rows = NC == 1 && ONE ? 2 : 1;
 template <typename P> constexpr int join_bytes = 2 * 32 + 2 * 8 * (int)sizeof(P);
 
 // Two columns.  Packed: one instruction for both, in the LayerNorm variants, which are short of issue slots (main kernel at 16384 x 2048:
-// 155 -> 122 us, at 16384 x 4096 310 -> 293); the RMSNorm ones, nearer to the memory's rate, run faster on single registers (204 against 218 us).
+// 155 -> 122 us, at 16384 x 4096 310 -> 293; whole gradient at 8192 x 8192 with a gate per row 655 -> 569); the RMSNorm ones, nearer to the
+// memory's rate, run faster on single registers (204 against 218 us).  So do bf16 LayerNorm rows beyond 8192 columns (NC = 4), where pairs
+// spill more than they save (4096 x 16384: 542 -> 535 us, with a gate per row 1079 -> 959); in fp32 pairs stay ahead there (706 -> 696, 1174 -> 1161).
+template <typename P, int KIND, int NC> constexpr bool kJoinPacked = KIND == 0 && (NC <= 2 || sizeof(P) == 4);
 template <bool PACKED> struct JoinPair;
 template <> struct JoinPair<true> {
   using T = uint64_t;
@@ -249,7 +252,7 @@ template <> struct JoinPair<false> {
 //   - two rows at a time (R = 2, for NC = 1 and one gate), so that their sums share barriers and their work interleaves.
 template <typename P, int KIND, int NC, bool STAGED, bool ONE>
 __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
-  using Q = JoinPair<KIND == 0>;
+  using Q = JoinPair<kJoinPacked<P, KIND, NC>>;
   using V = typename Q::T;
   constexpr int BYTES = join_bytes<P>;
   constexpr bool LN = KIND == 0, HOLD = NC == 1;
