@@ -202,11 +202,9 @@ __device__ __forceinline__ void cp_async4cols(float* dst, const float* src) { cp
 __device__ __forceinline__ void cp_async4cols(bf16* dst, const bf16* src) { cp_async8(dst, src); }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// at most n of this thread's newest groups still under way
+// at most n (0 or 1: no more than two stages) of this thread's newest groups still under way
 __device__ __forceinline__ void cp_async_wait_upto(int n) {
-  if (n >= 3) cp_async_wait<3>();
-  else if (n == 2) cp_async_wait<2>();
-  else if (n == 1) cp_async_wait<1>();
+  if (n > 0) cp_async_wait<1>();
   else cp_async_wait<0>();
 }
 // rows a block works on at a time
@@ -381,7 +379,6 @@ __global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
       dq[i] = LN ? Q::fma(g[i], S1[k][i], Q::mul(b[i], S0[LN ? k : 0][i])) : Q::mul(g[i], S1[k][i]);
     }
   };
-  // gains (with one gate: its product with the first) in registers; join_ld leaves zeros in columns that do not exist
   // gains and gate as the operand type, in registers (kept as fp32, gate times gain1 at once: 210 instead of 204 us at 16384 x 4096, RMSNorm)
   P hg2[HOLD ? 8 : 1], hg1[HOLD ? 8 : 1], hq[HOLD && ONE ? 8 : 1];
   if (HOLD) {
