@@ -111,8 +111,9 @@ __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
 // The issuing warp runs its loop as a whole and only `lead` (one lane) issues, so that descriptors, addresses and loop state are
-// uniform over the warp: 18.7 -> 17.0 us for a 5120 x 1280 x 1280 product, 148 -> 141 us for an orthogonalisation at 768 x 768, against
-// the loop inside `if (lane == 0)`.
+// uniform over the warp.  Against the loop inside `if (lane == 0)`: forward products (4096 x 1280 x 5120) 54 -> 46 us, dX
+// (4096 x 5120 x 1280) 53.8 -> 52.6, orthogonalisation at 768 x 768 148 -> 141 us; but dW, both of whose operands are MN-major,
+// 46.9 -> 48.3 us at 4096 x 3840 x 1280: it keeps the loop of one thread.
 __device__ __forceinline__ void tc_commit_lead(uint32_t bar, uint32_t lead) {
   asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
                "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(lead) : "memory");
@@ -673,7 +674,9 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int num_kb = (K + BK - 1) / BK;
-  // NS: `split` CTAs of a cluster share a tile, each takes its part of the k-blocks (one tile per cluster then)
+  // NS: `split` CTAs of a cluster share a tile, each takes its part of the k-blocks (one tile per cluster then).  The other instances name
+  // blockIdx.x and gridDim.x in their loops: out of variables the linear layers' dW and dX ran 6 to 13 % slower (4096 x 3840 x 1280
+  // dW 47.0 -> 53.4 us, dX 41.6 -> 46.9), whatever the compiler makes of it.
   const int Z = NS == 1 ? ns.split : 1, zr = Z > 1 ? (int)cluster_ctarank() : 0;
   const int kb0 = num_kb * zr / Z, kb1 = num_kb * (zr + 1) / Z, tile0 = blockIdx.x / Z, tile_step = gridDim.x / Z;
 
@@ -703,7 +706,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       int s = 0;
       uint32_t ph = 0;                   // ring position and its phase, advanced without divisions
       bool ok = true;
-      for (int tile = tile0; tile < num_tiles && ok; tile += tile_step) {
+      for (int tile = NS == 1 ? tile0 : blockIdx.x; tile < num_tiles && ok; tile += NS == 1 ? tile_step : gridDim.x) {
         const int m0 = tm_of(tile) * BM, n0 = tn_of(tile) * BN;
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_wait(empty_bar(s), ph ^ 1)) { atomicCAS(&g_tc_error, 0, 1); ok = false; break; }
@@ -731,9 +734,14 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       }
     }
   } else if (warp == 1) {
-    // ---------------- MMA issuer (one lane of a converged warp)
-    if (!poisoned) {
-      const uint32_t lead = lane == 0;
+    // ---------------- MMA issuer: one lane of a converged warp, or one thread
+    constexpr bool WARP = NS != 0 || !A_MN;
+    const uint32_t lead = lane == 0;
+    if (WARP ? !__any_sync(0xffffffffu, poisoned) : lead && !poisoned) {
+      auto wait = [&](uint32_t bar, uint32_t phase) {
+        const bool done = mbar_wait(bar, phase);
+        return WARP ? (bool)__all_sync(0xffffffffu, done) : done;
+      };
       // instruction descriptor: D fp32 (bits 4-5 = 1), A and B bf16 (bits 7-9, 10-12 = 1),
       // A / B major-ness (bits 15, 16: 1 = MN-major), N/8 at bits 17-22, M/16 at bits 24-28
       // (NS: both fp16, 0)
@@ -742,15 +750,15 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
       int s = 0, lt = 0;
       uint32_t ph = 0;
       bool ok = true;
-      for (int tile = tile0; tile < num_tiles && ok; tile += tile_step, ++lt) {
+      for (int tile = NS == 1 ? tile0 : blockIdx.x; tile < num_tiles && ok; tile += NS == 1 ? tile_step : gridDim.x, ++lt) {
         const int ab = lt & 1;
         const uint32_t aph = (lt >> 1) & 1;
         // the epilogue must have drained this accumulator (passes at once on its first use)
-        if (!__all_sync(0xffffffffu, mbar_wait(acc_empty(ab), aph ^ 1))) { if (lead) atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
+        if (!wait(acc_empty(ab), aph ^ 1)) { if (lead) atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
         tc_fence_after();
         const uint32_t tacc = tmem_base + (uint32_t)(ab * kAccStride);
         for (int kb = kb0; kb < kb1; ++kb) {
-          if (!__all_sync(0xffffffffu, mbar_wait(full_bar(s), ph))) { if (lead) atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
+          if (!wait(full_bar(s), ph)) { if (lead) atomicCAS(&g_tc_error, 0, 2); ok = false; break; }
           tc_fence_after();
           const uint32_t sa = base + s * kStageBytes, sb = sa + kABytes;
           const uint64_t da = make_desc(sa, A_MN), db = make_desc(sb, B_MN);
@@ -760,12 +768,15 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
             // 16 k-rows of 128 B (MN-major); descriptor addresses are in 16-byte units
             const uint64_t adv_a = A_MN ? (uint64_t)(kk * UMMA_K * 128 >> 4) : (uint64_t)(kk * UMMA_K * 2 >> 4);
             const uint64_t adv_b = B_MN ? (uint64_t)(kk * UMMA_K * 128 >> 4) : (uint64_t)(kk * UMMA_K * 2 >> 4);
-            tc_mma_lead(tacc, da + adv_a, db + adv_b, idesc, (kb > kb0 || kk > 0) ? 1u : 0u, lead);
+            if constexpr (WARP) tc_mma_lead(tacc, da + adv_a, db + adv_b, idesc, (kb > kb0 || kk > 0) ? 1u : 0u, lead);
+            else tc_mma(tacc, da + adv_a, db + adv_b, idesc, (kb > kb0 || kk > 0) ? 1u : 0u);
           }
-          tc_commit_lead(empty_bar(s), lead);       // frees the stage once these MMAs have read it
+          if constexpr (WARP) tc_commit_lead(empty_bar(s), lead);       // frees the stage once these MMAs have read it
+          else tc_commit(empty_bar(s));
           if (++s == S) { s = 0; ph ^= 1; }
         }
-        tc_commit_lead(acc_full(ab), lead);         // accumulator complete (or abandoned: g_tc_error tells the epilogue)
+        if constexpr (WARP) tc_commit_lead(acc_full(ab), lead);         // accumulator complete (or abandoned: g_tc_error tells the epilogue)
+        else tc_commit(acc_full(ab));
       }
     }
   } else {
@@ -773,7 +784,7 @@ gemm_tc_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constant
     const int q = warp & 3;
     uint8_t* stage = smem_gen + S * kStageBytes + 256 + (warp - 2) * kStoreStage;   // behind the barriers
     int lt = 0;
-    for (int tile = tile0; tile < num_tiles && !poisoned; tile += tile_step, ++lt) {
+    for (int tile = NS == 1 ? tile0 : blockIdx.x; tile < num_tiles && !poisoned; tile += NS == 1 ? tile_step : gridDim.x, ++lt) {
       const int ab = lt & 1;
       const uint32_t aph = (lt >> 1) & 1;
       auto wait_acc = [&]() {
