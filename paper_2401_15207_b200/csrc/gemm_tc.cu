@@ -895,7 +895,8 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
   // both CTAs of a pair read the same flag value only by luck, so decide nothing on it before the
   // pair has synchronised once; an early exit of one CTA alone would strand its peer
   // NS: `split` pairs of a cluster share a tile, each takes its part of the k-blocks (one tile per cluster then)
-  const uint32_t crank = cluster_ctarank(), rank = crank & 1, lead_rank = crank & ~1u;
+  // (a cluster of the others is the pair: the lead's rank is a constant there, 1-2 % of a forward product at 4096 x 3840 x 1280)
+  const uint32_t crank = cluster_ctarank(), rank = NS == 1 ? crank & 1 : crank, lead_rank = NS == 1 ? crank & ~1u : 0u;
   const int Z = NS == 1 ? ns.split : 1, zr = (int)(crank >> 1);
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t bar_base = base + S * kStage2Bytes;
