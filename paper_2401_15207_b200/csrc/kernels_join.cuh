@@ -248,8 +248,10 @@ template <> struct JoinPair<false> {
 //   - gains and gate stay in registers where they fit (NC = 1): beside the staging buffers little L1 is left to re-read them
 //     from (286 us).
 //   - two rows at a time (R = 2, for NC = 1 and one gate), so that their sums share barriers and their work interleaves.
+// The RMSNorm variants with one gate are given all 128 registers: left to itself the compiler may settle for 100 and order loads behind
+// sums (254 instead of 205 us at 16384 x 4096).  The LayerNorm ones lose by it (16384 x 2048: 135 -> 157 us).
 template <typename P, int KIND, int NC, bool STAGED, bool ONE>
-__global__ void __launch_bounds__(512) join_bwd_kernel(JoinBwd p) {
+__global__ void __launch_bounds__(512, KIND == 1 && ONE ? 1 : 0) join_bwd_kernel(JoinBwd p) {
   using Q = JoinPair<kJoinPacked<P, KIND, NC>>;
   using V = typename Q::T;
   constexpr int BYTES = join_bytes<P>;
