@@ -111,6 +111,7 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
     for (int i = 0; i < 32; ++i) f[i] = turn[lane * 32 + (lane ^ i)];
     __syncwarp();
   };
+  const int raised = tid == 0 ? *(volatile int*)&g_tc_error : 0;      // of an earlier launch
   double s = 0.0;
 #pragma unroll 1
   for (int k = 0; k < NH; ++k) {
@@ -145,6 +146,8 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
   }
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if (lane == 0) red[warp] = s;
+  int* const raised_s = reinterpret_cast<int*>(red + 16);
+  if (tid == 0) *raised_s = raised;
   cluster_sync_all();                                  // and every CTA of the cluster has started
   if (tid < (int)C) {                                  // this CTA's sum to all
     double t = 0.0;
@@ -331,14 +334,12 @@ __global__ void __launch_bounds__(kSmThreads, 1) ns_small_kernel(NsSmallArgs a) 
     }
     fence_proxy_async_all();
   }
-  // ---- the result, unless a product gave up on a wait: here, in another CTA of the cluster, or before this launch.  Every CTA sends its
-  // reading of the flag round, so that all decide alike and no matrix is half updated.
+  // ---- the result, unless a product gave up on a wait: here, in another CTA of the cluster, or before this launch.  Every CTA sends what it
+  // knows round, so that all decide alike and no matrix is half updated.
   const int gave_up = __syncthreads_or(!ok);
-  if (warp == 0) {
-    const int raised = __shfl_sync(0xffffffffu, lane == 0 ? *(volatile int*)&g_tc_error : 0, 0) | gave_up;
-    if (lane < (int)C) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(ns_peer(nrm_s + 4 * me, lane)), "r"(raised) : "memory");   // (the norm has been read)
-    __syncwarp();
-  }
+  if (tid < (int)C)                                    // (the norm's slots have been read)
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(ns_peer(nrm_s + 4 * me, tid)), "r"(*raised_s | gave_up) : "memory");
+  __syncwarp();
   cluster_sync_all();
   int hold = 0;
   for (int w = 0; w < (int)C; ++w) hold |= reinterpret_cast<const int*>(nrm)[w];
