@@ -89,12 +89,13 @@ __global__ void __launch_bounds__(256) ns_sumsq_kernel(const T* g, float* mom, i
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) ns_start_kernel(const T* g, const float* mom, int rows, int cols, float mu, int nesterov,
                                                        const double* part, int nparts, int prows, int pcols, float* x32,
-                                                       __half* x16) {
+                                                       __half* x16, int* verdict) {
   __shared__ double sh[8];
   __shared__ float s_inv;
   const int tid = threadIdx.y * blockDim.x + threadIdx.x;
   double s = 0.0;
   pdl_wait_prior();
+  if (blockIdx.x == 0 && tid == 0) *verdict = 0;        // for ns_finish_kernel
   for (int i = tid; i < nparts; i += 256) s += part[i];
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((tid & 31) == 0) sh[tid >> 5] = s;
@@ -129,13 +130,20 @@ __global__ void __launch_bounds__(256) ns_start_kernel(const T* g, const float* 
   }
   pdl_launch_next();
 }
-// The result out of the padded scratch: o in bf16, or the update of the master.  Writes nothing after a product gave up on a wait.
+// The result out of the padded scratch: o in bf16, or the update of the master.  Writes nothing after a product gave up on a wait: the first
+// block to come reads the flag for all, since another stream's products may raise it while this kernel runs, and no matrix is to be half updated.
 template <bool VEC>
 __global__ void __launch_bounds__(256) ns_finish_kernel(const float* x, int rows, int cols, int pcols, bf16* o,
                                                         float* master, bf16* param, float decay, float size,
-                                                        const int* tc_error) {
+                                                        const int* tc_error, int* verdict) {
+  __shared__ int go;
   pdl_wait_prior();
-  if (tc_error != nullptr && *tc_error != 0) return;
+  if (threadIdx.x == 0 && threadIdx.y == 0) {
+    const int mine = *(const volatile int*)tc_error != 0 ? 2 : 1, first = atomicCAS(verdict, 0, mine);
+    go = (first == 0 ? mine : first) == 1;
+  }
+  __syncthreads();
+  if (!go) return;
   for (int r = blockIdx.x * blockDim.y + threadIdx.y; r < rows; r += gridDim.x * blockDim.y) {
     const size_t off = (size_t)r * cols;
 #pragma unroll 2
@@ -156,10 +164,10 @@ __global__ void __launch_bounds__(256) ns_finish_kernel(const float* x, int rows
 }
 
 inline int ns_pad(int64_t n) { return n < 128 ? 128 : (int)((n + 63) / 64 * 64); }
-// scratch: partial sums | x32 | x16 twice | e | f | da | df, each a multiple of 256 bytes
+// scratch: partial sums, the verdict on the result behind them | x32 | x16 twice | e | f | da | df, each a multiple of 256 bytes
 inline size_t ns_scratch_bytes(int64_t rows, int64_t cols) {
   const size_t r = ns_pad(rows), c = ns_pad(cols), s = r < c ? r : c;
-  return ((size_t)kNsParts * 8 + 255) / 256 * 256 + r * c * 8 + s * s * 4 + 2 * ((s * 4 + 255) / 256 * 256);
+  return ((size_t)kNsParts * 8 + 8 + 255) / 256 * 256 + r * c * 8 + s * s * 4 + 2 * ((s * 4 + 255) / 256 * 256);
 }
 struct NsUpdate { bf16* o; float* master; bf16* param; float decay, size; };   // where the result goes: o, or master (and param)
 
@@ -173,7 +181,8 @@ inline cudaError_t launch_orthogonalize(cudaStream_t st, int64_t rows, int64_t c
   const int pr = ns_pad(rows), pc = ns_pad(cols), s = pr < pc ? pr : pc;
   char* w = (char*)scratch;
   auto take = [&](size_t bytes) { char* p = w; w += (bytes + 255) / 256 * 256; return p; };
-  double* part = (double*)take(kNsParts * 8);
+  double* part = (double*)take(kNsParts * 8 + 8);
+  int* verdict = (int*)(part + kNsParts);
   NsBuffers b;
   b.rows = pr; b.cols = pc;
   b.x32 = (float*)take((size_t)pr * pc * 4);
@@ -194,13 +203,13 @@ inline cudaError_t launch_orthogonalize(cudaStream_t st, int64_t rows, int64_t c
   const int R = (int)rows, C = (int)cols;
   cudaError_t e = launch_pdl(vec ? ns_sumsq_kernel<T, true> : ns_sumsq_kernel<T, false>, grid, block, 0, st, g, mom, R, C, mu, nesterov, part);
   if (e != cudaSuccess) return e;
-  e = vec ? launch_pdl(ns_start_kernel<T, true>, pgrid, block, 0, st, g, (const float*)mom, R, C, mu, nesterov, (const double*)part, (int)grid.x, pr, pc, b.x32, (__half*)b.x16[0])
-          : launch_pdl(ns_start_kernel<T, false>, pgrid, block, 0, st, g, (const float*)mom, R, C, mu, nesterov, (const double*)part, (int)grid.x, pr, pc, b.x32, (__half*)b.x16[0]);
+  e = vec ? launch_pdl(ns_start_kernel<T, true>, pgrid, block, 0, st, g, (const float*)mom, R, C, mu, nesterov, (const double*)part, (int)grid.x, pr, pc, b.x32, (__half*)b.x16[0], verdict)
+          : launch_pdl(ns_start_kernel<T, false>, pgrid, block, 0, st, g, (const float*)mom, R, C, mu, nesterov, (const double*)part, (int)grid.x, pr, pc, b.x32, (__half*)b.x16[0], verdict);
   if (e != cudaSuccess) return e;
   e = ns_products_launch(st, b, steps);
   if (e != cudaSuccess) return e;
-  return vec ? launch_pdl(ns_finish_kernel<true>, grid, block, 0, st, (const float*)b.x32, R, C, pc, to.o, to.master, to.param, to.decay, to.size, flag)
-             : launch_pdl(ns_finish_kernel<false>, grid, block, 0, st, (const float*)b.x32, R, C, pc, to.o, to.master, to.param, to.decay, to.size, flag);
+  return vec ? launch_pdl(ns_finish_kernel<true>, grid, block, 0, st, (const float*)b.x32, R, C, pc, to.o, to.master, to.param, to.decay, to.size, flag, verdict)
+             : launch_pdl(ns_finish_kernel<false>, grid, block, 0, st, (const float*)b.x32, R, C, pc, to.o, to.master, to.param, to.decay, to.size, flag, verdict);
 }
 
 }  // namespace hift
