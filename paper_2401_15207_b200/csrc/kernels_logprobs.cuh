@@ -145,7 +145,7 @@ struct LpArgs {
   const int32_t* tokens;
   int vocab, n_top;
   int64_t ld, rows;
-  float scale;
+  float scale, scale2;                    // 1 / T and log2(e) / T, each rounded once
   float *logp, *entropy, *stats, *top_logp;
   int32_t *top_ids, *bad;
 };
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const T* log
   const int per = (rw.nv + (int)parts - 1) / (int)parts;
   const int v0 = min(rw.nv, per * (int)part), v1 = min(rw.nv, v0 + per);
   const int ns = part == 0 ? rw.ns : 0;   // the single elements go to the first block's first threads
-  const float s2 = a.scale * kLog2E;
+  const float s2 = a.scale2;
 
   // ---- one pass: maximum, sum of e, sum of e log2 e (bounded, unlike e (x - m)), all relative to the thread's running maximum
   float tmax = -INFINITY, m = kLowest;

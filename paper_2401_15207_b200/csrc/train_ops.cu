@@ -21,10 +21,11 @@ hift_status status_of(cudaError_t e) {
 }
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-hift_status logprobs_cfg(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, double temperature, float* scale) {
+hift_status logprobs_cfg(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, double temperature, float* scale, float* scale2) {
   if (dtype < 0 || dtype > 1 || rows < 0 || rows > INT32_MAX || vocab < 1 || ld < vocab || ld > INT32_MAX - 65536) return HIFT_ERR_CFG;
   *scale = (float)(1.0 / temperature);
-  if (!(temperature > 0.0) || !isfinite(temperature) || !isnormal(*scale) || !isfinite(*scale * kLog2E)) return HIFT_ERR_CFG;
+  *scale2 = (float)(1.4426950408889634 / temperature);     // (from the rounded 1 / T: up to 1e-7 off, times |z - z_max| in every exponential)
+  if (!(temperature > 0.0) || !isfinite(temperature) || !isnormal(*scale) || !isfinite(*scale2)) return HIFT_ERR_CFG;
   return HIFT_OK;
 }
 
@@ -113,15 +114,15 @@ extern "C" {
 hift_status hift_k_token_logprobs(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void* logits, const int32_t* tokens,
                                   double temperature, int32_t n_top, float* logp, float* entropy, float* stats, int32_t* top_ids,
                                   float* top_logp, int32_t* bad, void* stream) {
-  float scale;
-  const hift_status s = logprobs_cfg(dtype, rows, vocab, ld, temperature, &scale);
+  float scale, scale2;
+  const hift_status s = logprobs_cfg(dtype, rows, vocab, ld, temperature, &scale, &scale2);
   if (s != HIFT_OK) return s;
   if (n_top < 0) return HIFT_ERR_CFG;
   if (n_top > HIFT_MAX_TOP) return HIFT_ERR_CAPACITY;
   if (rows == 0) return HIFT_OK;
   if (!logits || !tokens || !logp || (n_top > 0 && (!top_ids || !top_logp))) return HIFT_ERR_INPUT;
   if (!aligned(logits, dtype == 0 ? 4 : 2)) return HIFT_ERR_CFG;
-  const LpArgs a{tokens, (int)vocab, n_top, ld, rows, scale, logp, entropy, stats, top_logp, top_ids, bad};
+  const LpArgs a{tokens, (int)vocab, n_top, ld, rows, scale, scale2, logp, entropy, stats, top_logp, top_ids, bad};
   const cudaError_t e = dtype == 0 ? launch_token_logprobs((cudaStream_t)stream, (const float*)logits, a)
                                    : launch_token_logprobs((cudaStream_t)stream, (const bf16*)logits, a);
   return status_of(e);
@@ -130,8 +131,8 @@ hift_status hift_k_token_logprobs(int32_t dtype, int64_t rows, int64_t vocab, in
 hift_status hift_k_token_logprobs_bwd(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, const void* logits, const int32_t* tokens,
                                       double temperature, const float* stats, const float* entropy, const float* dlogp,
                                       const float* dentropy, void* dlogits, void* stream) {
-  float scale;
-  const hift_status s = logprobs_cfg(dtype, rows, vocab, ld, temperature, &scale);
+  float scale, scale2;
+  const hift_status s = logprobs_cfg(dtype, rows, vocab, ld, temperature, &scale, &scale2);
   if (s != HIFT_OK) return s;
   if (rows == 0) return HIFT_OK;
   if (!logits || !tokens || !stats || !dlogits || (!dlogp && !dentropy) || (dentropy && !entropy)) return HIFT_ERR_INPUT;
