@@ -164,7 +164,7 @@ hift_status hift_k_join_fwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
 }
 
 size_t hift_join_bwd_scratch_bytes(int64_t rows, int64_t cols, int64_t rows_per_gate) {
-  if (rows < 1 || cols < 1 || rows > INT32_MAX || cols > kJoinMaxCols) return 0;
+  if (rows < 1 || cols < 8 || cols % 8 || rows > INT32_MAX || cols > kJoinMaxCols) return 0;
   return (size_t)join_plan(rows, cols, rows_per_gate).ctas * cols * kJoinPlanes * sizeof(float);
 }
 

@@ -189,3 +189,10 @@ def test_orthogonalisation_takes_eight_steps_at_most(L, steps, want):
     (INPUT: the scratch buffer is missing, which is looked at after the steps.)"""
     assert L.hift_k_orthogonalize(0, 4, 64, P, P, steps, None, 1 << 30, None) == want
     assert L.hift_muon_step(4, 64, P, P, P, P, None, 1 << 30, 1e-3, 0.95, 1, 0.0, steps, None) == want
+
+
+@pytest.mark.parametrize("cols", [1, 4, 12, 4095])
+def test_join_scratch_of_columns_that_are_refused(L, cols):
+    """Columns that are no multiple of 8 have no size either."""
+    assert L.hift_join_bwd_scratch_bytes(100, cols, 100) == 0
+    assert L.hift_join_bwd_scratch_bytes(100, 8, 100) > 0
