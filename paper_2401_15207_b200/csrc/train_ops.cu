@@ -20,6 +20,7 @@ hift_status status_of(cudaError_t e) {
   return HIFT_ERR_CUDA;
 }
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+template <typename... Ptr> bool words(const Ptr*... p) { return (aligned(p, 4) && ...); }       // buffers of fp32 or int32
 
 hift_status logprobs_cfg(int32_t dtype, int64_t rows, int64_t vocab, int64_t ld, double temperature, float* scale, float* scale2) {
   if (dtype < 0 || dtype > 1 || rows < 0 || rows > INT32_MAX || vocab < 1 || ld < vocab || ld > INT32_MAX - 65536) return HIFT_ERR_CFG;
@@ -121,7 +122,7 @@ hift_status hift_k_token_logprobs(int32_t dtype, int64_t rows, int64_t vocab, in
   if (n_top > HIFT_MAX_TOP) return HIFT_ERR_CAPACITY;
   if (rows == 0) return HIFT_OK;
   if (!logits || !tokens || !logp || (n_top > 0 && (!top_ids || !top_logp))) return HIFT_ERR_INPUT;
-  if (!aligned(logits, dtype == 0 ? 4 : 2)) return HIFT_ERR_CFG;
+  if (!aligned(logits, dtype == 0 ? 4 : 2) || !words(tokens, logp, entropy, stats, top_ids, top_logp, bad)) return HIFT_ERR_CFG;
   const LpArgs a{tokens, (int)vocab, n_top, ld, rows, scale, scale2, logp, entropy, stats, top_logp, top_ids, bad};
   const cudaError_t e = dtype == 0 ? launch_token_logprobs((cudaStream_t)stream, (const float*)logits, a)
                                    : launch_token_logprobs((cudaStream_t)stream, (const bf16*)logits, a);
@@ -136,7 +137,7 @@ hift_status hift_k_token_logprobs_bwd(int32_t dtype, int64_t rows, int64_t vocab
   if (s != HIFT_OK) return s;
   if (rows == 0) return HIFT_OK;
   if (!logits || !tokens || !stats || !dlogits || (!dlogp && !dentropy) || (dentropy && !entropy)) return HIFT_ERR_INPUT;
-  if (!aligned(logits, dtype == 0 ? 4 : 2) || !aligned(dlogits, dtype == 0 ? 4 : 2)) return HIFT_ERR_CFG;
+  if (!aligned(logits, dtype == 0 ? 4 : 2) || !aligned(dlogits, dtype == 0 ? 4 : 2) || !words(tokens, stats, entropy, dlogp, dentropy)) return HIFT_ERR_CFG;
   const LpBwdArgs a{tokens, (int)vocab, 0, ld, rows, scale, stats, entropy, dlogp, dentropy};
   const cudaError_t e = dtype == 0 ? launch_token_logprobs_bwd((cudaStream_t)stream, (const float*)logits, (float*)dlogits, a)
                                    : launch_token_logprobs_bwd((cudaStream_t)stream, (const bf16*)logits, (bf16*)dlogits, a);
@@ -152,7 +153,7 @@ hift_status hift_k_join_fwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
   if (rows == 0) return HIFT_OK;
   if (!x || !h || !x_out || !stats || (gain2 && !y) || (kind == 0 && ((gain1 && !bias1) || (gain2 && !bias2)))) return HIFT_ERR_INPUT;
   if (!aligned(x, 16) || !aligned(h, 16) || !aligned(x_out, 16) || !aligned(gain1, 16) || !aligned(bias1, 16) || !aligned(gate, 16) ||
-      !aligned(gain2, 16) || !aligned(bias2, 16) || (gain2 && !aligned(y, 16))) return HIFT_ERR_CFG;
+      !aligned(gain2, 16) || !aligned(bias2, 16) || (gain2 && !aligned(y, 16)) || !words(stats)) return HIFT_ERR_CFG;
   JoinFwd p{x, h, gain1, bias1, gate, gain2, bias2, x_out, y, stats, rows, gate ? rows_per_gate : rows, (int)cols, (float)eps, (float)res_scale};
   int th, nc;
   // up to 4096 columns 8 warps of 16 columns a thread: 123 us at 16384 x 4096 bf16, the copy rate; 16 warps of 8 columns: 138
@@ -175,6 +176,7 @@ hift_status hift_k_join_bwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
                             size_t scratch_bytes, void* stream) {
   const hift_status s = join_cfg(dtype, kind, rows, cols, res_scale, gate, rows_per_gate);
   if (s != HIFT_OK) return s;
+  if (!words(stats, dgain1, dbias1, dgain2, dbias2)) return HIFT_ERR_CFG;
   cudaStream_t st = (cudaStream_t)stream;
   if (rows == 0) {                                         // no rows: the sums over them are zero
     for (float* q : {dgain1, dbias1, dgain2, dbias2})

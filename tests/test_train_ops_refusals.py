@@ -196,3 +196,26 @@ def test_join_scratch_of_columns_that_are_refused(L, cols):
     """Columns that are no multiple of 8 have no size either."""
     assert L.hift_join_bwd_scratch_bytes(100, cols, 100) == 0
     assert L.hift_join_bwd_scratch_bytes(100, 8, 100) > 0
+
+
+@pytest.mark.parametrize("name", ["tokens", "logp", "ent", "stats", "ids", "vals", "bad"])
+def test_token_logprobs_refuses_displaced_buffers(L, name):
+    """A buffer that does not start where its elements may is refused, not read."""
+    assert _logp(L, **{name: P + 2}) == CFG
+
+
+@pytest.mark.parametrize("name", ["tokens", "stats", "ent", "g", "h"])
+def test_token_logprobs_bwd_refuses_displaced_buffers(L, name):
+    a = dict(tokens=P, stats=P, ent=P, g=P, h=P)
+    a[name] = P + 1
+    assert L.hift_k_token_logprobs_bwd(1, 4, 100, 100, P, a["tokens"], 1.0, a["stats"], a["ent"], a["g"], a["h"], P, None) == CFG
+
+
+def test_join_refuses_displaced_statistics_and_sums(L):
+    assert L.hift_k_join_fwd(1, 0, 4, 64, 1e-5, 1.0, P, P, P, P, P, 2, P, P, P, P, P + 2, None) == CFG
+    names = ("stats", "dg1", "db1", "dg2", "db2")
+    for name in names:
+        a = {n: P + 2 if n == name else P for n in names}
+        assert L.hift_k_join_bwd(1, 0, 4, 64, 1.0, P, P, P, P, a["stats"], P, P, P, 2, P, P, P, a["dg1"], a["db1"], P, a["dg2"], a["db2"], P,
+                                 1 << 30, None) == CFG, name
+    assert L.hift_k_join_bwd(1, 0, 0, 64, 1.0, P, P, P, P, P, P, P, P, 2, P, P, P, P + 2, P, P, P, P, P, 1 << 30, None) == CFG
