@@ -518,7 +518,8 @@ hift_status hift_k_cross_entropy(int32_t dtype, int64_t rows, int64_t vocab, int
  * launch on `cuda_stream` (on the device that is current, whose buffers they are given), do not synchronise and do
  * not allocate.  They can be captured into a CUDA graph; the first call of an operator on a device sets its kernels up
  * and is made before any capture.  Calls that overlap on the GPU need scratch buffers of their own.  Inputs and outputs
- * must not overlap except where it is said.  A call that is refused launches nothing. */
+ * must not overlap except where it is said.  A call that is refused launches nothing: HIFT_ERR_CFG also for a buffer that
+ * does not start where its elements may, and for factors that are beyond fp32. */
 
 /* Log-probabilities of given tokens under rows of logits[rows, ld] (columns >= vocab are padding and not read):
  *     z = x / temperature,  log p = z - log sum exp z,  logp_dev[r] = log p[tokens_dev[r]],

@@ -40,7 +40,7 @@ void join_shape(int64_t cols, int most, int* threads, int* chunks) {
 }
 hift_status join_cfg(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, double res_scale, const void* gate, int64_t rows_per_gate) {
   if (dtype < 0 || dtype > 1 || kind < 0 || kind > 1 || rows < 0 || rows > INT32_MAX || cols < 8 || cols % 8) return HIFT_ERR_CFG;
-  if (!isfinite(res_scale) || (gate && rows_per_gate < 1)) return HIFT_ERR_CFG;
+  if (!isfinite((float)res_scale) || (gate && rows_per_gate < 1)) return HIFT_ERR_CFG;
   return cols > kJoinMaxCols ? HIFT_ERR_CAPACITY : HIFT_OK;
 }
 
@@ -149,7 +149,7 @@ hift_status hift_k_join_fwd(int32_t dtype, int32_t kind, int64_t rows, int64_t c
                             const void* gain2, const void* bias2, float* x_out, void* y, float* stats, void* stream) {
   const hift_status s = join_cfg(dtype, kind, rows, cols, res_scale, gate, rows_per_gate);
   if (s != HIFT_OK) return s;
-  if (!(eps >= 0.0) || !isfinite(eps)) return HIFT_ERR_CFG;
+  if (!(eps >= 0.0) || !isfinite((float)eps)) return HIFT_ERR_CFG;
   if (rows == 0) return HIFT_OK;
   if (!x || !h || !x_out || !stats || (gain2 && !y) || (kind == 0 && ((gain1 && !bias1) || (gain2 && !bias2)))) return HIFT_ERR_INPUT;
   if (!aligned(x, 16) || !aligned(h, 16) || !aligned(x_out, 16) || !aligned(gain1, 16) || !aligned(bias1, 16) || !aligned(gate, 16) ||
@@ -228,11 +228,11 @@ hift_status hift_muon_step(int64_t rows, int64_t cols, void* param_bf16, float* 
                            int32_t steps, void* stream) {
   const hift_status s = ns_cfg(rows, cols, steps, scratch, scratch_bytes);
   if (s != HIFT_OK) return s;
-  if (!isfinite(lr) || !isfinite(weight_decay) || !(momentum >= 0.0 && momentum < 1.0)) return HIFT_ERR_CFG;
+  const float decay = (float)(1.0 - lr * weight_decay), size = (float)(lr * 0.2 * sqrt((double)(rows > cols ? rows : cols)));
+  if (!isfinite(lr) || !isfinite(weight_decay) || !isfinite(decay) || !isfinite(size) || !(momentum >= 0.0 && momentum < 1.0)) return HIFT_ERR_CFG;
   if (!master || !grad || !momentum_buf) return HIFT_ERR_INPUT;
   if (!aligned(master, 4) || !aligned(grad, 4) || !aligned(momentum_buf, 4) || !aligned(param_bf16, 2)) return HIFT_ERR_CFG;
-  const double size = lr * 0.2 * sqrt((double)(rows > cols ? rows : cols));
-  const NsUpdate to{nullptr, master, (bf16*)param_bf16, (float)(1.0 - lr * weight_decay), (float)size};
+  const NsUpdate to{nullptr, master, (bf16*)param_bf16, decay, size};
   const cudaError_t e = launch_orthogonalize((cudaStream_t)stream, rows, cols, grad, momentum_buf, (float)momentum, nesterov != 0, steps, to, scratch);
   return status_of(e);
 }

@@ -219,3 +219,17 @@ def test_join_refuses_displaced_statistics_and_sums(L):
         assert L.hift_k_join_bwd(1, 0, 4, 64, 1.0, P, P, P, P, a["stats"], P, P, P, 2, P, P, P, a["dg1"], a["db1"], P, a["dg2"], a["db2"], P,
                                  1 << 30, None) == CFG, name
     assert L.hift_k_join_bwd(1, 0, 0, 64, 1.0, P, P, P, P, P, P, P, P, 2, P, P, P, P + 2, P, P, P, P, P, 1 << 30, None) == CFG
+
+
+def test_factors_beyond_fp32_are_refused(L):
+    """Finite numbers that the kernels' fp32 would hold as infinity: 0 times them would be NaN."""
+    def join(scale, eps):
+        return L.hift_k_join_fwd(1, 0, 4, 64, eps, scale, None, P, P, P, P, 2, P, P, P, P, P, None)
+    assert join(-3e38, 1e38) == INPUT                       # (x is missing, which is looked at later)
+    assert join(1e39, 1e-5) == CFG and join(-1e300, 1e-5) == CFG and join(1.0, 1e39) == CFG
+    assert L.hift_k_join_bwd(1, 0, 4, 64, 1e39, P, P, P, P, P, P, P, P, 2, P, P, P, P, P, P, P, P, P, 1 << 30, None) == CFG
+
+    def muon(lr, wd):
+        return L.hift_muon_step(4, 64, P, None, P, P, P, 1 << 30, lr, 0.95, 1, wd, 5, None)
+    assert muon(1e38, 0.0) == INPUT and muon(1e-3, 1e40) == INPUT
+    assert muon(1e39, 0.0) == CFG and muon(2.2e38, 0.0) == CFG and muon(1e-3, 1e42) == CFG and muon(1e200, 1e200) == CFG
