@@ -1,6 +1,6 @@
 // bf16 GEMM on the Blackwell tensor cores: tcgen05.mma with the accumulator in tensor memory,
 // operands staged in shared memory by TMA (no cluster multicast), an mbarrier ring between a
-// one-thread TMA producer, a one-thread MMA issuer and four epilogue warps.  The kernel is
+// one-thread TMA producer, an MMA issuer (one thread, or one lane of a converged warp) and four epilogue warps.  The kernel is
 // persistent (one CTA per SM) with two accumulators, so epilogues overlap the next tile's MMAs.
 //
 //   C[m,n] = sum_k A(m,k) * B(k,n) (+ bias[n]) (+ residual[m,n])

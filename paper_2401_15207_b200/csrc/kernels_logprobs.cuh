@@ -449,11 +449,12 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const T* log
 }
 
 // Threads of a block and blocks per row.  Small blocks: the end of a row (sums, alternatives) is a chain of short steps that other
-// rows' blocks on the same SM hide (4096 x 50257 bf16: 86 us with 256 threads, 78 with 128), down to 64 or 32 threads for short
+// rows' blocks on the same SM hide (4096 x 50257 bf16: 86 us with 256 threads, 78 with 128 on one box; 83 with 128 on others), down to 64 or 32 threads for short
 // rows, where that end is most of the work, as long as the SMs stay full (16384 x 4000: 74 us with 128, 58 with 64, 48 with 32; 16384 x
 // 16000: 125, 111, 120; but 4096 x 50257 with 64: 85); but enough threads in all, or loads in flight run short (512 x 128000:
 // 75 us with 128, 51 with 256; 2048 x 4000: 11 us with 128, 26 with 64).  While the rows alone still leave
-// SMs idle, up to eight blocks (a cluster) share a row, as long as each has two vectors a thread.
+// SMs idle, up to eight blocks (a cluster) share a row, as long as each has two vectors a thread.  148 SMs are assumed; on a device with another
+// number only the speed would change.
 inline void lp_shape(int64_t rows, int64_t vocab, int vec, int* threads, int* parts) {
   const int64_t nv = vocab / vec, fill = 148 * 1024;
   int th = 32;

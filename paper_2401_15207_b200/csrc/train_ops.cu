@@ -47,7 +47,8 @@ hift_status join_cfg(int32_t dtype, int32_t kind, int64_t rows, int64_t cols, do
 // Blocks of the backward kernel that an SM holds: its registers (128 a thread at most) and shared memory.
 constexpr size_t kJoinSmem = 208 * 1024;
 int join_ctas_per_sm(int th) { return th <= 64 ? 8 : 512 / th; }
-// how a backward call deals its rows out: the number of blocks, and whether a gate's rows are split over several
+// How a backward call deals its rows out: the number of blocks, and whether a gate's rows are split over several.  For 148 SMs whatever the
+// device: the scratch size, which follows from it, is asked for without one, and only the speed depends on it.
 struct JoinPlan { int ctas, split; int64_t gates_per_cta, rows_per_gate, n_gates; };
 JoinPlan join_plan(int64_t rows, int64_t cols, int64_t rows_per_gate) {
   int th, nc;
