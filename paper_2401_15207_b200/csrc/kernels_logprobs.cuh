@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const T* log
 }
 
 // Threads of a block and blocks per row.  Small blocks: the end of a row (sums, alternatives) is a chain of short steps that other
-// rows' blocks on the same SM hide (4096 x 50257 bf16: 86 us with 256 threads, 78 with 128 on one box; 83 with 128 on others), down to 64 or 32 threads for short
+// rows' blocks on the same SM hide (4096 x 50257 bf16: 86 us with 256 threads, 78 with 128 on one card, 83 on others), down to 64 or 32 threads for short
 // rows, where that end is most of the work, as long as the SMs stay full (16384 x 4000: 74 us with 128, 58 with 64, 48 with 32; 16384 x
 // 16000: 125, 111, 120; but 4096 x 50257 with 64: 85); but enough threads in all, or loads in flight run short (512 x 128000:
 // 75 us with 128, 51 with 256; 2048 x 4000: 11 us with 128, 26 with 64).  While the rows alone still leave
