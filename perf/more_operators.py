@@ -238,6 +238,11 @@ def _blocks(x, two):
     return torch.nn.functional.pad(x.view(-1, two, f), (0, -f % BLOCK)).unflatten(2, (-1, BLOCK))
 
 
+def _power(e):
+    """2 ** e as fp32, from its bits: pow() may be a rounding off, which breaks ties."""
+    return ((e.int() + 127) << 23).view(torch.float32)
+
+
 def _pack(x, two, form):
     """8-bit values and scale bytes: 2 ** (byte - 127) is the least power of two that brings a block into the range, 2 ** -110 at least."""
     b = _blocks(x.float(), two)
@@ -247,7 +252,7 @@ def _pack(x, two, form):
     head, shift = (0.875, 9) if form else (127.0 / 128.0, 7)  # most = head 2^shift
     e = torch.where(m > head, e - shift + 1, e - shift)
     e = torch.where(top == 0, -110, e).clamp(min=-110)
-    v = torch.ldexp(b, -e[..., None]).clamp(-most, most)
+    v = (b * _power(-e[..., None])).clamp(-most, most)
     q = v.to(torch.float8_e4m3fn) if form else v.round().to(torch.int8)
     return q.flatten(2)[..., : x.shape[1] // two].reshape(x.shape).contiguous(), (e + 127).to(torch.uint8).view(x.shape[0], -1)
 
@@ -255,8 +260,8 @@ def _pack(x, two, form):
 def _unpack(s, dt):
     two = 2 if s["kind"] == 2 else 1
     b = _blocks(s["q"].to(dt), two)
-    scale = torch.ldexp(torch.ones((), dtype=dt, device="cuda"), s["scales"].int().view(s["rows"], two, -1, 1) - 127)
-    return (b * scale).flatten(2)[..., : s["f"]]
+    scale = _power(s["scales"].int().view(s["rows"], two, -1, 1) - 127)
+    return (b * scale.to(dt)).flatten(2)[..., : s["f"]]
 
 
 def _act8_plain(s):
@@ -408,7 +413,7 @@ def _exact_unpacked(s):
     n, f = (2 if s["kind"] == 2 else 1), s["f"]
     col = torch.arange(n * f, device="cuda")
     byte = s["scales"][:, col // f * -(-f // BLOCK) + col % f // BLOCK]
-    return s["q"].double() * 2.0 ** (byte.double() - 127)
+    return s["q"].double() * ((byte.long() - 127 + 1023) << 52).view(torch.float64)
 
 
 def _exact_packed(x, f, form):
@@ -420,8 +425,11 @@ def _exact_packed(x, f, form):
     block = (col // f * top.shape[2] + col % f // BLOCK).expand(rows, -1)
     top = top.flatten(1).scatter_reduce_(1, block, x.abs(), "amax")
     m, e = torch.frexp(top / (448.0 if form else 127.0))
-    v = x / (2.0 ** torch.where(m == 0.5, e - 1, e).clamp(min=-110).double()).gather(1, block)
-    step = 2.0 ** (torch.frexp(v).exponent.clamp(min=-5).double() - 4) if form else 1.0
+    def power(k):                                             # its bits in 64
+        return ((k.long() + 1023) << 52).view(torch.float64)
+
+    v = x / power(torch.where(m == 0.5, e - 1, e).clamp(min=-110)).gather(1, block)
+    step = power(torch.frexp(v).exponent.clamp(min=-5) - 4) if form else 1.0
     return (v / step).round() * step
 
 
