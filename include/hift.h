@@ -610,6 +610,88 @@ hift_status hift_muon_step(int64_t rows, int64_t cols, void *param_bf16_dev, flo
                            float *momentum_dev, void *scratch_dev, size_t scratch_bytes, double lr, double momentum,
                            int32_t nesterov, double weight_decay, int32_t steps, void *cuda_stream);
 
+/* ---- operators of a transformer block beside the step ------------------------
+ * For blocks that the step's own architectures do not have, with the conventions of the operators above: caller-owned buffers, the stream
+ * and the current device given by the caller, no synchronisation, no allocation, capture into a CUDA graph after one first call on a
+ * device, scratch buffers of their own for calls that overlap.  Inputs and outputs must not overlap except where it is said. */
+
+/* Cosines and sines for rotary positions: cs_dev fp32 [n_pos, rot/2] cosines of pos * freq(j), then as many sines (what hift_k_linear_rope
+ * and hift_k_rope take).  Angles are formed in 64 bits.  With plain frequencies base^(-2j/rot), `scaling` for contexts longer than trained:
+ *   0 none;  1 linear: all frequencies / factor;  2 NTK-aware: base * factor^(rot/(rot-2)) for base (the fastest pair keeps its frequency,
+ *   the slowest gets 1/factor of it);
+ *   3 YaRN: plain for pairs that turn at least `fast` times over orig_len positions, / factor for at most `slow` times, linear in the pair's
+ *   index in between, and cosines and sines times 0.1 ln(factor) + 1;
+ *   4 banded: plain above `fast` turns over orig_len, / factor below `slow`, linear in the number of turns in between.
+ * factor >= 1 (read for 1 to 4), orig_len > 0 and 0 < slow < fast (read for 3 and 4).  rot even. */
+hift_status hift_rope_table(int32_t scaling, int64_t n_pos, int32_t rot, double base, double factor, double orig_len, double fast,
+                            double slow, float *cs_dev, void *cuda_stream);
+/* Rotary positions on the first n_heads * d_head columns of x_dev [rows, ld] into out_dev [rows, ld_out] (which may be x_dev itself, with
+ * the same ld): the first `rot` elements of every head are turned, the rest of it is copied; columns beyond the heads are neither read nor
+ * written.  For a qkv buffer: n_heads = the q and the k heads; for the two maps of differential attention: twice as many of half the size.
+ * layout 0: pair (j, j + rot/2), 1: pair (2j, 2j+1).  positions_dev int32 [rows], or NULL: row r has position r mod seq.  A position
+ * outside [0, n_pos) leaves its row unturned and sets *bad_dev (int32, may be NULL) to 1, which the library never clears.
+ * inverse != 0 turns back: the gradient of the turned rows into the rows before.  dtype 0 fp32, 1 bf16; computed in fp32, rounded once; any
+ * alignment of an element, any ld >= n_heads * d_head.  rows = 0 is allowed.  HIFT_ERR_CAPACITY if n_heads * d_head > HIFT_ROPE_MAX_WIDTH. */
+#define HIFT_ROPE_MAX_WIDTH 8388608
+hift_status hift_k_rope(int32_t dtype, int32_t layout, int64_t rows, int32_t n_heads, int32_t d_head, int32_t rot, const void *x_dev,
+                        int64_t ld, void *out_dev, int64_t ld_out, const float *cs_dev, int64_t n_pos, int64_t seq,
+                        const int32_t *positions_dev, int32_t inverse, int32_t *bad_dev, void *cuda_stream);
+
+/* Differential attention: the difference of two softmax maps with a learned weight per head,
+ *     a_m = softmax(q_m k_m^T / sqrt(d_head/2) + mask),   o_m = a_m v  (m = 1, 2),   o = o_1 - lambda_h o_2,
+ *     y = out_scale * gain * o / sqrt(mean(o^2) + eps)    per head (gain_dev NULL: no norm, y_dev NULL).
+ * qkv_dev [batch*seq, (n_heads + 2 n_kv_heads) * d_head]: the column blocks q | k | v of hift_k_attention_fwd; in a head of q or k the first
+ * half of its columns belongs to the first map, the second half to the second, while v is d_head wide.  Query head h reads key and value
+ * head h / (n_heads / n_kv_heads).  Masks as in hift_k_attention_fwd (causal; key_lens_dev int32 [batch] or NULL), but a length of
+ * 0 leaves nothing: zeros, lse = -inf, no gradient.  What a batch entry's keys beyond its length hold is read and has to be finite.
+ * lambda_dev fp32 [n_heads], gain_dev [d_head] of the operand type.  Out, all [batch*seq, n_heads * d_head] of the operand type: o_dev, o2_dev (o_2, what
+ * the gradient needs; may be NULL), y_dev; lse_dev fp32 [2, batch, n_heads, seq], the maps' log-sum-exps.
+ * d_head 16, 32, 64 or 128; dtype 0 fp32, 1 bf16.  bf16 heads of 64 and 128 in 16-byte-aligned buffers run on the tensor cores, with probabilities
+ * and their gradients rounded to bf16 as operands and sums in fp32; the rest runs on the CUDA cores in fp32.
+ * batch = 0 or seq = 0 is allowed. */
+hift_status hift_k_diff_attention_fwd(int32_t dtype, int32_t batch, int32_t seq, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
+                                      int32_t causal, const void *qkv_dev, const float *lambda_dev, const void *gain_dev, double eps,
+                                      double out_scale, void *o_dev, void *o2_dev, void *y_dev, float *lse_dev,
+                                      const int32_t *key_lens_dev, void *cuda_stream);
+/* Its gradient, from o_dev, o2_dev and lse_dev as the forward pass stored them.  dy_dev: the gradient of y (of o without a norm).  dqkv_dev has qkv's
+ * shape and is written whole (zeros at padded keys; shared key heads get the sum over their query heads); dlambda_dev fp32 [n_heads] and
+ * dgain_dev fp32 [d_head] may be NULL.  Sums run in a fixed order.  scratch_dev: 256-byte aligned,
+ * hift_diff_attention_bwd_scratch_bytes(...) bytes (norm != 0 with a gain; 0 for what the call does not take), HIFT_ERR_CAPACITY if
+ * scratch_bytes is less. */
+size_t      hift_diff_attention_bwd_scratch_bytes(int32_t dtype, int32_t batch, int32_t seq, int32_t n_heads, int32_t d_head, int32_t norm);
+hift_status hift_k_diff_attention_bwd(int32_t dtype, int32_t batch, int32_t seq, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
+                                      int32_t causal, const void *qkv_dev, const float *lambda_dev, const void *gain_dev, double eps,
+                                      double out_scale, const void *o_dev, const void *o2_dev, const float *lse_dev, const void *dy_dev,
+                                      void *dqkv_dev, float *dlambda_dev, float *dgain_dev, void *scratch_dev, size_t scratch_bytes,
+                                      const int32_t *key_lens_dev, void *cuda_stream);
+/* The weights as they are learned: lambda_h = exp(q1 . k1) - exp(q2 . k2) + init, w_dev fp32 [4, sets, d]: q1 | k1 | q2 | k2; sets = 1 (the
+ * same vectors for all heads, whose gradients are summed) or n_heads.  dw_dev has w's shape. */
+hift_status hift_k_diff_lambda(int32_t n_heads, int32_t sets, int32_t d, double init, const float *w_dev, float *lambda_dev, void *cuda_stream);
+hift_status hift_k_diff_lambda_bwd(int32_t n_heads, int32_t sets, int32_t d, const float *w_dev, const float *dlambda_dev, float *dw_dev,
+                                   void *cuda_stream);
+
+/* Activations kept in 8 bits for the backward pass, beside recomputing them.  Blocks of HIFT_ACT8_BLOCK consecutive columns of a row
+ * (the last one of a row may be shorter) share a scale 2^(byte - 127), the least power of two, 2^-110 at least, that brings the block's
+ * largest magnitude to at most 127 (format 0: int8) or 448 (format 1: e4m3); q = x / scale rounded to nearest even, and q * scale is exact in bf16 and
+ * fp32.  A block that holds a NaN or an infinity has byte 255 and comes back as NaNs.  q_dev: one byte a value; scales_dev:
+ * ceil(cols / HIFT_ACT8_BLOCK) bytes a row.
+ *   pack:   x_dev [rows, ld] -> q, scales          unpack: q, scales -> out_dev [rows, ld]    (columns beyond `cols` are left alone)
+ *   fwd:    act_dev[rows, f] = activation of pre_dev, and pre packed.  kind 1: GELU (erf), pre [rows, f]; 2: SwiGLU, pre [rows, 2f] = gate | up,
+ *           act = silu(gate) * up, q [rows, 2f] and the scale bytes of gate | up per row, each part with blocks of its own
+ *   bwd:    dpre_dev (pre's shape) from dact_dev [rows, f] at the packed values; act_dev [rows, f] (may be NULL): the activation at them, what the next
+ *           weight's gradient takes
+ * dtype: of x, out, pre, act, dact and dpre.  rows = 0 is allowed.  HIFT_ERR_CAPACITY for more than HIFT_ACT8_MAX_COLS columns. */
+#define HIFT_ACT8_BLOCK 32
+#define HIFT_ACT8_MAX_COLS 8388608
+hift_status hift_k_act8_pack(int32_t dtype, int32_t format, int64_t rows, int64_t cols, const void *x_dev, int64_t ld, void *q_dev,
+                             uint8_t *scales_dev, void *cuda_stream);
+hift_status hift_k_act8_unpack(int32_t dtype, int32_t format, int64_t rows, int64_t cols, const void *q_dev, const uint8_t *scales_dev,
+                               void *out_dev, int64_t ld, void *cuda_stream);
+hift_status hift_k_act8_fwd(int32_t dtype, int32_t format, int32_t kind, int64_t rows, int64_t f, const void *pre_dev, void *act_dev,
+                            void *q_dev, uint8_t *scales_dev, void *cuda_stream);
+hift_status hift_k_act8_bwd(int32_t dtype, int32_t format, int32_t kind, int64_t rows, int64_t f, const void *dact_dev, const void *q_dev,
+                            const uint8_t *scales_dev, void *dpre_dev, void *act_dev, void *cuda_stream);
+
 const char *hift_strerror(hift_status s);
 
 #ifdef __cplusplus

@@ -140,6 +140,18 @@ def _prototypes():
         "hift_orthogonalize_scratch_bytes": (sz, [i64, i64]),
         "hift_k_orthogonalize": (C.c_int, [i32, i64, i64, vp, vp, i32, vp, sz, vp]),
         "hift_muon_step": (C.c_int, [i64, i64, vp, vp, vp, vp, vp, sz, f64, f64, i32, f64, i32, vp]),
+        "hift_rope_table": (C.c_int, [i32, i64, i32, f64, f64, f64, f64, f64, vp, vp]),
+        "hift_k_rope": (C.c_int, [i32, i32, i64, i32, i32, i32, vp, i64, vp, i64, vp, i64, i64, vp, i32, vp, vp]),
+        "hift_k_diff_attention_fwd": (C.c_int, [i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, f64, f64, vp, vp, vp, vp, vp, vp]),
+        "hift_diff_attention_bwd_scratch_bytes": (sz, [i32, i32, i32, i32, i32, i32]),
+        "hift_k_diff_attention_bwd": (C.c_int, [i32, i32, i32, i32, i32, i32, i32, vp, vp, vp, f64, f64, vp, vp, vp, vp, vp, vp, vp,
+                                                vp, sz, vp, vp]),
+        "hift_k_diff_lambda": (C.c_int, [i32, i32, i32, f64, vp, vp, vp]),
+        "hift_k_diff_lambda_bwd": (C.c_int, [i32, i32, i32, vp, vp, vp, vp]),
+        "hift_k_act8_pack": (C.c_int, [i32, i32, i64, i64, vp, i64, vp, vp, vp]),
+        "hift_k_act8_unpack": (C.c_int, [i32, i32, i64, i64, vp, vp, vp, i64, vp]),
+        "hift_k_act8_fwd": (C.c_int, [i32, i32, i32, i64, i64, vp, vp, vp, vp, vp]),
+        "hift_k_act8_bwd": (C.c_int, [i32, i32, i32, i64, i64, vp, vp, vp, vp, vp, vp]),
     }
 
 
@@ -641,3 +653,64 @@ def muon_step(rows, cols, param_bf16, master, grad, momentum_buf, scratch, lr, m
     _check(lib().hift_muon_step(rows, cols, _ptr(param_bf16), _ptr(master), _ptr(grad), _ptr(momentum_buf), _ptr(scratch),
                                 _nbytes(scratch), lr, momentum, 1 if nesterov else 0, weight_decay, steps, _st(stream)),
            "hift_muon_step")
+
+
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_YARN, ROPE_BANDED = 0, 1, 2, 3, 4
+ACT8_BLOCK = 32
+ACT8_INT8, ACT8_E4M3 = 0, 1
+ACT8_GELU, ACT8_SWIGLU = 1, 2
+
+
+def rope_table(n_pos, rot, cs, base=10000.0, scaling=ROPE_PLAIN, factor=1.0, orig_len=1.0, fast=32.0, slow=1.0, stream=None):
+    """cs: fp32, n_pos * rot elements: cosines, then sines."""
+    _check(lib().hift_rope_table(scaling, n_pos, rot, base, factor, orig_len, fast, slow, _ptr(cs), _st(stream)), "hift_rope_table")
+
+
+def k_rope(dtype, layout, rows, n_heads, d_head, rot, x, ld, out, ld_out, cs, n_pos, seq=None, positions=None, inverse=False, bad=None,
+           stream=None):
+    """positions None: row r has position r mod seq (seq None: n_pos)."""
+    _check(lib().hift_k_rope(dtype, layout, rows, n_heads, d_head, rot, _ptr(x), ld, _ptr(out), ld_out, _ptr(cs), n_pos,
+                             n_pos if seq is None else seq, _ptr(positions), 1 if inverse else 0, _ptr(bad), _st(stream)), "hift_k_rope")
+
+
+def k_diff_attention_fwd(dtype, B, S, H, Hkv, dh, causal, qkv, lam, gain, eps, out_scale, o, o2, y, lse, key_lens=None, stream=None):
+    _check(lib().hift_k_diff_attention_fwd(dtype, B, S, H, Hkv, dh, 1 if causal else 0, _ptr(qkv), _ptr(lam), _ptr(gain), eps, out_scale,
+                                           _ptr(o), _ptr(o2), _ptr(y), _ptr(lse), _ptr(key_lens), _st(stream)),
+           "hift_k_diff_attention_fwd")
+
+
+def diff_attention_bwd_scratch_bytes(dtype, B, S, H, dh, norm) -> int:
+    return lib().hift_diff_attention_bwd_scratch_bytes(dtype, B, S, H, dh, 1 if norm else 0)
+
+
+def k_diff_attention_bwd(dtype, B, S, H, Hkv, dh, causal, qkv, lam, gain, eps, out_scale, o, o2, lse, dy, dqkv, dlam, dgain, scratch,
+                         key_lens=None, stream=None):
+    """scratch: a CUDA tensor of diff_attention_bwd_scratch_bytes(dtype, B, S, H, dh, gain is not None) bytes or more."""
+    _check(lib().hift_k_diff_attention_bwd(dtype, B, S, H, Hkv, dh, 1 if causal else 0, _ptr(qkv), _ptr(lam), _ptr(gain), eps, out_scale,
+                                           _ptr(o), _ptr(o2), _ptr(lse), _ptr(dy), _ptr(dqkv), _ptr(dlam), _ptr(dgain), _ptr(scratch),
+                                           _nbytes(scratch), _ptr(key_lens), _st(stream)), "hift_k_diff_attention_bwd")
+
+
+def k_diff_lambda(n_heads, sets, d, init, w, lam, stream=None):
+    _check(lib().hift_k_diff_lambda(n_heads, sets, d, init, _ptr(w), _ptr(lam), _st(stream)), "hift_k_diff_lambda")
+
+
+def k_diff_lambda_bwd(n_heads, sets, d, w, dlam, dw, stream=None):
+    _check(lib().hift_k_diff_lambda_bwd(n_heads, sets, d, _ptr(w), _ptr(dlam), _ptr(dw), _st(stream)), "hift_k_diff_lambda_bwd")
+
+
+def k_act8_pack(dtype, fmt, rows, cols, x, ld, q, scales, stream=None):
+    _check(lib().hift_k_act8_pack(dtype, fmt, rows, cols, _ptr(x), ld, _ptr(q), _ptr(scales), _st(stream)), "hift_k_act8_pack")
+
+
+def k_act8_unpack(dtype, fmt, rows, cols, q, scales, out, ld, stream=None):
+    _check(lib().hift_k_act8_unpack(dtype, fmt, rows, cols, _ptr(q), _ptr(scales), _ptr(out), ld, _st(stream)), "hift_k_act8_unpack")
+
+
+def k_act8_fwd(dtype, fmt, kind, rows, f, pre, act, q, scales, stream=None):
+    _check(lib().hift_k_act8_fwd(dtype, fmt, kind, rows, f, _ptr(pre), _ptr(act), _ptr(q), _ptr(scales), _st(stream)), "hift_k_act8_fwd")
+
+
+def k_act8_bwd(dtype, fmt, kind, rows, f, dact, q, scales, dpre, act=None, stream=None):
+    _check(lib().hift_k_act8_bwd(dtype, fmt, kind, rows, f, _ptr(dact), _ptr(q), _ptr(scales), _ptr(dpre), _ptr(act), _st(stream)),
+           "hift_k_act8_bwd")

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libhift.so")
-SOURCES = ["hift.cu", "gemm_tc.cu", "train_ops.cu"]
+SOURCES = ["hift.cu", "gemm_tc.cu", "train_ops.cu", "block_ops.cu"]
 
 
 def _newest_source_mtime() -> float:

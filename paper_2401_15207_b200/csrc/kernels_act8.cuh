@@ -1,0 +1,258 @@
+// Activations kept in 8 bits for the backward pass.  Blocks of 32 consecutive columns of a row share a scale 2^(byte - 127): the least power
+// of two that brings the block's largest magnitude into the format's range (int8: 127, e4m3: 448), 2^-110 at least, so that every value
+// that a block stands for is exact in bf16 and fp32.  A power of two costs up to one bit of int8's seven against a scale of top / 127, and
+// makes quotient, rounding and product free of any other error: the same 8 bits on every path.  A block that holds a NaN or an infinity
+// gets scale byte 255 (infinity as an fp32 exponent) and zeros: 0 * infinity is NaN, the whole block.
+//
+// Memory bounds all of these; the exponential or error function comes second.  Rows whose columns are a multiple of 8 in aligned buffers
+// go 8 columns to a thread (16 bytes of bf16, 8 bytes of q): four threads share a block, its maximum takes two shuffles.  Other rows go
+// one column to a thread, one block to a warp.
+#pragma once
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+
+namespace hift {
+
+constexpr int kAct8Block = 32;
+
+// scale byte of a block whose largest magnitude has these bits (of |x|; a NaN's bits are above infinity's)
+template <int FMT> __device__ __forceinline__ int act8_byte(uint32_t top) {
+  const int e = (int)(top >> 23);
+  const uint32_t m = top & 0x7FFFFFu;
+  if (e == 255) return 255;
+  // int8: 127 = 1.984375 * 2^6, e4m3: 448 = 1.75 * 2^8
+  const int b = FMT == 0 ? e - 6 + (m > 0x7E0000u) : e - 8 + (m > 0x600000u);
+  return max(b, 17);
+}
+__device__ __forceinline__ float act8_scale(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+__device__ __forceinline__ float act8_inverse(int byte) { return byte == 255 ? 0.f : __uint_as_float((uint32_t)(254 - byte) << 23); }
+
+// four values, scaled into range, as four bytes; round to nearest even
+template <int FMT> __device__ __forceinline__ uint32_t act8_quad(float a, float b, float c, float d) {
+  if (FMT == 0) {
+    const uint32_t i = (uint32_t)__float2int_rn(a) & 255u, j = (uint32_t)__float2int_rn(b) & 255u;
+    return i | j << 8 | ((uint32_t)__float2int_rn(c) & 255u) << 16 | (uint32_t)__float2int_rn(d) << 24;
+  }
+  const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+  return lo | (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3) << 16;
+}
+template <int FMT> __device__ __forceinline__ void act8_unquad(uint32_t q, float (&v)[4]) {
+  if (FMT == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(q >> 8 * i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(q >> 16 * i), __NV_E4M3);
+      const float2 f = __half22float2(__half2(h));
+      v[2 * i] = f.x; v[2 * i + 1] = f.y;
+    }
+  }
+}
+template <int FMT> __device__ __forceinline__ float act8_one(uint8_t q) {
+  float v[4];
+  act8_unquad<FMT>(q, v);
+  return v[0];
+}
+
+struct Act8 {
+  const void* x;             // pre-activations [rows, ld] (KIND 2: gate | up, [rows, 2 f])
+  const void* dy;            // gradient of the activation's output [rows, f]
+  void* y;                   // activation's output [rows, f], or nullptr
+  void* dx;                  // gradient of the pre-activations, or the unpacked values
+  uint8_t* q; uint8_t* scales;
+  int64_t rows, f, ld;       // ld: of x (packing alone) or of dx (unpacking alone)
+  int rows_per_block;        // rows of a block column (blockIdx.x), dealt to its threads (blockIdx.y) behind one another
+};
+// This thread's row and unit of it; false beyond the last row.  `units` a row.
+__device__ __forceinline__ bool act8_place(const Act8& p, int units, int64_t& row, int& unit) {
+  const int i = blockIdx.y * 256 + threadIdx.x, rb = i / units;
+  unit = i - rb * units;
+  row = (int64_t)blockIdx.x * p.rows_per_block + rb;
+  return rb < p.rows_per_block && row < p.rows;
+}
+// Rows to a block column: so many that the last of its blocks is at most a 32nd of them (a 64-bit division in every thread is dearer).
+inline dim3 act8_grid(Act8& p, int64_t units) {
+  p.rows_per_block = (int)((8191 + units) / units);
+  if (p.rows_per_block > p.rows) p.rows_per_block = (int)p.rows;
+  return dim3((unsigned)((p.rows + p.rows_per_block - 1) / p.rows_per_block), (unsigned)((units * p.rows_per_block + 255) / 256));
+}
+
+// KIND 0: none (packing alone), 1: GELU, 2: SwiGLU
+__device__ __forceinline__ float act8_sigmoid(float a) { return __fdividef(1.0f, 1.0f + __expf(-a)); }   // (0 where the sum is beyond 2^126)
+template <int KIND> __device__ __forceinline__ float act8_value(float a, float u) {
+  return KIND == 1 ? 0.5f * a * (1.0f + erff(a * 0.70710678118654752440f)) : a * act8_sigmoid(a) * u;
+}
+// dx (and the gradient of `up`), and the activation's value
+template <int KIND> __device__ __forceinline__ void act8_grad(float g, float a, float u, float& da, float& du, float& y) {
+  if (KIND == 1) {
+    const float cdf = 0.5f * (1.0f + erff(a * 0.70710678118654752440f));
+    da = g * fmaf(a, 0.39894228040143267794f * __expf(-0.5f * a * a), cdf);
+    y = a * cdf;
+  } else {
+    // 1 - sigmoid(a) as sigmoid(-a): no digits are lost where the sigmoid is nearly 1
+    const float sig = act8_sigmoid(a), rest = act8_sigmoid(-a), s = a * sig;
+    da = g * u * sig * fmaf(a, rest, 1.0f);
+    du = g * s;
+    y = s * u;
+  }
+}
+
+// ---- 8 columns a thread -------------------------------------------------------------------------------------------------------------
+// Thread i of a row: half i / units, columns 8 (i mod units) ..; units = 4 * ceil(f / 32), those at or beyond f / 8 idle in the last block.
+template <typename T, int FMT, int KIND>
+__global__ void __launch_bounds__(256) act8_fwd_vec_kernel(Act8 p) {
+  pdl_launch_next();
+  pdl_wait_prior();
+  constexpr int N = KIND == 2 ? 2 : 1;
+  const int nb = (int)((p.f + kAct8Block - 1) / kAct8Block), units = 4 * nb;
+  int64_t row;
+  int c;
+  const bool in = act8_place(p, units, row, c) && 8 * c < p.f;
+  float v[N][8];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if (in) {
+      load8((const T*)p.x + row * p.ld + n * p.f + 8 * c, v[n]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[n][j] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[n][j]) & 0x7FFFFFFFu);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int byte = act8_byte<FMT>(top);
+    const float inv = act8_inverse(byte);
+    if (in) {
+      uint2 w = make_uint2(0u, 0u);
+      if (byte != 255) {
+        w.x = act8_quad<FMT>(v[n][0] * inv, v[n][1] * inv, v[n][2] * inv, v[n][3] * inv);
+        w.y = act8_quad<FMT>(v[n][4] * inv, v[n][5] * inv, v[n][6] * inv, v[n][7] * inv);
+      }
+      *reinterpret_cast<uint2*>(p.q + (row * N + n) * p.f + 8 * c) = w;
+      if ((c & 3) == 0) p.scales[(row * N + n) * nb + (c >> 2)] = (uint8_t)byte;
+    }
+  }
+  if (KIND > 0 && in) {
+    float y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = act8_value<KIND>(v[0][j], v[N - 1][j]);
+    store8((T*)p.y + row * p.f + 8 * c, y);
+  }
+}
+template <typename T, int FMT, int KIND, bool AGAIN>
+__global__ void __launch_bounds__(256) act8_bwd_vec_kernel(Act8 p) {
+  pdl_launch_next();
+  pdl_wait_prior();
+  constexpr int N = KIND == 2 ? 2 : 1;
+  const int nb = (int)((p.f + kAct8Block - 1) / kAct8Block), units = (int)(p.f / 8);
+  int64_t row;
+  int c;
+  if (!act8_place(p, units, row, c)) return;
+  uint2 w[N];
+  int byte[N];
+  float g[8], v[N][8];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    w[n] = *reinterpret_cast<const uint2*>(p.q + (row * N + n) * p.f + 8 * c);
+    byte[n] = p.scales[(row * N + n) * nb + (c >> 2)];
+  }
+  if (KIND > 0) load8((const T*)p.dy + row * p.f + 8 * c, g);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const float s = act8_scale(byte[n]);
+    float a[4], b[4];
+    act8_unquad<FMT>(w[n].x, a);
+    act8_unquad<FMT>(w[n].y, b);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { v[n][j] = a[j] * s; v[n][4 + j] = b[j] * s; }
+  }
+  if constexpr (KIND == 0) {
+    store8((T*)p.dx + row * p.ld + 8 * c, v[0]);
+    return;
+  }
+  float y[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float da, du = 0.f;
+    act8_grad<KIND>(g[j], v[0][j], v[N - 1][j], da, du, y[j]);
+    v[0][j] = da;
+    if (N == 2) v[1][j] = du;
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n) store8((T*)p.dx + (row * N + n) * p.f + 8 * c, v[n]);
+  if (AGAIN) store8((T*)p.y + row * p.f + 8 * c, y);
+}
+
+// ---- any rows: one column a thread, one block of 32 a warp --------------------------------------------------------------------------
+template <typename T, int FMT, int KIND>
+__global__ void __launch_bounds__(256) act8_fwd_any_kernel(Act8 p) {
+  pdl_launch_next();
+  pdl_wait_prior();
+  constexpr int N = KIND == 2 ? 2 : 1;
+  const int nb = (int)((p.f + kAct8Block - 1) / kAct8Block), lane = threadIdx.x & 31;
+  int64_t row;
+  int c;
+  if (!act8_place(p, nb * kAct8Block, row, c)) return;     // whole warps
+  const int k = c / kAct8Block;
+  const bool in = c < p.f;
+  float v[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) v[n] = in ? to_f(((const T*)p.x)[row * p.ld + n * p.f + c]) : 0.f;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int byte = act8_byte<FMT>(__reduce_max_sync(0xffffffffu, __float_as_uint(v[n]) & 0x7FFFFFFFu));
+    const uint32_t w = byte == 255 ? 0u : act8_quad<FMT>(v[n] * act8_inverse(byte), 0.f, 0.f, 0.f);
+    if (in) p.q[(row * N + n) * p.f + c] = (uint8_t)w;
+    if (lane == 0) p.scales[(row * N + n) * nb + k] = (uint8_t)byte;
+  }
+  if (KIND > 0 && in) ((T*)p.y)[row * p.f + c] = from_f<T>(act8_value<KIND>(v[0], v[N - 1]));
+}
+template <typename T, int FMT, int KIND, bool AGAIN>
+__global__ void __launch_bounds__(256) act8_bwd_any_kernel(Act8 p) {
+  pdl_launch_next();
+  pdl_wait_prior();
+  constexpr int N = KIND == 2 ? 2 : 1;
+  const int nb = (int)((p.f + kAct8Block - 1) / kAct8Block);
+  int64_t row;
+  int c;
+  if (!act8_place(p, (int)p.f, row, c)) return;
+  float v[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    v[n] = act8_one<FMT>(p.q[(row * N + n) * p.f + c]) * act8_scale(p.scales[(row * N + n) * nb + c / kAct8Block]);
+  if (KIND == 0) { ((T*)p.dx)[row * p.ld + c] = from_f<T>(v[0]); return; }
+  float da, du = 0.f, y;
+  act8_grad<KIND>(to_f(((const T*)p.dy)[row * p.f + c]), v[0], v[N - 1], da, du, y);
+  ((T*)p.dx)[row * N * p.f + c] = from_f<T>(da);
+  if (N == 2) ((T*)p.dx)[(row * N + 1) * p.f + c] = from_f<T>(du);
+  if (AGAIN) ((T*)p.y)[row * p.f + c] = from_f<T>(y);
+}
+
+inline bool act8_aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+template <typename T, int FMT, int KIND>
+cudaError_t launch_act8_fwd(cudaStream_t st, Act8 p) {
+  const int64_t nb = (p.f + kAct8Block - 1) / kAct8Block;
+  const bool vec = p.f % 8 == 0 && p.ld % 8 == 0 && act8_aligned(p.x, 16) && act8_aligned(p.y, 16) && act8_aligned(p.q, 8);
+  const dim3 g = act8_grid(p, vec ? nb * 4 : nb * kAct8Block);
+  return launch_pdl(vec ? act8_fwd_vec_kernel<T, FMT, KIND> : act8_fwd_any_kernel<T, FMT, KIND>, g, dim3(256), 0, st, p);
+}
+template <typename T, int FMT, int KIND, bool AGAIN>
+cudaError_t launch_act8_bwd_y(cudaStream_t st, Act8 p) {
+  const bool vec = p.f % 8 == 0 && p.ld % 8 == 0 && act8_aligned(p.dy, 16) && act8_aligned(p.dx, 16) && act8_aligned(p.y, 16) && act8_aligned(p.q, 8);
+  const dim3 g = act8_grid(p, vec ? p.f / 8 : p.f);
+  return launch_pdl(vec ? act8_bwd_vec_kernel<T, FMT, KIND, AGAIN> : act8_bwd_any_kernel<T, FMT, KIND, AGAIN>, g, dim3(256), 0, st, p);
+}
+template <typename T, int FMT, int KIND>
+cudaError_t launch_act8_bwd(cudaStream_t st, const Act8& p) {
+  if constexpr (KIND == 0) return launch_act8_bwd_y<T, FMT, 0, false>(st, p);
+  else return p.y ? launch_act8_bwd_y<T, FMT, KIND, true>(st, p) : launch_act8_bwd_y<T, FMT, KIND, false>(st, p);
+}
+
+}  // namespace hift

@@ -1,0 +1,535 @@
+// Differential attention on CUDA cores, fp32 arithmetic, every type and head size; and the small kernels that the tensor-core path shares.
+//
+//   a_m = softmax(q_m k_m^T / sqrt(d) + mask), m = 1, 2;   o_m = a_m v;   o = o_1 - lambda_h o_2;   y = c gain o / rms(o)
+// A head has D = 2 d columns: q and k are the two maps' halves behind one another, v is D wide.  qkv[T, (H + 2 K) D]: H query heads, K key
+// heads, K value heads; query head h reads key head h / (H / K).  Nothing of size S x S is stored: one pass over the keys with each map's
+// running maximum and sum (its log-sum-exp saved), one tile of probabilities at a time in shared memory.
+//
+// Backward: with g the gradient of o, dP = g v^T is shared by the maps, and with D_1 = g.o_1 = g.(o + lambda o_2), D_2 = g.o_2
+//   dS_1 = P_1 (dP - D_1),  dS_2 = -lambda P_2 (dP - D_2),  dv = (P_1 - lambda P_2)^T g,  dq_m = dS_m k_m,  dk_m = dS_m^T q_m,
+//   dlambda = -sum D_2.
+// One kernel owns query rows (dq), one owns key rows (dk, dv; it walks the query heads of its key head in order): every output element has
+// one writer and a fixed order of summation.
+//
+// Tile 64 x 64 with 256 threads: a thread owns 4 x 4 scores (rows 4 ty .., columns tx + 16 j, so that with rows padded by 4 words the reads of
+// 16 bytes along a row are free of bank conflicts) and 4 rows x D / 16 columns of each output.
+#pragma once
+#include "common.cuh"
+
+namespace hift {
+
+struct DattnArgs {
+  const void* qkv; const float* lam; const void* gain; const int32_t* lens;
+  void* o; void* o2; void* y; float* lse;                  // forward; backward reads o, o2 and lse
+  const void* dy; const void* g; const float* dsum;        // g: gradient of o (dy itself without a norm); dsum: D_1 | D_2, each [B, H, S]
+  void* dqkv;
+  int B, S, H, K, causal;
+  float scale, eps, c;
+};
+
+__device__ __forceinline__ int dattn_len(const int32_t* __restrict__ lens, int b, int S) { return lens ? max(0, min(lens[b], S)) : S; }
+
+constexpr int kDaT = 64;                                   // rows and columns of a tile
+template <int D> constexpr int kDaLd = D + 4;              // words between rows of a staged tile
+constexpr int kDaPLd = kDaT + 4;
+template <int D> constexpr int kDaFwdSmem = (3 * kDaT * kDaLd<D> + kDaT * kDaPLd) * 4;
+template <int D> constexpr int kDaDqSmem = (4 * kDaT * kDaLd<D> + kDaT * kDaPLd) * 4;
+template <int D> constexpr int kDaDkvSmem = (4 * kDaT * kDaLd<D> + 3 * kDaT * kDaPLd + 4 * kDaT) * 4;
+
+// 64 rows of D elements, rows at or beyond `rows` as zeros
+template <typename T, int D>
+__device__ __forceinline__ void da_stage(float* dst, const T* __restrict__ src, int64_t ld, int rows) {
+  for (int i = threadIdx.x; i < kDaT * D; i += 256) {
+    const int r = i / D, c = i % D;
+    dst[r * kDaLd<D> + c] = r < rows ? to_f(src[r * ld + c]) : 0.f;
+  }
+}
+// s[i][j] = a[row 4 ty + i] . b[row tx + 16 j] over W words
+template <int D, int W>
+__device__ __forceinline__ void da_dots(float (&s)[4][4], const float* a, const float* b, int ty, int tx) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+  for (int e = 0; e < W; e += 4) {
+    float4 x[4], y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(a + (4 * ty + i) * kDaLd<D> + e);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(b + (tx + 16 * j) * kDaLd<D> + e);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        s[i][j] = fmaf(x[i].x, y[j].x, fmaf(x[i].y, y[j].y, fmaf(x[i].z, y[j].z, fmaf(x[i].w, y[j].w, s[i][j]))));
+  }
+}
+// acc[i][n] += sum_k p[row 4 ty + i][k] x[k][column n of this thread] over 64 k; CW columns a thread, of rows of `ld` words
+template <int CW>
+__device__ __forceinline__ void da_accumulate(float (&acc)[4][CW], const float* p, const float* x, int ld, int ty, int tx) {
+  constexpr int VW = CW < 4 ? CW : 4;                      // consecutive columns of a thread; the next ones are 16 VW further
+#pragma unroll 2
+  for (int k = 0; k < kDaT; k += 4) {
+    float4 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(p + (4 * ty + i) * kDaPLd + k);
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      float v[CW];
+#pragma unroll
+      for (int n = 0; n < CW; n += VW)
+#pragma unroll
+        for (int t = 0; t < VW; ++t) v[n + t] = x[(k + kk) * ld + n * 16 + tx * VW + t];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float f = kk == 0 ? w[i].x : kk == 1 ? w[i].y : kk == 2 ? w[i].z : w[i].w;
+#pragma unroll
+        for (int n = 0; n < CW; ++n) acc[i][n] = fmaf(f, v[n], acc[i][n]);
+      }
+    }
+  }
+}
+template <int CW> __device__ __forceinline__ int da_col(int n, int tx) {
+  constexpr int VW = CW < 4 ? CW : 4;
+  return n / VW * VW * 16 + tx * VW + n % VW;
+}
+__device__ __forceinline__ float half_warp_sum(float v) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+__device__ __forceinline__ float half_warp_max(float v) {
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+
+// Blocks of one launch are numbered along x alone (no limit of 65535 on heads or batch): the tiles with the most work first.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) dattn_fwd_kernel(DattnArgs a) {
+  constexpr int CW = D / 16, HD = D / 2;
+  extern __shared__ float da_smem[];
+  float *sq = da_smem, *sk = sq + kDaT * kDaLd<D>, *sv = sk + kDaT * kDaLd<D>, *sp = sv + kDaT * kDaLd<D>;
+  pdl_launch_next();
+  pdl_wait_prior();
+  const int ntile = (a.S + kDaT - 1) / kDaT, tile = ntile - 1 - (int)(blockIdx.x / (unsigned)(a.B * a.H));
+  const int bh = (int)(blockIdx.x % (unsigned)(a.B * a.H)), b = bh / a.H, h = bh % a.H, kh = h / (a.H / a.K);
+  const int q0 = tile * kDaT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int len = dattn_len(a.lens, b, a.S), kend = a.causal ? min(len, min(q0 + kDaT, a.S)) : len;
+  const int64_t ld = (int64_t)(a.H + 2 * a.K) * D;
+  const T* base = (const T*)a.qkv + (int64_t)b * a.S * ld;
+  da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0);
+  float acc[2][4][CW], m[2][4], l[2][4];
+#pragma unroll
+  for (int z = 0; z < 2; ++z)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m[z][i] = -INFINITY; l[z][i] = 0.f;
+#pragma unroll
+      for (int n = 0; n < CW; ++n) acc[z][i][n] = 0.f;
+    }
+  for (int k0 = 0; k0 < kend; k0 += kDaT) {
+    __syncthreads();
+    da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, a.S - k0);
+    da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0);          // (rows of padding may hold anything: 0 * NaN)
+    __syncthreads();
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      float s[4][4];
+      da_dots<D, HD>(s, sq + z * HD, sk + z * HD, ty, tx);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = k0 + tx + 16 * j;
+          s[i][j] = key >= len || (a.causal && key > q0 + 4 * ty + i) ? -INFINITY : s[i][j] * a.scale;
+          top = fmaxf(top, s[i][j]);
+        }
+        const float mn = fmaxf(m[z][i], half_warp_max(top)), ref = mn == -INFINITY ? 0.f : mn, corr = expf(m[z][i] - ref);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p = expf(s[i][j] - ref);
+          sum += p;
+          sp[(4 * ty + i) * kDaPLd + tx + 16 * j] = p;
+        }
+        l[z][i] = l[z][i] * corr + half_warp_sum(sum);
+        m[z][i] = mn;
+#pragma unroll
+        for (int n = 0; n < CW; ++n) acc[z][i][n] *= corr;
+      }
+      __syncwarp();                                        // a warp's 8 rows of P are its own
+      da_accumulate<CW>(acc[z], sp, sv, kDaLd<D>, ty, tx);
+      __syncwarp();
+    }
+  }
+  const float lam = a.lam[h];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int q = q0 + 4 * ty + i;
+    const float r1 = l[0][i] > 0.f ? 1.f / l[0][i] : l[0][i] == 0.f ? 0.f : l[0][i];          // no key: zeros; NaN stays
+    const float r2 = l[1][i] > 0.f ? 1.f / l[1][i] : l[1][i] == 0.f ? 0.f : l[1][i];
+    float o[CW], o2[CW], sq2 = 0.f;
+#pragma unroll
+    for (int n = 0; n < CW; ++n) {
+      o2[n] = acc[1][i][n] * r2;
+      o[n] = fmaf(-lam, o2[n], acc[0][i][n] * r1);
+      sq2 = fmaf(o[n], o[n], sq2);
+    }
+    float r = 0.f;
+    if (a.y) r = a.c / sqrtf(half_warp_sum(sq2) * (1.0f / D) + a.eps);
+    if (q >= a.S) continue;
+    const int64_t at = ((int64_t)b * a.S + q) * a.H * D + h * D;
+#pragma unroll
+    for (int n = 0; n < CW; ++n) {
+      const int c = da_col<CW>(n, tx);
+      ((T*)a.o)[at + c] = from_f<T>(o[n]);
+      if (a.o2) ((T*)a.o2)[at + c] = from_f<T>(o2[n]);
+      if (a.y) ((T*)a.y)[at + c] = from_f<T>(o[n] * r * to_f(((const T*)a.gain)[c]));
+    }
+    if (tx < 2) {
+      const int64_t row = ((int64_t)b * a.H + h) * a.S + q;
+      a.lse[(int64_t)tx * a.B * a.H * a.S + row] = tx == 0 ? m[0][i] + logf(l[0][i]) : m[1][i] + logf(l[1][i]);
+    }
+  }
+}
+
+// ---- backward ---------------------------------------------------------------------------------------------------------------------
+// A warp takes (token, head) rows of one head: the gradient g of o (through the norm), D_1, D_2, and per block the sums for dlambda and dgain.
+// D_1 and D_2 are taken with g as the products will read it (rounded to T): what is common to all of a row's dP then cancels in dP - D.
+// dlambda is taken with g in fp32.
+struct DattnPrep { DattnArgs a; void* g_out; float* dsum_out; float* dlam_part; float* dgain_part; int chunks, rows_per_chunk; };
+template <typename T, int D>
+__global__ void __launch_bounds__(256) dattn_prep_kernel(DattnPrep p) {
+  constexpr int E = D >= 32 ? D / 32 : 1, LANES = D / E;   // elements a lane; lanes with elements
+  __shared__ float red[8][D + 1];
+  pdl_launch_next();
+  pdl_wait_prior();
+  const DattnArgs& a = p.a;
+  const int h = blockIdx.x / p.chunks, ch = blockIdx.x % p.chunks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t rows = (int64_t)a.B * a.S, first = (int64_t)ch * p.rows_per_chunk, last = min(rows, first + p.rows_per_chunk);
+  const float lam = a.lam[h];
+  float gain[E], dgain[E], dlam = 0.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) { gain[e] = a.gain && lane < LANES ? to_f(((const T*)a.gain)[lane * E + e]) * a.c : 0.f; dgain[e] = 0.f; }
+  for (int64_t t = first + warp; t < last; t += 8) {
+    const int64_t at = (t * a.H + h) * D + lane * E;
+    float g[E], o[E], o2[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      g[e] = o[e] = o2[e] = 0.f;
+      if (lane < LANES) { g[e] = to_f(((const T*)a.dy)[at + e]); o[e] = to_f(((const T*)a.o)[at + e]); o2[e] = to_f(((const T*)a.o2)[at + e]); }
+    }
+    if (a.gain) {
+      float ss = 0.f, wo = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) { ss = fmaf(o[e], o[e], ss); wo = fmaf(g[e] * gain[e], o[e], wo); }
+      ss = warp_sum(ss);
+      wo = warp_sum(wo);
+      const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps), k = r * r * wo * (1.0f / D);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        dgain[e] = fmaf(g[e] * a.c, o[e] * r, dgain[e]);
+        g[e] = r * (g[e] * gain[e] - o[e] * k);
+      }
+    }
+    float d1 = 0.f, d2 = 0.f, d2x = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      d2x = fmaf(g[e], o2[e], d2x);
+      if (p.g_out) {
+        const T gr = from_f<T>(g[e]);
+        if (lane < LANES) ((T*)p.g_out)[at + e] = gr;
+        g[e] = to_f(gr);
+      }
+      d2 = fmaf(g[e], o2[e], d2);
+      d1 = fmaf(g[e], fmaf(lam, o2[e], o[e]), d1);
+    }
+    d1 = warp_sum(d1);
+    d2 = warp_sum(d2);
+    dlam -= d2x;                                           // the lanes' shares are summed at the end
+    if (lane == 0) {
+      const int64_t row = (t / a.S * a.H + h) * a.S + t % a.S;
+      p.dsum_out[row] = d1;
+      p.dsum_out[(int64_t)a.B * a.H * a.S + row] = d2;
+    }
+  }
+  dlam = warp_sum(dlam);
+  if (lane == 0) red[warp][D] = dlam;
+#pragma unroll
+  for (int e = 0; e < E; ++e) if (lane < LANES) red[warp][lane * E + e] = dgain[e];
+  __syncthreads();
+  if (threadIdx.x <= D && (threadIdx.x == D || a.gain)) {
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) s += red[w][threadIdx.x];
+    if (threadIdx.x == D) p.dlam_part[blockIdx.x] = s;
+    else p.dgain_part[(int64_t)blockIdx.x * D + threadIdx.x] = s;
+  }
+}
+// The partial sums' sums, in a fixed order: blocks 0 .. H - 1 one head's dlambda each, the others 32 columns of dgain each.
+__global__ void __launch_bounds__(256) dattn_sums_kernel(const float* __restrict__ dlam_part, const float* __restrict__ dgain_part,
+                                                         float* __restrict__ dlam, float* __restrict__ dgain, int H, int chunks, int D) {
+  __shared__ float red[33];
+  __shared__ float col[8][33];
+  pdl_launch_next();
+  pdl_wait_prior();
+  if ((int)blockIdx.x < H) {
+    float s = 0.f;
+    for (int i = threadIdx.x; i < chunks; i += 256) s += dlam_part[(int64_t)blockIdx.x * chunks + i];
+    s = block_sum(s, red);
+    if (threadIdx.x == 0) dlam[blockIdx.x] = s;
+    return;
+  }
+  const int c = ((int)blockIdx.x - H) * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+  float s = 0.f;
+  if (c < D)
+    for (int64_t i = w; i < (int64_t)H * chunks; i += 8) s += dgain_part[i * D + c];
+  col[w][threadIdx.x & 31] = s;
+  __syncthreads();
+  if (w == 0 && c < D) {
+#pragma unroll
+    for (int i = 1; i < 8; ++i) s += col[i][threadIdx.x];
+    dgain[c] = s;
+  }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) dattn_dq_kernel(DattnArgs a) {
+  constexpr int HD = D / 2, CW = HD / 16 > 0 ? HD / 16 : 1, COLS = CW * 16 > HD ? HD : CW * 16;
+  extern __shared__ float da_smem[];
+  float *sq = da_smem, *sg = sq + kDaT * kDaLd<D>, *sk = sg + kDaT * kDaLd<D>, *sv = sk + kDaT * kDaLd<D>, *sp = sv + kDaT * kDaLd<D>;
+  pdl_launch_next();
+  pdl_wait_prior();
+  const int ntile = (a.S + kDaT - 1) / kDaT, tile = ntile - 1 - (int)(blockIdx.x / (unsigned)(a.B * a.H));
+  const int bh = (int)(blockIdx.x % (unsigned)(a.B * a.H)), b = bh / a.H, h = bh % a.H, kh = h / (a.H / a.K);
+  const int q0 = tile * kDaT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int len = dattn_len(a.lens, b, a.S), kend = a.causal ? min(len, min(q0 + kDaT, a.S)) : len;
+  const int64_t ld = (int64_t)(a.H + 2 * a.K) * D, nrow = (int64_t)a.B * a.H * a.S;
+  const T* base = (const T*)a.qkv + (int64_t)b * a.S * ld;
+  da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0);
+  da_stage<T, D>(sg, (const T*)a.g + ((int64_t)b * a.S + q0) * a.H * D + h * D, (int64_t)a.H * D, a.S - q0);
+  const float lam = a.lam[h];
+  float acc[2][4][CW], lse[2][4], ds[2][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t row = ((int64_t)b * a.H + h) * a.S + min(q0 + 4 * ty + i, a.S - 1);
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      lse[z][i] = a.lse[z * nrow + row];
+      ds[z][i] = a.dsum[z * nrow + row];
+#pragma unroll
+      for (int n = 0; n < CW; ++n) acc[z][i][n] = 0.f;
+    }
+  }
+  for (int k0 = 0; k0 < kend; k0 += kDaT) {
+    __syncthreads();
+    da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, len - k0);
+    da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0);
+    __syncthreads();
+    float dp[4][4];
+    da_dots<D, D>(dp, sg, sv, ty, tx);
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      float s[4][4];
+      da_dots<D, HD>(s, sq + z * HD, sk + z * HD, ty, tx);
+      const float w = z == 0 ? a.scale : -lam * a.scale;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int key = k0 + tx + 16 * j, q = q0 + 4 * ty + i;
+          const bool seen = key < len && q < a.S && (!a.causal || key <= q);
+          sp[(4 * ty + i) * kDaPLd + tx + 16 * j] = seen ? w * expf(fmaf(s[i][j], a.scale, -lse[z][i])) * (dp[i][j] - ds[z][i]) : 0.f;
+        }
+      __syncwarp();
+      if (tx * CW < COLS) da_accumulate<CW>(acc[z], sp, sk + z * HD, kDaLd<D>, ty, tx);
+      __syncwarp();
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int q = q0 + 4 * ty + i;
+    if (q >= a.S || tx * CW >= COLS) continue;
+    T* row = (T*)a.dqkv + ((int64_t)b * a.S + q) * ld + h * D;
+#pragma unroll
+    for (int z = 0; z < 2; ++z)
+#pragma unroll
+      for (int n = 0; n < CW; ++n) row[z * HD + da_col<CW>(n, tx)] = from_f<T>(acc[z][i][n]);
+  }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) dattn_dkv_kernel(DattnArgs a) {
+  constexpr int HD = D / 2, CW = HD / 16 > 0 ? HD / 16 : 1, COLS = CW * 16 > HD ? HD : CW * 16, VW = D / 16;
+  extern __shared__ float da_smem[];
+  float *sk = da_smem, *sv = sk + kDaT * kDaLd<D>, *sq = sv + kDaT * kDaLd<D>, *sg = sq + kDaT * kDaLd<D>;
+  float* st[3];
+  st[0] = sg + kDaT * kDaLd<D>; st[1] = st[0] + kDaT * kDaPLd; st[2] = st[1] + kDaT * kDaPLd;
+  float* rowv = st[2] + kDaT * kDaPLd;                     // [lse 1 | lse 2 | D 1 | D 2][64 queries]
+  pdl_launch_next();
+  pdl_wait_prior();
+  const int tile = (int)(blockIdx.x / (unsigned)(a.B * a.K));                          // the first keys meet the most queries
+  const int bh = (int)(blockIdx.x % (unsigned)(a.B * a.K)), b = bh / a.K, kh = bh % a.K, group = a.H / a.K;
+  const int k0 = tile * kDaT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int len = dattn_len(a.lens, b, a.S);
+  const int64_t ld = (int64_t)(a.H + 2 * a.K) * D, nrow = (int64_t)a.B * a.H * a.S;
+  const T* base = (const T*)a.qkv + (int64_t)b * a.S * ld;
+  da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, len - k0);
+  da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0);
+  float dk[2][4][CW], dv[4][VW];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int n = 0; n < VW; ++n) dv[i][n] = 0.f;
+#pragma unroll
+    for (int z = 0; z < 2; ++z)
+#pragma unroll
+      for (int n = 0; n < CW; ++n) dk[z][i][n] = 0.f;
+  }
+  if (k0 < len) {                                          // the whole block
+    for (int h = kh * group; h < (kh + 1) * group; ++h) {
+      const float lam = a.lam[h];
+      for (int q0 = a.causal ? k0 : 0; q0 < a.S; q0 += kDaT) {
+        __syncthreads();
+        da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0);
+        da_stage<T, D>(sg, (const T*)a.g + ((int64_t)b * a.S + q0) * a.H * D + h * D, (int64_t)a.H * D, a.S - q0);
+        {
+          const int z = threadIdx.x >> 6;
+          const int64_t row = ((int64_t)b * a.H + h) * a.S + min(q0 + (int)(threadIdx.x & 63), a.S - 1);
+          rowv[threadIdx.x] = z < 2 ? a.lse[z * nrow + row] : a.dsum[(z - 2) * nrow + row];
+        }
+        __syncthreads();
+        float dp[4][4], mix[4][4];
+        da_dots<D, D>(dp, sv, sg, ty, tx);                 // [key][query]
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          float s[4][4];
+          da_dots<D, HD>(s, sk + z * HD, sq + z * HD, ty, tx);
+          const float w = z == 0 ? a.scale : -lam * a.scale;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const int c = tx + 16 * j, key = k0 + 4 * ty + i, q = q0 + c;
+              const bool seen = key < len && q < a.S && (!a.causal || key <= q);
+              const float p = seen ? expf(fmaf(s[i][j], a.scale, -rowv[z * kDaT + c])) : 0.f;
+              mix[i][j] = z == 0 ? p : fmaf(-lam, p, mix[i][j]);
+              st[z][(4 * ty + i) * kDaPLd + c] = seen ? w * p * (dp[i][j] - rowv[(2 + z) * kDaT + c]) : 0.f;
+              if (z == 1) st[2][(4 * ty + i) * kDaPLd + c] = mix[i][j];
+            }
+        }
+        __syncwarp();
+        da_accumulate<VW>(dv, st[2], sg, kDaLd<D>, ty, tx);
+        if (tx * CW < COLS) {
+          da_accumulate<CW>(dk[0], st[0], sq, kDaLd<D>, ty, tx);
+          da_accumulate<CW>(dk[1], st[1], sq + HD, kDaLd<D>, ty, tx);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int key = k0 + 4 * ty + i;
+    if (key >= a.S) continue;                              // rows of padding get zeros
+    T* row = (T*)a.dqkv + ((int64_t)b * a.S + key) * ld;
+#pragma unroll
+    for (int z = 0; z < 2; ++z)
+#pragma unroll
+      for (int n = 0; n < CW; ++n) if (tx * CW < COLS) row[(a.H + kh) * D + z * HD + da_col<CW>(n, tx)] = from_f<T>(dk[z][i][n]);
+#pragma unroll
+    for (int n = 0; n < VW; ++n) row[(a.H + a.K + kh) * D + da_col<VW>(n, tx)] = from_f<T>(dv[i][n]);
+  }
+}
+
+// ---- lambda -----------------------------------------------------------------------------------------------------------------------
+// lambda_h = exp(q1_h . k1_h) - exp(q2_h . k2_h) + init.  w: fp32 q1 | k1 | q2 | k2, each [sets, d]; one set for all heads, or one each.
+__global__ void __launch_bounds__(32) diff_lambda_kernel(const float* __restrict__ w, int sets, int d, float init, float* __restrict__ lam, int H) {
+  pdl_launch_next();
+  pdl_wait_prior();
+  const int64_t n = (int64_t)sets * d;
+  const float* p = w + (int64_t)(sets == 1 ? 0 : blockIdx.x) * d;
+  float a = 0.f, b = 0.f;
+  for (int i = threadIdx.x; i < d; i += 32) { a = fmaf(p[i], p[n + i], a); b = fmaf(p[2 * n + i], p[3 * n + i], b); }
+  a = warp_sum(a);
+  b = warp_sum(b);
+  if (threadIdx.x == 0) lam[blockIdx.x] = expf(a) - expf(b) + init;
+}
+__global__ void __launch_bounds__(32) diff_lambda_bwd_kernel(const float* __restrict__ w, int sets, int d, const float* __restrict__ dlam,
+                                                             float* __restrict__ dw, int H) {
+  pdl_launch_next();
+  pdl_wait_prior();
+  const int64_t n = (int64_t)sets * d, at = (int64_t)blockIdx.x * d;
+  const float* p = w + at;
+  float a = 0.f, b = 0.f, g = 0.f;
+  for (int i = threadIdx.x; i < d; i += 32) { a = fmaf(p[i], p[n + i], a); b = fmaf(p[2 * n + i], p[3 * n + i], b); }
+  a = expf(warp_sum(a));
+  b = expf(warp_sum(b));
+  if (sets == 1) {                                         // one set serves every head
+    for (int i = threadIdx.x; i < H; i += 32) g += dlam[i];
+    g = warp_sum(g);
+  } else {
+    g = dlam[blockIdx.x];
+  }
+  for (int i = threadIdx.x; i < d; i += 32) {
+    dw[at + i] = g * a * p[n + i];
+    dw[n + at + i] = g * a * p[i];
+    dw[2 * n + at + i] = -g * b * p[3 * n + i];
+    dw[3 * n + at + i] = -g * b * p[2 * n + i];
+  }
+}
+
+// ---- launches ---------------------------------------------------------------------------------------------------------------------
+inline bool dattn_head_ok(int D) { return D == 16 || D == 32 || D == 64 || D == 128; }
+#define HIFT_DATTN_SWITCH(D, CALL) switch (D) { case 16: return CALL(16); case 32: return CALL(32); case 64: return CALL(64); default: return CALL(128); }
+
+// (the attribute belongs to a device and is idempotent; 1 us beside a launch)
+template <typename A>
+cudaError_t dattn_launch(void (*kernel)(A), int64_t blocks, int smem, cudaStream_t st, const A& a) {
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  return e != cudaSuccess ? e : launch_pdl(kernel, dim3((unsigned)blocks), dim3(256), smem, st, a);
+}
+template <typename T> cudaError_t launch_dattn_fwd(cudaStream_t st, int D, const DattnArgs& a) {
+  const int64_t blocks = (int64_t)((a.S + kDaT - 1) / kDaT) * a.B * a.H;
+#define CALL(N) dattn_launch(dattn_fwd_kernel<T, N>, blocks, kDaFwdSmem<N>, st, a)
+  HIFT_DATTN_SWITCH(D, CALL)
+#undef CALL
+}
+template <typename T, int D> cudaError_t launch_dattn_bwd_d(cudaStream_t st, const DattnArgs& a) {
+  const int64_t tiles = (a.S + kDaT - 1) / kDaT;
+  const cudaError_t e = dattn_launch(dattn_dq_kernel<T, D>, tiles * a.B * a.H, kDaDqSmem<D>, st, a);
+  return e != cudaSuccess ? e : dattn_launch(dattn_dkv_kernel<T, D>, tiles * a.B * a.K, kDaDkvSmem<D>, st, a);
+}
+template <typename T> cudaError_t launch_dattn_bwd(cudaStream_t st, int D, const DattnArgs& a) {
+#define CALL(N) launch_dattn_bwd_d<T, N>(st, a)
+  HIFT_DATTN_SWITCH(D, CALL)
+#undef CALL
+}
+template <typename T> cudaError_t launch_dattn_prep(cudaStream_t st, int D, const DattnPrep& p) {
+#define CALL(N) launch_pdl(dattn_prep_kernel<T, N>, dim3((unsigned)(p.a.H * p.chunks)), dim3(256), 0, st, p)
+  HIFT_DATTN_SWITCH(D, CALL)
+#undef CALL
+}
+
+// The backward call's scratch: D_1 | D_2, the gradient of o where there is a norm, the partial sums.  Chunks of rows: enough blocks over the
+// heads for four rounds of 148 SMs, 64 rows at least.
+struct DattnPlan { int chunks, rows_per_chunk; size_t dsum, g, part, bytes; };
+inline DattnPlan dattn_plan(int es, int64_t B, int64_t S, int64_t H, int D, bool norm) {
+  DattnPlan p;
+  const int64_t rows = B * S;
+  int64_t want = (148 * 4 + H - 1) / H, most = (rows + 63) / 64;
+  if (want > most) want = most;
+  if (want < 1) want = 1;
+  p.rows_per_chunk = (int)((rows + want - 1) / want);
+  p.chunks = (int)((rows + p.rows_per_chunk - 1) / p.rows_per_chunk);
+  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  p.dsum = 0;
+  p.g = up((size_t)(2 * B * H * S) * 4);
+  p.part = p.g + (norm ? up((size_t)(rows * H * D) * es) : 0);
+  p.bytes = p.part + up((size_t)H * p.chunks * (norm ? D + 1 : 1) * 4);
+  return p;
+}
+
+}  // namespace hift
