@@ -112,6 +112,7 @@ hift_status hift_k_diff_attention_fwd(int32_t dtype, int32_t B, int32_t S, int32
   DattnArgs a = dattn_args(B, S, H, K, D, causal, qkv, lam, gain, eps, out_scale, key_lens);
   a.o = o; a.o2 = o2; a.y = y; a.lse = lse;
   cudaStream_t st = (cudaStream_t)stream;
+  if (dattn_tc_eligible(dtype, D, a)) return status_of(dattn_tc_fwd_launch(st, D, a));
   return status_of(dtype == 0 ? launch_dattn_fwd<float>(st, D, a) : launch_dattn_fwd<bf16>(st, D, a));
 }
 

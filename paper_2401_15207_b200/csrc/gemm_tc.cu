@@ -18,6 +18,9 @@
 // g_tc_error, and the kernel drains and releases its tensor memory normally.
 #include "gemm_tc.h"
 
+#include "common.cuh"
+#include "dattn_args.h"
+
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -1059,6 +1062,7 @@ gemm_tc2_kernel(const __grid_constant__ CUtensorMap tmap_a, const __grid_constan
 
 #include "attention_tc.cuh"
 #include "attention_bwd_tc.cuh"
+#include "dattn_fwd_tc.cuh"
 #include "ns_small.cuh"
 #include "ns_tiny.cuh"
 
@@ -1616,6 +1620,38 @@ cudaError_t attn_tc_bwd_launch(cudaStream_t st, int B, int S, int H, int dh, int
                                const float* lse, const float* dsum, void* dqkv, const int* lens, const DropArgs& da) {
   if (dh == 64) return attn_tc_bwd_inst<64>(st, B, S, H, causal, qkv, dout, lse, dsum, dqkv, lens, da);
   return attn_tc_bwd_inst<128>(st, B, S, H, causal, qkv, dout, lse, dsum, dqkv, lens, da);
+}
+
+// ------------------------------------------------------------------ differential attention
+bool dattn_tc_eligible(int dtype, int D, const DattnArgs& a) {
+  if (dtype != 1 || (D != 64 && D != 128) || gemm_tc_init() != 0) return false;
+  uintptr_t all = 0;
+  for (const void* p : {a.qkv, (const void*)a.o, (const void*)a.o2, (const void*)a.y, a.g, (const void*)a.dqkv}) all |= (uintptr_t)p;
+  return (all & 15) == 0;
+}
+// qkv-like bf16 rows [B][S][cols]: box = 64 columns x box_rows rows, 128-byte swizzle; rows beyond S read as zeros.  Encoded at every call:
+// buffers' addresses change from call to call.
+static bool dattn_map(const void* p, int64_t cols, int S, int B, uint32_t box_rows, CUtensorMap* out) {
+  cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)S, (cuuint64_t)B};
+  cuuint64_t strides[2] = {(cuuint64_t)cols * 2, (cuuint64_t)cols * S * 2};
+  cuuint32_t box[3] = {64, box_rows, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return g_encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// (the attribute belongs to a device, and operators take whichever is current; idempotent)
+template <typename... KArgs, typename... Args>
+static cudaError_t dattn_tc_launch(void (*kernel)(KArgs...), int64_t items, int threads, int smem, cudaStream_t st, Args&&... args) {
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const unsigned grid = (unsigned)(items < g_num_sms ? items : g_num_sms);          // persistent: one CTA per SM
+  return e != cudaSuccess ? e : launch_pdl_tc(kernel, dim3(grid), dim3(threads), smem, st, args...);
+}
+cudaError_t dattn_tc_fwd_launch(cudaStream_t st, int D, const DattnArgs& a) {
+  CUtensorMap tm;
+  if (!dattn_map(a.qkv, (int64_t)(a.H + 2 * a.K) * D, a.S, a.B, 128, &tm)) return cudaErrorInvalidValue;
+  const int64_t items = (int64_t)((a.S + 127) / 128) * a.B * a.H;
+  if (D == 64) return dattn_tc_launch(dattn_fwd_tc_kernel<64>, items, kDfThreads, DattnFwdCfg<64>::kSmem, st, tm, a);
+  return dattn_tc_launch(dattn_fwd_tc_kernel<128>, items, kDfThreads, DattnFwdCfg<128>::kSmem, st, tm, a);
 }
 
 int gemm_tc_set_error(int v) {

@@ -15,17 +15,9 @@
 // 16 bytes along a row are free of bank conflicts) and 4 rows x D / 16 columns of each output.
 #pragma once
 #include "common.cuh"
+#include "dattn_args.h"
 
 namespace hift {
-
-struct DattnArgs {
-  const void* qkv; const float* lam; const void* gain; const int32_t* lens;
-  void* o; void* o2; void* y; float* lse;                  // forward; backward reads o, o2 and lse
-  const void* dy; const void* g; const float* dsum;        // g: gradient of o (dy itself without a norm); dsum: D_1 | D_2, each [B, H, S]
-  void* dqkv;
-  int B, S, H, K, causal;
-  float scale, eps, c;
-};
 
 __device__ __forceinline__ int dattn_len(const int32_t* __restrict__ lens, int b, int S) { return lens ? max(0, min(lens[b], S)) : S; }
 
