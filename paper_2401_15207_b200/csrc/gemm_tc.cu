@@ -31,6 +31,7 @@
 
 #include <atomic>
 #include <mutex>
+#include <type_traits>
 #include <unordered_map>
 
 namespace hift {
@@ -1647,11 +1648,14 @@ static cudaError_t dattn_tc_launch(void (*kernel)(KArgs...), int64_t items, int 
   return e != cudaSuccess ? e : launch_pdl_tc(kernel, dim3(grid), dim3(threads), smem, st, args...);
 }
 cudaError_t dattn_tc_fwd_launch(cudaStream_t st, int D, const DattnArgs& a) {
-  CUtensorMap tm;
-  if (!dattn_map(a.qkv, (int64_t)(a.H + 2 * a.K) * D, a.S, a.B, 128, &tm)) return cudaErrorInvalidValue;
+  CUtensorMap tq, tkv, to, to2, ty;
+  const int64_t cols = (int64_t)(a.H + 2 * a.K) * D, out = (int64_t)a.H * D;
+  if (!dattn_map(a.qkv, cols, a.S, a.B, 128, &tq) || !dattn_map(a.qkv, cols, a.S, a.B, kDfKeys, &tkv) || !dattn_map(a.o, out, a.S, a.B, 32, &to) ||
+      !dattn_map(a.o2 ? a.o2 : a.o, out, a.S, a.B, 32, &to2) || !dattn_map(a.y ? a.y : a.o, out, a.S, a.B, 32, &ty))
+    return cudaErrorInvalidValue;
   const int64_t items = (int64_t)((a.S + 127) / 128) * a.B * a.H;
-  if (D == 64) return dattn_tc_launch(dattn_fwd_tc_kernel<64>, items, kDfThreads, DattnFwdCfg<64>::kSmem, st, tm, a);
-  return dattn_tc_launch(dattn_fwd_tc_kernel<128>, items, kDfThreads, DattnFwdCfg<128>::kSmem, st, tm, a);
+  if (D == 64) return dattn_tc_launch(dattn_fwd_tc_kernel<64>, items, kDfThreads, DattnFwdCfg<64>::kSmem, st, tq, tkv, to, to2, ty, a);
+  return dattn_tc_launch(dattn_fwd_tc_kernel<128>, items, kDfThreads, DattnFwdCfg<128>::kSmem, st, tq, tkv, to, to2, ty, a);
 }
 
 int gemm_tc_set_error(int v) {
