@@ -151,7 +151,9 @@ hift_status hift_k_diff_attention_bwd(int32_t dtype, int32_t B, int32_t S, int32
     const int blocks = H + (dgain ? (D + 31) / 32 : 0);
     e = launch_pdl(dattn_sums_kernel, dim3((unsigned)blocks), dim3(256), 0, st, (const float*)p.dlam_part, (const float*)p.dgain_part, dlam, dgain, H, pl.chunks, D);
   }
-  if (e == cudaSuccess) e = dtype == 0 ? launch_dattn_bwd<float>(st, D, a) : launch_dattn_bwd<bf16>(st, D, a);
+  if (e != cudaSuccess) return status_of(e);
+  if (dattn_tc_eligible(dtype, D, a)) return status_of(dattn_tc_bwd_launch(st, D, a));
+  e = dtype == 0 ? launch_dattn_bwd<float>(st, D, a) : launch_dattn_bwd<bf16>(st, D, a);
   return status_of(e);
 }
 

@@ -1,0 +1,416 @@
+// Differential attention backward on tcgen05 (bf16, heads of 64 and 128).  Included into gemm_tc.cu after dattn_fwd_tc.cuh.
+//
+// Two launches of one template, so that every output row has one writer and a fixed order of summation (no atomics):
+//   MODE 0 (dk, dv): a CTA owns 128 keys of a key head and streams the queries of all heads of its group, 64 at a time
+//   MODE 1 (dq)    : a CTA owns 128 queries and streams the keys, 64 at a time
+//              F0   F1    X0   X1     S_m = F0_m X0_m^T, m = 1, 2     dP = F1 X1^T     accumulators
+//   MODE 0     K    V     Q    g      scores^T                        (g V^T)^T        dv += (P_1 - lambda P_2)^T g,  dk_m += dS_m^T Q_m
+//   MODE 1     Q    g     K    V      scores                          g V^T            dq_m += dS_m K_m
+// (F0_m: the map's half of the columns; g: gradient of o.)  P_m = exp(scale S_m - lse_m),  dS_1 = P_1 (dP - D_1),  dS_2 = -lambda P_2 (dP - D_2);
+// dk and dq are multiplied by `scale` as they are stored.  dP is shared by the maps, and dv takes one product for both: 8 units of 128 x 64 x 64 a
+// step against the 10 of two plain attentions.  P and dS are rounded to bf16, the operand type of the products they feed; the accumulators are fp32.
+//   warp 0    : TMA producer         warp 1: issues every product (one elected thread); owns the tensor memory
+//   warps 4-11: element-wise, two warps to a lane quarter, 32 of the 64 streamed columns each: S_1, S_2 -> registers, exponentials; dP -> registers, dS;
+//               P and dS go back to tensor memory as bf16, the A operands of the accumulating products; at an item's end the accumulators -> global
+// Order of issue: S(t+1) as soon as S(t) has been read, so that it runs beside the exponentials of step t; then the accumulating products of t; then
+// dP(t+1), which therefore finds both its buffer and the P / dS buffers of step t free when it is done.
+// Tensor-memory columns: S_1 0, S_2 64, dP 128, [P_1 - lambda P_2 | dS_1] 192 (32 each; MODE 1: dS_1, dS_2), accumulators 256.  In MODE 0 dS_2 lies over
+// dP, each warp's part over columns that it alone has read.
+// What bounds it: products 1276 cycles a step at heads of 128 (1024 in MODE 1), exponentials 1024, both of the 128 x 64 tile.
+#pragma once
+
+constexpr int kDbThreads = 384, kDbX = 64, kDbStages = 3;
+template <int DH, int MODE> struct DattnBwdCfg {
+  static constexpr int kSpans = DH / 64;
+  static constexpr int kFBytes = 128 * DH * 2, kXBytes = kDbX * DH * 2;
+  static constexpr int kStage = 8 * 4096;                          // a 32 x 64 bf16 piece per element-wise warp
+  static constexpr int kCol = MODE == 0 ? 8 * 2 * 512 : 0;         // per warp, two steps: lse and D of its 32 queries
+  static constexpr int kSmem = 2 * kFBytes + kDbStages * 2 * kXBytes + kStage + kCol + 256 + 1024;
+};
+
+struct DattnBwdItem { int b, hk, f0, x_lo, per, nsteps, len; };    // hk: key head (MODE 0) or query head (MODE 1); per: steps of one head
+
+template <int DH, int MODE>
+__global__ void __launch_bounds__(kDbThreads, 1)
+dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_constant__ CUtensorMap map_f1, const __grid_constant__ CUtensorMap map_x0,
+                    const __grid_constant__ CUtensorMap map_x1, const __grid_constant__ CUtensorMap map_out, const DattnArgs a) {
+  typedef DattnBwdCfg<DH, MODE> Cfg;
+  constexpr int SP = Cfg::kSpans, HD = DH / 2, NS = kDbStages, FB = Cfg::kFBytes, XB = Cfg::kXBytes, FSPAN = 128 * 128, XSPAN = kDbX * 128;
+  extern __shared__ uint8_t smem_raw[];
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t sF0 = base, sF1 = sF0 + FB, sX = sF1 + FB, sStage = sX + NS * 2 * XB, sCol = sStage + Cfg::kStage, bar = sCol + Cfg::kCol;
+  const uint32_t f_full = bar, f_empty = bar + 8u, s_full = bar + 16u, s_free = bar + 24u, dp_full = bar + 32u, p_ready = bar + 40u, acc_full = bar + 48u,
+                 acc_free = bar + 56u, tmem_slot = bar + 112u;
+  auto x_full = [&](int i) { return bar + 64u + 8u * i; };
+  auto x_empty = [&](int i) { return bar + 88u + 8u * i; };
+  volatile uint32_t* slot_gen = reinterpret_cast<volatile uint32_t*>(gen + (tmem_slot - base));
+  volatile uint32_t* poison_gen = slot_gen + 2;
+
+  const int nfb = (a.S + 127) / 128, heads = MODE == 0 ? a.K : a.H, nbh = a.B * heads, nitems = nfb * nbh, group = a.H / a.K;
+  auto item_of = [&](int idx) {
+    DattnBwdItem it;
+    const int rank = idx / nbh, bh = idx - rank * nbh;
+    it.b = bh / heads;
+    it.hk = bh - it.b * heads;
+    it.len = a.lens ? max(0, min(a.lens[it.b], a.S)) : a.S;
+    it.x_lo = 0;
+    if (MODE == 0) {
+      it.f0 = rank * 128;
+      it.x_lo = a.causal ? it.f0 / kDbX : 0;
+      it.per = (a.S + kDbX - 1) / kDbX - it.x_lo;
+      it.nsteps = it.per * group;
+      if (it.f0 >= it.len) it.nsteps = 1;                          // padding alone: one step, all of it masked, writes the zeros
+    } else {
+      it.f0 = (a.causal ? nfb - 1 - rank : rank) * 128;
+      const int end = min(a.causal ? min(a.S, it.f0 + 128) : a.S, it.len);
+      it.per = it.nsteps = max(1, (end + kDbX - 1) / kDbX);
+    }
+    return it;
+  };
+
+  if (threadIdx.x == 0) {
+    mbar_init(f_full, 1); mbar_init(f_empty, 1);
+    mbar_init(s_full, 1); mbar_init(s_free, 8); mbar_init(dp_full, 1); mbar_init(p_ready, 8);
+    mbar_init(acc_full, 1); mbar_init(acc_free, 8);
+    for (int i = 0; i < NS; ++i) { mbar_init(x_full(i), 1); mbar_init(x_empty(i), 1); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    pdl_wait();                                                    // no global access before it, the flag included
+    *poison_gen = g_tc_error != 0 ? 1u : 0u;
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tm = __shfl_sync(0xffffffffu, *slot_gen, 0);
+  const bool poisoned = __any_sync(0xffffffffu, *poison_gen != 0);
+  pdl_trigger();
+  pdl_wait();
+  const uint32_t tDP = tm + 128u, tP = tm + 192u, tAcc = tm + 256u, tDv = tm + 384u;
+
+  if (warp == 0) {
+    if (!poisoned && elect_one()) {
+      // ---------------- TMA producer
+      int st = 0, n = 0;
+      uint32_t ph = 1;
+      bool ok = true;
+      for (int idx = dattn_item_at(n); idx < nitems && ok; idx = dattn_item_at(++n)) {
+        const DattnBwdItem it = item_of(idx);
+        const int colF0 = (MODE == 0 ? a.H + it.hk : it.hk) * DH, colF1 = (MODE == 0 ? a.H + a.K + it.hk : it.hk) * DH;
+        if (!mbar_wait(f_empty, (uint32_t)((n & 1) ^ 1))) { atomicCAS(&g_tc_error, 0, 7); break; }
+        mbar_expect_tx(f_full, 2 * FB);
+#pragma unroll
+        for (int sp = 0; sp < SP; ++sp) {
+          tma_load_3d(sF0 + sp * FSPAN, &map_f0, f_full, colF0 + sp * 64, it.f0, it.b);
+          tma_load_3d(sF1 + sp * FSPAN, &map_f1, f_full, colF1 + sp * 64, it.f0, it.b);
+        }
+        int x = it.x_lo, h = MODE == 0 ? it.hk * group : it.hk / group;
+        for (int t = 0; t < it.nsteps; ++t) {
+          if (!mbar_wait(x_empty(st), ph)) { atomicCAS(&g_tc_error, 0, 7); ok = false; break; }
+          const int colX0 = (MODE == 0 ? h : a.H + h) * DH, colX1 = (MODE == 0 ? h : a.H + a.K + h) * DH;
+          const uint32_t s0 = sX + st * 2 * XB;
+          mbar_expect_tx(x_full(st), 2 * XB);
+#pragma unroll
+          for (int sp = 0; sp < SP; ++sp) {
+            tma_load_3d(s0 + sp * XSPAN, &map_x0, x_full(st), colX0 + sp * 64, x * kDbX, it.b);
+            tma_load_3d(s0 + XB + sp * XSPAN, &map_x1, x_full(st), colX1 + sp * 64, x * kDbX, it.b);
+          }
+          if (++st == NS) { st = 0; ph ^= 1; }
+          if (++x == it.x_lo + it.per) { x = it.x_lo; ++h; }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (!poisoned) {
+      if (elect_one()) {
+        // ---------------- MMA issuer
+        const uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | (((uint32_t)kDbX >> 3) << 17) | ((128u >> 4) << 24);
+        const uint32_t idesc_h = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)HD >> 3) << 17) | ((128u >> 4) << 24);       // N = d
+        const uint32_t idesc_v = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)DH >> 3) << 17) | ((128u >> 4) << 24);       // N = 2 d
+        const uint64_t dF0 = desc_kmajor(sF0), dF1 = desc_kmajor(sF1), dX0 = desc_kmajor(sX);
+        auto k_off = [](int e, int span) { return (uint64_t)(((e / 4) * span + (e % 4) * 32) >> 4); };       // 16 columns, number e, of a K-major tile
+        auto issue_s = [&](int st) {
+          const uint64_t x0 = dX0 + (uint64_t)(st * (2 * XB >> 4));
+#pragma unroll
+          for (int e = 0; e < DH / 16; ++e)
+            tc_mma(tm + (e < HD / 16 ? 0u : 64u), dF0 + k_off(e, FSPAN), x0 + k_off(e, XSPAN), idesc_s, e % (HD / 16) > 0 ? 1u : 0u);
+          tc_commit(s_full);
+        };
+        auto issue_dp = [&](int st) {
+          const uint64_t x1 = dX0 + (uint64_t)((st * 2 * XB + XB) >> 4);
+#pragma unroll
+          for (int e = 0; e < DH / 16; ++e) tc_mma(tDP, dF1 + k_off(e, FSPAN), x1 + k_off(e, XSPAN), idesc_s, e > 0 ? 1u : 0u);
+          tc_commit(dp_full);
+        };
+        bool ok = true;
+        int n = 0, t = 0, g = 0, st = 0;                           // g: steps over all items; st: its ring slot
+        uint32_t ph = 0;
+        int idx = dattn_item_at(0), nsteps = idx < nitems ? item_of(idx).nsteps : 0;
+        if (nsteps) {
+          ok = mbar_wait(f_full, 0) && mbar_wait(x_full(0), 0);
+          if (ok) {
+            tc_fence_after();
+            issue_s(0);
+            issue_dp(0);
+            if (nsteps == 1) tc_commit(f_empty);
+          }
+        }
+        while (ok && idx < nitems) {
+          const bool last = t + 1 == nsteps;
+          const int next_idx = last ? dattn_item_at(n + 1) : idx, st1 = st + 1 == NS ? 0 : st + 1;
+          const uint32_t ph1 = st + 1 == NS ? ph ^ 1u : ph;
+          const bool more = next_idx < nitems;
+          if (!last) {                                             // scores of the next step beside the exponentials of this one
+            ok = mbar_wait(s_free, (uint32_t)(g & 1)) && mbar_wait(x_full(st1), ph1);
+            if (!ok) break;
+            tc_fence_after();
+            issue_s(st1);
+          }
+          ok = (t > 0 || n == 0 || mbar_wait(acc_free, (uint32_t)((n - 1) & 1))) && mbar_wait(p_ready, (uint32_t)(g & 1));
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t nX0 = desc_nmajor(sX, XSPAN) + (uint64_t)(st * (2 * XB >> 4)), nX1 = nX0 + (uint64_t)(XB >> 4);
+#pragma unroll
+          for (int m = 0; m < 2; ++m) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              // the map's half of X0's columns: the second span (heads of 128), or the second half of the one span
+              const uint64_t b = nX0 + (uint64_t)((kk * 16 * 128 + m * (DH == 128 ? XSPAN : 64)) >> 4);
+              const uint32_t p = MODE == 0 ? (m == 0 ? tP + 32u + kk * 8u : tDP + (kk >> 1) * 32u + (kk & 1) * 8u) : tP + m * 32u + kk * 8u;
+              tc_mma_ta(tAcc + (uint32_t)(m * HD), p, b, idesc_h, (t > 0 || kk > 0) ? 1u : 0u);
+            }
+          }
+          if (MODE == 0) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) tc_mma_ta(tDv, tP + kk * 8u, nX1 + (uint64_t)((kk * 16 * 128) >> 4), idesc_v, (t > 0 || kk > 0) ? 1u : 0u);
+          }
+          tc_commit(x_empty(st));
+          if (last) tc_commit(acc_full);
+          int next_steps = nsteps;
+          if (more) {
+            if (last) {                                            // another item: its fixed tiles take the place of this one's
+              next_steps = item_of(next_idx).nsteps;
+              ok = mbar_wait(s_free, (uint32_t)(g & 1)) && mbar_wait(f_full, (uint32_t)((n + 1) & 1)) && mbar_wait(x_full(st1), ph1);
+              if (!ok) break;
+              tc_fence_after();
+              issue_s(st1);
+            }
+            issue_dp(st1);
+            if (last ? next_steps == 1 : t + 2 == nsteps) tc_commit(f_empty);
+          }
+          ++g;
+          st = st1;
+          ph = ph1;
+          if (last) { t = 0; ++n; idx = next_idx; nsteps = next_steps; } else ++t;
+        }
+        if (!ok) atomicCAS(&g_tc_error, 0, 8);
+      }
+      __syncwarp();
+    }
+  } else if (warp >= 4) {
+    // ---------------- element-wise: thread = row of the fixed tile x 32 streamed columns
+    const int q = warp & 3, hc = (warp - 4) >> 2, r = q * 32 + lane;
+    const uint32_t lane_off = (uint32_t)(q * 32) << 16;
+    const float sl2 = a.scale * 1.4426950408889634f;
+    const uint64_t sc2 = f2_pack(sl2, sl2);
+    const int64_t nrow = (int64_t)a.B * a.H * a.S;
+    const uint32_t sPiece = sStage + (warp - 4) * 4096;
+    uint8_t* mine = gen + (sPiece - base) + lane * 128;
+    float* col = reinterpret_cast<float*>(gen + (sCol - base)) + (warp - 4) * 256;      // MODE 0: two buffers of 16 column pairs x (-lse_1, -lse_2, -D_1, -D_2)
+    bool ok = !poisoned;
+    int n = 0, g = 0;
+    // -lse (log2 units) and -D of one query and map; a query that sees no key, or none: P = 0 through -infinity
+    auto neg_lse = [&](int m, int64_t at, bool in) -> float {
+      const float v = in ? a.lse[m * nrow + at] : -INFINITY;
+      return v == -INFINITY ? -INFINITY : -v * 1.4426950408889634f;
+    };
+    for (int idx = dattn_item_at(n); idx < nitems && ok; idx = dattn_item_at(++n)) {
+      const DattnBwdItem it = item_of(idx);
+      const int frow = it.f0 + r;
+      int x = it.x_lo, h = MODE == 0 ? it.hk * group : it.hk;
+      float nl[2] = {0.f, 0.f}, nd[2] = {0.f, 0.f};
+      // MODE 0: this lane's column of the next step; MODE 1: this thread's row
+      auto fetch = [&](int xx, int hh) {
+        const int c = MODE == 0 ? xx * kDbX + hc * 32 + lane : frow;
+        const bool in = c < a.S;
+        const int64_t at = ((int64_t)it.b * a.H + hh) * a.S + c;
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+          nl[m] = neg_lse(m, at, in);
+          nd[m] = in ? -a.dsum[m * nrow + at] : 0.f;
+        }
+      };
+      fetch(x, h);
+      for (int t = 0; t < it.nsteps; ++t, ++g) {
+        const int x0 = x * kDbX;
+        const float lam = a.lam[h];
+        const uint64_t nlam2 = f2_pack(-lam, -lam);
+        float* cv = col + (g & 1) * 128;
+        if (MODE == 0) {
+          float* w = cv + (lane >> 1) * 8 + (lane & 1);
+          w[0] = nl[0]; w[2] = nl[1]; w[4] = nd[0]; w[6] = nd[1];
+          __syncwarp();
+        }
+        int nx = x + 1, nh = h;
+        if (MODE == 0 && nx == it.x_lo + it.per) { nx = it.x_lo; ++nh; }
+        if (MODE == 0 && t + 1 < it.nsteps) fetch(nx, nh);
+        bool ready = mbar_wait(s_full, (uint32_t)(g & 1));
+        if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 9);
+        ok = __all_sync(0xffffffffu, ready);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t v[2][32];
+        tmem_ld32_nowait(tm + lane_off + (uint32_t)(hc * 32), v[0]);
+        tmem_ld32_nowait(tm + lane_off + (uint32_t)(64 + hc * 32), v[1]);
+        tmem_ld_wait32(v[0]);
+        tmem_ld_wait32(v[1]);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(s_free);                        // the tensor core may overwrite the scores
+        // masks only where the tile meets the diagonal or the end of the keys (uniform): MODE 0 hides columns below `lo`, MODE 1 from `lo` on
+        int lo;
+        bool masked;
+        if (MODE == 0) {
+          masked = it.f0 + 128 > it.len || (a.causal && it.f0 + 127 > x0);
+          lo = frow >= it.len ? kDbX : a.causal ? frow - x0 : 0;
+        } else {
+          masked = x0 + kDbX > min(it.len, a.causal ? it.f0 + 1 : a.S);
+          lo = min(it.len, a.causal ? frow + 1 : a.S) - x0;
+        }
+        lo -= hc * 32;
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (MODE == 0 ? i < lo : i >= lo) v[0][i] = v[1][i] = 0xff800000u;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          uint64_t l1, l2;
+          if (MODE == 0) {
+            const float4 c = *reinterpret_cast<const float4*>(cv + i * 8);
+            l1 = f2_pack(c.x, c.y);
+            l2 = f2_pack(c.z, c.w);
+          } else {
+            l1 = f2_pack(nl[0], nl[0]);
+            l2 = f2_pack(nl[1], nl[1]);
+          }
+          float p, s;
+          f2_unpack(f2_fma(f2_pack(__uint_as_float(v[0][2 * i]), __uint_as_float(v[0][2 * i + 1])), sc2, l1), p, s);
+          v[0][2 * i] = __float_as_uint(ex2_approx(p));
+          v[0][2 * i + 1] = __float_as_uint(ex2_approx(s));
+          f2_unpack(f2_fma(f2_pack(__uint_as_float(v[1][2 * i]), __uint_as_float(v[1][2 * i + 1])), sc2, l2), p, s);
+          v[1][2 * i] = __float_as_uint(ex2_approx(p));
+          v[1][2 * i + 1] = __float_as_uint(ex2_approx(s));
+        }
+        ready = mbar_wait(dp_full, (uint32_t)(g & 1));
+        if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 9);
+        ok = __all_sync(0xffffffffu, ready);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t d[32], w1[16], w2[16], wv[16];
+        tmem_ld32_nowait(tDP + lane_off + (uint32_t)(hc * 32), d);
+        tmem_ld_wait32(d);
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (MODE == 0 ? i < lo : i >= lo) d[i] = 0u;           // (what a hidden key's value holds does not matter)
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          uint64_t d1, d2;
+          if (MODE == 0) {
+            const float4 c = *reinterpret_cast<const float4*>(cv + i * 8 + 4);
+            d1 = f2_pack(c.x, c.y);
+            d2 = f2_pack(c.z, c.w);
+          } else {
+            d1 = f2_pack(nd[0], nd[0]);
+            d2 = f2_pack(nd[1], nd[1]);
+          }
+          const uint64_t dp = f2_pack(__uint_as_float(d[2 * i]), __uint_as_float(d[2 * i + 1]));
+          const uint64_t p1 = f2_pack(__uint_as_float(v[0][2 * i]), __uint_as_float(v[0][2 * i + 1]));
+          const uint64_t p2 = f2_mul(f2_pack(__uint_as_float(v[1][2 * i]), __uint_as_float(v[1][2 * i + 1])), nlam2);
+          float e0, e1;
+          f2_unpack(f2_mul(p1, f2_add(dp, d1)), e0, e1);
+          w1[i] = bf16_pair(e0, e1);
+          f2_unpack(f2_mul(p2, f2_add(dp, d2)), e0, e1);
+          w2[i] = bf16_pair(e0, e1);
+          if (MODE == 0) {
+            f2_unpack(f2_add(p1, p2), e0, e1);
+            wv[i] = bf16_pair(e0, e1);
+          }
+        }
+        // dP of this step is behind the accumulating products of the last one: what they read may be overwritten
+        if (MODE == 0) {
+          tmem_st16(tP + lane_off + (uint32_t)(hc * 16), wv);
+          tmem_st16(tP + lane_off + 32u + (uint32_t)(hc * 16), w1);
+          tmem_st16(tDP + lane_off + (uint32_t)(hc * 32), w2);
+        } else {
+          tmem_st16(tP + lane_off + (uint32_t)(hc * 16), w1);
+          tmem_st16(tP + lane_off + 32u + (uint32_t)(hc * 16), w2);
+        }
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_ready);
+        x = nx;
+        h = nh;
+      }
+      if (!ok) break;
+      // ---------------- accumulators -> global: this warp's 32 rows x half of the columns, dk (or dq) and dv, through its piece
+      const bool ready = mbar_wait(acc_full, (uint32_t)(n & 1));
+      if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 9);
+      ok = __all_sync(0xffffffffu, ready);
+      if (!ok) break;
+      tc_fence_after();
+      // heads of 128: this warp's 64 columns; heads of 64: its 32 of the 64
+      constexpr int CW = DH / 2;
+      uint32_t o0[MODE == 0 ? CW : 1], o1[CW];
+#pragma unroll
+      for (int c = 0; c < CW; c += 32) {
+        tmem_ld32_nowait(tAcc + lane_off + (uint32_t)(hc * CW + c), reinterpret_cast<uint32_t (&)[32]>(o1[c]));
+        if (MODE == 0) tmem_ld32_nowait(tDv + lane_off + (uint32_t)(hc * CW + c), reinterpret_cast<uint32_t (&)[32]>(o0[MODE == 0 ? c : 0]));
+      }
+#pragma unroll
+      for (int c = 0; c < CW; c += 32) {
+        tmem_ld_wait32(reinterpret_cast<uint32_t (&)[32]>(o1[c]));
+        if (MODE == 0) tmem_ld_wait32(reinterpret_cast<uint32_t (&)[32]>(o0[MODE == 0 ? c : 0]));
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(acc_free);
+      const int row = it.f0 + q * 32;
+      auto store = [&](const uint32_t (&o)[CW], float mul, int column) {
+        if (lane == 0) bulk_wait_read();                           // what left through the piece before
+        __syncwarp();
+#pragma unroll
+        for (int sg = 0; sg < CW / 8; ++sg) {
+          uint32_t w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = bf16_pair(__uint_as_float(o[8 * sg + 2 * i]) * mul, __uint_as_float(o[8 * sg + 2 * i + 1]) * mul);
+          // 128-byte rows, swizzled over 128 bytes (heads of 128), or 64-byte rows, swizzled over 64
+          const int at = DH == 128 ? lane * 128 + ((sg ^ (lane & 7)) << 4) : lane * 64 + ((sg ^ ((lane >> 1) & 3)) << 4);
+          *reinterpret_cast<uint4*>(mine - lane * 128 + at) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (row < a.S) tma_store_3d(&map_out, sPiece, column + hc * CW, row, it.b);
+          bulk_commit();
+        }
+      };
+      store(o1, a.scale, (MODE == 0 ? a.H + it.hk : it.hk) * DH);
+      if constexpr (MODE == 0) store(o0, 1.0f, (a.H + a.K + it.hk) * DH);
+    }
+    if (lane == 0) bulk_wait();
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    __syncwarp();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "r"(512) : "memory");
+  }
+}
