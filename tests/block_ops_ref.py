@@ -2,6 +2,7 @@
 in 8 bits, written from their formulas with torch in double precision, with the error bounds of their 16-bit forms."""
 import math
 
+import numpy as np
 import torch
 
 UB = 2.0 ** -8          # half a step of bf16, relative
@@ -156,6 +157,11 @@ def dattn_bwd(qkv, lam, gain, eps, c, o, o2, lse, dy, B, S, H, K, D, causal, len
 
 
 # ------------------------------------------------------------------ 8 bits
+def pow2(e):
+    """2 ** e of whole numbers, exactly."""
+    return torch.from_numpy(np.ldexp(1.0, e.cpu().numpy().astype(np.int64))).to(e.device)
+
+
 def pack(x, fmt, parts=1):
     """Values in range and scale exponents' bytes; x [rows, parts * f] fp64 of finite values (non-finite blocks: byte 255, zeros)."""
     rows, f = x.shape[0], x.shape[1] // parts
@@ -166,11 +172,11 @@ def pack(x, fmt, parts=1):
     e = torch.full(top.shape, -110, dtype=torch.int64, device=x.device)
     for n in range(-110, 128):                                   # the least power of two that brings it into range
         e = torch.where(top > (448.0 if fmt else 127.0) * 2.0 ** n, n + 1, e)
-    v = x / torch.pow(torch.tensor(2.0, dtype=torch.float64, device="cpu"), e.cpu().double()).to(x.device)[..., None]
+    v = x / pow2(e)[..., None]
     if fmt == 0:
         v = v.round()
     else:
-        step = torch.ldexp(torch.ones((), dtype=torch.float64), (torch.frexp(v.cpu())[1].clamp(min=-5) - 4)).to(x.device)
+        step = pow2(torch.frexp(v)[1].clamp(min=-5) - 4)
         v = (v / step).round() * step
     byte = torch.where(bad, 255, e + 127)
     return v.flatten(2)[..., :f].reshape(rows, parts * f), byte.flatten(1)
@@ -179,7 +185,7 @@ def pack(x, fmt, parts=1):
 def unpack(q, byte, parts=1):
     """What 8-bit values [rows, parts * f] (as numbers) stand for."""
     rows, f = q.shape[0], q.shape[1] // parts
-    s = torch.ldexp(torch.ones((), dtype=torch.float64), byte.cpu().int() - 127).to(q.device)
+    s = pow2(byte.int() - 127)
     s = torch.where(byte == 255, math.nan, s).view(rows, parts, -1).repeat_interleave(32, 2)[..., :f]
     return q.double() * s.reshape(rows, parts * f)
 
