@@ -31,8 +31,10 @@ __device__ __forceinline__ float act8_inverse(int byte) { return byte == 255 ? 0
 // four values, scaled into range, as four bytes; round to nearest even
 template <int FMT> __device__ __forceinline__ uint32_t act8_quad(float a, float b, float c, float d) {
   if (FMT == 0) {
-    const uint32_t i = (uint32_t)__float2int_rn(a) & 255u, j = (uint32_t)__float2int_rn(b) & 255u;
-    return i | j << 8 | ((uint32_t)__float2int_rn(c) & 255u) << 16 | (uint32_t)__float2int_rn(d) << 24;
+    // |v| <= 127: added to 1.5 * 2^23, whose step is 1, v is rounded to nearest even and its two's complement is the low byte (a conversion
+    // instruction has an eighth of an addition's rate)
+    const uint32_t lo = __byte_perm(__float_as_uint(a + 12582912.0f), __float_as_uint(b + 12582912.0f), 0x0040);
+    return __byte_perm(lo, __byte_perm(__float_as_uint(c + 12582912.0f), __float_as_uint(d + 12582912.0f), 0x0040), 0x5410);
   }
   const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
   return lo | (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3) << 16;
@@ -40,7 +42,8 @@ template <int FMT> __device__ __forceinline__ uint32_t act8_quad(float a, float 
 template <int FMT> __device__ __forceinline__ void act8_unquad(uint32_t q, float (&v)[4]) {
   if (FMT == 0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (float)(int8_t)(q >> 8 * i);
+    for (int i = 0; i < 4; ++i)                              // 2^23 + (value + 128) as fp32 from its bytes, less 2^23 + 128
+      v[i] = __uint_as_float(__byte_perm(q ^ 0x80808080u, 0x4B000000u, 0x7540 + i)) - 8388736.0f;
   } else {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -91,12 +94,43 @@ template <int KIND> __device__ __forceinline__ void act8_grad(float g, float a, 
     da = g * fmaf(a, 0.39894228040143267794f * __expf(-0.5f * a * a), cdf);
     y = a * cdf;
   } else {
-    // 1 - sigmoid(a) as sigmoid(-a): no digits are lost where the sigmoid is nearly 1
-    const float sig = act8_sigmoid(a), rest = act8_sigmoid(-a), s = a * sig;
+    // 1 - sigmoid(a) as exp(-a) sigmoid(a) where the sigmoid is nearly 1: no digits are lost
+    const float e = __expf(-a), sig = __fdividef(1.0f, 1.0f + e), rest = a > 0.f ? e * sig : 1.0f - sig, s = a * sig;
     da = g * u * sig * fmaf(a, rest, 1.0f);
     du = g * s;
     y = s * u;
   }
+}
+
+// 8 elements as they lie in memory; as floats; and the bits of the largest magnitude (those of a NaN are above infinity's)
+template <typename T> struct Act8Raw { uint4 w[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ void act8_load(const T* p, Act8Raw<T>& r) {
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = reinterpret_cast<const uint4*>(p)[i];
+}
+__device__ __forceinline__ uint32_t act8_floats(const Act8Raw<float>& r, float (&v)[8]) {
+  const uint32_t w[8] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w, r.w[1].x, r.w[1].y, r.w[1].z, r.w[1].w};
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    v[j] = __uint_as_float(w[j]);
+    top = max(top, w[j] & 0x7FFFFFFFu);
+  }
+  return top;
+}
+__device__ __forceinline__ uint32_t act8_floats(const Act8Raw<bf16>& r, float (&v)[8]) {
+  const uint32_t w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
+  __nv_bfloat162 h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    const uint32_t b = w[i] & 0x7FFF7FFFu;
+    h[i] = *reinterpret_cast<const __nv_bfloat162*>(&b);
+  }
+  const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+  const uint32_t u = *reinterpret_cast<const uint32_t*>(&m);
+  return max(u << 16, u & 0xFFFF0000u);
 }
 
 // ---- 8 columns a thread -------------------------------------------------------------------------------------------------------------
@@ -111,20 +145,14 @@ __global__ void __launch_bounds__(256) act8_fwd_vec_kernel(Act8 p) {
   int c;
   const bool in = act8_place(p, units, row, c) && 8 * c < p.f;
   float v[N][8];
+  Act8Raw<T> raw[N] = {};
+  if (in) {
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    if (in) {
-      load8((const T*)p.x + row * p.ld + n * p.f + 8 * c, v[n]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[n][j] = 0.f;
-    }
+    for (int n = 0; n < N; ++n) act8_load((const T*)p.x + row * p.ld + n * p.f + 8 * c, raw[n]);
   }
 #pragma unroll
   for (int n = 0; n < N; ++n) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[n][j]) & 0x7FFFFFFFu);
+    uint32_t top = act8_floats(raw[n], v[n]);
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const int byte = act8_byte<FMT>(top);

@@ -1,9 +1,9 @@
 // Rotary positions on caller-owned buffers: the pairs of the first `rot` elements of every head turned by angle(pos, j),
 //   y1 = x1 cos - x2 sin,   y2 = x2 cos + x1 sin     (the gradient: the same with -sin),
 // pair j = (j, j + rot / 2) in the half layout, (2 j, 2 j + 1) in the interleaved one; the rest of a head is copied.
-// Memory bounds it: every element is read and written once.  A thread takes 2 V elements (V pairs) of up to G heads of one row, so that
-// it loads its V cosines and sines once for them and has 2 G loads of 16 bytes in flight.
-// 16384 rows x 40 heads x 128, half of each head rotated, bf16: see the table of the operators for the figures.
+// Memory bounds it: every element is read and written once.  A thread takes 2 V elements (V pairs, two loads of 16 bytes) of one head; its V
+// cosines and sines come from L1 and L2.  (Four heads a thread, which loads them once for the four, costs 90 registers: 69 -> 82 us for 16384 rows x
+// 40 heads x 128 bf16, half of each head turned.)
 #pragma once
 #include "common.cuh"
 
@@ -21,33 +21,28 @@ struct RopeOp {
 
 template <typename T, int V> struct alignas(sizeof(T) * V) RopeVec { T v[V]; };
 
-template <typename T, int V, int LAYOUT, int G>
+template <typename T, int V, int LAYOUT>
 __global__ void __launch_bounds__(256) rope_rows_kernel(RopeOp p) {
   pdl_launch_next();
   pdl_wait_prior();
   typedef RopeVec<T, V> Vec;
   const int half = p.rot / 2, turn_units = half / V, units = turn_units + p.copy_units;
-  const int per_row = units * ((p.heads + G - 1) / G);
+  const int per_row = units * p.heads;
   const int i = blockIdx.y * 256 + threadIdx.x;
   const int rb = i / per_row, k = i - rb * per_row;
   const int64_t row = (int64_t)blockIdx.x * p.rows_per_block + rb;
   if (rb >= p.rows_per_block || row >= p.rows) return;
-  const int h0 = k / units * G, u = k - k / units * units;
-  const T* xr = (const T*)p.x + row * p.ld;
-  T* yr = (T*)p.out + row * p.ld_out;
+  const int h = k / units, u = k - h * units;
+  const T* x = (const T*)p.x + row * p.ld + (int64_t)h * p.dh;
+  T* y = (T*)p.out + row * p.ld_out + (int64_t)h * p.dh;
   if (u >= turn_units) {                                   // behind the rotated part: copied
     const int e = p.rot + (u - turn_units) * 2 * V;
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      if (h0 + g >= p.heads) break;
-      const int64_t at = (int64_t)(h0 + g) * p.dh + e;
-      if (V > 1 || e + 1 < p.dh) {
-        const Vec a = *reinterpret_cast<const Vec*>(xr + at), b = *reinterpret_cast<const Vec*>(xr + at + V);
-        *reinterpret_cast<Vec*>(yr + at) = a;
-        *reinterpret_cast<Vec*>(yr + at + V) = b;
-      } else {
-        yr[at] = xr[at];
-      }
+    if (V > 1 || e + 1 < p.dh) {
+      const Vec a = *reinterpret_cast<const Vec*>(x + e), b = *reinterpret_cast<const Vec*>(x + e + V);
+      *reinterpret_cast<Vec*>(y + e) = a;
+      *reinterpret_cast<Vec*>(y + e + V) = b;
+    } else {
+      y[e] = x[e];
     }
     return;
   }
@@ -57,47 +52,39 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(RopeOp p) {
     if (p.bad && k == 0) *p.bad = 1;
     pos = 0;
   }
-  float c[V], s[V];
+  alignas(16) float c[V], s[V];
   const float* ct = p.cs + (int64_t)pos * half + u * V;
   const float* st = ct + (int64_t)p.n_pos * half;
+  typedef RopeVec<float, (V < 4 ? V : 4)> Cs;
 #pragma unroll
-  for (int j = 0; j < V; ++j) {                            // consecutive words, which the compiler may not assume to be aligned
-    c[j] = in ? ct[j] : 1.f;
-    s[j] = in ? st[j] * p.sign : 0.f;
+  for (int j = 0; j < V; j += (V < 4 ? V : 4)) {
+    *reinterpret_cast<Cs*>(c + j) = *reinterpret_cast<const Cs*>(ct + j);
+    *reinterpret_cast<Cs*>(s + j) = *reinterpret_cast<const Cs*>(st + j);
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    c[j] = in ? c[j] : 1.f;
+    s[j] = in ? s[j] * p.sign : 0.f;
   }
   const int e0 = LAYOUT == 0 ? u * V : u * 2 * V, e1 = LAYOUT == 0 ? e0 + half : e0 + V;
-  Vec a[G], b[G];
+  const Vec a = *reinterpret_cast<const Vec*>(x + e0), b = *reinterpret_cast<const Vec*>(x + e1);
+  Vec o0, o1;
 #pragma unroll
-  for (int g = 0; g < G; ++g) {
-    if (h0 + g < p.heads) {
-      const T* x = xr + (int64_t)(h0 + g) * p.dh;
-      a[g] = *reinterpret_cast<const Vec*>(x + e0);
-      b[g] = *reinterpret_cast<const Vec*>(x + e1);
+  for (int j = 0; j < V; ++j) {                            // fp32, rounded once
+    if (LAYOUT == 0) {
+      const float x1 = to_f(a.v[j]), x2 = to_f(b.v[j]);
+      o0.v[j] = from_f<T>(x1 * c[j] - x2 * s[j]);
+      o1.v[j] = from_f<T>(x2 * c[j] + x1 * s[j]);
+    } else {                                               // pair j lies at elements 2 j, 2 j + 1 of the 2 V
+      const float x1 = 2 * j < V ? to_f(a.v[(2 * j) % V]) : to_f(b.v[(2 * j) % V]);
+      const float x2 = 2 * j + 1 < V ? to_f(a.v[(2 * j + 1) % V]) : to_f(b.v[(2 * j + 1) % V]);
+      const T y1 = from_f<T>(x1 * c[j] - x2 * s[j]), y2 = from_f<T>(x2 * c[j] + x1 * s[j]);
+      if (2 * j < V) o0.v[(2 * j) % V] = y1; else o1.v[(2 * j) % V] = y1;
+      if (2 * j + 1 < V) o0.v[(2 * j + 1) % V] = y2; else o1.v[(2 * j + 1) % V] = y2;
     }
   }
-#pragma unroll
-  for (int g = 0; g < G; ++g) {
-    if (h0 + g < p.heads) {
-      T* y = yr + (int64_t)(h0 + g) * p.dh;
-      Vec o0, o1;
-#pragma unroll
-      for (int j = 0; j < V; ++j) {                        // fp32, rounded once
-        if (LAYOUT == 0) {
-          const float x1 = to_f(a[g].v[j]), x2 = to_f(b[g].v[j]);
-          o0.v[j] = from_f<T>(x1 * c[j] - x2 * s[j]);
-          o1.v[j] = from_f<T>(x2 * c[j] + x1 * s[j]);
-        } else {                                           // pair j lies at elements 2 j, 2 j + 1 of the 2 V
-          const float x1 = 2 * j < V ? to_f(a[g].v[(2 * j) % V]) : to_f(b[g].v[(2 * j) % V]);
-          const float x2 = 2 * j + 1 < V ? to_f(a[g].v[(2 * j + 1) % V]) : to_f(b[g].v[(2 * j + 1) % V]);
-          const T y1 = from_f<T>(x1 * c[j] - x2 * s[j]), y2 = from_f<T>(x2 * c[j] + x1 * s[j]);
-          if (2 * j < V) o0.v[(2 * j) % V] = y1; else o1.v[(2 * j) % V] = y1;
-          if (2 * j + 1 < V) o0.v[(2 * j + 1) % V] = y2; else o1.v[(2 * j + 1) % V] = y2;
-        }
-      }
-      *reinterpret_cast<Vec*>(y + e0) = o0;
-      *reinterpret_cast<Vec*>(y + e1) = o1;
-    }
-  }
+  *reinterpret_cast<Vec*>(y + e0) = o0;
+  *reinterpret_cast<Vec*>(y + e1) = o1;
 }
 
 // The table of cosines and sines: angle(pos, j) = (pos * pos_scale) * freq(j) in 64 bits, the cosine and sine rounded once, times `mag`.
@@ -145,22 +132,21 @@ template <typename T, int V>
 cudaError_t launch_rope_v(cudaStream_t st, int layout, RopeOp p) {
   // the rest of a head is in place already where x is the output
   p.copy_units = p.x == p.out ? 0 : (p.dh - p.rot + 2 * V - 1) / (2 * V);
-  const int units = p.rot / 2 / V + p.copy_units;
-  // four heads a thread where that still gives every SM its 2048 threads
-  const bool four = p.rows * units * ((p.heads + 3) / 4) >= 148 * 2048;
-  const int64_t per_row = (int64_t)units * (four ? (p.heads + 3) / 4 : p.heads);
-  p.rows_per_block = per_row >= 256 ? 1 : (int)(256 / per_row);
+  const int64_t per_row = (int64_t)(p.rot / 2 / V + p.copy_units) * p.heads;
+  // rows to a block column: so many that the last of its blocks is at most a 16th of them
+  p.rows_per_block = (int)((4095 + per_row) / per_row);
+  if (p.rows_per_block > p.rows) p.rows_per_block = (int)p.rows;
   const dim3 g((unsigned)((p.rows + p.rows_per_block - 1) / p.rows_per_block), (unsigned)((per_row * p.rows_per_block + 255) / 256));
-  if (layout == 0) return launch_pdl(four ? rope_rows_kernel<T, V, 0, 4> : rope_rows_kernel<T, V, 0, 1>, g, dim3(256), 0, st, p);
-  return launch_pdl(four ? rope_rows_kernel<T, V, 1, 4> : rope_rows_kernel<T, V, 1, 1>, g, dim3(256), 0, st, p);
+  return launch_pdl(layout == 0 ? rope_rows_kernel<T, V, 0> : rope_rows_kernel<T, V, 1>, g, dim3(256), 0, st, p);
 }
-// The widest vector (16 bytes at most) that divides the halves of the rotated part, the rest of a head, heads and rows, and fits the addresses.
+// The widest vector (16 bytes at most) that divides the halves of the rotated part, the rest of a head, heads and rows, and fits the addresses
+// (the table's too: rot / 2 is a multiple of v).
 template <typename T>
 cudaError_t launch_rope(cudaStream_t st, int layout, const RopeOp& p) {
   auto fits = [&](int v) {
     const int64_t b = v * (int64_t)sizeof(T);
     return p.rot % (2 * v) == 0 && (p.dh - p.rot) % (2 * v) == 0 && p.ld % v == 0 && p.ld_out % v == 0 &&
-           (((uintptr_t)p.x | (uintptr_t)p.out) & (uintptr_t)(b - 1)) == 0;
+           (((uintptr_t)p.x | (uintptr_t)p.out) & (uintptr_t)(b - 1)) == 0 && ((uintptr_t)p.cs & (uintptr_t)(v >= 4 ? 15 : 4 * v - 1)) == 0;
   };
   if (sizeof(T) == 2 && fits(8)) return launch_rope_v<T, sizeof(T) == 2 ? 8 : 4>(st, layout, p);
   if (fits(4)) return launch_rope_v<T, 4>(st, layout, p);
