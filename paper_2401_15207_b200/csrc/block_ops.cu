@@ -111,6 +111,7 @@ hift_status hift_k_diff_attention_fwd(int32_t dtype, int32_t B, int32_t S, int32
   if (!elements(dtype, {qkv, gain, o, o2, y}) || !words(lam, lse, key_lens)) return HIFT_ERR_CFG;
   DattnArgs a = dattn_args(B, S, H, K, D, causal, qkv, lam, gain, eps, out_scale, key_lens);
   a.o = o; a.o2 = o2; a.y = y; a.lse = lse;
+  a.vec = aligned(qkv, 16);
   cudaStream_t st = (cudaStream_t)stream;
   if (dattn_tc_eligible(dtype, D, a)) return status_of(dattn_tc_fwd_launch(st, D, a));
   return status_of(dtype == 0 ? launch_dattn_fwd<float>(st, D, a) : launch_dattn_fwd<bf16>(st, D, a));
@@ -144,12 +145,13 @@ hift_status hift_k_diff_attention_bwd(int32_t dtype, int32_t B, int32_t S, int32
   a.o = (void*)o; a.o2 = (void*)o2; a.lse = (float*)lse; a.dy = dy; a.dqkv = dqkv;
   a.dsum = (float*)(w + pl.dsum);
   a.g = gain ? (void*)(w + pl.g) : dy;
+  a.vec = aligned(qkv, 16) && aligned(a.g, 16);
   float* dlam_part = (float*)(w + pl.part);
   const DattnPrep p{a, gain ? (void*)(w + pl.g) : nullptr, (float*)(w + pl.dsum), dlam_part, dlam_part + (size_t)H * pl.chunks, pl.chunks, pl.rows_per_chunk};
   cudaError_t e = dtype == 0 ? launch_dattn_prep<float>(st, D, p) : launch_dattn_prep<bf16>(st, D, p);
   if (e == cudaSuccess && (dlam || dgain)) {
     const int blocks = H + (dgain ? (D + 31) / 32 : 0);
-    e = launch_pdl(dattn_sums_kernel, dim3((unsigned)blocks), dim3(256), 0, st, (const float*)p.dlam_part, (const float*)p.dgain_part, dlam, dgain, H, pl.chunks, D);
+    e = launch_pdl(dattn_sums_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)p.dlam_part, (const float*)p.dgain_part, dlam, dgain, H, pl.chunks, D);
   }
   if (e != cudaSuccess) return status_of(e);
   if (dattn_tc_eligible(dtype, D, a)) return status_of(dattn_tc_bwd_launch(st, D, a));

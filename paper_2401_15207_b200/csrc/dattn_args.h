@@ -11,6 +11,7 @@ struct DattnArgs {
   const void* dy; const void* g; const float* dsum;        // g: gradient of o (dy itself without a norm); dsum: D_1 | D_2, each [B, H, S]
   void* dqkv;
   int B, S, H, K, causal;
+  int vec;                                                 // qkv and g start at 16-byte boundaries
   float scale, eps, c;
 };
 

@@ -10,7 +10,7 @@
 // dk and dq are multiplied by `scale` as they are stored.  dP is shared by the maps, and dv takes one product for both: 8 units of 128 x 64 x 64 a
 // step against the 10 of two plain attentions.  P and dS are rounded to bf16, the operand type of the products they feed; the accumulators are fp32.
 //   warp 0    : TMA producer         warp 1: issues every product (one elected thread); owns the tensor memory
-//   warps 4-11: element-wise, two warps to a lane quarter, 32 of the 64 streamed columns each: S_1, S_2 -> registers, exponentials; dP -> registers, dS;
+//   warps 4-19: element-wise, four warps to a lane quarter, 16 of the 64 streamed columns each: S_1, S_2 -> registers, exponentials; dP -> registers, dS;
 //               P and dS go back to tensor memory as bf16, the A operands of the accumulating products; at an item's end the accumulators -> global
 // Order of issue: S(t+1) as soon as S(t) has been read, so that it runs beside the exponentials of step t; then the accumulating products of t; then
 // dP(t+1), which therefore finds both its buffer and the P / dS buffers of step t free when it is done.
@@ -19,15 +19,19 @@
 // What bounds it: products 1276 cycles a step at heads of 128 (1024 in MODE 1), exponentials 1024, both of the 128 x 64 tile.
 #pragma once
 
-constexpr int kDbThreads = 384, kDbX = 64, kDbStages = 3;
+constexpr int kDbThreads = 640, kDbEw = 16, kDbX = 64, kDbStages = 3;
 template <int DH, int MODE> struct DattnBwdCfg {
   static constexpr int kSpans = DH / 64;
   static constexpr int kFBytes = 128 * DH * 2, kXBytes = kDbX * DH * 2;
-  static constexpr int kStage = 8 * 4096;                          // a 32 x 64 bf16 piece per element-wise warp
-  static constexpr int kCol = MODE == 0 ? 8 * 2 * 512 : 0;         // per warp, two steps: lse and D of its 32 queries
+  static constexpr int kStage = kDbEw * 32 * (DH / 4) * 2;         // a piece of 32 rows x a quarter of the columns per element-wise warp
+  static constexpr int kCol = MODE == 0 ? kDbEw * 2 * 256 : 0;     // per warp, two steps: lse and D of its 16 queries
   static constexpr int kSmem = 2 * kFBytes + kDbStages * 2 * kXBytes + kStage + kCol + 256 + 1024;
 };
 
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
 struct DattnBwdItem { int b, hk, f0, x_lo, per, nsteps, len; };    // hk: key head (MODE 0) or query head (MODE 1); per: steps of one head
 
 template <int DH, int MODE>
@@ -72,8 +76,8 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
 
   if (threadIdx.x == 0) {
     mbar_init(f_full, 1); mbar_init(f_empty, 1);
-    mbar_init(s_full, 1); mbar_init(s_free, 8); mbar_init(dp_full, 1); mbar_init(p_ready, 8);
-    mbar_init(acc_full, 1); mbar_init(acc_free, 8);
+    mbar_init(s_full, 1); mbar_init(s_free, kDbEw); mbar_init(dp_full, 1); mbar_init(p_ready, kDbEw);
+    mbar_init(acc_full, 1); mbar_init(acc_free, kDbEw);
     for (int i = 0; i < NS; ++i) { mbar_init(x_full(i), 1); mbar_init(x_empty(i), 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_wait();                                                    // no global access before it, the flag included
@@ -180,7 +184,7 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
             for (int kk = 0; kk < 4; ++kk) {
               // the map's half of X0's columns: the second span (heads of 128), or the second half of the one span
               const uint64_t b = nX0 + (uint64_t)((kk * 16 * 128 + m * (DH == 128 ? XSPAN : 64)) >> 4);
-              const uint32_t p = MODE == 0 ? (m == 0 ? tP + 32u + kk * 8u : tDP + (kk >> 1) * 32u + (kk & 1) * 8u) : tP + m * 32u + kk * 8u;
+              const uint32_t p = MODE == 0 ? (m == 0 ? tP + 32u + kk * 8u : tDP + kk * 16u) : tP + m * 32u + kk * 8u;
               tc_mma_ta(tAcc + (uint32_t)(m * HD), p, b, idesc_h, (t > 0 || kk > 0) ? 1u : 0u);
             }
           }
@@ -212,62 +216,68 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
       __syncwarp();
     }
   } else if (warp >= 4) {
-    // ---------------- element-wise: thread = row of the fixed tile x 32 streamed columns
+    // ---------------- element-wise: thread = row of the fixed tile x 16 streamed columns
     const int q = warp & 3, hc = (warp - 4) >> 2, r = q * 32 + lane;
     const uint32_t lane_off = (uint32_t)(q * 32) << 16;
     const float sl2 = a.scale * 1.4426950408889634f;
     const uint64_t sc2 = f2_pack(sl2, sl2);
     const int64_t nrow = (int64_t)a.B * a.H * a.S;
-    const uint32_t sPiece = sStage + (warp - 4) * 4096;
-    uint8_t* mine = gen + (sPiece - base) + lane * 128;
-    float* col = reinterpret_cast<float*>(gen + (sCol - base)) + (warp - 4) * 256;      // MODE 0: two buffers of 16 column pairs x (-lse_1, -lse_2, -D_1, -D_2)
+    const uint32_t sPiece = sStage + (warp - 4) * (32 * (DH / 4) * 2);
+    uint8_t* piece = gen + (sPiece - base);
+    float* col = reinterpret_cast<float*>(gen + (sCol - base)) + (warp - 4) * 128;      // MODE 0: two buffers of 8 column pairs x (-lse_1, -lse_2, -D_1, -D_2)
     bool ok = !poisoned;
     int n = 0, g = 0;
-    // -lse (log2 units) and -D of one query and map; a query that sees no key, or none: P = 0 through -infinity
-    auto neg_lse = [&](int m, int64_t at, bool in) -> float {
-      const float v = in ? a.lse[m * nrow + at] : -INFINITY;
-      return v == -INFINITY ? -INFINITY : -v * 1.4426950408889634f;
-    };
+    // -lse in log2 units; a query that sees no key, or is none: P = 0 through -infinity
+    auto neg_log2 = [](float v) { return v == -INFINITY ? -INFINITY : -v * 1.4426950408889634f; };
     for (int idx = dattn_item_at(n); idx < nitems && ok; idx = dattn_item_at(++n)) {
       const DattnBwdItem it = item_of(idx);
       const int frow = it.f0 + r;
       int x = it.x_lo, h = MODE == 0 ? it.hk * group : it.hk;
-      float nl[2] = {0.f, 0.f}, nd[2] = {0.f, 0.f};
-      // MODE 0: this lane's column of the next step; MODE 1: this thread's row
+      // lse and D as they lie in memory, of this lane's column of the next step (MODE 0; nothing touches them before that step, so that no step waits
+      // for them) or of this thread's row (MODE 1)
+      float rl[2], rd[2];
       auto fetch = [&](int xx, int hh) {
-        const int c = MODE == 0 ? xx * kDbX + hc * 32 + lane : frow;
+        const int c = MODE == 0 ? xx * kDbX + hc * 16 + (lane & 15) : frow;
         const bool in = c < a.S;
-        const int64_t at = ((int64_t)it.b * a.H + hh) * a.S + c;
+        const int64_t at = ((int64_t)it.b * a.H + hh) * a.S + (in ? c : 0);
 #pragma unroll
         for (int m = 0; m < 2; ++m) {
-          nl[m] = neg_lse(m, at, in);
-          nd[m] = in ? -a.dsum[m * nrow + at] : 0.f;
+          rl[m] = in ? a.lse[m * nrow + at] : -INFINITY;
+          rd[m] = in ? a.dsum[m * nrow + at] : 0.f;
         }
       };
       fetch(x, h);
+      float lam = a.lam[h], lam_next = lam;
+      float nl[2], nd[2];                                          // MODE 1
+      if (MODE == 1) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m) { nl[m] = neg_log2(rl[m]); nd[m] = -rd[m]; }
+      }
       for (int t = 0; t < it.nsteps; ++t, ++g) {
         const int x0 = x * kDbX;
-        const float lam = a.lam[h];
         const uint64_t nlam2 = f2_pack(-lam, -lam);
-        float* cv = col + (g & 1) * 128;
+        float* cv = col + (g & 1) * 64;
         if (MODE == 0) {
-          float* w = cv + (lane >> 1) * 8 + (lane & 1);
-          w[0] = nl[0]; w[2] = nl[1]; w[4] = nd[0]; w[6] = nd[1];
+          float* w = cv + ((lane & 15) >> 1) * 8 + (lane & 1);
+          if (lane < 16) { w[0] = neg_log2(rl[0]); w[2] = neg_log2(rl[1]); w[4] = -rd[0]; w[6] = -rd[1]; }
           __syncwarp();
         }
         int nx = x + 1, nh = h;
         if (MODE == 0 && nx == it.x_lo + it.per) { nx = it.x_lo; ++nh; }
-        if (MODE == 0 && t + 1 < it.nsteps) fetch(nx, nh);
+        if (MODE == 0 && t + 1 < it.nsteps) {
+          fetch(nx, nh);
+          if (nh != h) lam_next = a.lam[nh];
+        }
         bool ready = mbar_wait(s_full, (uint32_t)(g & 1));
         if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 9);
         ok = __all_sync(0xffffffffu, ready);
         if (!ok) break;
         tc_fence_after();
-        uint32_t v[2][32];
-        tmem_ld32_nowait(tm + lane_off + (uint32_t)(hc * 32), v[0]);
-        tmem_ld32_nowait(tm + lane_off + (uint32_t)(64 + hc * 32), v[1]);
-        tmem_ld_wait32(v[0]);
-        tmem_ld_wait32(v[1]);
+        uint32_t v[2][16];
+        tmem_ld16_nowait(tm + lane_off + (uint32_t)(hc * 16), v[0]);
+        tmem_ld16_nowait(tm + lane_off + (uint32_t)(64 + hc * 16), v[1]);
+        tmem_ld_wait16(v[0]);
+        tmem_ld_wait16(v[1]);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(s_free);                        // the tensor core may overwrite the scores
@@ -281,14 +291,14 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
           masked = x0 + kDbX > min(it.len, a.causal ? it.f0 + 1 : a.S);
           lo = min(it.len, a.causal ? frow + 1 : a.S) - x0;
         }
-        lo -= hc * 32;
+        lo -= hc * 16;
         if (masked) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
+          for (int i = 0; i < 16; ++i)
             if (MODE == 0 ? i < lo : i >= lo) v[0][i] = v[1][i] = 0xff800000u;
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 8; ++i) {
           uint64_t l1, l2;
           if (MODE == 0) {
             const float4 c = *reinterpret_cast<const float4*>(cv + i * 8);
@@ -311,16 +321,16 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         ok = __all_sync(0xffffffffu, ready);
         if (!ok) break;
         tc_fence_after();
-        uint32_t d[32], w1[16], w2[16], wv[16];
-        tmem_ld32_nowait(tDP + lane_off + (uint32_t)(hc * 32), d);
-        tmem_ld_wait32(d);
+        uint32_t d[16], w1[8], w2[8], wv[8];
+        tmem_ld16_nowait(tDP + lane_off + (uint32_t)(hc * 16), d);
+        tmem_ld_wait16(d);
         if (masked) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
+          for (int i = 0; i < 16; ++i)
             if (MODE == 0 ? i < lo : i >= lo) d[i] = 0u;           // (what a hidden key's value holds does not matter)
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < 8; ++i) {
           uint64_t d1, d2;
           if (MODE == 0) {
             const float4 c = *reinterpret_cast<const float4*>(cv + i * 8 + 4);
@@ -345,12 +355,12 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         }
         // dP of this step is behind the accumulating products of the last one: what they read may be overwritten
         if (MODE == 0) {
-          tmem_st16(tP + lane_off + (uint32_t)(hc * 16), wv);
-          tmem_st16(tP + lane_off + 32u + (uint32_t)(hc * 16), w1);
-          tmem_st16(tDP + lane_off + (uint32_t)(hc * 32), w2);
+          tmem_st8(tP + lane_off + (uint32_t)(hc * 8), wv);
+          tmem_st8(tP + lane_off + 32u + (uint32_t)(hc * 8), w1);
+          tmem_st8(tDP + lane_off + (uint32_t)(hc * 16), w2);
         } else {
-          tmem_st16(tP + lane_off + (uint32_t)(hc * 16), w1);
-          tmem_st16(tP + lane_off + 32u + (uint32_t)(hc * 16), w2);
+          tmem_st8(tP + lane_off + (uint32_t)(hc * 8), w1);
+          tmem_st8(tP + lane_off + 32u + (uint32_t)(hc * 8), w2);
         }
         tmem_st_wait();
         tc_fence_before();
@@ -358,26 +368,27 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         if (lane == 0) mbar_arrive(p_ready);
         x = nx;
         h = nh;
+        lam = lam_next;
       }
       if (!ok) break;
-      // ---------------- accumulators -> global: this warp's 32 rows x half of the columns, dk (or dq) and dv, through its piece
+      // ---------------- accumulators -> global: this warp's 32 rows x a quarter of the columns, of dk (or dq) and of dv, through its piece
       const bool ready = mbar_wait(acc_full, (uint32_t)(n & 1));
       if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 9);
       ok = __all_sync(0xffffffffu, ready);
       if (!ok) break;
       tc_fence_after();
-      // heads of 128: this warp's 64 columns; heads of 64: its 32 of the 64
-      constexpr int CW = DH / 2;
-      uint32_t o0[MODE == 0 ? CW : 1], o1[CW];
-#pragma unroll
-      for (int c = 0; c < CW; c += 32) {
-        tmem_ld32_nowait(tAcc + lane_off + (uint32_t)(hc * CW + c), reinterpret_cast<uint32_t (&)[32]>(o1[c]));
-        if (MODE == 0) tmem_ld32_nowait(tDv + lane_off + (uint32_t)(hc * CW + c), reinterpret_cast<uint32_t (&)[32]>(o0[MODE == 0 ? c : 0]));
-      }
-#pragma unroll
-      for (int c = 0; c < CW; c += 32) {
-        tmem_ld_wait32(reinterpret_cast<uint32_t (&)[32]>(o1[c]));
-        if (MODE == 0) tmem_ld_wait32(reinterpret_cast<uint32_t (&)[32]>(o0[MODE == 0 ? c : 0]));
+      constexpr int CW = DH / 4;
+      uint32_t o1[CW], o0[MODE == 0 ? CW : 1];
+      if constexpr (CW == 32) {
+        tmem_ld32_nowait(tAcc + lane_off + (uint32_t)(hc * CW), o1);
+        if constexpr (MODE == 0) tmem_ld32_nowait(tDv + lane_off + (uint32_t)(hc * CW), o0);
+        tmem_ld_wait32(o1);
+        if constexpr (MODE == 0) tmem_ld_wait32(o0);
+      } else {
+        tmem_ld16_nowait(tAcc + lane_off + (uint32_t)(hc * CW), o1);
+        if constexpr (MODE == 0) tmem_ld16_nowait(tDv + lane_off + (uint32_t)(hc * CW), o0);
+        tmem_ld_wait16(o1);
+        if constexpr (MODE == 0) tmem_ld_wait16(o0);
       }
       tc_fence_before();
       __syncwarp();
@@ -391,9 +402,9 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
           uint32_t w[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) w[i] = bf16_pair(__uint_as_float(o[8 * sg + 2 * i]) * mul, __uint_as_float(o[8 * sg + 2 * i + 1]) * mul);
-          // 128-byte rows, swizzled over 128 bytes (heads of 128), or 64-byte rows, swizzled over 64
-          const int at = DH == 128 ? lane * 128 + ((sg ^ (lane & 7)) << 4) : lane * 64 + ((sg ^ ((lane >> 1) & 3)) << 4);
-          *reinterpret_cast<uint4*>(mine - lane * 128 + at) = make_uint4(w[0], w[1], w[2], w[3]);
+          // 64-byte rows, swizzled over 64 bytes (heads of 128), or 32-byte rows, swizzled over 32
+          const int at = DH == 128 ? lane * 64 + ((sg ^ ((lane >> 1) & 3)) << 4) : lane * 32 + ((sg ^ ((lane >> 2) & 1)) << 4);
+          *reinterpret_cast<uint4*>(piece + at) = make_uint4(w[0], w[1], w[2], w[3]);
         }
         fence_async_smem();
         __syncwarp();

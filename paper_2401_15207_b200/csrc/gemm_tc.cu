@@ -1631,7 +1631,7 @@ bool dattn_tc_eligible(int dtype, int D, const DattnArgs& a) {
   for (const void* p : {a.qkv, (const void*)a.o, (const void*)a.o2, (const void*)a.y, a.g, (const void*)a.dqkv}) all |= (uintptr_t)p;
   return (all & 15) == 0;
 }
-// qkv-like bf16 rows [B][S][cols]: box = 64 columns (128-byte swizzle) or 32 (64-byte) x box_rows rows; rows beyond S read as zeros.  Encoded at every call:
+// qkv-like bf16 rows [B][S][cols]: box = 64, 32 or 16 columns (swizzled over their 128, 64 or 32 bytes) x box_rows rows; rows beyond S read as zeros.  Encoded at every call:
 // buffers' addresses change from call to call.
 static bool dattn_map(const void* p, int64_t cols, int S, int B, uint32_t box_rows, CUtensorMap* out, uint32_t box_cols = 64) {
   cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)S, (cuuint64_t)B};
@@ -1639,7 +1639,7 @@ static bool dattn_map(const void* p, int64_t cols, int S, int B, uint32_t box_ro
   cuuint32_t box[3] = {box_cols, box_rows, 1};
   cuuint32_t estr[3] = {1, 1, 1};
   return g_encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                  box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : box_cols == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 // (the attribute belongs to a device, and operators take whichever is current; idempotent)
 template <typename... KArgs, typename... Args>
@@ -1663,7 +1663,7 @@ static cudaError_t dattn_tc_bwd_inst(cudaStream_t st, const DattnArgs& a) {
   CUtensorMap qkv_f, qkv_x, g_f, g_x, out;
   const int64_t cols = (int64_t)(a.H + 2 * a.K) * DH, gc = (int64_t)a.H * DH;
   if (!dattn_map(a.qkv, cols, a.S, a.B, 128, &qkv_f) || !dattn_map(a.qkv, cols, a.S, a.B, kDbX, &qkv_x) || !dattn_map(a.g, gc, a.S, a.B, 128, &g_f) ||
-      !dattn_map(a.g, gc, a.S, a.B, kDbX, &g_x) || !dattn_map(a.dqkv, cols, a.S, a.B, 32, &out, DH / 2))
+      !dattn_map(a.g, gc, a.S, a.B, kDbX, &g_x) || !dattn_map(a.dqkv, cols, a.S, a.B, 32, &out, DH / 4))
     return cudaErrorInvalidValue;
   const int64_t tiles = (a.S + 127) / 128 * (int64_t)a.B;
   const cudaError_t e = dattn_tc_launch(dattn_bwd_tc_kernel<DH, 0>, tiles * a.K, kDbThreads, DattnBwdCfg<DH, 0>::kSmem, st, qkv_f, qkv_f, qkv_x, g_x, out, a);

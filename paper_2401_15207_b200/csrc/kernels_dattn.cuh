@@ -28,9 +28,21 @@ template <int D> constexpr int kDaFwdSmem = (3 * kDaT * kDaLd<D> + kDaT * kDaPLd
 template <int D> constexpr int kDaDqSmem = (4 * kDaT * kDaLd<D> + kDaT * kDaPLd) * 4;
 template <int D> constexpr int kDaDkvSmem = (4 * kDaT * kDaLd<D> + 3 * kDaT * kDaPLd + 4 * kDaT) * 4;
 
-// 64 rows of D elements, rows at or beyond `rows` as zeros
+// 64 rows of D elements, rows at or beyond `rows` as zeros; `vec`: rows start at 16-byte boundaries
 template <typename T, int D>
-__device__ __forceinline__ void da_stage(float* dst, const T* __restrict__ src, int64_t ld, int rows) {
+__device__ __forceinline__ void da_stage(float* dst, const T* __restrict__ src, int64_t ld, int rows, bool vec) {
+  if (vec) {
+    constexpr int N = kDaT * D / 8;                        // groups of 8 elements
+#pragma unroll
+    for (int k = 0; k < (N + 255) / 256; ++k) {
+      const int i = threadIdx.x + 256 * k, r = i / (D / 8), c = i % (D / 8) * 8;
+      if (N % 256 && i >= N) break;
+      float v[8] = {};
+      if (r < rows) load8(src + r * ld + c, v);
+      store8(dst + r * kDaLd<D> + c, v);
+    }
+    return;
+  }
   for (int i = threadIdx.x; i < kDaT * D; i += 256) {
     const int r = i / D, c = i % D;
     dst[r * kDaLd<D> + c] = r < rows ? to_f(src[r * ld + c]) : 0.f;
@@ -111,7 +123,7 @@ __global__ void __launch_bounds__(256) dattn_fwd_kernel(DattnArgs a) {
   const int len = dattn_len(a.lens, b, a.S), kend = a.causal ? min(len, min(q0 + kDaT, a.S)) : len;
   const int64_t ld = (int64_t)(a.H + 2 * a.K) * D;
   const T* base = (const T*)a.qkv + (int64_t)b * a.S * ld;
-  da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0);
+  da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0, a.vec);
   float acc[2][4][CW], m[2][4], l[2][4];
 #pragma unroll
   for (int z = 0; z < 2; ++z)
@@ -123,8 +135,8 @@ __global__ void __launch_bounds__(256) dattn_fwd_kernel(DattnArgs a) {
     }
   for (int k0 = 0; k0 < kend; k0 += kDaT) {
     __syncthreads();
-    da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, a.S - k0);
-    da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0);          // (rows of padding may hold anything: 0 * NaN)
+    da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, a.S - k0, a.vec);
+    da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0, a.vec);          // (rows of padding may hold anything: 0 * NaN)
     __syncthreads();
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
@@ -189,101 +201,119 @@ __global__ void __launch_bounds__(256) dattn_fwd_kernel(DattnArgs a) {
 }
 
 // ---- backward ---------------------------------------------------------------------------------------------------------------------
-// A warp takes (token, head) rows of one head: the gradient g of o (through the norm), D_1, D_2, and per block the sums for dlambda and dgain.
-// D_1 and D_2 are taken with g as the products will read it (rounded to T): what is common to all of a row's dP then cancels in dP - D.
-// dlambda is taken with g in fp32.
+// Groups of D / 8 lanes (heads of 16 to 128: 2 to 16 lanes) take (token, head) rows of one head: the gradient g of o (through the norm), D_1, D_2, and per block
+// the sums for dlambda and dgain.  D_1 and D_2 are taken with g as the products will read it (rounded to T): what is common to all of a row's dP
+// then cancels in dP - D.  dlambda is taken with g in fp32.  Memory bounds it: dy, o and o_2 are read once.  VEC: 16-byte accesses.
 struct DattnPrep { DattnArgs a; void* g_out; float* dsum_out; float* dlam_part; float* dgain_part; int chunks, rows_per_chunk; };
-template <typename T, int D>
+template <bool VEC, typename T> __device__ __forceinline__ void da_load8(const T* p, float (&v)[8]) {
+  if (VEC) { load8(p, v); return; }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = to_f(p[i]);
+}
+template <int L> __device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+template <typename T, int D, bool VEC>
 __global__ void __launch_bounds__(256) dattn_prep_kernel(DattnPrep p) {
-  constexpr int E = D >= 32 ? D / 32 : 1, LANES = D / E;   // elements a lane; lanes with elements
-  __shared__ float red[8][D + 1];
+  constexpr int L = D / 8, R = 256 / L;                    // lanes of a row, rows of a block at a time
+  __shared__ float red[R][D + 1];
   pdl_launch_next();
   pdl_wait_prior();
   const DattnArgs& a = p.a;
-  const int h = blockIdx.x / p.chunks, ch = blockIdx.x % p.chunks, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // the heads of a chunk of rows behind one another: what runs at once reads whole rows
+  const int ch = blockIdx.x / a.H, h = blockIdx.x % a.H, slot = h * p.chunks + ch, part = threadIdx.x % L, r = threadIdx.x / L;
   const int64_t rows = (int64_t)a.B * a.S, first = (int64_t)ch * p.rows_per_chunk, last = min(rows, first + p.rows_per_chunk);
   const float lam = a.lam[h];
-  float gain[E], dgain[E], dlam = 0.f;
+  float gain[8], dgain[8], dlam = 0.f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) { gain[e] = a.gain && lane < LANES ? to_f(((const T*)a.gain)[lane * E + e]) * a.c : 0.f; dgain[e] = 0.f; }
-  for (int64_t t = first + warp; t < last; t += 8) {
-    const int64_t at = (t * a.H + h) * D + lane * E;
-    float g[E], o[E], o2[E];
+  for (int e = 0; e < 8; ++e) { gain[e] = a.gain ? to_f(((const T*)a.gain)[part * 8 + e]) * a.c : 0.f; dgain[e] = 0.f; }
+#pragma unroll 2
+  for (int64_t t0 = first; t0 < last; t0 += R) {           // (whole warps: the sums below are over lanes)
+    const int64_t t = t0 + r;
+    const bool in = t < last;
+    const int64_t at = (t * a.H + h) * D + part * 8;
+    float g[8], o[8], o2[8];
+    if (in) {
+      da_load8<VEC>((const T*)a.dy + at, g);
+      da_load8<VEC>((const T*)a.o + at, o);
+      da_load8<VEC>((const T*)a.o2 + at, o2);
+    } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      g[e] = o[e] = o2[e] = 0.f;
-      if (lane < LANES) { g[e] = to_f(((const T*)a.dy)[at + e]); o[e] = to_f(((const T*)a.o)[at + e]); o2[e] = to_f(((const T*)a.o2)[at + e]); }
+      for (int e = 0; e < 8; ++e) g[e] = o[e] = o2[e] = 0.f;
     }
     if (a.gain) {
       float ss = 0.f, wo = 0.f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) { ss = fmaf(o[e], o[e], ss); wo = fmaf(g[e] * gain[e], o[e], wo); }
-      ss = warp_sum(ss);
-      wo = warp_sum(wo);
-      const float r = 1.0f / sqrtf(ss * (1.0f / D) + a.eps), k = r * r * wo * (1.0f / D);
+      for (int e = 0; e < 8; ++e) { ss = fmaf(o[e], o[e], ss); wo = fmaf(g[e] * gain[e], o[e], wo); }
+      ss = lanes_sum<L>(ss);
+      wo = lanes_sum<L>(wo);
+      const float rn = 1.0f / sqrtf(ss * (1.0f / D) + a.eps), k = rn * rn * wo * (1.0f / D);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        dgain[e] = fmaf(g[e] * a.c, o[e] * r, dgain[e]);
-        g[e] = r * (g[e] * gain[e] - o[e] * k);
+      for (int e = 0; e < 8; ++e) {
+        dgain[e] = fmaf(g[e] * a.c, o[e] * rn, dgain[e]);
+        g[e] = rn * (g[e] * gain[e] - o[e] * k);
       }
     }
-    float d1 = 0.f, d2 = 0.f, d2x = 0.f;
+    float d1 = 0.f, d2 = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      d2x = fmaf(g[e], o2[e], d2x);
-      if (p.g_out) {
-        const T gr = from_f<T>(g[e]);
-        if (lane < LANES) ((T*)p.g_out)[at + e] = gr;
-        g[e] = to_f(gr);
-      }
+    for (int e = 0; e < 8; ++e) {
+      dlam = fmaf(-g[e], o2[e], dlam);
+      if (p.g_out) g[e] = to_f(from_f<T>(g[e]));
       d2 = fmaf(g[e], o2[e], d2);
       d1 = fmaf(g[e], fmaf(lam, o2[e], o[e]), d1);
     }
-    d1 = warp_sum(d1);
-    d2 = warp_sum(d2);
-    dlam -= d2x;                                           // the lanes' shares are summed at the end
-    if (lane == 0) {
-      const int64_t row = (t / a.S * a.H + h) * a.S + t % a.S;
-      p.dsum_out[row] = d1;
-      p.dsum_out[(int64_t)a.B * a.H * a.S + row] = d2;
+    d1 = lanes_sum<L>(d1);
+    d2 = lanes_sum<L>(d2);
+    if (in) {
+      if (p.g_out) store8((T*)p.g_out + at, g);            // (the scratch is aligned)
+      if (part == 0) {
+        const int64_t b = t / a.S, row = (b * a.H + h) * a.S + (t - b * a.S);
+        p.dsum_out[row] = d1;
+        p.dsum_out[(int64_t)a.B * a.H * a.S + row] = d2;
+      }
     }
   }
-  dlam = warp_sum(dlam);
-  if (lane == 0) red[warp][D] = dlam;
+  dlam = lanes_sum<L>(dlam);
+  if (part == 0) red[r][D] = dlam;
 #pragma unroll
-  for (int e = 0; e < E; ++e) if (lane < LANES) red[warp][lane * E + e] = dgain[e];
+  for (int e = 0; e < 8; ++e) red[r][part * 8 + e] = dgain[e];
   __syncthreads();
   if (threadIdx.x <= D && (threadIdx.x == D || a.gain)) {
     float s = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) s += red[w][threadIdx.x];
-    if (threadIdx.x == D) p.dlam_part[blockIdx.x] = s;
-    else p.dgain_part[(int64_t)blockIdx.x * D + threadIdx.x] = s;
+#pragma unroll 8
+    for (int i = 0; i < R; ++i) s += red[i][threadIdx.x];
+    if (threadIdx.x == D) p.dlam_part[slot] = s;
+    else p.dgain_part[(int64_t)slot * D + threadIdx.x] = s;
   }
 }
 // The partial sums' sums, in a fixed order: blocks 0 .. H - 1 one head's dlambda each, the others 32 columns of dgain each.
-__global__ void __launch_bounds__(256) dattn_sums_kernel(const float* __restrict__ dlam_part, const float* __restrict__ dgain_part,
-                                                         float* __restrict__ dlam, float* __restrict__ dgain, int H, int chunks, int D) {
+__global__ void __launch_bounds__(1024) dattn_sums_kernel(const float* __restrict__ dlam_part, const float* __restrict__ dgain_part,
+                                                          float* __restrict__ dlam, float* __restrict__ dgain, int H, int chunks, int D) {
   __shared__ float red[33];
-  __shared__ float col[8][33];
+  __shared__ float col[32][33];
   pdl_launch_next();
   pdl_wait_prior();
   if ((int)blockIdx.x < H) {
+    if (!dlam) return;
     float s = 0.f;
-    for (int i = threadIdx.x; i < chunks; i += 256) s += dlam_part[(int64_t)blockIdx.x * chunks + i];
+    for (int i = threadIdx.x; i < chunks; i += 1024) s += dlam_part[(int64_t)blockIdx.x * chunks + i];
     s = block_sum(s, red);
     if (threadIdx.x == 0) dlam[blockIdx.x] = s;
     return;
   }
-  const int c = ((int)blockIdx.x - H) * 32 + (threadIdx.x & 31), w = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, c = ((int)blockIdx.x - H) * 32 + lane, w = threadIdx.x >> 5;
   float s = 0.f;
-  if (c < D)
-    for (int64_t i = w; i < (int64_t)H * chunks; i += 8) s += dgain_part[i * D + c];
-  col[w][threadIdx.x & 31] = s;
+  if (c < D) {
+#pragma unroll 4
+    for (int i = w; i < H * chunks; i += 32) s += dgain_part[(int64_t)i * D + c];
+  }
+  col[w][lane] = s;
   __syncthreads();
   if (w == 0 && c < D) {
 #pragma unroll
-    for (int i = 1; i < 8; ++i) s += col[i][threadIdx.x];
+    for (int i = 1; i < 32; ++i) s += col[i][lane];
     dgain[c] = s;
   }
 }
@@ -301,8 +331,8 @@ __global__ void __launch_bounds__(256) dattn_dq_kernel(DattnArgs a) {
   const int len = dattn_len(a.lens, b, a.S), kend = a.causal ? min(len, min(q0 + kDaT, a.S)) : len;
   const int64_t ld = (int64_t)(a.H + 2 * a.K) * D, nrow = (int64_t)a.B * a.H * a.S;
   const T* base = (const T*)a.qkv + (int64_t)b * a.S * ld;
-  da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0);
-  da_stage<T, D>(sg, (const T*)a.g + ((int64_t)b * a.S + q0) * a.H * D + h * D, (int64_t)a.H * D, a.S - q0);
+  da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0, a.vec);
+  da_stage<T, D>(sg, (const T*)a.g + ((int64_t)b * a.S + q0) * a.H * D + h * D, (int64_t)a.H * D, a.S - q0, a.vec);
   const float lam = a.lam[h];
   float acc[2][4][CW], lse[2][4], ds[2][4];
 #pragma unroll
@@ -318,8 +348,8 @@ __global__ void __launch_bounds__(256) dattn_dq_kernel(DattnArgs a) {
   }
   for (int k0 = 0; k0 < kend; k0 += kDaT) {
     __syncthreads();
-    da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, len - k0);
-    da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0);
+    da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, len - k0, a.vec);
+    da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0, a.vec);
     __syncthreads();
     float dp[4][4];
     da_dots<D, D>(dp, sg, sv, ty, tx);
@@ -369,8 +399,8 @@ __global__ void __launch_bounds__(256) dattn_dkv_kernel(DattnArgs a) {
   const int len = dattn_len(a.lens, b, a.S);
   const int64_t ld = (int64_t)(a.H + 2 * a.K) * D, nrow = (int64_t)a.B * a.H * a.S;
   const T* base = (const T*)a.qkv + (int64_t)b * a.S * ld;
-  da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, len - k0);
-  da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0);
+  da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, len - k0, a.vec);
+  da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0, a.vec);
   float dk[2][4][CW], dv[4][VW];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -386,8 +416,8 @@ __global__ void __launch_bounds__(256) dattn_dkv_kernel(DattnArgs a) {
       const float lam = a.lam[h];
       for (int q0 = a.causal ? k0 : 0; q0 < a.S; q0 += kDaT) {
         __syncthreads();
-        da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0);
-        da_stage<T, D>(sg, (const T*)a.g + ((int64_t)b * a.S + q0) * a.H * D + h * D, (int64_t)a.H * D, a.S - q0);
+        da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0, a.vec);
+        da_stage<T, D>(sg, (const T*)a.g + ((int64_t)b * a.S + q0) * a.H * D + h * D, (int64_t)a.H * D, a.S - q0, a.vec);
         {
           const int z = threadIdx.x >> 6;
           const int64_t row = ((int64_t)b * a.H + h) * a.S + min(q0 + (int)(threadIdx.x & 63), a.S - 1);
@@ -500,7 +530,8 @@ template <typename T> cudaError_t launch_dattn_bwd(cudaStream_t st, int D, const
 #undef CALL
 }
 template <typename T> cudaError_t launch_dattn_prep(cudaStream_t st, int D, const DattnPrep& p) {
-#define CALL(N) launch_pdl(dattn_prep_kernel<T, N>, dim3((unsigned)(p.a.H * p.chunks)), dim3(256), 0, st, p)
+  const bool vec = (((uintptr_t)p.a.dy | (uintptr_t)p.a.o | (uintptr_t)p.a.o2) & 15) == 0;
+#define CALL(N) launch_pdl(vec ? dattn_prep_kernel<T, N, true> : dattn_prep_kernel<T, N, false>, dim3((unsigned)(p.a.H * p.chunks)), dim3(256), 0, st, p)
   HIFT_DATTN_SWITCH(D, CALL)
 #undef CALL
 }
