@@ -10,7 +10,7 @@
 // dk and dq are multiplied by `scale` as they are stored.  dP is shared by the maps, and dv takes one product for both: 8 units of 128 x 64 x 64 a
 // step against the 10 of two plain attentions.  P and dS are rounded to bf16, the operand type of the products they feed; the accumulators are fp32.
 //   warp 0    : TMA producer         warp 1: issues every product (one elected thread); owns the tensor memory
-//   warps 4-19: element-wise, four warps to a lane quarter, 16 of the 64 streamed columns each: S_1, S_2 -> registers, exponentials; dP -> registers, dS;
+//   warps 4.. : element-wise, two or four warps to a lane quarter, their share of the 64 streamed columns each: S_1, S_2 -> registers, exponentials; dP, dS;
 //               P and dS go back to tensor memory as bf16, the A operands of the accumulating products; at an item's end the accumulators -> global
 // Order of issue: S(t+1) as soon as S(t) has been read, so that it runs beside the exponentials of step t; then the accumulating products of t; then
 // dP(t+1), which therefore finds both its buffer and the P / dS buffers of step t free when it is done.
@@ -19,34 +19,48 @@
 // What bounds it: products 1276 cycles a step at heads of 128 (1024 in MODE 1), exponentials 1024, both of the 128 x 64 tile.
 #pragma once
 
-constexpr int kDbThreads = 640, kDbEw = 16, kDbX = 64, kDbStages = 3;
+constexpr int kDbX = 64, kDbStages = 3;
 template <int DH, int MODE> struct DattnBwdCfg {
   static constexpr int kSpans = DH / 64;
   static constexpr int kFBytes = 128 * DH * 2, kXBytes = kDbX * DH * 2;
-  static constexpr int kStage = kDbEw * 32 * (DH / 4) * 2;         // a piece of 32 rows x a quarter of the columns per element-wise warp
-  static constexpr int kCol = MODE == 0 ? kDbEw * 2 * 256 : 0;     // per warp, two steps: lse and D of its 16 queries
-  static constexpr int kSmem = 2 * kFBytes + kDbStages * 2 * kXBytes + kStage + kCol + 256 + 1024;
+  // Element-wise warps to a lane quarter.  MODE 0: two, of 32 streamed columns each (four: 180 -> 207 us at 4096 x 16 heads of 128, for each column's lse
+  // and D are read from shared memory by every thread and the instructions bound it); MODE 1: four, of 16 (two: 135 -> 140 us)
+  static constexpr int kParts = MODE == 0 ? 2 : 4, kEw = 4 * kParts, kThreads = 128 + 32 * kEw;
+  static constexpr int kNF = DH == 64 ? 2 : 1;                     // sets of fixed tiles: the next item's are fetched beside this one's steps
+  static constexpr int kStage = kEw * 32 * (DH / kParts) * 2;      // a piece of 32 rows x this warp's share of the columns per element-wise warp
+  static constexpr int kCol = MODE == 0 ? kEw * 2 * 512 : 0;       // per warp, two steps: lse and D of its 32 queries
+  static constexpr int kSmem = kNF * 2 * kFBytes + kDbStages * 2 * kXBytes + kStage + kCol + 256 + 1024;
 };
 
 __device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&v)[8]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                ::"r"(addr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
+// loads and stores of as many columns as the array has registers
+__device__ __forceinline__ void tm_load(uint32_t addr, uint32_t (&v)[32]) { tmem_ld32_nowait(addr, v); }
+__device__ __forceinline__ void tm_load(uint32_t addr, uint32_t (&v)[16]) { tmem_ld16_nowait(addr, v); }
+__device__ __forceinline__ void tm_loaded(uint32_t (&v)[32]) { tmem_ld_wait32(v); }
+__device__ __forceinline__ void tm_loaded(uint32_t (&v)[16]) { tmem_ld_wait16(v); }
+__device__ __forceinline__ void tm_store(uint32_t addr, const uint32_t (&v)[16]) { tmem_st16(addr, v); }
+__device__ __forceinline__ void tm_store(uint32_t addr, const uint32_t (&v)[8]) { tmem_st8(addr, v); }
 struct DattnBwdItem { int b, hk, f0, x_lo, per, nsteps, len; };    // hk: key head (MODE 0) or query head (MODE 1); per: steps of one head
 
 template <int DH, int MODE>
-__global__ void __launch_bounds__(kDbThreads, 1)
+__global__ void __launch_bounds__(DattnBwdCfg<DH, MODE>::kThreads, 1)
 dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_constant__ CUtensorMap map_f1, const __grid_constant__ CUtensorMap map_x0,
                     const __grid_constant__ CUtensorMap map_x1, const __grid_constant__ CUtensorMap map_out, const DattnArgs a) {
   typedef DattnBwdCfg<DH, MODE> Cfg;
   constexpr int SP = Cfg::kSpans, HD = DH / 2, NS = kDbStages, FB = Cfg::kFBytes, XB = Cfg::kXBytes, FSPAN = 128 * 128, XSPAN = kDbX * 128;
+  constexpr int NF = Cfg::kNF, NP = Cfg::kParts, EW = Cfg::kEw, XC = kDbX / NP;        // XC: streamed columns of a thread
   extern __shared__ uint8_t smem_raw[];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
-  const uint32_t sF0 = base, sF1 = sF0 + FB, sX = sF1 + FB, sStage = sX + NS * 2 * XB, sCol = sStage + Cfg::kStage, bar = sCol + Cfg::kCol;
-  const uint32_t f_full = bar, f_empty = bar + 8u, s_full = bar + 16u, s_free = bar + 24u, dp_full = bar + 32u, p_ready = bar + 40u, acc_full = bar + 48u,
-                 acc_free = bar + 56u, tmem_slot = bar + 112u;
+  const uint32_t sF = base, sX = sF + NF * 2 * FB, sStage = sX + NS * 2 * XB, sCol = sStage + Cfg::kStage, bar = sCol + Cfg::kCol;
+  const uint32_t s_full = bar + 16u, s_free = bar + 24u, dp_full = bar + 32u, p_ready = bar + 40u, acc_full = bar + 48u, acc_free = bar + 56u,
+                 tmem_slot = bar + 144u;
+  auto f_full = [&](int n) { return bar + 112u + 8u * (n % NF); };           // the set of fixed tiles of item n; its phase is n / NF
+  auto f_empty = [&](int n) { return bar + 128u + 8u * (n % NF); };
   auto x_full = [&](int i) { return bar + 64u + 8u * i; };
   auto x_empty = [&](int i) { return bar + 88u + 8u * i; };
   volatile uint32_t* slot_gen = reinterpret_cast<volatile uint32_t*>(gen + (tmem_slot - base));
@@ -75,9 +89,9 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
   };
 
   if (threadIdx.x == 0) {
-    mbar_init(f_full, 1); mbar_init(f_empty, 1);
-    mbar_init(s_full, 1); mbar_init(s_free, kDbEw); mbar_init(dp_full, 1); mbar_init(p_ready, kDbEw);
-    mbar_init(acc_full, 1); mbar_init(acc_free, kDbEw);
+    for (int i = 0; i < NF; ++i) { mbar_init(f_full(i), 1); mbar_init(f_empty(i), 1); }
+    mbar_init(s_full, 1); mbar_init(s_free, EW); mbar_init(dp_full, 1); mbar_init(p_ready, EW);
+    mbar_init(acc_full, 1); mbar_init(acc_free, EW);
     for (int i = 0; i < NS; ++i) { mbar_init(x_full(i), 1); mbar_init(x_empty(i), 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_wait();                                                    // no global access before it, the flag included
@@ -105,12 +119,13 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
       for (int idx = dattn_item_at(n); idx < nitems && ok; idx = dattn_item_at(++n)) {
         const DattnBwdItem it = item_of(idx);
         const int colF0 = (MODE == 0 ? a.H + it.hk : it.hk) * DH, colF1 = (MODE == 0 ? a.H + a.K + it.hk : it.hk) * DH;
-        if (!mbar_wait(f_empty, (uint32_t)((n & 1) ^ 1))) { atomicCAS(&g_tc_error, 0, 7); break; }
-        mbar_expect_tx(f_full, 2 * FB);
+        if (!mbar_wait(f_empty(n), (uint32_t)(((n / NF) & 1) ^ 1))) { atomicCAS(&g_tc_error, 0, 7); break; }
+        mbar_expect_tx(f_full(n), 2 * FB);
+        const uint32_t sF0 = sF + (n % NF) * 2 * FB;
 #pragma unroll
         for (int sp = 0; sp < SP; ++sp) {
-          tma_load_3d(sF0 + sp * FSPAN, &map_f0, f_full, colF0 + sp * 64, it.f0, it.b);
-          tma_load_3d(sF1 + sp * FSPAN, &map_f1, f_full, colF1 + sp * 64, it.f0, it.b);
+          tma_load_3d(sF0 + sp * FSPAN, &map_f0, f_full(n), colF0 + sp * 64, it.f0, it.b);
+          tma_load_3d(sF0 + FB + sp * FSPAN, &map_f1, f_full(n), colF1 + sp * 64, it.f0, it.b);
         }
         int x = it.x_lo, h = MODE == 0 ? it.hk * group : it.hk / group;
         for (int t = 0; t < it.nsteps; ++t) {
@@ -135,16 +150,18 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         const uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | (((uint32_t)kDbX >> 3) << 17) | ((128u >> 4) << 24);
         const uint32_t idesc_h = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)HD >> 3) << 17) | ((128u >> 4) << 24);       // N = d
         const uint32_t idesc_v = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)DH >> 3) << 17) | ((128u >> 4) << 24);       // N = 2 d
-        const uint64_t dF0 = desc_kmajor(sF0), dF1 = desc_kmajor(sF1), dX0 = desc_kmajor(sX);
+        const uint64_t dF = desc_kmajor(sF), dX0 = desc_kmajor(sX);
         auto k_off = [](int e, int span) { return (uint64_t)(((e / 4) * span + (e % 4) * 32) >> 4); };       // 16 columns, number e, of a K-major tile
-        auto issue_s = [&](int st) {
+        auto issue_s = [&](int item, int st) {
+          const uint64_t dF0 = dF + (uint64_t)((item % NF) * (2 * FB >> 4));
           const uint64_t x0 = dX0 + (uint64_t)(st * (2 * XB >> 4));
 #pragma unroll
           for (int e = 0; e < DH / 16; ++e)
             tc_mma(tm + (e < HD / 16 ? 0u : 64u), dF0 + k_off(e, FSPAN), x0 + k_off(e, XSPAN), idesc_s, e % (HD / 16) > 0 ? 1u : 0u);
           tc_commit(s_full);
         };
-        auto issue_dp = [&](int st) {
+        auto issue_dp = [&](int item, int st) {
+          const uint64_t dF1 = dF + (uint64_t)(((item % NF) * 2 * FB + FB) >> 4);
           const uint64_t x1 = dX0 + (uint64_t)((st * 2 * XB + XB) >> 4);
 #pragma unroll
           for (int e = 0; e < DH / 16; ++e) tc_mma(tDP, dF1 + k_off(e, FSPAN), x1 + k_off(e, XSPAN), idesc_s, e > 0 ? 1u : 0u);
@@ -155,12 +172,12 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         uint32_t ph = 0;
         int idx = dattn_item_at(0), nsteps = idx < nitems ? item_of(idx).nsteps : 0;
         if (nsteps) {
-          ok = mbar_wait(f_full, 0) && mbar_wait(x_full(0), 0);
+          ok = mbar_wait(f_full(0), 0) && mbar_wait(x_full(0), 0);
           if (ok) {
             tc_fence_after();
-            issue_s(0);
-            issue_dp(0);
-            if (nsteps == 1) tc_commit(f_empty);
+            issue_s(0, 0);
+            issue_dp(0, 0);
+            if (nsteps == 1) tc_commit(f_empty(0));
           }
         }
         while (ok && idx < nitems) {
@@ -172,7 +189,7 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
             ok = mbar_wait(s_free, (uint32_t)(g & 1)) && mbar_wait(x_full(st1), ph1);
             if (!ok) break;
             tc_fence_after();
-            issue_s(st1);
+            issue_s(n, st1);
           }
           ok = (t > 0 || n == 0 || mbar_wait(acc_free, (uint32_t)((n - 1) & 1))) && mbar_wait(p_ready, (uint32_t)(g & 1));
           if (!ok) break;
@@ -184,7 +201,7 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
             for (int kk = 0; kk < 4; ++kk) {
               // the map's half of X0's columns: the second span (heads of 128), or the second half of the one span
               const uint64_t b = nX0 + (uint64_t)((kk * 16 * 128 + m * (DH == 128 ? XSPAN : 64)) >> 4);
-              const uint32_t p = MODE == 0 ? (m == 0 ? tP + 32u + kk * 8u : tDP + kk * 16u) : tP + m * 32u + kk * 8u;
+              const uint32_t p = MODE == 0 ? (m == 0 ? tP + 32u + kk * 8u : tDP + kk * 16u / XC * XC + kk * 16u % XC / 2u) : tP + m * 32u + kk * 8u;
               tc_mma_ta(tAcc + (uint32_t)(m * HD), p, b, idesc_h, (t > 0 || kk > 0) ? 1u : 0u);
             }
           }
@@ -198,13 +215,13 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
           if (more) {
             if (last) {                                            // another item: its fixed tiles take the place of this one's
               next_steps = item_of(next_idx).nsteps;
-              ok = mbar_wait(s_free, (uint32_t)(g & 1)) && mbar_wait(f_full, (uint32_t)((n + 1) & 1)) && mbar_wait(x_full(st1), ph1);
+              ok = mbar_wait(s_free, (uint32_t)(g & 1)) && mbar_wait(f_full(n + 1), (uint32_t)(((n + 1) / NF) & 1)) && mbar_wait(x_full(st1), ph1);
               if (!ok) break;
               tc_fence_after();
-              issue_s(st1);
+              issue_s(n + 1, st1);
             }
-            issue_dp(st1);
-            if (last ? next_steps == 1 : t + 2 == nsteps) tc_commit(f_empty);
+            issue_dp(last ? n + 1 : n, st1);
+            if (last ? next_steps == 1 : t + 2 == nsteps) tc_commit(f_empty(last ? n + 1 : n));
           }
           ++g;
           st = st1;
@@ -216,15 +233,15 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
       __syncwarp();
     }
   } else if (warp >= 4) {
-    // ---------------- element-wise: thread = row of the fixed tile x 16 streamed columns
+    // ---------------- element-wise: thread = row of the fixed tile x XC streamed columns
     const int q = warp & 3, hc = (warp - 4) >> 2, r = q * 32 + lane;
     const uint32_t lane_off = (uint32_t)(q * 32) << 16;
     const float sl2 = a.scale * 1.4426950408889634f;
     const uint64_t sc2 = f2_pack(sl2, sl2);
     const int64_t nrow = (int64_t)a.B * a.H * a.S;
-    const uint32_t sPiece = sStage + (warp - 4) * (32 * (DH / 4) * 2);
+    const uint32_t sPiece = sStage + (warp - 4) * (32 * (DH / NP) * 2);
     uint8_t* piece = gen + (sPiece - base);
-    float* col = reinterpret_cast<float*>(gen + (sCol - base)) + (warp - 4) * 128;      // MODE 0: two buffers of 8 column pairs x (-lse_1, -lse_2, -D_1, -D_2)
+    float* col = reinterpret_cast<float*>(gen + (sCol - base)) + (warp - 4) * 256;      // MODE 0: two buffers of XC / 2 column pairs x (-lse_1, -lse_2, -D_1, -D_2)
     bool ok = !poisoned;
     int n = 0, g = 0;
     // -lse in log2 units; a query that sees no key, or is none: P = 0 through -infinity
@@ -237,7 +254,7 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
       // for them) or of this thread's row (MODE 1)
       float rl[2], rd[2];
       auto fetch = [&](int xx, int hh) {
-        const int c = MODE == 0 ? xx * kDbX + hc * 16 + (lane & 15) : frow;
+        const int c = MODE == 0 ? xx * kDbX + hc * XC + (lane & (XC - 1)) : frow;
         const bool in = c < a.S;
         const int64_t at = ((int64_t)it.b * a.H + hh) * a.S + (in ? c : 0);
 #pragma unroll
@@ -256,10 +273,10 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
       for (int t = 0; t < it.nsteps; ++t, ++g) {
         const int x0 = x * kDbX;
         const uint64_t nlam2 = f2_pack(-lam, -lam);
-        float* cv = col + (g & 1) * 64;
+        float* cv = col + (g & 1) * 128;
         if (MODE == 0) {
-          float* w = cv + ((lane & 15) >> 1) * 8 + (lane & 1);
-          if (lane < 16) { w[0] = neg_log2(rl[0]); w[2] = neg_log2(rl[1]); w[4] = -rd[0]; w[6] = -rd[1]; }
+          float* w = cv + ((lane & (XC - 1)) >> 1) * 8 + (lane & 1);
+          if (lane < XC) { w[0] = neg_log2(rl[0]); w[2] = neg_log2(rl[1]); w[4] = -rd[0]; w[6] = -rd[1]; }
           __syncwarp();
         }
         int nx = x + 1, nh = h;
@@ -273,11 +290,11 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         ok = __all_sync(0xffffffffu, ready);
         if (!ok) break;
         tc_fence_after();
-        uint32_t v[2][16];
-        tmem_ld16_nowait(tm + lane_off + (uint32_t)(hc * 16), v[0]);
-        tmem_ld16_nowait(tm + lane_off + (uint32_t)(64 + hc * 16), v[1]);
-        tmem_ld_wait16(v[0]);
-        tmem_ld_wait16(v[1]);
+        uint32_t v[2][XC];
+        tm_load(tm + lane_off + (uint32_t)(hc * XC), v[0]);
+        tm_load(tm + lane_off + (uint32_t)(64 + hc * XC), v[1]);
+        tm_loaded(v[0]);
+        tm_loaded(v[1]);
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(s_free);                        // the tensor core may overwrite the scores
@@ -291,14 +308,14 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
           masked = x0 + kDbX > min(it.len, a.causal ? it.f0 + 1 : a.S);
           lo = min(it.len, a.causal ? frow + 1 : a.S) - x0;
         }
-        lo -= hc * 16;
+        lo -= hc * XC;
         if (masked) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
+          for (int i = 0; i < XC; ++i)
             if (MODE == 0 ? i < lo : i >= lo) v[0][i] = v[1][i] = 0xff800000u;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < XC / 2; ++i) {
           uint64_t l1, l2;
           if (MODE == 0) {
             const float4 c = *reinterpret_cast<const float4*>(cv + i * 8);
@@ -321,16 +338,16 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         ok = __all_sync(0xffffffffu, ready);
         if (!ok) break;
         tc_fence_after();
-        uint32_t d[16], w1[8], w2[8], wv[8];
-        tmem_ld16_nowait(tDP + lane_off + (uint32_t)(hc * 16), d);
-        tmem_ld_wait16(d);
+        uint32_t d[XC], w1[XC / 2], w2[XC / 2], wv[XC / 2];
+        tm_load(tDP + lane_off + (uint32_t)(hc * XC), d);
+        tm_loaded(d);
         if (masked) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
+          for (int i = 0; i < XC; ++i)
             if (MODE == 0 ? i < lo : i >= lo) d[i] = 0u;           // (what a hidden key's value holds does not matter)
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < XC / 2; ++i) {
           uint64_t d1, d2;
           if (MODE == 0) {
             const float4 c = *reinterpret_cast<const float4*>(cv + i * 8 + 4);
@@ -355,12 +372,12 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         }
         // dP of this step is behind the accumulating products of the last one: what they read may be overwritten
         if (MODE == 0) {
-          tmem_st8(tP + lane_off + (uint32_t)(hc * 8), wv);
-          tmem_st8(tP + lane_off + 32u + (uint32_t)(hc * 8), w1);
-          tmem_st8(tDP + lane_off + (uint32_t)(hc * 16), w2);
+          tm_store(tP + lane_off + (uint32_t)(hc * (XC / 2)), wv);
+          tm_store(tP + lane_off + 32u + (uint32_t)(hc * (XC / 2)), w1);
+          tm_store(tDP + lane_off + (uint32_t)(hc * XC), w2);
         } else {
-          tmem_st8(tP + lane_off + (uint32_t)(hc * 8), w1);
-          tmem_st8(tP + lane_off + 32u + (uint32_t)(hc * 8), w2);
+          tm_store(tP + lane_off + (uint32_t)(hc * (XC / 2)), w1);
+          tm_store(tP + lane_off + 32u + (uint32_t)(hc * (XC / 2)), w2);
         }
         tmem_st_wait();
         tc_fence_before();
@@ -377,33 +394,36 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
       ok = __all_sync(0xffffffffu, ready);
       if (!ok) break;
       tc_fence_after();
-      constexpr int CW = DH / 4;
-      uint32_t o1[CW], o0[MODE == 0 ? CW : 1];
-      if constexpr (CW == 32) {
-        tmem_ld32_nowait(tAcc + lane_off + (uint32_t)(hc * CW), o1);
-        if constexpr (MODE == 0) tmem_ld32_nowait(tDv + lane_off + (uint32_t)(hc * CW), o0);
-        tmem_ld_wait32(o1);
-        if constexpr (MODE == 0) tmem_ld_wait32(o0);
-      } else {
-        tmem_ld16_nowait(tAcc + lane_off + (uint32_t)(hc * CW), o1);
-        if constexpr (MODE == 0) tmem_ld16_nowait(tDv + lane_off + (uint32_t)(hc * CW), o0);
-        tmem_ld_wait16(o1);
-        if constexpr (MODE == 0) tmem_ld_wait16(o0);
+      constexpr int CW = DH / NP, CL = CW < 32 ? CW : 32;          // columns of this warp, and of one load
+      uint32_t o1[CW / CL][CL], o0[MODE == 0 ? CW / CL : 1][CL];
+#pragma unroll
+      for (int c = 0; c < CW / CL; ++c) {
+        tm_load(tAcc + lane_off + (uint32_t)(hc * CW + c * CL), o1[c]);
+        if constexpr (MODE == 0) tm_load(tDv + lane_off + (uint32_t)(hc * CW + c * CL), o0[c]);
+      }
+#pragma unroll
+      for (int c = 0; c < CW / CL; ++c) {
+        tm_loaded(o1[c]);
+        if constexpr (MODE == 0) tm_loaded(o0[c]);
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(acc_free);
       const int row = it.f0 + q * 32;
-      auto store = [&](const uint32_t (&o)[CW], float mul, int column) {
+      auto store = [&](const uint32_t (&o)[CW / CL][CL], float mul, int column) {
         if (lane == 0) bulk_wait_read();                           // what left through the piece before
         __syncwarp();
 #pragma unroll
         for (int sg = 0; sg < CW / 8; ++sg) {
           uint32_t w[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = bf16_pair(__uint_as_float(o[8 * sg + 2 * i]) * mul, __uint_as_float(o[8 * sg + 2 * i + 1]) * mul);
-          // 64-byte rows, swizzled over 64 bytes (heads of 128), or 32-byte rows, swizzled over 32
-          const int at = DH == 128 ? lane * 64 + ((sg ^ ((lane >> 1) & 3)) << 4) : lane * 32 + ((sg ^ ((lane >> 2) & 1)) << 4);
+          for (int i = 0; i < 4; ++i) {
+            const int e = 8 * sg + 2 * i;
+            w[i] = bf16_pair(__uint_as_float(o[e / CL][e % CL]) * mul, __uint_as_float(o[e / CL][e % CL + 1]) * mul);
+          }
+          // rows of 128, 64 or 32 bytes, swizzled over as many
+          const int sw = CW == 64 ? lane & 7 : CW == 32 ? (lane >> 1) & 3 : (lane >> 2) & 1;
+          const int at = lane * (CW * 2) + ((sg ^ sw) << 4);
           *reinterpret_cast<uint4*>(piece + at) = make_uint4(w[0], w[1], w[2], w[3]);
         }
         fence_async_smem();

@@ -1660,14 +1660,15 @@ cudaError_t dattn_tc_fwd_launch(cudaStream_t st, int D, const DattnArgs& a) {
 }
 template <int DH>
 static cudaError_t dattn_tc_bwd_inst(cudaStream_t st, const DattnArgs& a) {
-  CUtensorMap qkv_f, qkv_x, g_f, g_x, out;
+  CUtensorMap qkv_f, qkv_x, g_f, g_x, out0, out1;
   const int64_t cols = (int64_t)(a.H + 2 * a.K) * DH, gc = (int64_t)a.H * DH;
   if (!dattn_map(a.qkv, cols, a.S, a.B, 128, &qkv_f) || !dattn_map(a.qkv, cols, a.S, a.B, kDbX, &qkv_x) || !dattn_map(a.g, gc, a.S, a.B, 128, &g_f) ||
-      !dattn_map(a.g, gc, a.S, a.B, kDbX, &g_x) || !dattn_map(a.dqkv, cols, a.S, a.B, 32, &out, DH / 4))
+      !dattn_map(a.g, gc, a.S, a.B, kDbX, &g_x) || !dattn_map(a.dqkv, cols, a.S, a.B, 32, &out0, DH / DattnBwdCfg<DH, 0>::kParts) ||
+      !dattn_map(a.dqkv, cols, a.S, a.B, 32, &out1, DH / DattnBwdCfg<DH, 1>::kParts))
     return cudaErrorInvalidValue;
   const int64_t tiles = (a.S + 127) / 128 * (int64_t)a.B;
-  const cudaError_t e = dattn_tc_launch(dattn_bwd_tc_kernel<DH, 0>, tiles * a.K, kDbThreads, DattnBwdCfg<DH, 0>::kSmem, st, qkv_f, qkv_f, qkv_x, g_x, out, a);
-  return e != cudaSuccess ? e : dattn_tc_launch(dattn_bwd_tc_kernel<DH, 1>, tiles * a.H, kDbThreads, DattnBwdCfg<DH, 1>::kSmem, st, qkv_f, g_f, qkv_x, qkv_x, out, a);
+  const cudaError_t e = dattn_tc_launch(dattn_bwd_tc_kernel<DH, 0>, tiles * a.K, DattnBwdCfg<DH, 0>::kThreads, DattnBwdCfg<DH, 0>::kSmem, st, qkv_f, qkv_f, qkv_x, g_x, out0, a);
+  return e != cudaSuccess ? e : dattn_tc_launch(dattn_bwd_tc_kernel<DH, 1>, tiles * a.H, DattnBwdCfg<DH, 1>::kThreads, DattnBwdCfg<DH, 1>::kSmem, st, qkv_f, g_f, qkv_x, qkv_x, out1, a);
 }
 cudaError_t dattn_tc_bwd_launch(cudaStream_t st, int D, const DattnArgs& a) {
   return D == 64 ? dattn_tc_bwd_inst<64>(st, a) : dattn_tc_bwd_inst<128>(st, a);
