@@ -150,7 +150,7 @@ hift_status hift_k_diff_attention_bwd(int32_t dtype, int32_t B, int32_t S, int32
   const DattnPrep p{a, gain ? (void*)(w + pl.g) : nullptr, (float*)(w + pl.dsum), dlam_part, dlam_part + (size_t)H * pl.chunks, pl.chunks, pl.rows_per_chunk};
   cudaError_t e = dtype == 0 ? launch_dattn_prep<float>(st, D, p) : launch_dattn_prep<bf16>(st, D, p);
   if (e == cudaSuccess && (dlam || dgain)) {
-    const int blocks = H + (dgain ? (D + 31) / 32 : 0);
+    const int blocks = H + (dgain ? D / 8 : 0);
     e = launch_pdl(dattn_sums_kernel, dim3((unsigned)blocks), dim3(1024), 0, st, (const float*)p.dlam_part, (const float*)p.dgain_part, dlam, dgain, H, pl.chunks, D);
   }
   if (e != cudaSuccess) return status_of(e);

@@ -12,24 +12,27 @@
 //   warp 0    : TMA producer         warp 1: issues every product (one elected thread); owns the tensor memory
 //   warps 4.. : element-wise, two or four warps to a lane quarter, their share of the 64 streamed columns each: S_1, S_2 -> registers, exponentials; dP, dS;
 //               P and dS go back to tensor memory as bf16, the A operands of the accumulating products; at an item's end the accumulators -> global
-// Order of issue: S(t+1) as soon as S(t) has been read, so that it runs beside the exponentials of step t; then the accumulating products of t; then
-// dP(t+1), which therefore finds both its buffer and the P / dS buffers of step t free when it is done.
-// Tensor-memory columns: S_1 0, S_2 64, dP 128, [P_1 - lambda P_2 | dS_1] 192 (32 each; MODE 1: dS_1, dS_2), accumulators 256.  In MODE 0 dS_2 lies over
-// dP, each warp's part over columns that it alone has read.
+// Two steps in flight (MODE 1, and heads of 64): two sets of S_1, S_2, dP (columns 192 u ..), accumulators behind 384.  P and dS lie over the scores, each
+// warp's part over columns that it alone has read; the order of issue is  accumulating products of t, then S(t+2) and dP(t+2) into the same set.
+// One step in flight (MODE 0 at heads of 128, whose accumulators take 256 columns): S_1 0, S_2 64, dP 128, [P_1 - lambda P_2 | dS_1] 192 (32 each), dS_2 over
+// dP in the same way, accumulators 256.  S(t+1) is issued as soon as S(t) has been read, so that it runs beside the exponentials of step t; then
+// the accumulating products of t; then dP(t+1), which finds both its buffer and the P / dS buffers of step t free when it is done.
 // What bounds it: products 1276 cycles a step at heads of 128 (1024 in MODE 1), exponentials 1024, both of the 128 x 64 tile.
 #pragma once
 
-constexpr int kDbX = 64, kDbStages = 3;
+constexpr int kDbX = 64;
 template <int DH, int MODE> struct DattnBwdCfg {
   static constexpr int kSpans = DH / 64;
   static constexpr int kFBytes = 128 * DH * 2, kXBytes = kDbX * DH * 2;
   // Element-wise warps to a lane quarter.  MODE 0: two, of 32 streamed columns each (four: 180 -> 207 us at 4096 x 16 heads of 128, for each column's lse
   // and D are read from shared memory by every thread and the instructions bound it); MODE 1: four, of 16 (two: 135 -> 140 us)
   static constexpr int kParts = MODE == 0 ? 2 : 4, kEw = 4 * kParts, kThreads = 128 + 32 * kEw;
+  static constexpr bool kTwo = MODE == 1 || DH == 64;              // two steps in flight: the accumulators leave tensor memory for two sets of S and dP
+  static constexpr int kStages = kTwo ? 4 : 3;
   static constexpr int kNF = DH == 64 ? 2 : 1;                     // sets of fixed tiles: the next item's are fetched beside this one's steps
   static constexpr int kStage = kEw * 32 * (DH / kParts) * 2;      // a piece of 32 rows x this warp's share of the columns per element-wise warp
   static constexpr int kCol = MODE == 0 ? kEw * 2 * 512 : 0;       // per warp, two steps: lse and D of its 32 queries
-  static constexpr int kSmem = kNF * 2 * kFBytes + kDbStages * 2 * kXBytes + kStage + kCol + 256 + 1024;
+  static constexpr int kSmem = kNF * 2 * kFBytes + kStages * 2 * kXBytes + kStage + kCol + 256 + 1024;
 };
 
 __device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&v)[8]) {
@@ -50,19 +53,22 @@ __global__ void __launch_bounds__(DattnBwdCfg<DH, MODE>::kThreads, 1)
 dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_constant__ CUtensorMap map_f1, const __grid_constant__ CUtensorMap map_x0,
                     const __grid_constant__ CUtensorMap map_x1, const __grid_constant__ CUtensorMap map_out, const DattnArgs a) {
   typedef DattnBwdCfg<DH, MODE> Cfg;
-  constexpr int SP = Cfg::kSpans, HD = DH / 2, NS = kDbStages, FB = Cfg::kFBytes, XB = Cfg::kXBytes, FSPAN = 128 * 128, XSPAN = kDbX * 128;
+  constexpr int SP = Cfg::kSpans, HD = DH / 2, NS = Cfg::kStages, FB = Cfg::kFBytes, XB = Cfg::kXBytes, FSPAN = 128 * 128, XSPAN = kDbX * 128;
   constexpr int NF = Cfg::kNF, NP = Cfg::kParts, EW = Cfg::kEw, XC = kDbX / NP;        // XC: streamed columns of a thread
+  constexpr bool TWO = Cfg::kTwo;
   extern __shared__ uint8_t smem_raw[];
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
   const uint32_t sF = base, sX = sF + NF * 2 * FB, sStage = sX + NS * 2 * XB, sCol = sStage + Cfg::kStage, bar = sCol + Cfg::kCol;
-  const uint32_t s_full = bar + 16u, s_free = bar + 24u, dp_full = bar + 32u, p_ready = bar + 40u, acc_full = bar + 48u, acc_free = bar + 56u,
-                 tmem_slot = bar + 144u;
-  auto f_full = [&](int n) { return bar + 112u + 8u * (n % NF); };           // the set of fixed tiles of item n; its phase is n / NF
-  auto f_empty = [&](int n) { return bar + 128u + 8u * (n % NF); };
+  // two steps in flight: s_full(u) covers S and dP of set u; one step: u = 0, and dP has a barrier of its own
+  auto s_full = [&](int u) { return bar + (TWO ? 8u * u : 0u); };
+  auto p_ready = [&](int u) { return bar + 16u + (TWO ? 8u * u : 0u); };
+  const uint32_t s_free = bar + 32u, dp_full = bar + 40u, acc_full = bar + 48u, acc_free = bar + 56u, tmem_slot = bar + 160u;
+  auto f_full = [&](int n) { return bar + 128u + 8u * (n % NF); };           // the set of fixed tiles of item n; its phase is n / NF
+  auto f_empty = [&](int n) { return bar + 144u + 8u * (n % NF); };
   auto x_full = [&](int i) { return bar + 64u + 8u * i; };
-  auto x_empty = [&](int i) { return bar + 88u + 8u * i; };
+  auto x_empty = [&](int i) { return bar + 96u + 8u * i; };
   volatile uint32_t* slot_gen = reinterpret_cast<volatile uint32_t*>(gen + (tmem_slot - base));
   volatile uint32_t* poison_gen = slot_gen + 2;
 
@@ -90,7 +96,8 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < NF; ++i) { mbar_init(f_full(i), 1); mbar_init(f_empty(i), 1); }
-    mbar_init(s_full, 1); mbar_init(s_free, EW); mbar_init(dp_full, 1); mbar_init(p_ready, EW);
+    for (int u = 0; u < (TWO ? 2 : 1); ++u) { mbar_init(s_full(u), 1); mbar_init(p_ready(u), EW); }
+    mbar_init(s_free, EW); mbar_init(dp_full, 1);
     mbar_init(acc_full, 1); mbar_init(acc_free, EW);
     for (int i = 0; i < NS; ++i) { mbar_init(x_full(i), 1); mbar_init(x_empty(i), 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -108,7 +115,15 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
   const bool poisoned = __any_sync(0xffffffffu, *poison_gen != 0);
   pdl_trigger();
   pdl_wait();
-  const uint32_t tDP = tm + 128u, tP = tm + 192u, tAcc = tm + 256u, tDv = tm + 384u;
+  auto t_s = [&](int m, int u) { return tm + (TWO ? 192u * u : 0u) + 64u * m; };
+  auto t_dp = [&](int u) { return tm + (TWO ? 192u * u : 0u) + 128u; };
+  const uint32_t tAcc = tm + (TWO ? 384u : 256u), tDv = tm + (TWO ? 448u : 384u);
+  // packed P_1 - lambda P_2 (w = 0, MODE 0), dS_1 (1), dS_2 (2) of streamed column c (a multiple of 16, or of XC)
+  auto t_p = [&](int w, int c, int u) -> uint32_t {
+    const uint32_t own = (uint32_t)(c / XC * XC + c % XC / 2);     // over columns that the same warp has read
+    if (TWO) return w == 2 ? t_s(1, u) + own : t_s(0, u) + own + (MODE == 0 && w == 1 ? XC / 2 : 0);
+    return w == 2 ? t_dp(u) + own : tm + 192u + 32u * w + (uint32_t)(c / 2);
+  };
 
   if (warp == 0) {
     if (!poisoned && elect_one()) {
@@ -152,48 +167,18 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         const uint32_t idesc_v = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)DH >> 3) << 17) | ((128u >> 4) << 24);       // N = 2 d
         const uint64_t dF = desc_kmajor(sF), dX0 = desc_kmajor(sX);
         auto k_off = [](int e, int span) { return (uint64_t)(((e / 4) * span + (e % 4) * 32) >> 4); };       // 16 columns, number e, of a K-major tile
-        auto issue_s = [&](int item, int st) {
-          const uint64_t dF0 = dF + (uint64_t)((item % NF) * (2 * FB >> 4));
-          const uint64_t x0 = dX0 + (uint64_t)(st * (2 * XB >> 4));
+        auto issue_s = [&](int item, int st, int u) {
+          const uint64_t dF0 = dF + (uint64_t)((item % NF) * (2 * FB >> 4)), x0 = dX0 + (uint64_t)(st * (2 * XB >> 4));
 #pragma unroll
           for (int e = 0; e < DH / 16; ++e)
-            tc_mma(tm + (e < HD / 16 ? 0u : 64u), dF0 + k_off(e, FSPAN), x0 + k_off(e, XSPAN), idesc_s, e % (HD / 16) > 0 ? 1u : 0u);
-          tc_commit(s_full);
+            tc_mma(t_s(e < HD / 16 ? 0 : 1, u), dF0 + k_off(e, FSPAN), x0 + k_off(e, XSPAN), idesc_s, e % (HD / 16) > 0 ? 1u : 0u);
         };
-        auto issue_dp = [&](int item, int st) {
-          const uint64_t dF1 = dF + (uint64_t)(((item % NF) * 2 * FB + FB) >> 4);
-          const uint64_t x1 = dX0 + (uint64_t)((st * 2 * XB + XB) >> 4);
+        auto issue_dp = [&](int item, int st, int u) {
+          const uint64_t dF1 = dF + (uint64_t)(((item % NF) * 2 * FB + FB) >> 4), x1 = dX0 + (uint64_t)((st * 2 * XB + XB) >> 4);
 #pragma unroll
-          for (int e = 0; e < DH / 16; ++e) tc_mma(tDP, dF1 + k_off(e, FSPAN), x1 + k_off(e, XSPAN), idesc_s, e > 0 ? 1u : 0u);
-          tc_commit(dp_full);
+          for (int e = 0; e < DH / 16; ++e) tc_mma(t_dp(u), dF1 + k_off(e, FSPAN), x1 + k_off(e, XSPAN), idesc_s, e > 0 ? 1u : 0u);
         };
-        bool ok = true;
-        int n = 0, t = 0, g = 0, st = 0;                           // g: steps over all items; st: its ring slot
-        uint32_t ph = 0;
-        int idx = dattn_item_at(0), nsteps = idx < nitems ? item_of(idx).nsteps : 0;
-        if (nsteps) {
-          ok = mbar_wait(f_full(0), 0) && mbar_wait(x_full(0), 0);
-          if (ok) {
-            tc_fence_after();
-            issue_s(0, 0);
-            issue_dp(0, 0);
-            if (nsteps == 1) tc_commit(f_empty(0));
-          }
-        }
-        while (ok && idx < nitems) {
-          const bool last = t + 1 == nsteps;
-          const int next_idx = last ? dattn_item_at(n + 1) : idx, st1 = st + 1 == NS ? 0 : st + 1;
-          const uint32_t ph1 = st + 1 == NS ? ph ^ 1u : ph;
-          const bool more = next_idx < nitems;
-          if (!last) {                                             // scores of the next step beside the exponentials of this one
-            ok = mbar_wait(s_free, (uint32_t)(g & 1)) && mbar_wait(x_full(st1), ph1);
-            if (!ok) break;
-            tc_fence_after();
-            issue_s(n, st1);
-          }
-          ok = (t > 0 || n == 0 || mbar_wait(acc_free, (uint32_t)((n - 1) & 1))) && mbar_wait(p_ready, (uint32_t)(g & 1));
-          if (!ok) break;
-          tc_fence_after();
+        auto issue_acc = [&](int st, int u, bool first) {
           const uint64_t nX0 = desc_nmajor(sX, XSPAN) + (uint64_t)(st * (2 * XB >> 4)), nX1 = nX0 + (uint64_t)(XB >> 4);
 #pragma unroll
           for (int m = 0; m < 2; ++m) {
@@ -201,32 +186,108 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
             for (int kk = 0; kk < 4; ++kk) {
               // the map's half of X0's columns: the second span (heads of 128), or the second half of the one span
               const uint64_t b = nX0 + (uint64_t)((kk * 16 * 128 + m * (DH == 128 ? XSPAN : 64)) >> 4);
-              const uint32_t p = MODE == 0 ? (m == 0 ? tP + 32u + kk * 8u : tDP + kk * 16u / XC * XC + kk * 16u % XC / 2u) : tP + m * 32u + kk * 8u;
-              tc_mma_ta(tAcc + (uint32_t)(m * HD), p, b, idesc_h, (t > 0 || kk > 0) ? 1u : 0u);
+              tc_mma_ta(tAcc + (uint32_t)(m * HD), t_p(1 + m, kk * 16, u), b, idesc_h, (!first || kk > 0) ? 1u : 0u);
             }
           }
           if (MODE == 0) {
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) tc_mma_ta(tDv, tP + kk * 8u, nX1 + (uint64_t)((kk * 16 * 128) >> 4), idesc_v, (t > 0 || kk > 0) ? 1u : 0u);
+            for (int kk = 0; kk < 4; ++kk) tc_mma_ta(tDv, t_p(0, kk * 16, u), nX1 + (uint64_t)((kk * 16 * 128) >> 4), idesc_v, (!first || kk > 0) ? 1u : 0u);
           }
           tc_commit(x_empty(st));
-          if (last) tc_commit(acc_full);
-          int next_steps = nsteps;
-          if (more) {
-            if (last) {                                            // another item: its fixed tiles take the place of this one's
-              next_steps = item_of(next_idx).nsteps;
-              ok = mbar_wait(s_free, (uint32_t)(g & 1)) && mbar_wait(f_full(n + 1), (uint32_t)(((n + 1) / NF) & 1)) && mbar_wait(x_full(st1), ph1);
+        };
+        bool ok = true;
+        int n = 0, t = 0, g = 0, st = 0;                           // g: steps over all items; st: its ring slot
+        uint32_t ph = 0;
+        int idx = dattn_item_at(0), nsteps = idx < nitems ? item_of(idx).nsteps : 0;
+        if (TWO) {
+          // the step whose S and dP are issued next, two ahead of the one whose products accumulate
+          int sn = 0, sj = 0, sg = 0, sst = 0, ssteps = nsteps;
+          uint32_t sph = 0;
+          bool live = nsteps > 0;
+          auto ahead = [&]() -> bool {
+            if ((sj == 0 && !mbar_wait(f_full(sn), (uint32_t)((sn / NF) & 1))) || !mbar_wait(x_full(sst), sph)) return false;
+            tc_fence_after();
+            issue_s(sn, sst, sg & 1);
+            issue_dp(sn, sst, sg & 1);
+            tc_commit(s_full(sg & 1));
+            ++sg;
+            if (++sst == NS) { sst = 0; sph ^= 1u; }
+            if (++sj == ssteps) {
+              tc_commit(f_empty(sn));
+              sj = 0;
+              const int i = dattn_item_at(++sn);
+              live = i < nitems;
+              if (live) ssteps = item_of(i).nsteps;
+            }
+            return true;
+          };
+          for (int i = 0; i < 2 && live && ok; ++i) ok = ahead();
+          while (ok && idx < nitems) {
+            ok = (t > 0 || n == 0 || mbar_wait(acc_free, (uint32_t)((n - 1) & 1))) && mbar_wait(p_ready(g & 1), (uint32_t)((g >> 1) & 1));
+            if (!ok) break;
+            tc_fence_after();
+            issue_acc(st, g & 1, t == 0);
+            const bool last = t + 1 == nsteps;
+            if (last) tc_commit(acc_full);
+            if (live) ok = ahead();
+            ++g;
+            if (++st == NS) st = 0;
+            if (last) {
+              t = 0;
+              idx = dattn_item_at(++n);
+              if (idx < nitems) nsteps = item_of(idx).nsteps;
+            } else {
+              ++t;
+            }
+          }
+        } else {
+          if (nsteps) {
+            ok = mbar_wait(f_full(0), 0) && mbar_wait(x_full(0), 0);
+            if (ok) {
+              tc_fence_after();
+              issue_s(0, 0, 0);
+              tc_commit(s_full(0));
+              issue_dp(0, 0, 0);
+              tc_commit(dp_full);
+              if (nsteps == 1) tc_commit(f_empty(0));
+            }
+          }
+          while (ok && idx < nitems) {
+            const bool last = t + 1 == nsteps;
+            const int next_idx = last ? dattn_item_at(n + 1) : idx, st1 = st + 1 == NS ? 0 : st + 1;
+            const uint32_t ph1 = st + 1 == NS ? ph ^ 1u : ph;
+            const bool more = next_idx < nitems;
+            if (!last) {                                           // scores of the next step beside the exponentials of this one
+              ok = mbar_wait(s_free, (uint32_t)(g & 1)) && mbar_wait(x_full(st1), ph1);
               if (!ok) break;
               tc_fence_after();
-              issue_s(n + 1, st1);
+              issue_s(n, st1, 0);
+              tc_commit(s_full(0));
             }
-            issue_dp(last ? n + 1 : n, st1);
-            if (last ? next_steps == 1 : t + 2 == nsteps) tc_commit(f_empty(last ? n + 1 : n));
+            ok = (t > 0 || n == 0 || mbar_wait(acc_free, (uint32_t)((n - 1) & 1))) && mbar_wait(p_ready(0), (uint32_t)(g & 1));
+            if (!ok) break;
+            tc_fence_after();
+            issue_acc(st, 0, t == 0);
+            if (last) tc_commit(acc_full);
+            int next_steps = nsteps;
+            if (more) {
+              if (last) {                                          // another item: its fixed tiles take the place of this one's
+                next_steps = item_of(next_idx).nsteps;
+                ok = mbar_wait(s_free, (uint32_t)(g & 1)) && mbar_wait(f_full(n + 1), (uint32_t)(((n + 1) / NF) & 1)) && mbar_wait(x_full(st1), ph1);
+                if (!ok) break;
+                tc_fence_after();
+                issue_s(n + 1, st1, 0);
+                tc_commit(s_full(0));
+              }
+              issue_dp(last ? n + 1 : n, st1, 0);
+              tc_commit(dp_full);
+              if (last ? next_steps == 1 : t + 2 == nsteps) tc_commit(f_empty(last ? n + 1 : n));
+            }
+            ++g;
+            st = st1;
+            ph = ph1;
+            if (last) { t = 0; ++n; idx = next_idx; nsteps = next_steps; } else ++t;
           }
-          ++g;
-          st = st1;
-          ph = ph1;
-          if (last) { t = 0; ++n; idx = next_idx; nsteps = next_steps; } else ++t;
         }
         if (!ok) atomicCAS(&g_tc_error, 0, 8);
       }
@@ -285,19 +346,23 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
           fetch(nx, nh);
           if (nh != h) lam_next = a.lam[nh];
         }
-        bool ready = mbar_wait(s_full, (uint32_t)(g & 1));
+        const int u = TWO ? g & 1 : 0;
+        const uint32_t par = (uint32_t)((TWO ? g >> 1 : g) & 1);
+        bool ready = mbar_wait(s_full(u), par);
         if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 9);
         ok = __all_sync(0xffffffffu, ready);
         if (!ok) break;
         tc_fence_after();
         uint32_t v[2][XC];
-        tm_load(tm + lane_off + (uint32_t)(hc * XC), v[0]);
-        tm_load(tm + lane_off + (uint32_t)(64 + hc * XC), v[1]);
+        tm_load(t_s(0, u) + lane_off + (uint32_t)(hc * XC), v[0]);
+        tm_load(t_s(1, u) + lane_off + (uint32_t)(hc * XC), v[1]);
         tm_loaded(v[0]);
         tm_loaded(v[1]);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(s_free);                        // the tensor core may overwrite the scores
+        if (!TWO) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(s_free);                      // the tensor core may overwrite the scores
+        }
         // masks only where the tile meets the diagonal or the end of the keys (uniform): MODE 0 hides columns below `lo`, MODE 1 from `lo` on
         int lo;
         bool masked;
@@ -333,13 +398,15 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
           v[1][2 * i] = __float_as_uint(ex2_approx(p));
           v[1][2 * i + 1] = __float_as_uint(ex2_approx(s));
         }
-        ready = mbar_wait(dp_full, (uint32_t)(g & 1));
-        if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 9);
-        ok = __all_sync(0xffffffffu, ready);
-        if (!ok) break;
-        tc_fence_after();
+        if (!TWO) {
+          ready = mbar_wait(dp_full, par);
+          if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 9);
+          ok = __all_sync(0xffffffffu, ready);
+          if (!ok) break;
+          tc_fence_after();
+        }
         uint32_t d[XC], w1[XC / 2], w2[XC / 2], wv[XC / 2];
-        tm_load(tDP + lane_off + (uint32_t)(hc * XC), d);
+        tm_load(t_dp(u) + lane_off + (uint32_t)(hc * XC), d);
         tm_loaded(d);
         if (masked) {
 #pragma unroll
@@ -370,19 +437,14 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
             wv[i] = bf16_pair(e0, e1);
           }
         }
-        // dP of this step is behind the accumulating products of the last one: what they read may be overwritten
-        if (MODE == 0) {
-          tm_store(tP + lane_off + (uint32_t)(hc * (XC / 2)), wv);
-          tm_store(tP + lane_off + 32u + (uint32_t)(hc * (XC / 2)), w1);
-          tm_store(tDP + lane_off + (uint32_t)(hc * XC), w2);
-        } else {
-          tm_store(tP + lane_off + (uint32_t)(hc * (XC / 2)), w1);
-          tm_store(tP + lane_off + 32u + (uint32_t)(hc * (XC / 2)), w2);
-        }
+        // (one step in flight: dP of this step is behind the accumulating products of the last one, so what they read may be overwritten)
+        if (MODE == 0) tm_store(t_p(0, hc * XC, u) + lane_off, wv);
+        tm_store(t_p(1, hc * XC, u) + lane_off, w1);
+        tm_store(t_p(2, hc * XC, u) + lane_off, w2);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(p_ready);
+        if (lane == 0) mbar_arrive(p_ready(u));
         x = nx;
         h = nh;
         lam = lam_next;

@@ -288,11 +288,11 @@ __global__ void __launch_bounds__(256) dattn_prep_kernel(DattnPrep p) {
     else p.dgain_part[(int64_t)slot * D + threadIdx.x] = s;
   }
 }
-// The partial sums' sums, in a fixed order: blocks 0 .. H - 1 one head's dlambda each, the others 32 columns of dgain each.
+// The partial sums' sums, in a fixed order: blocks 0 .. H - 1 one head's dlambda each, the others 8 columns of dgain each.
 __global__ void __launch_bounds__(1024) dattn_sums_kernel(const float* __restrict__ dlam_part, const float* __restrict__ dgain_part,
                                                           float* __restrict__ dlam, float* __restrict__ dgain, int H, int chunks, int D) {
   __shared__ float red[33];
-  __shared__ float col[32][33];
+  __shared__ float col[128][9];
   pdl_launch_next();
   pdl_wait_prior();
   if ((int)blockIdx.x < H) {
@@ -303,18 +303,17 @@ __global__ void __launch_bounds__(1024) dattn_sums_kernel(const float* __restric
     if (threadIdx.x == 0) dlam[blockIdx.x] = s;
     return;
   }
-  const int lane = threadIdx.x & 31, c = ((int)blockIdx.x - H) * 32 + lane, w = threadIdx.x >> 5;
+  const int c8 = threadIdx.x & 7, c = ((int)blockIdx.x - H) * 8 + c8, w = threadIdx.x >> 3;       // D is a multiple of 8
   float s = 0.f;
-  if (c < D) {
 #pragma unroll 4
-    for (int i = w; i < H * chunks; i += 32) s += dgain_part[(int64_t)i * D + c];
-  }
-  col[w][lane] = s;
+  for (int i = w; i < H * chunks; i += 128) s += dgain_part[(int64_t)i * D + c];
+  col[w][c8] = s;
   __syncthreads();
-  if (w == 0 && c < D) {
-#pragma unroll
-    for (int i = 1; i < 32; ++i) s += col[i][lane];
-    dgain[c] = s;
+  if (threadIdx.x < 8) {
+    s = 0.f;
+#pragma unroll 16
+    for (int i = 0; i < 128; ++i) s += col[i][threadIdx.x];
+    dgain[((int)blockIdx.x - H) * 8 + threadIdx.x] = s;
   }
 }
 
@@ -536,13 +535,13 @@ template <typename T> cudaError_t launch_dattn_prep(cudaStream_t st, int D, cons
 #undef CALL
 }
 
-// The backward call's scratch: D_1 | D_2, the gradient of o where there is a norm, the partial sums.  Chunks of rows: enough blocks over the
-// heads for four rounds of 148 SMs, 64 rows at least.
+// The backward call's scratch: D_1 | D_2, the gradient of o where there is a norm, the partial sums.  Chunks of rows: blocks over the heads for eight
+// on each of 148 SMs, 32 rows at least.
 struct DattnPlan { int chunks, rows_per_chunk; size_t dsum, g, part, bytes; };
 inline DattnPlan dattn_plan(int es, int64_t B, int64_t S, int64_t H, int D, bool norm) {
   DattnPlan p;
   const int64_t rows = B * S;
-  int64_t want = (148 * 4 + H - 1) / H, most = (rows + 63) / 64;
+  int64_t want = (148 * 8 + H - 1) / H, most = (rows + 31) / 32;
   if (want > most) want = most;
   if (want < 1) want = 1;
   p.rows_per_chunk = (int)((rows + want - 1) / want);
