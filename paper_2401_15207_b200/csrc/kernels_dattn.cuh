@@ -12,7 +12,8 @@
 // one writer and a fixed order of summation.
 //
 // Tile 64 x 64 with 256 threads: a thread owns 4 x 4 scores (rows 4 ty .., columns tx + 16 j, so that with rows padded by 4 words the reads of
-// 16 bytes along a row are free of bank conflicts) and 4 rows x D / 16 columns of each output.
+// 16 bytes along a row are free of bank conflicts) and 4 rows x 4 or 8 columns of each output.  Where that leaves most of 148 SMs without a block, tiles
+// of 16 rows (RI = 1: one row a thread), whose blocks take a quarter of the time.
 #pragma once
 #include "common.cuh"
 #include "dattn_args.h"
@@ -21,18 +22,19 @@ namespace hift {
 
 __device__ __forceinline__ int dattn_len(const int32_t* __restrict__ lens, int b, int S) { return lens ? max(0, min(lens[b], S)) : S; }
 
-constexpr int kDaT = 64;                                   // rows and columns of a tile
+constexpr int kDaT = 64;                                   // streamed columns of a tile
 template <int D> constexpr int kDaLd = D + 4;              // words between rows of a staged tile
 constexpr int kDaPLd = kDaT + 4;
-template <int D> constexpr int kDaFwdSmem = (3 * kDaT * kDaLd<D> + kDaT * kDaPLd) * 4;
-template <int D> constexpr int kDaDqSmem = (4 * kDaT * kDaLd<D> + kDaT * kDaPLd) * 4;
-template <int D> constexpr int kDaDkvSmem = (4 * kDaT * kDaLd<D> + 3 * kDaT * kDaPLd + 4 * kDaT) * 4;
+// RI: rows of a thread, so 16 RI owned rows of a tile
+template <int D, int RI> constexpr int kDaFwdSmem = ((16 * RI + 2 * kDaT) * kDaLd<D> + 16 * RI * kDaPLd) * 4;
+template <int D, int RI> constexpr int kDaDqSmem = (2 * (16 * RI + kDaT) * kDaLd<D> + 16 * RI * kDaPLd) * 4;
+template <int D, int RI> constexpr int kDaDkvSmem = (2 * (16 * RI + kDaT) * kDaLd<D> + 3 * 16 * RI * kDaPLd + 4 * kDaT) * 4;
 
-// 64 rows of D elements, rows at or beyond `rows` as zeros; `vec`: rows start at 16-byte boundaries
-template <typename T, int D>
+// ROWS rows of D elements, rows at or beyond `rows` as zeros; `vec`: rows start at 16-byte boundaries
+template <typename T, int D, int ROWS>
 __device__ __forceinline__ void da_stage(float* dst, const T* __restrict__ src, int64_t ld, int rows, bool vec) {
   if (vec) {
-    constexpr int N = kDaT * D / 8;                        // groups of 8 elements
+    constexpr int N = ROWS * D / 8;                        // groups of 8 elements
 #pragma unroll
     for (int k = 0; k < (N + 255) / 256; ++k) {
       const int i = threadIdx.x + 256 * k, r = i / (D / 8), c = i % (D / 8) * 8;
@@ -43,61 +45,73 @@ __device__ __forceinline__ void da_stage(float* dst, const T* __restrict__ src, 
     }
     return;
   }
-  for (int i = threadIdx.x; i < kDaT * D; i += 256) {
+  for (int i = threadIdx.x; i < ROWS * D; i += 256) {
     const int r = i / D, c = i % D;
     dst[r * kDaLd<D> + c] = r < rows ? to_f(src[r * ld + c]) : 0.f;
   }
 }
-// s[i][j] = a[row 4 ty + i] . b[row tx + 16 j] over W words
-template <int D, int W>
-__device__ __forceinline__ void da_dots(float (&s)[4][4], const float* a, const float* b, int ty, int tx) {
+// s[i][j] = a[row RI ty + i] . b[row tx + 16 j] over W words
+template <int D, int W, int RI>
+__device__ __forceinline__ void da_dots(float (&s)[RI][4], const float* a, const float* b, int ty, int tx) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < RI; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
 #pragma unroll 4
   for (int e = 0; e < W; e += 4) {
-    float4 x[4], y[4];
+    float4 x[RI], y[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4*>(a + (4 * ty + i) * kDaLd<D> + e);
+    for (int i = 0; i < RI; ++i) x[i] = *reinterpret_cast<const float4*>(a + (RI * ty + i) * kDaLd<D> + e);
 #pragma unroll
     for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4*>(b + (tx + 16 * j) * kDaLd<D> + e);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < RI; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j)
         s[i][j] = fmaf(x[i].x, y[j].x, fmaf(x[i].y, y[j].y, fmaf(x[i].z, y[j].z, fmaf(x[i].w, y[j].w, s[i][j]))));
   }
 }
-// acc[i][n] += sum_k p[row 4 ty + i][k] x[k][column n of this thread] over 64 k; CW columns a thread, of rows of `ld` words
-template <int CW>
-__device__ __forceinline__ void da_accumulate(float (&acc)[4][CW], const float* p, const float* x, int ld, int ty, int tx) {
-  constexpr int VW = CW < 4 ? CW : 4;                      // consecutive columns of a thread; the next ones are 16 VW further
+// An output tile of 16 RI rows x N columns: a thread owns rows RI ty .. and CW columns.  Narrow tiles (N < 64) leave lanes over, which take a share of
+// the 64 k each (KS shares), so that four columns to a thread keep 16 products to each pair of 16-byte reads; the shares are added at the end.
+template <int N, int RI> struct DaOut {
+  static constexpr int G = N < 64 ? N / 4 : 16, KS = 16 / G, CW = N <= 64 ? 4 : N / 16;
+  static __device__ __forceinline__ int col(int n, int tx) { return n / 4 * 64 + tx % G * 4 + n % 4; }
+  // acc[i][n] += sum over this thread's k of p[row RI ty + i][k] x[k][its column n]
+  static __device__ __forceinline__ void accumulate(float (&acc)[RI][CW], const float* p, const float* x, int ld, int ty, int tx) {
+    const int k0 = tx / G * (kDaT / KS);
 #pragma unroll 2
-  for (int k = 0; k < kDaT; k += 4) {
-    float4 w[4];
+    for (int kk = 0; kk < kDaT / KS; kk += 4) {
+      const int k = k0 + kk;
+      float4 w[RI];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const float4*>(p + (4 * ty + i) * kDaPLd + k);
+      for (int i = 0; i < RI; ++i) w[i] = *reinterpret_cast<const float4*>(p + (RI * ty + i) * kDaPLd + k);
 #pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      float v[CW];
+      for (int j = 0; j < 4; ++j) {
+        float v[CW];
 #pragma unroll
-      for (int n = 0; n < CW; n += VW)
+        for (int n = 0; n < CW; n += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(x + (k + j) * ld + col(n, tx));
+          v[n] = f.x; v[n + 1] = f.y; v[n + 2] = f.z; v[n + 3] = f.w;
+        }
 #pragma unroll
-        for (int t = 0; t < VW; ++t) v[n + t] = x[(k + kk) * ld + n * 16 + tx * VW + t];
+        for (int i = 0; i < RI; ++i) {
+          const float f = j == 0 ? w[i].x : j == 1 ? w[i].y : j == 2 ? w[i].z : w[i].w;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float f = kk == 0 ? w[i].x : kk == 1 ? w[i].y : kk == 2 ? w[i].z : w[i].w;
-#pragma unroll
-        for (int n = 0; n < CW; ++n) acc[i][n] = fmaf(f, v[n], acc[i][n]);
+          for (int n = 0; n < CW; ++n) acc[i][n] = fmaf(f, v[n], acc[i][n]);
+        }
       }
     }
   }
-}
-template <int CW> __device__ __forceinline__ int da_col(int n, int tx) {
-  constexpr int VW = CW < 4 ? CW : 4;
-  return n / VW * VW * 16 + tx * VW + n % VW;
-}
+  static __device__ __forceinline__ void join(float (&acc)[RI][CW]) {         // every lane ends with the whole sums
+#pragma unroll
+    for (int o = G; o < 16; o *= 2)
+#pragma unroll
+      for (int i = 0; i < RI; ++i)
+#pragma unroll
+        for (int n = 0; n < CW; ++n) acc[i][n] += __shfl_xor_sync(0xffffffffu, acc[i][n], o);
+  }
+  static __device__ __forceinline__ bool writes(int tx) { return tx < G; }
+};
 __device__ __forceinline__ float half_warp_sum(float v) {
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -110,45 +124,47 @@ __device__ __forceinline__ float half_warp_max(float v) {
 }
 
 // Blocks of one launch are numbered along x alone (no limit of 65535 on heads or batch): the tiles with the most work first.
-template <typename T, int D>
+template <typename T, int D, int RI>
 __global__ void __launch_bounds__(256) dattn_fwd_kernel(DattnArgs a) {
-  constexpr int CW = D / 16, HD = D / 2;
+  typedef DaOut<D, RI> Out;
+  constexpr int CW = Out::CW, HD = D / 2;
+  constexpr int TR = 16 * RI;                              // rows this block owns
   extern __shared__ float da_smem[];
-  float *sq = da_smem, *sk = sq + kDaT * kDaLd<D>, *sv = sk + kDaT * kDaLd<D>, *sp = sv + kDaT * kDaLd<D>;
+  float *sq = da_smem, *sk = sq + TR * kDaLd<D>, *sv = sk + kDaT * kDaLd<D>, *sp = sv + kDaT * kDaLd<D>;
   pdl_launch_next();
   pdl_wait_prior();
-  const int ntile = (a.S + kDaT - 1) / kDaT, tile = ntile - 1 - (int)(blockIdx.x / (unsigned)(a.B * a.H));
+  const int ntile = (a.S + TR - 1) / TR, tile = ntile - 1 - (int)(blockIdx.x / (unsigned)(a.B * a.H));
   const int bh = (int)(blockIdx.x % (unsigned)(a.B * a.H)), b = bh / a.H, h = bh % a.H, kh = h / (a.H / a.K);
-  const int q0 = tile * kDaT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int len = dattn_len(a.lens, b, a.S), kend = a.causal ? min(len, min(q0 + kDaT, a.S)) : len;
+  const int q0 = tile * TR, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int len = dattn_len(a.lens, b, a.S), kend = a.causal ? min(len, min(q0 + TR, a.S)) : len;
   const int64_t ld = (int64_t)(a.H + 2 * a.K) * D;
   const T* base = (const T*)a.qkv + (int64_t)b * a.S * ld;
-  da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0, a.vec);
-  float acc[2][4][CW], m[2][4], l[2][4];
+  da_stage<T, D, TR>(sq, base + q0 * ld + h * D, ld, a.S - q0, a.vec);
+  float acc[2][RI][CW], m[2][RI], l[2][RI];
 #pragma unroll
   for (int z = 0; z < 2; ++z)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < RI; ++i) {
       m[z][i] = -INFINITY; l[z][i] = 0.f;
 #pragma unroll
       for (int n = 0; n < CW; ++n) acc[z][i][n] = 0.f;
     }
   for (int k0 = 0; k0 < kend; k0 += kDaT) {
     __syncthreads();
-    da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, a.S - k0, a.vec);
-    da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0, a.vec);          // (rows of padding may hold anything: 0 * NaN)
+    da_stage<T, D, kDaT>(sk, base + k0 * ld + (a.H + kh) * D, ld, a.S - k0, a.vec);
+    da_stage<T, D, kDaT>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0, a.vec);          // (rows of padding may hold anything: 0 * NaN)
     __syncthreads();
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      float s[4][4];
-      da_dots<D, HD>(s, sq + z * HD, sk + z * HD, ty, tx);
+      float s[RI][4];
+      da_dots<D, HD, RI>(s, sq + z * HD, sk + z * HD, ty, tx);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < RI; ++i) {
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int key = k0 + tx + 16 * j;
-          s[i][j] = key >= len || (a.causal && key > q0 + 4 * ty + i) ? -INFINITY : s[i][j] * a.scale;
+          s[i][j] = key >= len || (a.causal && key > q0 + RI * ty + i) ? -INFINITY : s[i][j] * a.scale;
           top = fmaxf(top, s[i][j]);
         }
         const float mn = fmaxf(m[z][i], half_warp_max(top)), ref = mn == -INFINITY ? 0.f : mn, corr = expf(m[z][i] - ref);
@@ -157,7 +173,7 @@ __global__ void __launch_bounds__(256) dattn_fwd_kernel(DattnArgs a) {
         for (int j = 0; j < 4; ++j) {
           const float p = expf(s[i][j] - ref);
           sum += p;
-          sp[(4 * ty + i) * kDaPLd + tx + 16 * j] = p;
+          sp[(RI * ty + i) * kDaPLd + tx + 16 * j] = p;
         }
         l[z][i] = l[z][i] * corr + half_warp_sum(sum);
         m[z][i] = mn;
@@ -165,14 +181,16 @@ __global__ void __launch_bounds__(256) dattn_fwd_kernel(DattnArgs a) {
         for (int n = 0; n < CW; ++n) acc[z][i][n] *= corr;
       }
       __syncwarp();                                        // a warp's 8 rows of P are its own
-      da_accumulate<CW>(acc[z], sp, sv, kDaLd<D>, ty, tx);
+      Out::accumulate(acc[z], sp, sv, kDaLd<D>, ty, tx);
       __syncwarp();
     }
   }
   const float lam = a.lam[h];
+  Out::join(acc[0]);
+  Out::join(acc[1]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int q = q0 + 4 * ty + i;
+  for (int i = 0; i < RI; ++i) {
+    const int q = q0 + RI * ty + i;
     const float r1 = l[0][i] > 0.f ? 1.f / l[0][i] : l[0][i] == 0.f ? 0.f : l[0][i];          // no key: zeros; NaN stays
     const float r2 = l[1][i] > 0.f ? 1.f / l[1][i] : l[1][i] == 0.f ? 0.f : l[1][i];
     float o[CW], o2[CW], sq2 = 0.f;
@@ -183,12 +201,12 @@ __global__ void __launch_bounds__(256) dattn_fwd_kernel(DattnArgs a) {
       sq2 = fmaf(o[n], o[n], sq2);
     }
     float r = 0.f;
-    if (a.y) r = a.c / sqrtf(half_warp_sum(sq2) * (1.0f / D) + a.eps);
+    if (a.y) r = a.c / sqrtf(half_warp_sum(sq2) * (1.0f / (D * Out::KS)) + a.eps);      // (each column KS times)
     if (q >= a.S) continue;
     const int64_t at = ((int64_t)b * a.S + q) * a.H * D + h * D;
 #pragma unroll
-    for (int n = 0; n < CW; ++n) {
-      const int c = da_col<CW>(n, tx);
+    for (int n = 0; n < CW && Out::writes(tx); ++n) {
+      const int c = Out::col(n, tx);
       ((T*)a.o)[at + c] = from_f<T>(o[n]);
       if (a.o2) ((T*)a.o2)[at + c] = from_f<T>(o2[n]);
       if (a.y) ((T*)a.y)[at + c] = from_f<T>(o[n] * r * to_f(((const T*)a.gain)[c]));
@@ -269,7 +287,8 @@ __global__ void __launch_bounds__(256) dattn_prep_kernel(DattnPrep p) {
     if (in) {
       if (p.g_out) store8((T*)p.g_out + at, g);            // (the scratch is aligned)
       if (part == 0) {
-        const int64_t b = t / a.S, row = (b * a.H + h) * a.S + (t - b * a.S);
+        const uint32_t b = (uint32_t)t / (uint32_t)a.S;
+        const int64_t row = ((int64_t)b * a.H + h) * a.S + (t - (int64_t)b * a.S);
         p.dsum_out[row] = d1;
         p.dsum_out[(int64_t)a.B * a.H * a.S + row] = d2;
       }
@@ -317,26 +336,28 @@ __global__ void __launch_bounds__(1024) dattn_sums_kernel(const float* __restric
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, int RI>
 __global__ void __launch_bounds__(256) dattn_dq_kernel(DattnArgs a) {
-  constexpr int HD = D / 2, CW = HD / 16 > 0 ? HD / 16 : 1, COLS = CW * 16 > HD ? HD : CW * 16;
+  constexpr int HD = D / 2, CW = DaOut<HD, RI>::CW;
+  typedef DaOut<HD, RI> Out;
+  constexpr int TR = 16 * RI;                              // rows this block owns
   extern __shared__ float da_smem[];
-  float *sq = da_smem, *sg = sq + kDaT * kDaLd<D>, *sk = sg + kDaT * kDaLd<D>, *sv = sk + kDaT * kDaLd<D>, *sp = sv + kDaT * kDaLd<D>;
+  float *sq = da_smem, *sg = sq + TR * kDaLd<D>, *sk = sg + TR * kDaLd<D>, *sv = sk + kDaT * kDaLd<D>, *sp = sv + kDaT * kDaLd<D>;
   pdl_launch_next();
   pdl_wait_prior();
-  const int ntile = (a.S + kDaT - 1) / kDaT, tile = ntile - 1 - (int)(blockIdx.x / (unsigned)(a.B * a.H));
+  const int ntile = (a.S + TR - 1) / TR, tile = ntile - 1 - (int)(blockIdx.x / (unsigned)(a.B * a.H));
   const int bh = (int)(blockIdx.x % (unsigned)(a.B * a.H)), b = bh / a.H, h = bh % a.H, kh = h / (a.H / a.K);
-  const int q0 = tile * kDaT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int len = dattn_len(a.lens, b, a.S), kend = a.causal ? min(len, min(q0 + kDaT, a.S)) : len;
+  const int q0 = tile * TR, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int len = dattn_len(a.lens, b, a.S), kend = a.causal ? min(len, min(q0 + TR, a.S)) : len;
   const int64_t ld = (int64_t)(a.H + 2 * a.K) * D, nrow = (int64_t)a.B * a.H * a.S;
   const T* base = (const T*)a.qkv + (int64_t)b * a.S * ld;
-  da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0, a.vec);
-  da_stage<T, D>(sg, (const T*)a.g + ((int64_t)b * a.S + q0) * a.H * D + h * D, (int64_t)a.H * D, a.S - q0, a.vec);
+  da_stage<T, D, TR>(sq, base + q0 * ld + h * D, ld, a.S - q0, a.vec);
+  da_stage<T, D, TR>(sg, (const T*)a.g + ((int64_t)b * a.S + q0) * a.H * D + h * D, (int64_t)a.H * D, a.S - q0, a.vec);
   const float lam = a.lam[h];
-  float acc[2][4][CW], lse[2][4], ds[2][4];
+  float acc[2][RI][CW], lse[2][RI], ds[2][RI];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t row = ((int64_t)b * a.H + h) * a.S + min(q0 + 4 * ty + i, a.S - 1);
+  for (int i = 0; i < RI; ++i) {
+    const int64_t row = ((int64_t)b * a.H + h) * a.S + min(q0 + RI * ty + i, a.S - 1);
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
       lse[z][i] = a.lse[z * nrow + row];
@@ -347,62 +368,67 @@ __global__ void __launch_bounds__(256) dattn_dq_kernel(DattnArgs a) {
   }
   for (int k0 = 0; k0 < kend; k0 += kDaT) {
     __syncthreads();
-    da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, len - k0, a.vec);
-    da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0, a.vec);
+    da_stage<T, D, kDaT>(sk, base + k0 * ld + (a.H + kh) * D, ld, len - k0, a.vec);
+    da_stage<T, D, kDaT>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0, a.vec);
     __syncthreads();
-    float dp[4][4];
-    da_dots<D, D>(dp, sg, sv, ty, tx);
+    float dp[RI][4];
+    da_dots<D, D, RI>(dp, sg, sv, ty, tx);
 #pragma unroll
     for (int z = 0; z < 2; ++z) {
-      float s[4][4];
-      da_dots<D, HD>(s, sq + z * HD, sk + z * HD, ty, tx);
+      float s[RI][4];
+      da_dots<D, HD, RI>(s, sq + z * HD, sk + z * HD, ty, tx);
       const float w = z == 0 ? a.scale : -lam * a.scale;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < RI; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int key = k0 + tx + 16 * j, q = q0 + 4 * ty + i;
+          const int key = k0 + tx + 16 * j, q = q0 + RI * ty + i;
           const bool seen = key < len && q < a.S && (!a.causal || key <= q);
-          sp[(4 * ty + i) * kDaPLd + tx + 16 * j] = seen ? w * expf(fmaf(s[i][j], a.scale, -lse[z][i])) * (dp[i][j] - ds[z][i]) : 0.f;
+          sp[(RI * ty + i) * kDaPLd + tx + 16 * j] = seen ? w * expf(fmaf(s[i][j], a.scale, -lse[z][i])) * (dp[i][j] - ds[z][i]) : 0.f;
         }
       __syncwarp();
-      if (tx * CW < COLS) da_accumulate<CW>(acc[z], sp, sk + z * HD, kDaLd<D>, ty, tx);
+      Out::accumulate(acc[z], sp, sk + z * HD, kDaLd<D>, ty, tx);
       __syncwarp();
     }
   }
+  Out::join(acc[0]);
+  Out::join(acc[1]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int q = q0 + 4 * ty + i;
-    if (q >= a.S || tx * CW >= COLS) continue;
+  for (int i = 0; i < RI; ++i) {
+    const int q = q0 + RI * ty + i;
+    if (q >= a.S || !Out::writes(tx)) continue;
     T* row = (T*)a.dqkv + ((int64_t)b * a.S + q) * ld + h * D;
 #pragma unroll
     for (int z = 0; z < 2; ++z)
 #pragma unroll
-      for (int n = 0; n < CW; ++n) row[z * HD + da_col<CW>(n, tx)] = from_f<T>(acc[z][i][n]);
+      for (int n = 0; n < CW; ++n) row[z * HD + Out::col(n, tx)] = from_f<T>(acc[z][i][n]);
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, int RI>
 __global__ void __launch_bounds__(256) dattn_dkv_kernel(DattnArgs a) {
-  constexpr int HD = D / 2, CW = HD / 16 > 0 ? HD / 16 : 1, COLS = CW * 16 > HD ? HD : CW * 16, VW = D / 16;
+  typedef DaOut<D / 2, RI> Half;
+  typedef DaOut<D, RI> Whole;
+  constexpr int HD = D / 2, CW = Half::CW, VW = Whole::CW;
+  constexpr int TR = 16 * RI;                              // rows this block owns
   extern __shared__ float da_smem[];
-  float *sk = da_smem, *sv = sk + kDaT * kDaLd<D>, *sq = sv + kDaT * kDaLd<D>, *sg = sq + kDaT * kDaLd<D>;
+  float *sk = da_smem, *sv = sk + TR * kDaLd<D>, *sq = sv + TR * kDaLd<D>, *sg = sq + kDaT * kDaLd<D>;
   float* st[3];
-  st[0] = sg + kDaT * kDaLd<D>; st[1] = st[0] + kDaT * kDaPLd; st[2] = st[1] + kDaT * kDaPLd;
-  float* rowv = st[2] + kDaT * kDaPLd;                     // [lse 1 | lse 2 | D 1 | D 2][64 queries]
+  st[0] = sg + kDaT * kDaLd<D>; st[1] = st[0] + TR * kDaPLd; st[2] = st[1] + TR * kDaPLd;
+  float* rowv = st[2] + TR * kDaPLd;                     // [lse 1 | lse 2 | D 1 | D 2][64 queries]
   pdl_launch_next();
   pdl_wait_prior();
   const int tile = (int)(blockIdx.x / (unsigned)(a.B * a.K));                          // the first keys meet the most queries
   const int bh = (int)(blockIdx.x % (unsigned)(a.B * a.K)), b = bh / a.K, kh = bh % a.K, group = a.H / a.K;
-  const int k0 = tile * kDaT, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  const int k0 = tile * TR, tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int len = dattn_len(a.lens, b, a.S);
   const int64_t ld = (int64_t)(a.H + 2 * a.K) * D, nrow = (int64_t)a.B * a.H * a.S;
   const T* base = (const T*)a.qkv + (int64_t)b * a.S * ld;
-  da_stage<T, D>(sk, base + k0 * ld + (a.H + kh) * D, ld, len - k0, a.vec);
-  da_stage<T, D>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0, a.vec);
-  float dk[2][4][CW], dv[4][VW];
+  da_stage<T, D, TR>(sk, base + k0 * ld + (a.H + kh) * D, ld, len - k0, a.vec);
+  da_stage<T, D, TR>(sv, base + k0 * ld + (a.H + a.K + kh) * D, ld, len - k0, a.vec);
+  float dk[2][RI][CW], dv[RI][VW];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < RI; ++i) {
 #pragma unroll
     for (int n = 0; n < VW; ++n) dv[i][n] = 0.f;
 #pragma unroll
@@ -413,55 +439,56 @@ __global__ void __launch_bounds__(256) dattn_dkv_kernel(DattnArgs a) {
   if (k0 < len) {                                          // the whole block
     for (int h = kh * group; h < (kh + 1) * group; ++h) {
       const float lam = a.lam[h];
-      for (int q0 = a.causal ? k0 : 0; q0 < a.S; q0 += kDaT) {
+      for (int q0 = a.causal ? k0 / kDaT * kDaT : 0; q0 < a.S; q0 += kDaT) {
         __syncthreads();
-        da_stage<T, D>(sq, base + q0 * ld + h * D, ld, a.S - q0, a.vec);
-        da_stage<T, D>(sg, (const T*)a.g + ((int64_t)b * a.S + q0) * a.H * D + h * D, (int64_t)a.H * D, a.S - q0, a.vec);
+        da_stage<T, D, kDaT>(sq, base + q0 * ld + h * D, ld, a.S - q0, a.vec);
+        da_stage<T, D, kDaT>(sg, (const T*)a.g + ((int64_t)b * a.S + q0) * a.H * D + h * D, (int64_t)a.H * D, a.S - q0, a.vec);
         {
           const int z = threadIdx.x >> 6;
           const int64_t row = ((int64_t)b * a.H + h) * a.S + min(q0 + (int)(threadIdx.x & 63), a.S - 1);
           rowv[threadIdx.x] = z < 2 ? a.lse[z * nrow + row] : a.dsum[(z - 2) * nrow + row];
         }
         __syncthreads();
-        float dp[4][4], mix[4][4];
-        da_dots<D, D>(dp, sv, sg, ty, tx);                 // [key][query]
+        float dp[RI][4], mix[RI][4];
+        da_dots<D, D, RI>(dp, sv, sg, ty, tx);                 // [key][query]
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
-          float s[4][4];
-          da_dots<D, HD>(s, sk + z * HD, sq + z * HD, ty, tx);
+          float s[RI][4];
+          da_dots<D, HD, RI>(s, sk + z * HD, sq + z * HD, ty, tx);
           const float w = z == 0 ? a.scale : -lam * a.scale;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < RI; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const int c = tx + 16 * j, key = k0 + 4 * ty + i, q = q0 + c;
+              const int c = tx + 16 * j, key = k0 + RI * ty + i, q = q0 + c;
               const bool seen = key < len && q < a.S && (!a.causal || key <= q);
               const float p = seen ? expf(fmaf(s[i][j], a.scale, -rowv[z * kDaT + c])) : 0.f;
               mix[i][j] = z == 0 ? p : fmaf(-lam, p, mix[i][j]);
-              st[z][(4 * ty + i) * kDaPLd + c] = seen ? w * p * (dp[i][j] - rowv[(2 + z) * kDaT + c]) : 0.f;
-              if (z == 1) st[2][(4 * ty + i) * kDaPLd + c] = mix[i][j];
+              st[z][(RI * ty + i) * kDaPLd + c] = seen ? w * p * (dp[i][j] - rowv[(2 + z) * kDaT + c]) : 0.f;
+              if (z == 1) st[2][(RI * ty + i) * kDaPLd + c] = mix[i][j];
             }
         }
         __syncwarp();
-        da_accumulate<VW>(dv, st[2], sg, kDaLd<D>, ty, tx);
-        if (tx * CW < COLS) {
-          da_accumulate<CW>(dk[0], st[0], sq, kDaLd<D>, ty, tx);
-          da_accumulate<CW>(dk[1], st[1], sq + HD, kDaLd<D>, ty, tx);
-        }
+        Whole::accumulate(dv, st[2], sg, kDaLd<D>, ty, tx);
+        Half::accumulate(dk[0], st[0], sq, kDaLd<D>, ty, tx);
+        Half::accumulate(dk[1], st[1], sq + HD, kDaLd<D>, ty, tx);
       }
     }
   }
+  Whole::join(dv);
+  Half::join(dk[0]);
+  Half::join(dk[1]);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int key = k0 + 4 * ty + i;
+  for (int i = 0; i < RI; ++i) {
+    const int key = k0 + RI * ty + i;
     if (key >= a.S) continue;                              // rows of padding get zeros
     T* row = (T*)a.dqkv + ((int64_t)b * a.S + key) * ld;
 #pragma unroll
     for (int z = 0; z < 2; ++z)
 #pragma unroll
-      for (int n = 0; n < CW; ++n) if (tx * CW < COLS) row[(a.H + kh) * D + z * HD + da_col<CW>(n, tx)] = from_f<T>(dk[z][i][n]);
+      for (int n = 0; n < CW && Half::writes(tx); ++n) row[(a.H + kh) * D + z * HD + Half::col(n, tx)] = from_f<T>(dk[z][i][n]);
 #pragma unroll
-    for (int n = 0; n < VW; ++n) row[(a.H + a.K + kh) * D + da_col<VW>(n, tx)] = from_f<T>(dv[i][n]);
+    for (int n = 0; n < VW && Whole::writes(tx); ++n) row[(a.H + a.K + kh) * D + Whole::col(n, tx)] = from_f<T>(dv[i][n]);
   }
 }
 
@@ -512,16 +539,25 @@ cudaError_t dattn_launch(void (*kernel)(A), int64_t blocks, int smem, cudaStream
   const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   return e != cudaSuccess ? e : launch_pdl(kernel, dim3((unsigned)blocks), dim3(256), smem, st, a);
 }
+// Small tiles where four times the blocks still find an SM each (2 x 131 x 4 heads of 32: see the table of the operators).
+inline bool dattn_small(int S, int64_t heads) { return (int64_t)((S + 15) / 16) * heads <= 2 * 148; }
+template <typename T, int D> cudaError_t launch_dattn_fwd_d(cudaStream_t st, const DattnArgs& a) {
+  const int64_t bh = (int64_t)a.B * a.H;
+  if (dattn_small(a.S, bh)) return dattn_launch(dattn_fwd_kernel<T, D, 1>, (a.S + 15) / 16 * bh, kDaFwdSmem<D, 1>, st, a);
+  return dattn_launch(dattn_fwd_kernel<T, D, 4>, (a.S + 63) / 64 * bh, kDaFwdSmem<D, 4>, st, a);
+}
 template <typename T> cudaError_t launch_dattn_fwd(cudaStream_t st, int D, const DattnArgs& a) {
-  const int64_t blocks = (int64_t)((a.S + kDaT - 1) / kDaT) * a.B * a.H;
-#define CALL(N) dattn_launch(dattn_fwd_kernel<T, N>, blocks, kDaFwdSmem<N>, st, a)
+#define CALL(N) launch_dattn_fwd_d<T, N>(st, a)
   HIFT_DATTN_SWITCH(D, CALL)
 #undef CALL
 }
 template <typename T, int D> cudaError_t launch_dattn_bwd_d(cudaStream_t st, const DattnArgs& a) {
-  const int64_t tiles = (a.S + kDaT - 1) / kDaT;
-  const cudaError_t e = dattn_launch(dattn_dq_kernel<T, D>, tiles * a.B * a.H, kDaDqSmem<D>, st, a);
-  return e != cudaSuccess ? e : dattn_launch(dattn_dkv_kernel<T, D>, tiles * a.B * a.K, kDaDkvSmem<D>, st, a);
+  const int64_t bh = (int64_t)a.B * a.H, bk = (int64_t)a.B * a.K, small = (a.S + 15) / 16, tiles = (a.S + 63) / 64;
+  const cudaError_t e = dattn_small(a.S, bh) ? dattn_launch(dattn_dq_kernel<T, D, 1>, small * bh, kDaDqSmem<D, 1>, st, a)
+                                             : dattn_launch(dattn_dq_kernel<T, D, 4>, tiles * bh, kDaDqSmem<D, 4>, st, a);
+  if (e != cudaSuccess) return e;
+  return dattn_small(a.S, bk) ? dattn_launch(dattn_dkv_kernel<T, D, 1>, small * bk, kDaDkvSmem<D, 1>, st, a)
+                              : dattn_launch(dattn_dkv_kernel<T, D, 4>, tiles * bk, kDaDkvSmem<D, 4>, st, a);
 }
 template <typename T> cudaError_t launch_dattn_bwd(cudaStream_t st, int D, const DattnArgs& a) {
 #define CALL(N) launch_dattn_bwd_d<T, N>(st, a)
