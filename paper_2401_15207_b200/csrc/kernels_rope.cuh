@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(RopeOp p) {
     }
     return;
   }
-  int pos = p.positions ? p.positions[row] : (int)(row % p.seq);
+  int pos = p.positions ? p.positions[row] : (int)((uint32_t)row % (uint32_t)p.seq);          // rows are below 2^31
   const bool in = pos >= 0 && pos < p.n_pos;
   if (!in) {                                               // the row stays as it is
     if (p.bad && k == 0) *p.bad = 1;
