@@ -10,6 +10,7 @@
 // dk and dq are multiplied by `scale` as they are stored.  dP is shared by the maps, and dv takes one product for both: 8 units of 128 x 64 x 64 a
 // step against the 10 of two plain attentions.  P and dS are rounded to bf16, the operand type of the products they feed; the accumulators are fp32.
 //   warp 0    : TMA producer         warp 1: issues every product (one elected thread); owns the tensor memory
+//   warp 2    : MODE 1 with key lengths, K's rows of hidden keys -> zeros
 //   warps 4.. : element-wise, two or four warps to a lane quarter, their share of the 64 streamed columns each: S_1, S_2 -> registers, exponentials; dP, dS;
 //               P and dS go back to tensor memory as bf16, the A operands of the accumulating products; at an item's end the accumulators -> global
 // Two steps in flight (MODE 1, and heads of 64): two sets of S_1, S_2, dP (columns 192 u ..), accumulators behind 384.  P and dS lie over the scores, each
@@ -70,6 +71,7 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
   auto f_empty = [&](int n) { return bar + 144u + 8u * (n % NF); };
   auto x_full = [&](int i) { return bar + 64u + 8u * i; };
   auto x_empty = [&](int i) { return bar + 96u + 8u * i; };
+  auto x_ok = [&](int i) { return bar + 176u + 8u * i; };
   volatile uint32_t* slot_gen = reinterpret_cast<volatile uint32_t*>(gen + (tmem_slot - base));
   volatile uint32_t* poison_gen = slot_gen + 2;
 
@@ -100,7 +102,7 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
     for (int u = 0; u < (TWO ? 2 : 1); ++u) { mbar_init(s_full(u), 1); mbar_init(p_ready(u), EW); }
     mbar_init(s_free, EW); mbar_init(dp_full, 1);
     mbar_init(acc_full, 1); mbar_init(acc_free, EW);
-    for (int i = 0; i < NS; ++i) { mbar_init(x_full(i), 1); mbar_init(x_empty(i), 1); }
+    for (int i = 0; i < NS; ++i) { mbar_init(x_full(i), 1); mbar_init(x_empty(i), 1); mbar_init(x_ok(i), 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     pdl_wait();                                                    // no global access before it, the flag included
     *poison_gen = g_tc_error != 0 ? 1u : 0u;
@@ -206,7 +208,7 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
           uint32_t sph = 0;
           bool live = nsteps > 0;
           auto ahead = [&]() -> bool {
-            if ((sj == 0 && !mbar_wait(f_full(sn), (uint32_t)((sn / NF) & 1))) || !mbar_wait(x_full(sst), sph)) return false;
+            if ((sj == 0 && !mbar_wait(f_full(sn), (uint32_t)((sn / NF) & 1))) || !mbar_wait(MODE == 1 && a.lens ? x_ok(sst) : x_full(sst), sph)) return false;
             tc_fence_after();
             issue_s(sn, sst, sg & 1);
             issue_dp(sn, sst, sg & 1);
@@ -293,6 +295,25 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         if (!ok) atomicCAS(&g_tc_error, 0, 8);
       }
       __syncwarp();
+    }
+  } else if (MODE == 1 && warp == 2) {
+    if (!poisoned && a.lens) {
+      // ---------------- hidden keys: rows of a block of K behind the entry's length become zeros (dS is 0 there, but 0 times NaN is not)
+      int st = 0, n = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int idx = dattn_item_at(n); idx < nitems && ok; idx = dattn_item_at(++n)) {
+        const DattnBwdItem it = item_of(idx);
+        for (int t = 0; t < it.nsteps; ++t) {
+          const bool ready = mbar_wait(x_full(st), ph);
+          if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 7);
+          ok = __all_sync(0xffffffffu, ready);
+          if (!ok) break;
+          zero_rows<SP, kDbX>(gen + (sX + st * 2 * XB - base), it.len - t * kDbX, lane);
+          if (lane == 0) mbar_arrive(x_ok(st));
+          if (++st == NS) { st = 0; ph ^= 1u; }
+        }
+      }
     }
   } else if (warp >= 4) {
     // ---------------- element-wise: thread = row of the fixed tile x XC streamed columns

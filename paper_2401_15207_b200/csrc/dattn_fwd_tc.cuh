@@ -7,6 +7,7 @@
 //                sequence are zeros and never the next entry's
 //   warp 1     : issues everything (one elected thread), in the order  P_m V of block j, S_m of block j + 2  for m = 1, 2; owns the tensor
 //                memory.  (An issuer for each map: 138 -> 153 us)
+//   warp 2     : with key lengths, V's rows of hidden keys -> zeros
 //   warps 4-11 : softmax, four warps to a map, one thread to a query row: S_m -> registers, mask, maximum, exponentials, P_m as bf16 over
 //                S_m's columns in tensor memory (the A operand of P_m V: no shared-memory traffic for it).  The rounding of P to bf16 is the
 //                operand type's; the row's sum takes the values before it
@@ -78,6 +79,16 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// Zeros in rows `from` .. ROWS - 1 of a tile of SP spans of ROWS rows x 128 bytes (a whole warp), before the tensor core reads them.
+template <int SP, int ROWS> __device__ __forceinline__ void zero_rows(uint8_t* tile, int from, int lane) {
+  if (from >= ROWS) return;
+  for (int r = max(from, 0) + (lane >> 3); r < ROWS; r += 4) {
+#pragma unroll
+    for (int sp = 0; sp < SP; ++sp) *reinterpret_cast<uint4*>(tile + sp * (ROWS * 128) + r * 128 + (lane & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+  }
+  fence_async_smem();
+  __syncwarp();
+}
 // Items: (batch, head, 128 query rows), the longest first, dealt forwards on even rounds and backwards on odd ones (as in attention_tc.cuh).
 struct DattnItem { int b, h, q0, nblk, len; };
 __device__ __forceinline__ DattnItem dattn_item(int idx, int nqb, int nbh, int H, int S, int causal, const int* __restrict__ lens) {
@@ -111,6 +122,7 @@ dattn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
   auto k_empty = [&](int i) { return bar + 32u + 8u * i; };
   auto v_full = [&](int i) { return bar + 64u + 8u * i; };
   auto v_empty = [&](int i) { return bar + 96u + 8u * i; };
+  auto v_ok = [&](int i) { return bar + 24u + 32u * i; };          // (each fourth word of the rows above: three stages)
   auto q_full = [&](int i) { return bar + 128u + 8u * i; };
   auto q_empty = [&](int i) { return bar + 144u + 8u * i; };
   auto s_full = [&](int m, int u) { return bar + 160u + 16u * m + 8u * u; };
@@ -129,7 +141,7 @@ dattn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
   auto item_of = [&](int idx) { return dattn_item(idx, nqb, nbh, a.H, a.S, a.causal, a.lens); };
 
   if (threadIdx.x == 0) {
-    for (int i = 0; i < NS; ++i) { mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); mbar_init(v_full(i), 1); mbar_init(v_empty(i), 1); }
+    for (int i = 0; i < NS; ++i) { mbar_init(k_full(i), 1); mbar_init(k_empty(i), 1); mbar_init(v_full(i), 1); mbar_init(v_empty(i), 1); mbar_init(v_ok(i), 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(q_full(i), 1); mbar_init(q_empty(i), 1); mbar_init(pv_done(i), 1);
       for (int u = 0; u < 2; ++u) { mbar_init(s_full(i, u), 1); mbar_init(p_ready(i, u), 4); }
@@ -178,6 +190,23 @@ dattn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
           for (int sp = 0; sp < SP; ++sp) tma_load_3d(sV + st * BB + sp * KSPAN, &tmap_kv, v_full(st), colV + sp * 64, j * kDfKeys, it.b);
         }
       }
+    } else if (warp == 2 && !poisoned && a.lens) {
+      // ---------------- values of hidden keys: rows of a block of V behind the entry's length become zeros (P is 0 there, but 0 times NaN is not)
+      int st = 0, n = 0;
+      uint32_t ph = 0;
+      bool ok = true;
+      for (int idx = dattn_item_at(n); idx < nitems && ok; idx = dattn_item_at(++n)) {
+        const DattnItem it = item_of(idx);
+        for (int j = 0; j < it.nblk; ++j) {
+          const bool ready = mbar_wait(v_full(st), ph);
+          if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 4);
+          ok = __all_sync(0xffffffffu, ready);
+          if (!ok) break;
+          zero_rows<SP, kDfKeys>(gen + (sV + st * BB - base), it.len - j * kDfKeys, lane);
+          if (lane == 0) mbar_arrive(v_ok(st));
+          if (++st == NS) { st = 0; ph ^= 1; }
+        }
+      }
     } else if (warp == 1 && !poisoned) {
       if (elect_one()) {
         // ---------------- MMA issuer
@@ -223,7 +252,7 @@ dattn_fwd_tc_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
           constexpr int m = decltype(map)::value;
           const int u = g & 1;
           if (m == 0) {
-            if (!mbar_wait(v_full(st), ph)) return false;
+            if (!mbar_wait(a.lens ? v_ok(st) : v_full(st), ph)) return false;
             // an item's first products overwrite an accumulator that its previous item's epilogue has read
             if (j == 0 && !mbar_wait(o_free(n % NO), (uint32_t)(((n / NO) & 1) ^ 1))) return false;
           }

@@ -148,6 +148,24 @@ def test_differential_attention_bad_values_stay_in_their_entry(code, D):
         assert bool(got[n][S + 60:2 * S].isnan().any())
 
 
+@pytest.mark.parametrize("code,D", [(0, 32), (0, 64), (1, 32), (1, 64), (1, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_differential_attention_whatever_padded_keys_hold(code, D, causal):
+    """NaN and infinity in k and v at padded keys change no bit of any output; lengths of 0, inside a tile, at its end, and whole."""
+    torch = _torch()
+    B, S, H, K = 5, 210, 4, 2
+    lens = [0, 70, 128, 210, 1]
+    s = _dattn_case(code, B, S, H, K, D, True, 14, lens)
+    kv = s["qkv"].view(B, S, H + 2 * K, D)[:, :, H:]
+    clean = _dattn_run(code, B, S, H, K, D, causal, s)
+    for b, n in enumerate(lens):
+        kv[b, n:] = NAN
+        kv[b, n + 1::3] = INF
+    got = _dattn_run(code, B, S, H, K, D, causal, s)
+    for n in got:
+        assert torch.equal(got[n], clean[n]), n
+
+
 @pytest.mark.parametrize("code,D", [(0, 32), (1, 32), (1, 64), (1, 128)])
 def test_differential_attention_repeats_its_bits(code, D):
     torch = _torch()
