@@ -160,8 +160,12 @@ __global__ void __launch_bounds__(256) act8_fwd_vec_kernel(Act8 p) {
     if (in) {
       uint2 w = make_uint2(0u, 0u);
       if (byte != 255) {
-        w.x = act8_quad<FMT>(v[n][0] * inv, v[n][1] * inv, v[n][2] * inv, v[n][3] * inv);
-        w.y = act8_quad<FMT>(v[n][4] * inv, v[n][5] * inv, v[n][6] * inv, v[n][7] * inv);
+        const uint64_t ip = f2_pack(inv, inv);
+        float s[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) f2_unpack(f2_mul(f2_pack(v[n][j], v[n][j + 1]), ip), s[j], s[j + 1]);
+        w.x = act8_quad<FMT>(s[0], s[1], s[2], s[3]);
+        w.y = act8_quad<FMT>(s[4], s[5], s[6], s[7]);
       }
       *reinterpret_cast<uint2*>(p.q + (row * N + n) * p.f + 8 * c) = w;
       if ((c & 3) == 0) p.scales[(row * N + n) * nb + (c >> 2)] = (uint8_t)byte;

@@ -267,23 +267,30 @@ __global__ void __launch_bounds__(256) dattn_prep_kernel(DattnPrep p) {
       for (int e = 0; e < 8; ++e) { ss = fmaf(o[e], o[e], ss); wo = fmaf(g[e] * gain[e], o[e], wo); }
       ss = lanes_sum<L>(ss);
       wo = lanes_sum<L>(wo);
-      const float rn = 1.0f / sqrtf(ss * (1.0f / D) + a.eps), k = rn * rn * wo * (1.0f / D);
+      const float rn = rsqrtf(ss * (1.0f / D) + a.eps), k = rn * rn * rn * wo * (1.0f / D);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        dgain[e] = fmaf(g[e] * a.c, o[e] * rn, dgain[e]);
-        g[e] = rn * (g[e] * gain[e] - o[e] * k);
+        const float gr = g[e] * rn;
+        dgain[e] = fmaf(gr, o[e], dgain[e]);               // (times c at the end)
+        g[e] = fmaf(gr, gain[e], -k * o[e]);
       }
     }
     float d1 = 0.f, d2 = 0.f;
+    if (p.g_out && sizeof(T) == 2) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        dlam = fmaf(-g[e], o2[e], dlam);
+        g[e] = to_f(from_f<T>(g[e]));
+      }
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      dlam = fmaf(-g[e], o2[e], dlam);
-      if (p.g_out) g[e] = to_f(from_f<T>(g[e]));
       d2 = fmaf(g[e], o2[e], d2);
-      d1 = fmaf(g[e], fmaf(lam, o2[e], o[e]), d1);
+      d1 = fmaf(g[e], o[e], d1);
     }
-    d1 = lanes_sum<L>(d1);
+    if (!p.g_out || sizeof(T) == 4) dlam -= d2;            // g was not rounded
     d2 = lanes_sum<L>(d2);
+    d1 = fmaf(lam, d2, lanes_sum<L>(d1));                  // g . (o + lambda o_2)
     if (in) {
       if (p.g_out) store8((T*)p.g_out + at, g);            // (the scratch is aligned)
       if (part == 0) {
@@ -297,7 +304,7 @@ __global__ void __launch_bounds__(256) dattn_prep_kernel(DattnPrep p) {
   dlam = lanes_sum<L>(dlam);
   if (part == 0) red[r][D] = dlam;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) red[r][part * 8 + e] = dgain[e];
+  for (int e = 0; e < 8; ++e) red[r][part * 8 + e] = dgain[e] * a.c;
   __syncthreads();
   if (threadIdx.x <= D && (threadIdx.x == D || a.gain)) {
     float s = 0.f;
