@@ -211,6 +211,52 @@ def test_differential_attention_off_the_16_byte_grid(D):
     assert P.tc_error_flag() == 0
 
 
+@pytest.mark.parametrize("code,D", [(0, 32), (1, 64), (1, 128)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_differential_attention_every_buffer_off_the_grid(code, D, norm):
+    """Every buffer one element behind a 16-byte boundary; and each alone, the others on it, with the same results within the types' roundings."""
+    import paper_2401_15207_b200 as P
+    torch = _torch()
+    B, S, H, K, dt = 2, 90, 2, 1, _types(code)
+    s = _dattn_case(code, B, S, H, K, D, norm, 15, [90, 41])
+    T = B * S
+    w = torch.empty(P.diff_attention_bwd_scratch_bytes(code, B, S, H, D, norm), dtype=torch.uint8, device="cuda")
+
+    def run(shifted):
+        def at(name, shape, src=None, dtype=dt):
+            n = int(torch.Size(shape).numel())
+            k = 1 if name in shifted else 0
+            t = torch.full((n + 8,), 3.0, dtype=dtype, device="cuda")[k:k + n].view(shape)
+            if src is not None:
+                t.copy_(src)
+            return t
+        qkv, dy = at("qkv", s["qkv"].shape, s["qkv"]), at("dy", s["dy"].shape, s["dy"])
+        gain = at("gain", (D,), s["gain"]) if norm else None
+        lam = at("lam", (H,), s["lam"], torch.float32)
+        o, o2 = at("o", (T, H * D)), at("o2", (T, H * D))
+        y = at("y", (T, H * D)) if norm else None
+        lse, dlam = at("lse", (2 * B * H, S), dtype=torch.float32), at("dlam", (H,), dtype=torch.float32)
+        dgain = at("dgain", (D,), dtype=torch.float32) if norm else None
+        dqkv = at("dqkv", s["qkv"].shape)
+        args = (code, B, S, H, K, D, True, qkv, lam, gain, 1e-5, 0.4)
+        P.k_diff_attention_fwd(*args, o, o2, y, lse, key_lens=s["lens"])
+        P.k_diff_attention_bwd(*args, o, o2, lse, dy, dqkv, dlam, dgain, w, key_lens=s["lens"])
+        torch.cuda.synchronize()
+        return [t.double() for t in (o, o2, y, lse, dqkv, dlam, dgain) if t is not None]
+    names = ["qkv", "dy", "gain", "lam", "o", "o2", "y", "lse", "dlam", "dgain", "dqkv"]
+    want = run([])
+    for shifted in [names] + [[n] for n in names]:
+        for g, r in zip(run(shifted), want):
+            # the tensor cores' way and the CUDA cores' differ by roundings of P, dS and the results: a few half steps of the type, relative to the whole
+            assert float((g - r).norm()) <= (4 * R.UB if code else 1e-5) * float(r.norm()), shifted
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_differential_attention_of_9001_tokens(D):
+    s = _dattn_case(1, 1, 9001, 1, 1, D, True, 16, [8900])
+    _dattn_check(1, 1, 9001, 1, 1, D, True, s)
+
+
 def test_differential_attention_beyond_2_31_elements():
     """The last entry of a batch whose qkv has more than 2^31 elements, against the same entry alone."""
     torch = _torch()
@@ -530,6 +576,36 @@ def test_activations_in_8_bits_with_bad_values(fmt, kind):
         for part in range(kind):
             assert torch.equal(dpre[:, part * f:(part + 1) * f].isnan(), bad)
         assert bool(act[1, 40].isnan()) and bool(act[1, 41].isfinite()) and (sc == 255).sum() == 3
+
+
+@pytest.mark.parametrize("code", [0, 1])
+@pytest.mark.parametrize("kind", [1, 2])
+def test_activations_in_8_bits_off_the_16_byte_grid(code, kind):
+    """Buffers that start at any element (any byte for the packed values) give the same bits as aligned ones."""
+    import paper_2401_15207_b200 as P
+    torch = _torch()
+    rows, f, dt = 19, 128, _types(code)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    pre, dy = (torch.randn(rows, n * f, generator=g, device="cuda").to(dt) for n in (kind, 1))
+
+    def run(shifted):
+        def at(name, cols, dtype, src=None):
+            k = int(name in shifted)
+            t = torch.zeros(rows * cols + 16, dtype=dtype, device="cuda")[k:k + rows * cols].view(rows, cols)
+            if src is not None:
+                t.copy_(src)
+            return t
+        x, d, q, sc = at("pre", kind * f, dt, pre), at("dy", f, dt, dy), at("q", kind * f, torch.int8), at("sc", kind * f // 32, torch.uint8)
+        act, dpre, act2, back = at("act", f, dt), at("dpre", kind * f, dt), at("act2", f, dt), at("back", kind * f, dt)
+        P.k_act8_fwd(code, 0, kind, rows, f, x, act, q, sc)
+        P.k_act8_bwd(code, 0, kind, rows, f, d, q, sc, dpre, act2)
+        P.k_act8_unpack(code, 0, rows, kind * f, q, sc, back, kind * f)      # (f is a multiple of 32: the parts' blocks are those of whole rows)
+        return [t.clone() for t in (act, q, sc, dpre, act2, back)]
+    names = ["pre", "dy", "q", "sc", "act", "dpre", "act2", "back"]
+    want = run([])
+    for shifted in [names] + [[n] for n in names]:
+        for a, b in zip(run(shifted), want):
+            assert torch.equal(a, b), shifted
 
 
 def test_pack_beyond_2_31_elements():
