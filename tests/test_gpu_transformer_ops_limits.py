@@ -1,0 +1,70 @@
+"""The block operators beside the step at the ends of their ranges: far tails, the largest values, tiny eps, positions outside the table,
+buffers off the 16-byte grid, and the sums over all rows at lengths where a missing part would not show in a norm."""
+import math
+
+import pytest
+
+import block_ops_ref as R
+from test_gpu_transformer_ops import _dattn_case, _dattn_check, _dattn_run, _types
+
+pytestmark = pytest.mark.gpu
+NAN, INF = float("nan"), float("inf")
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _unit(code):
+    return R.UB if code else R.U32
+
+
+# ------------------------------------------------------------------ 8 bits
+def _act8(code, fmt, kind, pre, dy):
+    """Forward and backward: act, the packed values as numbers, scale bytes, dpre, the activation formed again."""
+    import paper_2401_15207_b200 as P
+    torch = _torch()
+    rows, f = dy.shape
+    dt, nb = _types(code), -(-f // 32)
+    act, again, dpre = (torch.full((rows, n * f), NAN, dtype=dt, device="cuda") for n in (1, 1, kind))
+    q, sc = torch.zeros(rows, kind * f, dtype=torch.int8, device="cuda"), torch.zeros(rows, kind * nb, dtype=torch.uint8, device="cuda")
+    P.k_act8_fwd(code, fmt, kind, rows, f, pre, act, q, sc)
+    P.k_act8_bwd(code, fmt, kind, rows, f, dy, q, sc, dpre, again)
+    return act, (q if fmt == 0 else q.view(torch.float8_e4m3fn)).double(), sc, dpre, again
+
+
+def _near(got, want, err, unit, what):
+    """Within err, half a step of the stored type, and the smallest normal fp32."""
+    off = (got.double() - want).abs() - err - 1.001 * unit * want.abs() - 2.0 ** -126
+    assert bool((off <= 0).all()), (what, float(off.max()), want.flatten()[int(off.argmax())].item())
+
+
+@pytest.mark.parametrize("code", [0, 1])
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("f", [256, 251])
+def test_gelu_tail_keeps_its_digits(code, fmt, f):
+    """GELU and its derivative from -12 to 12, every value within a bound relative to itself: in 1 + erf(x) nothing is left at a = -5.5.
+    Half steps of fp32 in the smaller of cdf and 1 - cdf, exp(-a^2/2) t Q(t): t carries 5 (a product and sum of one rounding, a quick division of two steps), which
+    t Q amplifies up to 2.6 times; 6 of Q and its fit; 4 of the quick exponential; its argument three roundings, a^2 / 2 of each; two products.  So 25 + 2 a^2,
+    then 2 of the cdf itself and of its product with a."""
+    torch = _torch()
+    rows = 40
+    # rows of like magnitudes, so that the 8 bits keep them apart: -12 .. -0.3, and as far up
+    top = torch.linspace(0.3, 12.0, rows, device="cuda")[:, None]
+    pre = top * torch.linspace(-1.0, 1.0, f, device="cuda")[None]
+    pre = pre.to(_types(code))
+    dy = torch.full((rows, f), 0.01, device="cuda").to(_types(code)) * (1 + torch.arange(f, device="cuda") % 3).to(_types(code))
+    act, num, sc, dpre, again = _act8(code, fmt, 1, pre, dy)
+    kept = R.unpack(num, sc)
+    assert float(kept.min()) < -11 and bool(((kept < -5) & (kept > -6)).any())
+
+    def normal(x):                                           # (ndtr is 1 + erf in 64 bits, which loses digits from -7 on)
+        low = 0.5 * torch.special.erfc(x.abs() / math.sqrt(2))
+        return torch.where(x < 0, low, 1 - low), (25 + 2 * x * x) * low
+    for x, got in ((R.f64(pre), act), (kept, again)):
+        cdf, half_steps = normal(x)
+        _near(got, x * cdf, x.abs() * (half_steps + 3 * cdf) * R.U32, _unit(code), "gelu")
+    (cdf, half_steps), pdf = normal(kept), torch.exp(-kept * kept / 2) / math.sqrt(2 * math.pi)
+    err = half_steps + 4 * cdf + (12 + 1.5 * kept * kept) * kept.abs() * pdf
+    _near(dpre, R.f64(dy) * (cdf + kept * pdf), R.f64(dy) * err * R.U32, _unit(code), "derivative")
