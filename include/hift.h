@@ -673,7 +673,8 @@ hift_status hift_k_diff_lambda_bwd(int32_t n_heads, int32_t sets, int32_t d, con
 /* Activations kept in 8 bits for the backward pass, beside recomputing them.  Blocks of HIFT_ACT8_BLOCK consecutive columns of a row
  * (the last one of a row may be shorter) share a scale 2^(byte - 127), the least power of two, 2^-110 at least, that brings the block's
  * largest magnitude to at most 127 (format 0: int8) or 448 (format 1: e4m3); q = x / scale rounded to nearest even, and q * scale is exact in bf16 and
- * fp32.  A block that holds a NaN or an infinity has byte 255 and comes back as NaNs.  q_dev: one byte a value; scales_dev:
+ * fp32; only where that would be 2^128 the largest code that is finite is kept (63 * 2^122, or 240 * 2^120: less than a step away).  A block that holds a
+ * NaN or an infinity has byte 255 and comes back as NaNs.  q_dev: one byte a value; scales_dev:
  * ceil(cols / HIFT_ACT8_BLOCK) bytes a row.
  *   pack:   x_dev [rows, ld] -> q, scales          unpack: q, scales -> out_dev [rows, ld]    (columns beyond `cols` are left alone)
  *   fwd:    act_dev[rows, f] = activation of pre_dev, and pre packed.  kind 1: GELU (erf), pre [rows, f]; 2: SwiGLU, pre [rows, 2f] = gate | up,

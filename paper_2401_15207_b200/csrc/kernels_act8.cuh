@@ -28,6 +28,13 @@ template <int FMT> __device__ __forceinline__ int act8_byte(uint32_t top) {
 __device__ __forceinline__ float act8_scale(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 __device__ __forceinline__ float act8_inverse(int byte) { return byte == 255 ? 0.f : __uint_as_float((uint32_t)(254 - byte) << 23); }
 
+// At the topmost scale the codes from 64 (int8) or 256 (e4m3) on stand for 2^128: the largest one below it is kept instead.  (No other block pays for more
+// than the comparison.)
+template <int FMT> constexpr int kAct8TopByte = FMT == 0 ? 249 : 247;
+template <int FMT> __device__ __forceinline__ float act8_below_top(float v) {
+  constexpr float most = FMT == 0 ? 63.f : 240.f;
+  return fminf(fmaxf(v, -most), most);
+}
 // four values, scaled into range, as four bytes; round to nearest even
 template <int FMT> __device__ __forceinline__ uint32_t act8_quad(float a, float b, float c, float d) {
   if (FMT == 0) {
@@ -180,6 +187,10 @@ __global__ void __launch_bounds__(256) act8_fwd_vec_kernel(Act8 p) {
         float s[8];
 #pragma unroll
         for (int j = 0; j < 8; j += 2) f2_unpack(f2_mul(f2_pack(v[n][j], v[n][j + 1]), ip), s[j], s[j + 1]);
+        if (byte == kAct8TopByte<FMT>) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) s[j] = act8_below_top<FMT>(s[j]);
+        }
         w.x = act8_quad<FMT>(s[0], s[1], s[2], s[3]);
         w.y = act8_quad<FMT>(s[4], s[5], s[6], s[7]);
       }
@@ -256,7 +267,9 @@ __global__ void __launch_bounds__(256) act8_fwd_any_kernel(Act8 p) {
 #pragma unroll
   for (int n = 0; n < N; ++n) {
     const int byte = act8_byte<FMT>(__reduce_max_sync(0xffffffffu, __float_as_uint(v[n]) & 0x7FFFFFFFu));
-    const uint32_t w = byte == 255 ? 0u : act8_quad<FMT>(v[n] * act8_inverse(byte), 0.f, 0.f, 0.f);
+    float s = v[n] * act8_inverse(byte);
+    if (byte == kAct8TopByte<FMT>) s = act8_below_top<FMT>(s);
+    const uint32_t w = byte == 255 ? 0u : act8_quad<FMT>(s, 0.f, 0.f, 0.f);
     if (in) p.q[(row * N + n) * p.f + c] = (uint8_t)w;
     if (lane == 0) p.scales[(row * N + n) * nb + k] = (uint8_t)byte;
   }

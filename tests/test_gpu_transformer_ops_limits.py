@@ -68,3 +68,40 @@ def test_gelu_tail_keeps_its_digits(code, fmt, f):
     (cdf, half_steps), pdf = normal(kept), torch.exp(-kept * kept / 2) / math.sqrt(2 * math.pi)
     err = half_steps + 4 * cdf + (12 + 1.5 * kept * kept) * kept.abs() * pdf
     _near(dpre, R.f64(dy) * (cdf + kept * pdf), R.f64(dy) * err * R.U32, _unit(code), "derivative")
+
+
+@pytest.mark.parametrize("code", [0, 1])
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("f", [128, 77])
+def test_pack_the_largest_values(code, fmt, f):
+    """Blocks whose largest magnitude would round to 2^128 keep the largest code that is finite: what comes back is finite, and off by less than a step."""
+    import paper_2401_15207_b200 as P
+    torch = _torch()
+    dt = _types(code)
+    most = float(torch.finfo(dt).max)
+    step = 2.0 ** 122 if fmt == 0 else 2.0 ** 124            # of the topmost scale, near 2^128
+    vals = [most, -most, 1.9375 * 2.0 ** 127, 1.96875 * 2.0 ** 127, 1.75 * 2.0 ** 127, -1.984375 * 2.0 ** 127, 2.0 ** 127, -1.8125 * 2.0 ** 127, 1e38, 1.0]
+    x = torch.zeros(len(vals), f, dtype=dt, device="cuda")
+    x[:, ::32] = torch.tensor(vals, dtype=dt, device="cuda")[:, None]
+    x[:, 5::32] = torch.tensor(-3e37, dtype=dt, device="cuda")
+    x[:, 9] = 1.0
+    nb = -(-f // 32)
+    q, sc = torch.zeros(len(vals), f, dtype=torch.int8, device="cuda"), torch.zeros(len(vals), nb, dtype=torch.uint8, device="cuda")
+    P.k_act8_pack(code, fmt, len(vals), f, x, f, q, sc)
+    want, byte = R.pack(R.f64(x), fmt)
+    assert torch.equal(sc.long(), byte)
+    limit = 63.0 if fmt == 0 else 240.0                      # times 2^(249 - 127), or 2^(247 - 127): the last step below 2^128
+    topmost = (byte == (249 if fmt == 0 else 247)).repeat_interleave(32, 1)[:, :f]
+    want = torch.where(topmost, want.clamp(-limit, limit), want)
+    num = (q if fmt == 0 else q.view(torch.float8_e4m3fn)).double()
+    assert torch.equal(num, want) and bool(topmost.any())
+    for out_code in (0, 1):
+        back = torch.full((len(vals), f), NAN, dtype=_types(out_code), device="cuda")
+        P.k_act8_unpack(out_code, fmt, len(vals), f, q, sc, back, f)
+        assert bool(back.isfinite().all()) and torch.equal(back.double(), R.unpack(want, byte))
+        assert float((back.double() - x.double()).abs().max()) < step
+    # through the activations: no infinity or NaN out of finite values
+    for kind in (1, 2):
+        pre = x if kind == 1 else torch.cat([x, torch.full_like(x, 0.5)], 1)
+        act, _, _, dpre, again = _act8(code, fmt, kind, pre.contiguous(), torch.full_like(x, 1e-3))
+        assert bool(dpre.isfinite().all()) and bool(again.isfinite().all())
