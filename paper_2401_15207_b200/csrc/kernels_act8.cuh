@@ -90,7 +90,14 @@ inline dim3 act8_grid(Act8& p, int64_t units) {
 }
 
 // KIND 0: none (packing alone), 1: GELU, 2: SwiGLU
-__device__ __forceinline__ float act8_sigmoid(float a) { return __fdividef(1.0f, 1.0f + __expf(-a)); }   // (0 where the sum is beyond 2^126)
+// sigmoid(a), and 1 - sigmoid(a) = sigmoid(-a): with t = exp(-|a|) one is 1 / (1 + t) and the other t / (1 + t), so that neither loses digits to a
+// difference, nor the small one its value where exp(|a|) is beyond what a quick division or fp32 itself holds.  (SwiGLU of 8192 x 11008
+// bf16 forward 141 -> 144 us, the gradient as before; sums and products of pairs 151.)
+__device__ __forceinline__ float act8_sigmoid(float a, float& rest) {
+  const float t = __expf(-fabsf(a)), r = __fdividef(1.0f, 1.0f + t), s = t * r;
+  rest = a < 0.f ? r : s;
+  return a < 0.f ? s : r;
+}
 // Normal distribution cdf and e = exp(-a^2 / 2).  With z = |a| / sqrt(2) and t = 1 / (1 + 0.45 z), erfc(z) / 2 = exp(-z^2) t Q(t): Q, of nine degrees, fitted
 // to the least largest relative error over all z >= 0 (3.2e-8; 5 half steps of fp32 as evaluated).  The lower tail is that product itself: in
 // 1 + erf its digits cancel (4 % off at a = -5, nothing left at -5.5).  One exponential serves the density too.  (GELU of 16384 x 5120 bf16, int8:
@@ -107,7 +114,7 @@ __device__ __forceinline__ float act8_normal(float a, float& e) {
 }
 template <int KIND> __device__ __forceinline__ float act8_value(float a, float u) {
   float e;
-  return KIND == 1 ? a * act8_normal(a, e) : a * act8_sigmoid(a) * u;
+  return KIND == 1 ? a * act8_normal(a, e) : a * act8_sigmoid(a, e) * u;
 }
 // dx (and the gradient of `up`), and the activation's value
 template <int KIND> __device__ __forceinline__ void act8_grad(float g, float a, float u, float& da, float& du, float& y) {
@@ -117,8 +124,8 @@ template <int KIND> __device__ __forceinline__ void act8_grad(float g, float a, 
     da = g * fmaf(a, 0.39894228040143267794f * e, cdf);
     y = a * cdf;
   } else {
-    // 1 - sigmoid(a) as exp(-a) sigmoid(a) where the sigmoid is nearly 1: no digits are lost
-    const float e = __expf(-a), sig = __fdividef(1.0f, 1.0f + e), rest = a > 0.f ? e * sig : 1.0f - sig, s = a * sig;
+    float rest;
+    const float sig = act8_sigmoid(a, rest), s = a * sig;
     da = g * u * sig * fmaf(a, rest, 1.0f);
     du = g * s;
     y = s * u;

@@ -105,3 +105,36 @@ def test_pack_the_largest_values(code, fmt, f):
         pre = x if kind == 1 else torch.cat([x, torch.full_like(x, 0.5)], 1)
         act, _, _, dpre, again = _act8(code, fmt, kind, pre.contiguous(), torch.full_like(x, 1e-3))
         assert bool(dpre.isfinite().all()) and bool(again.isfinite().all())
+
+
+@pytest.mark.parametrize("code", [0, 1])
+@pytest.mark.parametrize("fmt", [0, 1])
+@pytest.mark.parametrize("f", [64, 45])
+def test_swiglu_of_far_negative_gates(code, fmt, f):
+    """Gates at which sigmoid(a) is below the smallest normal number, times a large `up`: values that the type can hold are not lost.
+    exp(a): 2 (2 + 1.173 |a|) half steps and |a| of its argument's rounding, a division of 4, three products; below 2^-126 half a unit of 2^-149 for each of
+    the exponential, the quotient and their products."""
+    torch = _torch()
+    rows = 6
+    a = torch.tensor([-80.0, -88.0, -92.0, -96.0, -60.0, -100.0], device="cuda")[:, None].expand(rows, f).clone()
+    a[:, ::5] = -72.0
+    u = torch.full((rows, f), 2.0 ** 100, device="cuda")
+    u[:, ::3] = -(2.0 ** 98)
+    pre = torch.cat([a, u], 1).to(_types(code))
+    dy = torch.full((rows, f), 1.0, device="cuda").to(_types(code))
+    act, num, sc, dpre, again = _act8(code, fmt, 2, pre, dy)
+    tiny = 3 * 2.0 ** -149
+
+    def rel(x):
+        return (16 + 4.4 * x.abs()) * R.U32
+    kept = R.unpack(num, sc, 2)
+    for x, got in ((R.f64(pre), act), (kept, again)):
+        g, w = x[:, :f], x[:, f:]
+        y = g * torch.sigmoid(g) * w
+        assert float(y.abs().min()) > 2.0 ** -60
+        _near(got, y, rel(g) * y.abs() + tiny * (1 + g.abs()) * w.abs(), _unit(code), "swiglu")
+    g, w = kept[:, :f], kept[:, f:]
+    s = torch.sigmoid(g)
+    d = w * s * (1 + g * torch.sigmoid(-g))
+    _near(dpre[:, :f], d, (rel(g) * w * s * (1 + g.abs())).abs() + tiny * w.abs() * (1 + g.abs()), _unit(code), "gate")
+    _near(dpre[:, f:], g * s, rel(g) * (g * s).abs() + tiny * (1 + g.abs()), _unit(code), "up")
