@@ -267,12 +267,13 @@ __global__ void __launch_bounds__(256) dattn_prep_kernel(DattnPrep p) {
       for (int e = 0; e < 8; ++e) { ss = fmaf(o[e], o[e], ss); wo = fmaf(g[e] * gain[e], o[e], wo); }
       ss = lanes_sum<L>(ss);
       wo = lanes_sum<L>(wo);
-      const float rn = rsqrtf(ss * (1.0f / D) + a.eps), k = rn * rn * rn * wo * (1.0f / D);
+      // rn may be up to eps^-1/2: its square fits fp32 (eps is a normal number), its cube need not, so the third factor goes to o first
+      const float rn = rsqrtf(ss * (1.0f / D) + a.eps), k = rn * rn * wo * (1.0f / D);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float gr = g[e] * rn;
         dgain[e] = fmaf(gr, o[e], dgain[e]);               // (times c at the end)
-        g[e] = fmaf(gr, gain[e], -k * o[e]);
+        g[e] = fmaf(gr, gain[e], -k * (rn * o[e]));
       }
     }
     float d1 = 0.f, d2 = 0.f;

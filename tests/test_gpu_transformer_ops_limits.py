@@ -138,3 +138,19 @@ def test_swiglu_of_far_negative_gates(code, fmt, f):
     d = w * s * (1 + g * torch.sigmoid(-g))
     _near(dpre[:, :f], d, (rel(g) * w * s * (1 + g.abs())).abs() + tiny * w.abs() * (1 + g.abs()), _unit(code), "gate")
     _near(dpre[:, f:], g * s, rel(g) * (g * s).abs() + tiny * (1 + g.abs()), _unit(code), "up")
+
+
+# ------------------------------------------------------------------ differential attention
+@pytest.mark.parametrize("code,D", [(0, 16), (0, 64), (1, 32), (1, 64), (1, 128)])
+@pytest.mark.parametrize("size", [1.0, 1e-20])
+@pytest.mark.parametrize("eps", [1e-30, 2e-38])
+def test_differential_attention_norm_with_a_tiny_eps(code, D, size, eps):
+    """An eps whose power of -3/2 fp32 does not hold: entries of length 0 (rows of zeros) and rows far below sqrt(eps) have the gradients of the formula."""
+    torch = _torch()
+    B, S, H, K = 3, 70, 2, 1
+    s = _dattn_case(code, B, S, H, K, D, True, 31, [70, 0, 33])
+    s["qkv"].view(B * S, H + 2 * K, D)[:, H + K:] *= size
+    out = _dattn_check(code, B, S, H, K, D, True, s, eps=eps)
+    for n in ("dqkv", "dlam", "dgain"):
+        assert bool(out[n].isfinite().all()), n
+    assert not bool(out["dqkv"][S:2 * S].any())              # the entry of length 0
