@@ -154,3 +154,30 @@ def test_differential_attention_norm_with_a_tiny_eps(code, D, size, eps):
     for n in ("dqkv", "dlam", "dgain"):
         assert bool(out[n].isfinite().all()), n
     assert not bool(out["dqkv"][S:2 * S].any())              # the entry of length 0
+
+
+# ------------------------------------------------------------------ rotary positions
+@pytest.mark.parametrize("code", [0, 1])
+@pytest.mark.parametrize("layout", [0, 1])
+@pytest.mark.parametrize("d,rot", [(64, 64), (64, 32), (10, 6)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_rope_leaves_rows_outside_the_table_as_they_are(code, layout, d, rot, in_place):
+    """Bit for bit: infinities, NaN and zeros of either sign beside one another in a pair."""
+    import paper_2401_15207_b200 as P
+    torch = _torch()
+    rows, heads, n_pos = 24, 3, 9
+    g = torch.Generator(device="cuda").manual_seed(d)
+    x = torch.randn(rows, heads * d, generator=g, device="cuda")
+    odd = torch.tensor([INF, -INF, NAN, -0.0, 0.0, 1.0], device="cuda")
+    x = torch.where(torch.rand(x.shape, generator=g, device="cuda") < 0.6, odd[torch.randint(0, 6, x.shape, generator=g, device="cuda")], x).to(_types(code))
+    pos = torch.randint(0, n_pos, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    out_of = torch.arange(rows, device="cuda") % 4 == 1
+    pos[out_of] = torch.tensor([-1, n_pos, 2 ** 31 - 1, -2 ** 31, n_pos + 7, -5], dtype=torch.int32, device="cuda")
+    cs = torch.empty(2, n_pos, rot // 2, device="cuda")
+    P.rope_table(n_pos, rot, cs)
+    bits = torch.int16 if code else torch.int32
+    for inverse in (False, True):
+        src, bad = x.clone(), torch.zeros(1, dtype=torch.int32, device="cuda")
+        out = src if in_place else torch.empty_like(x)
+        P.k_rope(code, layout, rows, heads, d, rot, src, heads * d, out, heads * d, cs, n_pos, positions=pos, inverse=inverse, bad=bad)
+        assert torch.equal(out[out_of].view(bits), x[out_of].view(bits)) and int(bad) == 1
