@@ -619,8 +619,9 @@ hift_status hift_muon_step(int64_t rows, int64_t cols, void *param_bf16_dev, flo
  * and hift_k_rope take).  Angles are formed in 64 bits.  With plain frequencies base^(-2j/rot), `scaling` for contexts longer than trained:
  *   0 none;  1 linear: all frequencies / factor;  2 NTK-aware: base * factor^(rot/(rot-2)) for base (the fastest pair keeps its frequency,
  *   the slowest gets 1/factor of it);
- *   3 YaRN: plain for pairs that turn at least `fast` times over orig_len positions, / factor for at most `slow` times, linear in the pair's
- *   index in between, and cosines and sines times 0.1 ln(factor) + 1;
+ *   3 YaRN: plain for pairs that turn at least `fast` times over orig_len positions, / factor for at most `slow` times, in between linear in the pair's
+ *   index, and cosines and sines times 0.1 ln(factor) + 1.  The ramp runs from the index at which a pair turns `fast` times, rounded down (0 at least), to that
+ *   of `slow` times, rounded up (rot - 1 at most);
  *   4 banded: plain above `fast` turns over orig_len, / factor below `slow`, linear in the number of turns in between.
  * factor >= 1 (read for 1 to 4), orig_len > 0 and 0 < slow < fast (read for 3 and 4).  rot even. */
 hift_status hift_rope_table(int32_t scaling, int64_t n_pos, int32_t rot, double base, double factor, double orig_len, double fast,

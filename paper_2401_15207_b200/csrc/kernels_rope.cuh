@@ -89,10 +89,10 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(RopeOp p) {
   *reinterpret_cast<Vec*>(y + e1) = o1;
 }
 
-// The table of cosines and sines: angle(pos, j) = (pos * pos_scale) * freq(j) in 64 bits, the cosine and sine rounded once, times `mag`.
+// The table of cosines and sines: angle(pos, j) = pos * freq(j) in 64 bits, the cosine and sine rounded once, times `mag`.
 //   kind 0 plain: base^(-2j/rot);  1 linear: that / factor;  2 NTK-aware: base grown so that the slowest pair turns `factor` times slower;
-//   kind 3 (YaRN): per pair between plain (pairs that turn at least beta_fast times over orig_len) and / factor (at most beta_slow times), linear in j;
-//   kind 4 (banded): plain above high_freq turns over orig_len, / factor below low_freq, in between linear in the number of turns.
+//   kind 3 (YaRN): per pair between plain (pairs that turn at least `fast` times over orig_len) and / factor (at most `slow` times), linear in j;
+//   kind 4 (banded): plain above `fast` turns over orig_len, / factor below `slow`, in between linear in the number of turns.
 struct RopeTable { int kind, n_pos, half; double base, factor, orig_len, fast, slow; float mag; float* cs; };
 __host__ __device__ inline double rope_frequency(const RopeTable& t, int j) {
   const double rot = 2.0 * t.half, two_pi = 6.283185307179586476925286766559;
@@ -102,14 +102,14 @@ __host__ __device__ inline double rope_frequency(const RopeTable& t, int j) {
   if (t.kind == 0 || t.kind == 2) return f;
   if (t.kind == 1) return f / t.factor;
   if (t.kind == 3) {
-    // the pair index at which a pair turns n times over orig_len
-    double lo = floor(rot * log(t.orig_len / (t.fast * two_pi)) / (2.0 * log(t.base)));
-    double hi = ceil(rot * log(t.orig_len / (t.slow * two_pi)) / (2.0 * log(t.base)));
-    lo = lo < 0.0 ? 0.0 : lo;
-    hi = hi > rot - 1.0 ? rot - 1.0 : hi;
-    if (hi <= lo) hi = lo + 0.001;
-    double ramp = (j - lo) / (hi - lo);
-    ramp = ramp < 0.0 ? 0.0 : ramp > 1.0 ? 1.0 : ramp;
+    // the pair indices at which a pair turns `fast` and `slow` times over orig_len, outwards to whole ones
+    const double lo = floor(rot * log(t.orig_len / (t.fast * two_pi)) / (2.0 * log(t.base)));
+    const double hi = ceil(rot * log(t.orig_len / (t.slow * two_pi)) / (2.0 * log(t.base)));
+    if (hi <= 0.0) return f / t.factor;                    // even the first pair turns `slow` times at most
+    if (j <= lo) return f;
+    const double from = lo < 0.0 ? 0.0 : lo, to = hi > rot - 1.0 ? rot - 1.0 : hi;
+    if (j >= to) return f / t.factor;
+    const double ramp = (j - from) / (to - from);          // from <= j < to
     return f * (1.0 - ramp) + f / t.factor * ramp;
   }
   const double turns = t.orig_len * f / two_pi;

@@ -181,3 +181,35 @@ def test_rope_leaves_rows_outside_the_table_as_they_are(code, layout, d, rot, in
         out = src if in_place else torch.empty_like(x)
         P.k_rope(code, layout, rows, heads, d, rot, src, heads * d, out, heads * d, cs, n_pos, positions=pos, inverse=inverse, bad=bad)
         assert torch.equal(out[out_of].view(bits), x[out_of].view(bits)) and int(bad) == 1
+
+
+def _yarn(n_pos, rot, base, factor, orig_len, fast, slow):
+    """Cosines and sines, the ramp's ends found by looking for them: the last whole pair index that turns at least `fast` times over orig_len, the
+    first one that turns at most `slow` times."""
+    torch = _torch()
+
+    def turns(j):
+        return orig_len * base ** (-2.0 * j / rot) / (2 * math.pi)
+    wide = range(-4 * rot, 5 * rot)
+    lo = max(max((j for j in wide if turns(j) >= fast), default=wide[0]), 0)
+    hi = min(min((j for j in wide if turns(j) <= slow), default=wide[-1]), rot - 1)
+    f = []
+    for j in range(rot // 2):
+        share = 1.0 if j >= hi else 0.0 if j <= lo else (j - lo) / (hi - lo)
+        f.append(base ** (-2.0 * j / rot) * (1 - share + share / factor))
+    ang = torch.arange(n_pos, dtype=torch.float64)[:, None] * torch.tensor(f, dtype=torch.float64)
+    return torch.stack([ang.cos(), ang.sin()]) * (1 + 0.1 * math.log(factor))
+
+
+@pytest.mark.parametrize("orig_len,fast,slow", [(1.0, 32.0, 1.0), (6.0, 32.0, 1.0), (6.5, 32.0, 1.0), (50.0, 9.0, 8.0), (100.0, 32.0, 1.0), (2048.0, 32.0, 1.0), (4096.0, 8.0, 0.5),
+                                                (1e6, 2.0, 1.0), (1e9, 32.0, 1.0)])
+@pytest.mark.parametrize("rot,base", [(2, 1e4), (8, 1e4), (64, 1e4), (128, 5e5)])
+def test_yarn_table_from_its_definition(orig_len, fast, slow, rot, base):
+    """Short trained lengths, over which even the first pair turns at most `slow` times, and long ones, over which the last turns `fast` times, among them."""
+    import paper_2401_15207_b200 as P
+    torch = _torch()
+    n_pos, factor = 300, 4.0
+    cs = torch.full((2, n_pos, rot // 2), NAN, device="cuda")
+    P.rope_table(n_pos, rot, cs, base=base, scaling=P.binding.ROPE_YARN, factor=factor, orig_len=orig_len, fast=fast, slow=slow)
+    want = _yarn(n_pos, rot, base, factor, orig_len, fast, slow)
+    assert float((cs.double().cpu() - want).abs().max()) <= 1.2 * 2 * R.U32 + 1e-12 * n_pos       # two roundings of values up to 1.14; the angles'
