@@ -647,8 +647,9 @@ hift_status hift_k_rope(int32_t dtype, int32_t layout, int64_t rows, int32_t n_h
  * 0 leaves nothing: zeros, lse = -inf, no gradient.  What k and v hold at padded keys does not matter, NaN included.
  * lambda_dev fp32 [n_heads], gain_dev [d_head] of the operand type.  Out, all [batch*seq, n_heads * d_head] of the operand type: o_dev, o2_dev (o_2, what
  * the gradient needs; may be NULL), y_dev; lse_dev fp32 [2, batch, n_heads, seq], the maps' log-sum-exps.
- * d_head 16, 32, 64 or 128; dtype 0 fp32, 1 bf16.  bf16 heads of 64 and 128 in 16-byte-aligned buffers run on the tensor cores, with probabilities
- * and their gradients rounded to bf16 as operands and sums in fp32; the rest runs on the CUDA cores in fp32.
+ * d_head 16, 32, 64 or 128; dtype 0 fp32, 1 bf16.  bf16 heads of 64 and 128 with qkv, o, o2 and y (in the gradient qkv, dqkv and, without a norm, dy)
+ * 16-byte aligned run on the tensor cores, with probabilities, their gradients and, behind a norm, the gradient of o rounded to bf16 as operands and
+ * sums in fp32; the rest runs on the CUDA cores in fp32.
  * batch = 0 or seq = 0 is allowed. */
 hift_status hift_k_diff_attention_fwd(int32_t dtype, int32_t batch, int32_t seq, int32_t n_heads, int32_t n_kv_heads, int32_t d_head,
                                       int32_t causal, const void *qkv_dev, const float *lambda_dev, const void *gain_dev, double eps,

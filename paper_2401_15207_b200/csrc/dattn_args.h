@@ -15,7 +15,7 @@ struct DattnArgs {
   float scale, eps, c;
 };
 
-// Tensor-core kernels (gemm_tc.cu): bf16, heads of 64 or 128, every buffer 16-byte aligned, this device set up (gemm_tc_init).
+// Tensor-core kernels (gemm_tc.cu): bf16, heads of 64 or 128, the buffers that they move by TMA 16-byte aligned, this device set up (gemm_tc_init).
 bool dattn_tc_eligible(int dtype, int D, const DattnArgs& a);
 cudaError_t dattn_tc_fwd_launch(cudaStream_t st, int D, const DattnArgs& a);
 cudaError_t dattn_tc_bwd_launch(cudaStream_t st, int D, const DattnArgs& a);

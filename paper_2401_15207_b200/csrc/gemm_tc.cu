@@ -1627,9 +1627,9 @@ cudaError_t attn_tc_bwd_launch(cudaStream_t st, int B, int S, int H, int dh, int
 // ------------------------------------------------------------------ differential attention
 bool dattn_tc_eligible(int dtype, int D, const DattnArgs& a) {
   if (dtype != 1 || (D != 64 && D != 128) || gemm_tc_init() != 0) return false;
-  uintptr_t all = 0;
-  for (const void* p : {a.qkv, (const void*)a.o, (const void*)a.o2, (const void*)a.y, a.g, (const void*)a.dqkv}) all |= (uintptr_t)p;
-  return (all & 15) == 0;
+  // what the call's own kernels reach by TMA: the gradient's take qkv, g and dqkv (o and o_2 are read by its preparation, from any address)
+  const uintptr_t all = a.dqkv ? (uintptr_t)a.g | (uintptr_t)a.dqkv : (uintptr_t)a.o | (uintptr_t)a.o2 | (uintptr_t)a.y;
+  return (((uintptr_t)a.qkv | all) & 15) == 0;
 }
 // qkv-like bf16 rows [B][S][cols]: box = 64, 32 or 16 columns (swizzled over their 128, 64 or 32 bytes) x box_rows rows; rows beyond S read as zeros.  Encoded at every call:
 // buffers' addresses change from call to call.

@@ -213,3 +213,25 @@ def test_yarn_table_from_its_definition(orig_len, fast, slow, rot, base):
     P.rope_table(n_pos, rot, cs, base=base, scaling=P.binding.ROPE_YARN, factor=factor, orig_len=orig_len, fast=fast, slow=slow)
     want = _yarn(n_pos, rot, base, factor, orig_len, fast, slow)
     assert float((cs.double().cpu() - want).abs().max()) <= 1.2 * 2 * R.U32 + 1e-12 * n_pos       # two roundings of values up to 1.14; the angles'
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("norm", [False, True])
+def test_differential_attention_gradient_reads_o_and_o2_anywhere(D, norm):
+    """The products of the gradient do not read o and o_2: where these start decides nothing, and the results have the same bits."""
+    import paper_2401_15207_b200 as P
+    torch = _torch()
+    B, S, H, K = 2, 150, 4, 2
+    s = _dattn_case(1, B, S, H, K, D, norm, 33, [150, 71])
+    a = _dattn_run(1, B, S, H, K, D, True, s)
+    w = torch.empty(P.diff_attention_bwd_scratch_bytes(1, B, S, H, D, norm), dtype=torch.uint8, device="cuda")
+
+    def off_grid(t):
+        n = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")[1:].view(t.shape)
+        n.copy_(t)
+        assert n.data_ptr() % 16 == 2
+        return n
+    for o, o2 in ((off_grid(a["o"]), a["o2"]), (a["o"], off_grid(a["o2"]))):
+        dqkv, dlam = torch.full_like(s["qkv"], NAN), torch.empty(H, device="cuda")
+        P.k_diff_attention_bwd(1, B, S, H, K, D, True, s["qkv"], s["lam"], s["gain"], 1e-5, 0.4, o, o2, a["lse"], s["dy"], dqkv, dlam, None, w, key_lens=s["lens"])
+        assert torch.equal(dqkv, a["dqkv"]) and torch.equal(dlam, a["dlam"][0])
