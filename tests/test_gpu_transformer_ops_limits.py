@@ -235,3 +235,38 @@ def test_differential_attention_gradient_reads_o_and_o2_anywhere(D, norm):
         dqkv, dlam = torch.full_like(s["qkv"], NAN), torch.empty(H, device="cuda")
         P.k_diff_attention_bwd(1, B, S, H, K, D, True, s["qkv"], s["lam"], s["gain"], 1e-5, 0.4, o, o2, a["lse"], s["dy"], dqkv, dlam, None, w, key_lens=s["lens"])
         assert torch.equal(dqkv, a["dqkv"]) and torch.equal(dlam, a["dlam"][0])
+
+
+@pytest.mark.parametrize("code,B,S,H,K,D", [(1, 2, 1500, 24, 6, 128), (1, 1, 9001, 2, 1, 64), (0, 3, 700, 4, 4, 16), (0, 64, 33, 5, 1, 32), (1, 300, 40, 3, 3, 32),
+                                            (0, 1, 2000, 1, 1, 128)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_differential_attention_sums_over_all_rows(code, B, S, H, K, D, norm):
+    """dlambda and dgain at lengths of many partial sums, within the roundings that a term meets on its way: those of one thread's terms, of the lanes and rows
+    of a block, of the blocks' sums.  That is a small part of the sums themselves, so that no missing part goes by."""
+    torch = _torch()
+    s = _dattn_case(code, B, S, H, K, D, norm, 35, [S - 3 * (i % 2) for i in range(B)])
+    out = _dattn_run(code, B, S, H, K, D, True, s)
+    heads = lambda t: R.f64(t).view(B * S, H, D)                                  # noqa: E731
+    g, o, o2 = heads(s["dy"]), heads(out["o"]), heads(out["o2"])
+    # a block takes at least 32 rows and at most what gives each head ceil(1184 / H) blocks, 256 / (D / 8) rows at a time
+    rows = B * S
+    per_block = max(32, -(-rows // -(-1184 // H))) + 1
+    chunks, at_once = -(-rows // (per_block - 1)), 2048 // D
+    turns = -(-per_block // at_once)
+    size = g.abs()
+    if norm:
+        gain = R.f64(s["gain"]) * 0.4
+        r = 1 / torch.sqrt((o * o).mean(-1, keepdim=True) + 1e-5)
+        t = o * r
+        want = (g * t).sum((0, 1)) * 0.4
+        # the norm: 8 + 4 terms' sums, a root, a few products: 24 half steps of each term
+        bound = (turns + at_once + H * chunks // 128 + 128 + 32) * R.U32 * (g * t).abs().sum((0, 1)) * 0.4
+        assert float(bound.max()) <= 0.1 * float(want.abs().mean()), (float(bound.max()), float(want.abs().mean()))
+        assert bool(((out["dgain"][0].double() - want).abs() <= bound).all())
+        w = g * gain
+        size = r * (w.abs() + t.abs() * (w * t).abs().mean(-1, keepdim=True))
+        g = r * (w - t * (w * t).mean(-1, keepdim=True))
+    want = -(g * o2).sum((0, 2))
+    bound = (8 * turns + 4 + at_once + chunks // 1024 + 16 + 24) * R.U32 * (size * o2.abs()).sum((0, 2))
+    assert float(bound.max()) <= 0.1 * float(want.abs().mean()), (float(bound.max()), float(want.abs().mean()))
+    assert bool(((out["dlam"][0].double() - want).abs() <= bound).all())
