@@ -644,7 +644,8 @@ hift_status hift_k_rope(int32_t dtype, int32_t layout, int64_t rows, int32_t n_h
  * qkv_dev [batch*seq, (n_heads + 2 n_kv_heads) * d_head]: the column blocks q | k | v of hift_k_attention_fwd; in a head of q or k the first
  * half of its columns belongs to the first map, the second half to the second, while v is d_head wide.  Query head h reads key and value
  * head h / (n_heads / n_kv_heads).  Masks as in hift_k_attention_fwd (causal; key_lens_dev int32 [batch] or NULL), but a length of
- * 0 leaves nothing: zeros, lse = -inf, no gradient.  What k and v hold at padded keys does not matter, NaN included.
+ * 0 leaves nothing: zeros, lse = -inf, no gradient.  What k and v hold at padded keys does not matter, NaN included; a NaN or an infinity elsewhere may
+ * reach any row of its batch entry, rows that the causal mask hides it from among them (0 times NaN), but no other entry.
  * lambda_dev fp32 [n_heads], gain_dev [d_head] of the operand type.  Out, all [batch*seq, n_heads * d_head] of the operand type: o_dev, o2_dev (o_2, what
  * the gradient needs; may be NULL), y_dev; lse_dev fp32 [2, batch, n_heads, seq], the maps' log-sum-exps.
  * d_head 16, 32, 64 or 128; dtype 0 fp32, 1 bf16.  bf16 heads of 64 and 128 with qkv, o, o2 and y (in the gradient qkv, dqkv and, without a norm, dy)

@@ -8,7 +8,8 @@
 //   MODE 1     Q    g     K    V      scores                          g V^T            dq_m += dS_m K_m
 // (F0_m: the map's half of the columns; g: gradient of o.)  P_m = exp(scale S_m - lse_m),  dS_1 = P_1 (dP - D_1),  dS_2 = -lambda P_2 (dP - D_2);
 // dk and dq are multiplied by `scale` as they are stored.  dP is shared by the maps, and dv takes one product for both: 8 units of 128 x 64 x 64 a
-// step against the 10 of two plain attentions.  P and dS are rounded to bf16, the operand type of the products they feed; the accumulators are fp32.
+// step against the 10 of two plain attentions.  P, dS and, behind a norm, g are rounded to bf16, the operand type of the products they feed (dqkv 2.4e-3 off relative to its norm, 3.0e-3
+// with the norm, where its own rounding alone is 1.7e-3; what a rounding of g leaves would take a second product of dP and of dv, 4 units more); the accumulators are fp32.
 //   warp 0    : TMA producer         warp 1: issues every product (one elected thread); owns the tensor memory
 //   warp 2    : MODE 1 with key lengths, K's rows of hidden keys -> zeros
 //   warps 4.. : element-wise, two or four warps to a lane quarter, their share of the 64 streamed columns each: S_1, S_2 -> registers, exponentials; dP, dS;
@@ -19,7 +20,9 @@
 // dP in the same way, accumulators 256.  S(t+1) is issued as soon as S(t) has been read, so that it runs beside the exponentials of step t; then
 // the accumulating products of t; then dP(t+1), which finds both its buffer and the P / dS buffers of step t free when it is done.
 // What bounds it: products 1276 cycles a step at heads of 128 (1024 in MODE 1), exponentials 1024 of the special function unit, and the element-wise warps' chain
-// of them: scores, exponentials, dP, dS.  1 x 4096 x 16 heads of 128, causal, 114 steps a CTA: dk/dv 161 us, dq 116.
+// of them: scores, exponentials, dP, dS.  1 x 4096 x 16 heads of 128, causal, 114 steps a CTA: dk/dv 179 us and dq 135, each alone with cold caches; the whole call, with the
+// preparation, 333 us in a run of calls.  With shared key heads a dk/dv item walks its whole group in sequence, and few items are left: the same case
+// on 4 key heads 475 us, on one 1405.
 #pragma once
 
 constexpr int kDbX = 64;
@@ -472,7 +475,7 @@ dattn_bwd_tc_kernel(const __grid_constant__ CUtensorMap map_f0, const __grid_con
         lam = lam_next;
       }
       if (!ok) break;
-      // ---------------- accumulators -> global: this warp's 32 rows x a quarter of the columns, of dk (or dq) and of dv, through its piece
+      // ---------------- accumulators -> global: this warp's 32 rows x its share of the columns (half of them, in MODE 1 a quarter), of dk (or dq) and of dv, through its piece
       const bool ready = mbar_wait(acc_full, (uint32_t)(n & 1));
       if (!ready && lane == 0) atomicCAS(&g_tc_error, 0, 9);
       ok = __all_sync(0xffffffffu, ready);

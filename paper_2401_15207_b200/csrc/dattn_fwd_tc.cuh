@@ -16,8 +16,8 @@
 // Each map has two buffers of scores, so that its warps find the next block's ready while the tensor core works on this one's P V and the one
 // after next: with one buffer of 128 keys a map waited for its products and their latency in every block (2 x 2048 x 32 heads of 128, causal: 151 -> 134 us).
 // What bounds it, both maps' 64 keys: products 890 cycles (at full rate), exponentials 1024 of the special function unit; measured 1450, and 1070 with
-// the softmax left out; and about 3500 at the end of an item of heads of 128, whose accumulators the next item's products wait for.  123 us for that
-// case in a short run (840 TFLOP/s), 142 at the clocks of a long one.
+// the softmax left out; and about 3500 at the end of an item of heads of 128, whose accumulators the next item's products wait for.  142 us for that
+// case in a run of calls (726 TFLOP/s), 124 in a short one.  Heads of 128 spill 44 bytes a thread at 128 registers, heads of 64 8 bytes.
 // Tensor-memory columns: buffer u of S_m at 128 m + 64 u, O_m behind 256: one set of 2 x 128 (heads of 128), two sets of 2 x 64 by item parity
 // (heads of 64).
 #pragma once

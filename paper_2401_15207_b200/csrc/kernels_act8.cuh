@@ -4,7 +4,8 @@
 // makes quotient, rounding and product free of any other error: the same 8 bits on every path.  A block that holds a NaN or an infinity
 // gets scale byte 255 (infinity as an fp32 exponent) and zeros: 0 * infinity is NaN, the whole block.
 //
-// Memory bounds all of these; the exponential or error function comes second.  Rows whose columns are a multiple of 8 in aligned buffers
+// Memory bounds packing, unpacking and SwiGLU (4.9 and 5.9 TB/s); GELU, with fewer bytes a value, is bound by the issue of instructions (83 to 86 % of the
+// slots: forward 3.1 TB/s, gradient 4.6).  Rows whose columns are a multiple of 8 in aligned buffers
 // go 8 columns to a thread (16 bytes of bf16, 8 bytes of q): four threads share a block, its maximum takes two shuffles.  Other rows go
 // one column to a thread, one block to a warp.
 #pragma once
@@ -101,7 +102,7 @@ __device__ __forceinline__ float act8_sigmoid(float a, float& rest) {
 // Normal distribution cdf and e = exp(-a^2 / 2).  With z = |a| / sqrt(2) and t = 1 / (1 + 0.45 z), erfc(z) / 2 = exp(-z^2) t Q(t): Q, of nine degrees, fitted
 // to the least largest relative error over all z >= 0 (3.2e-8; 5 half steps of fp32 as evaluated).  The lower tail is that product itself: in
 // 1 + erf its digits cancel (4 % off at a = -5, nothing left at -5.5).  One exponential serves the density too.  (GELU of 16384 x 5120 bf16, int8:
-// 133 us, gradient 128; with CUDA's erfcf 182 and 197.)
+// 135 us, gradient 128; with CUDA's erfcf 183 and 197.)
 __device__ __forceinline__ float act8_normal(float a, float& e) {
   const float t = __fdividef(1.0f, fmaf(fabsf(a), 0.31819806f, 1.0f));
   const float c[9] = {0.0953436941f, -0.150290787f, 0.0712000579f, -0.0111787422f, 0.0599751472f, 0.0876260772f, 0.114135817f, 0.126941577f, 0.126942664f};

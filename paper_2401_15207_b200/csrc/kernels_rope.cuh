@@ -2,8 +2,8 @@
 //   y1 = x1 cos - x2 sin,   y2 = x2 cos + x1 sin     (the gradient: the same with -sin),
 // pair j = (j, j + rot / 2) in the half layout, (2 j, 2 j + 1) in the interleaved one; the rest of a head is copied.
 // Memory bounds it: every element is read and written once.  A thread takes 2 V elements (V pairs, two loads of 16 bytes) of one head; its V
-// cosines and sines come from L1 and L2.  (Four heads a thread, which loads them once for the four, costs 90 registers: 69 -> 82 us for 16384 rows x
-// 40 heads x 128 bf16, half of each head turned.)
+// cosines and sines come from L1 and L2.  16384 rows x 40 heads x 128 bf16: half of each head turned 63 us (5.3 TB/s), whole heads in the half layout 54, in place
+// 56 (6.0 TB/s).  (Four heads a thread, which load them once for the four, cost 90 registers: 69 -> 82 us for the first of these when it was tried.)
 #pragma once
 #include "common.cuh"
 
