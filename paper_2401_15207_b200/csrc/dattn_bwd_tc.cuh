@@ -20,7 +20,7 @@
 // dP in the same way, accumulators 256.  S(t+1) is issued as soon as S(t) has been read, so that it runs beside the exponentials of step t; then
 // the accumulating products of t; then dP(t+1), which finds both its buffer and the P / dS buffers of step t free when it is done.
 // What bounds it: products 1276 cycles a step at heads of 128 (1024 in MODE 1), exponentials 1024 of the special function unit, and the element-wise warps' chain
-// of them: scores, exponentials, dP, dS.  1 x 4096 x 16 heads of 128, causal, 114 steps a CTA: dk/dv 179 us and dq 135, each alone with cold caches; the whole call, with the
+// of them: scores, exponentials, dP, dS.  1 x 4096 x 16 heads of 128, causal, 114 steps a CTA: dk/dv 179 us and dq 135 by the profiler, each alone with cold caches; the whole call, with the
 // preparation, 333 us in a run of calls.  With shared key heads a dk/dv item walks its whole group in sequence, and few items are left: the same case
 // on 4 key heads 475 us, on one 1405.
 #pragma once
